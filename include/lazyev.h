@@ -135,7 +135,7 @@ int lazyev_prefill(lazyev_t* h, const void* k, const void* v, int n_tokens);
  * Forget the cached sequences and make the handle ready for a new prompt (lazyev_prefill,
  * lazyev_prefill_observed or lazyev_load_state) on the same memory, configuration and stream:
  * t and n return to 0, budget_now to the create-time budget, the device status word is
- * cleared; the page table is kept.  Asynchronous on the bound stream.  (The paper processes
+ * cleared, a prefix is detached; the page table, rotation and norm are kept.  Asynchronous on the bound stream.  (The paper processes
  * one generation at a time; a server reuses the cache memory for the next batch of requests.)
  * Errors: ESTATE (not bound), ECUDA.
  */
@@ -267,6 +267,110 @@ int lazyev_copy_state(lazyev_t* dst, lazyev_t* src);
  */
 int lazyev_evict(lazyev_t* h, int* evicted);
 
+/* ---- Rows straight from a model's projections --------------------------------------------------------
+ * lazyev_prefill() and lazyev_decode_step() take queries and keys that are ready for attention, in the cache's own order.
+ * The calls of this section take them as a projection leaves them: strided views, not yet normalised or rotated.
+ * All of them need a bound handle whose device is the current one (ESTATE otherwise) and run on its stream; they
+ * read the views during the call's kernels only.  (The paper works inside a model that does this; it has no counterpart.)
+ */
+enum { LAZYEV_BF16 = 0, LAZYEV_FP16 = 1, LAZYEV_FP32 = 2 };
+
+/* Head rows of 128 contiguous elements: element d of head `head` of token i of sequence b in layer l is at
+ * data[l * stride_layer + b * stride_batch + i * stride_token + head * stride_head + d]; strides in elements (of
+ * dimensions of extent one: ignored).  data must be 16-byte aligned and every stride a multiple of 16 bytes; inputs may
+ * repeat rows (stride 0), outputs may not overlap. */
+typedef struct lazyev_rows {
+    void* data;
+    int dtype;             /* LAZYEV_BF16, LAZYEV_FP16 or LAZYEV_FP32 */
+    long long stride_layer, stride_batch, stride_token, stride_head;
+} lazyev_rows_t;
+
+/*
+ * Position rotation of queries and keys: pair j of a row turns by position * inv_freq[j] radians, and both of its
+ * elements are multiplied by `amplitude` (1 = a pure rotation):
+ *   (z_a, z_b) = amplitude * (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
+ * Pair j is elements (j, j + pairs), or (2 j, 2 j + 1) with interleaved != 0; the elements from 2 * pairs on stay as
+ * they are.  inv_freq is a host array that is copied.  pairs = 0 switches the rotation off (the state after create);
+ * else a multiple of 8 up to 64.  Angles are formed and reduced in 64 bits, whatever the position.
+ * Errors: EINVAL (pairs, null or non-finite inv_freq, non-finite amplitude).
+ */
+int lazyev_set_rope(lazyev_t* h, const double* inv_freq, int pairs, int interleaved, float amplitude);
+
+/*
+ * RMS norm of every query and key head before the rotation: y = x * rsqrt(mean(x^2) + eps) * w.  q_weight, k_weight:
+ * device pointers, float32 [layers][128], 16-byte aligned, read by every later call of this section (they stay the
+ * caller's and must stay valid); NULL for either: that side is not normalised.  Errors: EINVAL (misaligned, eps not
+ * positive and finite while a weight is given).
+ */
+int lazyev_set_head_norm(lazyev_t* h, const float* q_weight, const float* k_weight, float eps);
+
+/*
+ * Norm and rotation of queries and / or keys, in one pass: rows of n_tokens tokens of every sequence and layer, q with
+ * q_heads heads, k with kv_heads (either pair may be NULL).  Arithmetic in float32, one rounding to the output's
+ * type; any of the three types on either side.  Output views may equal the input's (in place).  positions: device
+ * int32 [batch][n_tokens], or NULL for first_position + i.  Nothing in the cache is read or changed.
+ * Errors: EINVAL (views, n_tokens <= 0, no rows at all), ESTATE, ECUDA.
+ */
+int lazyev_norm_rope(lazyev_t* h, const lazyev_rows_t* q, const lazyev_rows_t* k, int n_tokens, const int32_t* positions,
+                     int first_position, const lazyev_rows_t* q_out, const lazyev_rows_t* k_out);
+
+/*
+ * Append n_tokens tokens to every unit: keys normalised and rotated as set above, values as they are, both rounded to
+ * bf16 and written into the pages.  On an empty cache this is a prompt load (like lazyev_prefill(), TS = 0, MRI = 0);
+ * later calls continue it, chunk by chunk, or add the next turn of a conversation to a cache that has been decoded on: the tokens
+ * get TS = t, MRI = 0 and the next positions, and decode steps count on from there.  No attention runs and nothing is
+ * evicted before the next decode step whose t is a multiple of the window.
+ *   k, v       : views of kv_heads heads
+ *   positions  : device int32 [batch][n_tokens] that the keys are rotated by; NULL = the cache's own positions, i.e.
+ *                those after the tokens that came before (evicted ones and an attached prefix's counted)
+ * Errors: EINVAL (views, n_tokens <= 0), ECAPACITY (n + n_tokens > capacity), ESTATE, ECUDA.
+ */
+int lazyev_append(lazyev_t* h, const lazyev_rows_t* k, const lazyev_rows_t* v, int n_tokens, const int32_t* positions);
+
+/*
+ * lazyev_decode_step() from projected rows: views of one token (stride_token is ignored).  The query heads are
+ * normalised and rotated into scratch and the new token is appended in one launch, then the step runs as it does there;
+ * positions: device int32 [batch] or NULL.  Errors as for lazyev_decode_step(), plus EINVAL for the views.
+ */
+int lazyev_decode_step_rows(lazyev_t* h, const lazyev_rows_t* q, const lazyev_rows_t* k, const lazyev_rows_t* v,
+                            const int32_t* positions, void* out);
+
+/* ---- A prefix that sequences share --------------------------------------------------------------------
+ * Several sequences that continue one prompt (samples of one question, questions about one document) need its keys and
+ * values once.  `prefix` is another handle that holds the prompt -- filled by lazyev_prefill(), _prefill_observed() or
+ * lazyev_append(), evicted down or not -- with batch P dividing this handle's batch: sequence b of this handle
+ * continues sequence b / (batch / P) of `prefix`.  From then on every attention of this handle runs over the prefix's tokens
+ * followed by the sequence's own:
+ *   out = softmax([q K_prefix^T, q K_own^T] / sqrt(128)) [V_prefix; V_own]
+ * with the prefix's part computed for all its sequences at once on the tensor cores.  Probabilities, Eq. (1), the budget
+ * and eviction concern the own tokens; their probabilities are those of the joint softmax.  Prefix tokens count as
+ * protected: they are neither tracked nor evicted.  A handle with a prefix may be decoded with no own token
+ * yet.  Own tokens appended from now on get the positions after the prefix's.
+ *   workspace : device memory of lazyev_query_prefix_workspace() bytes, 256-byte aligned, for as long as the prefix is attached
+ * While it is attached the prefix must not change: lazyev_decode_step*(), _append(), _evict*(), _reset() and _destroy() on
+ * it answer ESTATE.  It may serve several handles at once, on their own streams; the attached handle is ordered after
+ * everything queued on the prefix's stream.  The slots behind the prefix's last token are zeroed.  lazyev_reset() detaches, and so does lazyev_destroy().
+ * Errors: EINVAL (null, the handle itself, other shapes, batch not divisible, other device, misaligned workspace), ESTATE
+ * (not bound, prefix empty, a prefix is attached already, or either handle has a prefix and is one), ECUDA.
+ */
+int lazyev_query_prefix_workspace(const lazyev_t* h, const lazyev_t* prefix, size_t* bytes);
+int lazyev_attach_prefix(lazyev_t* h, lazyev_t* prefix, void* workspace);
+/* Ends the sharing (0 when there was none): this handle's attention covers its own tokens only from here on, and work
+ * queued on the prefix's stream later waits for what is queued here.  Errors: ECUDA. */
+int lazyev_detach_prefix(lazyev_t* h);
+
+/*
+ * Attention of one query row per head over everything cached -- the attached prefix and the own tokens -- without a new
+ * token: for the tokens that lazyev_append() loaded last, or to ask again.  q, out as for lazyev_decode_step().  The
+ * probabilities of the own tokens are stored as by a decode step; TS, MRI, t and n do not change.
+ * Errors: EINVAL (null; q not 16-byte aligned while a prefix is attached), ESTATE (nothing cached), ECUDA.
+ */
+int lazyev_attend(lazyev_t* h, const void* q, void* out);
+
+/* Byte offsets inside the bound state region, for code that reads it on the device: the page table, int32 [units][pages_per_unit];
+ * (TS, MRI), int32 pairs; positions, int32; probabilities, float32; all [units][capacity].  Any pointer may be NULL. */
+int lazyev_query_state_layout(const lazyev_t* h, size_t* page_table, size_t* ts_mri, size_t* pos, size_t* pbar);
+
 /*
  * lazyev_evict() with its work lists inside the library.  (The paper has no counterpart; this
  * is a deployment convenience.)
@@ -319,6 +423,9 @@ typedef struct lazyev_info {
     long long launches;  /* kernels launched by this handle so far           */
     long long evictions; /* eviction events so far                           */
     int host_ranges;     /* unit ranges (decode launches) the last lazyev_decode_step_host call was split into */
+    int prefix_tokens;   /* cached tokens of the attached prefix (0 = none)  */
+    int prefix_blocks;   /* blocks of the prefix launch                      */
+    int next_position;   /* position of the next token                       */
 } lazyev_info_t;
 
 int lazyev_get_info(const lazyev_t* h, lazyev_info_t* out);

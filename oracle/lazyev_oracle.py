@@ -384,3 +384,52 @@ class OracleUnit:
         self.track(pbar if pbar_override is None else pbar_override)
         info = self.evict_if_due()
         return out, pbar, info
+
+
+def norm_rope(x, weight, eps, positions, inv_freq, interleaved=False, amplitude=1.0) -> np.ndarray:
+    """RMS norm (weight None: none) and position rotation of head rows x [tokens, ..., D] at positions [tokens]; pair j
+    (elements j and j + pairs, or 2 j and 2 j + 1) turns by positions * inv_freq[j]."""
+    x = np.array(x, dtype=np.float64)
+    if weight is not None:
+        x = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps) * np.asarray(weight, dtype=np.float64)
+    pairs = len(inv_freq)
+    out = x.copy()
+    for j in range(pairs):
+        a, b = (2 * j, 2 * j + 1) if interleaved else (j, j + pairs)
+        t = np.asarray(positions, dtype=np.float64) * float(inv_freq[j])
+        t = t.reshape(t.shape + (1,) * (x.ndim - 2))
+        c, s = amplitude * np.cos(t), amplitude * np.sin(t)
+        out[..., a] = x[..., a] * c - x[..., b] * s
+        out[..., b] = x[..., b] * c + x[..., a] * s
+    return out
+
+
+class PrefixedUnit(OracleUnit):
+    """A unit whose queries also attend to the tokens of a prefix (K [N, D], V [N, D], never tracked or evicted), and
+    whose own tokens come after them: positions start at `first`."""
+
+    def __init__(self, prefix_k, prefix_v, first, *args, **kw):
+        super().__init__(*args, **kw)
+        self.prefix_k = np.asarray(prefix_k, dtype=np.float64)
+        self.prefix_v = np.asarray(prefix_v, dtype=np.float64)
+        self.P = int(first)              # append() numbers a new token P + t - 1
+
+    def load(self, K, V) -> None:
+        """More tokens without attention: TS = t, MRI = 0, the next positions."""
+        m = len(K)
+        self.pos = np.append(self.pos, self.P + self.t + np.arange(m))
+        for k, v in zip(K, V):
+            self._append_row(k, v)
+        self.TS = np.append(self.TS, np.full(m, self.t))
+        self.MRI = np.append(self.MRI, np.zeros(m, dtype=np.int64))
+        self.P += m
+
+    def look(self, q):
+        """Eq. (attn) over prefix and own tokens: (out [G, D], pbar of the own tokens)."""
+        out, p = attention(q, np.vstack([self.prefix_k, self.K]), np.vstack([self.prefix_v, self.V]))
+        self.last_pbar = p.mean(axis=0)[len(self.prefix_k):]
+        return out, self.last_pbar
+
+    def attend(self, q, k_new, v_new):
+        self.append(k_new, v_new)
+        return self.look(q)

@@ -18,6 +18,7 @@ from . import build as _build
 OK, EINVAL, ESTATE, ECAPACITY, EDEVICE, ECUDA = 0, -1, -2, -3, -4, -5
 SCORE_H1_PLUS_H2, SCORE_H1_ONLY, SCORE_H2_ONLY, SCORE_H1_PLUS_H2_DECREASING = 0, 1, 2, 3
 PROMPT_TILED, PROMPT_REPLAY = 0, 1
+BF16, FP16, FP32 = 0, 1, 2
 
 
 class Info(C.Structure):
@@ -25,7 +26,9 @@ class Info(C.Structure):
         "layers", "batch", "q_heads", "kv_heads", "head_dim", "units", "budget", "budget_now", "window",
         "n_recent", "n_initial", "capacity", "pages_per_unit", "t", "n", "prefill", "splits", "stages",
         "groups", "tail_units", "tail_splits", "grid", "smem_bytes")] + [("launches", C.c_longlong), ("evictions", C.c_longlong),
-                                                                           ("host_ranges", C.c_int)]
+                                                                           ("host_ranges", C.c_int),
+                                                                           ("prefix_tokens", C.c_int), ("prefix_blocks", C.c_int),
+                                                                           ("next_position", C.c_int)]
 
 
 class Counters(C.Structure):
@@ -37,6 +40,11 @@ class Profile(C.Structure):
         "append_ms", "decode_ms", "select_ms", "compact_ms", "decode_bytes", "select_bytes", "compact_bytes",
         "compact_rows")] + [(n, C.c_longlong) for n in (
             "append_launches", "decode_launches", "select_launches", "compact_launches")]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int), ("stride_layer", C.c_longlong), ("stride_batch", C.c_longlong),
+                ("stride_token", C.c_longlong), ("stride_head", C.c_longlong)]
 
 
 class Dump(C.Structure):
@@ -73,6 +81,16 @@ _PROTOS = {
     "lazyev_decode_step_host_async": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
     "lazyev_host_wait": [C.c_void_p, C.c_int],
     "lazyev_copy_state": [C.c_void_p, C.c_void_p],
+    "lazyev_set_rope": [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float],
+    "lazyev_set_head_norm": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_float],
+    "lazyev_norm_rope": [C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.c_int, C.c_void_p, C.c_int, C.POINTER(Rows), C.POINTER(Rows)],
+    "lazyev_append": [C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.c_int, C.c_void_p],
+    "lazyev_decode_step_rows": [C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.c_void_p, C.c_void_p],
+    "lazyev_query_prefix_workspace": [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)],
+    "lazyev_attach_prefix": [C.c_void_p, C.c_void_p, C.c_void_p],
+    "lazyev_detach_prefix": [C.c_void_p],
+    "lazyev_attend": [C.c_void_p, C.c_void_p, C.c_void_p],
+    "lazyev_query_state_layout": [C.c_void_p, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
     "lazyev_evict": [C.c_void_p, C.POINTER(C.c_int)],
     "lazyev_evict_static": [C.c_void_p, C.POINTER(C.c_int)],
     "lazyev_get_info": [C.c_void_p, C.POINTER(Info)],
@@ -138,6 +156,8 @@ class Engine:
         import torch
         self._torch = torch
         self._h = C.c_void_p()
+        self._norm = self._prefix = None          # tensors and the engine that the handle reads
+        self._shape = layers, batch, q_heads, kv_heads
         self._check(lib().lazyev_create(C.byref(self._h), layers, q_heads, kv_heads, head_dim, budget, window,
                                         threshold), create=True)
         self._check(lib().lazyev_set_batch(self._h, batch))
@@ -148,7 +168,9 @@ class Engine:
         kv, st, sc = C.c_size_t(), C.c_size_t(), C.c_size_t()
         self._check(lib().lazyev_query_sizes(self._h, C.byref(kv), C.byref(st), C.byref(sc)))
         self.device = torch.device(device)
+        self._types = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
         with torch.cuda.device(self.device):
+            self._index = torch.device("cuda", torch.cuda.current_device())
             self.kv_pool = torch.empty(kv.value, dtype=torch.uint8, device=self.device)
             self.state = torch.empty(st.value, dtype=torch.uint8, device=self.device)
             self.scratch = torch.empty(sc.value, dtype=torch.uint8, device=self.device)
@@ -164,8 +186,9 @@ class Engine:
 
     def close(self) -> None:
         if self._h:
-            lib().lazyev_destroy(self._h)
+            self._check(lib().lazyev_destroy(self._h))      # refused while other engines share this one as their prefix
             self._h = C.c_void_p()
+            self._prefix = None
 
     def __del__(self):
         try:
@@ -237,6 +260,90 @@ class Engine:
     def copy_state_from(self, src: "Engine") -> None:
         """lazyev_copy_state(self, src): this handle becomes a copy of src's cached sequences."""
         self._check(lib().lazyev_copy_state(self._h, src._h))
+
+    def _rows(self, x, heads: int, tokens: int) -> Rows:
+        """A tensor [layers, batch, tokens, heads, 128] (of one token: the dimension may be left out) as the library's view."""
+        shape, stride = x.shape, x.stride()
+        layers, batch = self._shape[:2]
+        if len(shape) == 4 and tokens == 1:
+            shape, stride = (*shape[:2], 1, *shape[2:]), (*stride[:2], 0, *stride[2:])
+        if tuple(shape) != (layers, batch, tokens, heads, 128) or stride[4] != 1:
+            raise ValueError(f"rows must be [{layers}, {batch}, {tokens}, {heads}, 128] with contiguous rows, not {tuple(x.shape)}")
+        if x.device != self._index:
+            raise ValueError(f"rows must be on {self._index}, not {x.device}")
+        return Rows(x.data_ptr(), self._types[x.dtype], *stride[:4])
+
+    def _positions(self, positions, tokens: int) -> int:
+        if positions is None:
+            return 0
+        if (positions.dtype != self._torch.int32 or positions.device != self._index or not positions.is_contiguous()
+                or positions.numel() != self._shape[1] * tokens):
+            raise ValueError(f"positions must be contiguous int32 [{self._shape[1]}, {tokens}] on {self._index}")
+        return positions.data_ptr()
+
+    def set_rope(self, inv_freq, interleaved: bool = False, amplitude: float = 1.0) -> None:
+        """lazyev_set_rope: one frequency (radians per position) per rotating pair; an empty sequence switches it off."""
+        f = np.ascontiguousarray(inv_freq, dtype=np.float64)
+        self._check(lib().lazyev_set_rope(self._h, f.ctypes.data, f.size, int(interleaved), amplitude))
+
+    def set_head_norm(self, q_weight, k_weight, eps: float) -> None:
+        """lazyev_set_head_norm: float32 CUDA tensors [layers, 128], or None for no norm on that side."""
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dtype != self._torch.float32 or w.device != self._index or tuple(w.shape) != (self._shape[0], 128)):
+                raise ValueError(f"norm weights must be float32 [{self._shape[0]}, 128] on {self._index}")
+        self._check(lib().lazyev_set_head_norm(self._h, _ptr(q_weight), _ptr(k_weight), eps))
+        self._norm = q_weight, k_weight
+
+    def norm_rope(self, q, k, q_out, k_out, positions=None, first_position: int = 0) -> None:
+        """lazyev_norm_rope: q [layers, batch, tokens, q_heads, 128], k with kv_heads (either may be None), strided as they are."""
+        tokens = (q if q is not None else k).shape[2]
+        _, _, hq, hkv = self._shape
+        rows = [None if x is None else self._rows(x, heads, tokens) for x, heads in ((q, hq), (k, hkv), (q_out, hq), (k_out, hkv))]
+        self._check(lib().lazyev_norm_rope(self._h, rows[0], rows[1], tokens, self._positions(positions, tokens), first_position,
+                                           rows[2], rows[3]))
+
+    def append(self, k, v, positions=None) -> None:
+        """lazyev_append: k, v [layers, batch, tokens, kv_heads, 128], strided as they are."""
+        tokens, heads = k.shape[2], self._shape[3]
+        self._check(lib().lazyev_append(self._h, self._rows(k, heads, tokens), self._rows(v, heads, tokens), tokens,
+                                        self._positions(positions, tokens)))
+
+    def decode_step_rows(self, q, k, v, out, positions=None) -> None:
+        """lazyev_decode_step_rows: q, k, v [layers, batch, (1,) heads, 128], strided as they are; out as for decode_step."""
+        _, _, hq, hkv = self._shape
+        self._check(lib().lazyev_decode_step_rows(self._h, self._rows(q, hq, 1), self._rows(k, hkv, 1), self._rows(v, hkv, 1),
+                                                  self._positions(positions, 1), _ptr(out)))
+
+    def attach_prefix(self, prefix: "Engine") -> None:
+        """lazyev_attach_prefix; the workspace is allocated here and the prefix kept alive while it is attached."""
+        n = C.c_size_t()
+        self._check(lib().lazyev_query_prefix_workspace(self._h, prefix._h, C.byref(n)))
+        workspace = self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device)
+        workspace.record_stream(self.stream)
+        self._check(lib().lazyev_attach_prefix(self._h, prefix._h, workspace.data_ptr()))
+        self._prefix = prefix, workspace
+
+    def detach_prefix(self) -> None:
+        self._check(lib().lazyev_detach_prefix(self._h))
+
+    def attend(self, q, out) -> None:
+        """lazyev_attend: q, out as for decode_step."""
+        self._check(lib().lazyev_attend(self._h, _ptr(q), _ptr(out)))
+
+    def state_views(self) -> dict:
+        """Views of the live device memory (valid while the engine is): pages [pages, 2 (K, V), 64, 128] bf16 in the
+        stored order, page_table [units, pages_per_unit], and per unit and slot ts_mri [.., 2], pos and pbar."""
+        t, inf, off = self._torch, self.info(), [C.c_size_t() for _ in range(4)]
+        self._check(lib().lazyev_query_state_layout(self._h, *(C.byref(o) for o in off)))
+
+        def view(o, dtype, *shape):
+            n = 4 * int(np.prod(shape))
+            return self.state[o.value:o.value + n].view(dtype).view(*shape)
+
+        u, cap = inf.units, inf.capacity
+        return {"pages": self.kv_pool.view(t.bfloat16).view(-1, 2, 64, 128),
+                "page_table": view(off[0], t.int32, u, inf.pages_per_unit), "ts_mri": view(off[1], t.int32, u, cap, 2),
+                "pos": view(off[2], t.int32, u, cap), "pbar": view(off[3], t.float32, u, cap)}
 
     def evict(self) -> int:
         n = C.c_int()

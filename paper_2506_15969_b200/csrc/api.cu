@@ -48,6 +48,7 @@ struct lazyev {
     uint8_t* stage_out[2] = {nullptr, nullptr};
     double* stage_score = nullptr;
     unsigned long long* stage_hist = nullptr;
+    uint8_t* stage_rows = nullptr;         // queries of lazyev_decode_step_rows(), normalised and rotated
     double* h2_table = nullptr;            // H2 term per MRI value (scratch), valid for h2_table_mode
     int h2_table_mode = -1;
     // host-buffer entry point: copy streams and events, created at its first call
@@ -62,8 +63,21 @@ struct lazyev {
     long long host_seq = 0;
     bool slot_busy[2] = {false, false};
     int last_host_ranges = 0;
+    // what the calls that take projected rows do to queries and keys
+    double inv_freq[kMaxPairs] = {0};
+    int pairs = 0, interleaved = 0;
+    float amplitude = 1.f, norm_eps = 0.f;
+    const float* q_weight = nullptr;
+    const float* k_weight = nullptr;
+    // a prefix shared by this handle's sequences (another handle), and how many handles share this one
+    lazyev* shared = nullptr;
+    PrefixPlan prefix_plan = {};
+    float* prefix_o = nullptr;
+    float2* prefix_ml = nullptr;
+    int users = 0;
     // progress
     int t = 0, n = 0, prefill = 0;
+    int pos_base = 0;                      // position of the first own token: the prefix's next one
     long long launches = 0, evictions = 0;
     DecodePlan last_plan = {};
     int last_grid = 0, last_tail_units = 0, last_tail_splits = 0;
@@ -116,7 +130,7 @@ void derive(lazyev_t* h) {
 struct Sizes {
     size_t kv, state, scratch;
     size_t off_tsm, off_pos, off_pbar, off_status;                                  // inside state
-    size_t off_first, off_rlist, off_q, off_k, off_v, off_out, off_score, off_hist, off_h2;    // inside scratch
+    size_t off_first, off_rlist, off_q, off_k, off_v, off_out, off_score, off_hist, off_h2, off_rows;    // inside scratch
 };
 
 Sizes sizes_of(const lazyev_t* h) {
@@ -154,6 +168,8 @@ Sizes sizes_of(const lazyev_t* h) {
     off += align_up((size_t)kMaxHistBins * sizeof(unsigned long long), 256);
     s.off_h2 = off;
     off += align_up((size_t)kH2TableEntries * sizeof(double), 256);
+    s.off_rows = off;
+    off += align_up(qbytes, 256);
     s.scratch = off;
     return s;
 }
@@ -305,13 +321,35 @@ struct NewToken {
     int position;
 };
 
-// The decode launches of one step: attention of q over the first n cached tokens of every unit with
-// tracking at time t.  `tok` (may be null) is the token to append at slot n - 1 first: as a launch of
+// The prefix launch of a step (a handle with a shared prefix): partial sums of every query row over the prefix, which
+// the decode launches start from.
+cudaError_t run_prefix(lazyev_t* h, const void* q) {
+    const lazyev_t* src = h->shared;
+    PrefixArgs a;
+    a.pool = src->pool;
+    a.page_table = src->st.page_table;
+    a.n = src->n;
+    a.pages_per_unit = src->pages_per_unit;
+    a.total_pages = src->units * src->pages_per_unit;
+    a.layers = h->layers;
+    a.q = q;
+    a.o = h->prefix_o;
+    a.ml = h->prefix_ml;
+    a.status = h->st.status;
+    a.wait_limit_ns = h->wait_limit_ns;
+    a.stop_after_tiles = h->stop_after_pages;
+    h->launches += 1;
+    return prefix_launch(h->prefix_plan, a, h->stream);
+}
+
+// The decode launches of one step: attention of q over the shared prefix, if there is one, and the first n cached
+// tokens of every unit with tracking (unless `track` is false) at time t.  `tok` (may be null) is the token to append at slot n - 1 first: as a launch of
 // its own, or -- when every block of the decode launch takes exactly one unit, the launch-latency-sized
 // problems -- inside the decode launch.
-int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPipe* pipe, const NewToken* tok = nullptr) {
+int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPipe* pipe, const NewToken* tok = nullptr,
+               bool track = true) {
     cudaError_t e = cudaSuccess;
-    DecodeConfig c{h->units, h->group, h->pages_per_unit, h->capacity, h->alpha, h->force_splits, h->force_stages, h->force_groups,
+    DecodeConfig c{h->units, h->group, h->pages_per_unit, h->capacity, track ? h->alpha : INFINITY, h->force_splits, h->force_stages, h->force_groups,
                    h->wait_limit_ns, h->stop_after_pages};
     // Launch shape, chosen per number of pages in use and cached.  For every cluster size whose logits
     // fit, a small time model gives the time of the rounds of the round-robin walk; the main launch is
@@ -391,6 +429,14 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     const int main_units = h->units - shape.tail_units;
     const int clusters = shape.clusters < main_units ? shape.clusters : main_units;
     const bool fuse_append = tok && h->fuse_append && shape.tail_units == 0 && main_units <= clusters;
+    PrefixView prefix = {};
+    if (h->shared) {
+        if ((uintptr_t)q & 15) return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned while a prefix is attached");
+        prefix.plan = h->prefix_plan;
+        prefix.o = h->prefix_o;
+        prefix.ml = h->prefix_ml;
+        if (!pipe && (e = run_prefix(h, q)) != cudaSuccess) return cuda_fail(h, e, "prefix kernel launch");
+    }
     if (tok && !fuse_append) {
         SpanGuard g(h, kSpanAppend, 0.0);
         e = append_launch(geometry(h), h->pool, h->st, tok->k, tok->v, n - 1, t, tok->position, h->stream);
@@ -429,6 +475,10 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
                                     count[r] * unit_bytes, cudaMemcpyHostToDevice, h->copy_in);
                 if (e == cudaSuccess) e = cudaEventRecord(h->ev_in[r], h->copy_in);
             }
+            if (h->shared) {       // the prefix launch takes all queries at once
+                if (e == cudaSuccess) e = cudaStreamWaitEvent(h->stream, h->ev_in[ranges - 1], 0);
+                if (e == cudaSuccess) e = run_prefix(h, q);
+            }
         }
         // The last round's units do not depend on the main launch: on a lower-priority stream of their own,
         // forked here (after the append), their blocks take the SMs that the main launch's blocks leave as
@@ -451,7 +501,7 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
             if (e != cudaSuccess) break;
             // a range of the main walk continues it; the last round's units are a walk of their own
             DecodeArgs a{h->pool, h->st, q, out, n, t, begin[r], count[r], is_tail ? 0 : begin[r] / clusters,
-                         fuse_append ? tok->k : nullptr, fuse_append ? tok->v : nullptr, fuse_append ? tok->position : 0};
+                         fuse_append ? tok->k : nullptr, fuse_append ? tok->v : nullptr, fuse_append ? tok->position : 0, prefix};
             const bool beside = is_tail && fork;
             if (e != cudaSuccess) break;
             e = decode_launch(c, is_tail ? tail_plan : plan, is_tail ? count[r] : (clusters < count[r] ? clusters : count[r]), a,
@@ -478,8 +528,10 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     return LAZYEV_OK;
 }
 
-int run_step(lazyev_t* h, const void* q, const void* k_new, const void* v_new, void* out, const HostPipe* pipe = nullptr) {
-    if (!h->prefilled) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
+// Refuses a decode step before anything is queued.
+int check_step(lazyev_t* h) {
+    if (!h->prefilled && !h->shared) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
+    if (h->users > 0) return fail(h, LAZYEV_ESTATE, "decode_step on a handle that others share as their prefix");
     if (h->n + 1 > h->capacity) return fail(h, LAZYEV_ECAPACITY, "cache full (%d slots per unit)", h->capacity);
     const int t = h->t + 1, n = h->n + 1;
     // A step whose automatic eviction could not run is refused before anything is queued.
@@ -487,13 +539,89 @@ int run_step(lazyev_t* h, const void* q, const void* k_new, const void* v_new, v
         return fail(h, LAZYEV_EINVAL,
                     "step %d would evict over %d candidates, more than the selection supports; nothing was done", t,
                     n - h->n_recent - h->n_initial);
-    const NewToken tok{k_new, v_new, h->prefill + t - 1};
-    const int rc = run_decode(h, q, out, n, t, pipe, &tok);
-    if (rc != LAZYEV_OK) return rc;
-    h->t = t;
-    h->n = n;
+    return LAZYEV_OK;
+}
+
+// The step after its token is in the cache.
+int finish_step(lazyev_t* h) {
+    h->t += 1;
+    h->n += 1;
+    h->prefilled = true;                    // (a handle with a prefix may start with no own token)
     if (h->auto_evict) return run_evict(h, nullptr, h->src, h->first_moved, h->radix_list);
     return LAZYEV_OK;
+}
+
+int run_step(lazyev_t* h, const void* q, const void* k_new, const void* v_new, void* out, const HostPipe* pipe = nullptr) {
+    int rc = check_step(h);
+    if (rc != LAZYEV_OK) return rc;
+    const NewToken tok{k_new, v_new, h->pos_base + h->prefill + h->t};
+    rc = run_decode(h, q, out, h->n + 1, h->t + 1, pipe, &tok);
+    return rc != LAZYEV_OK ? rc : finish_step(h);
+}
+
+// ---- projected rows ------------------------------------------------------------------------------------
+// The handle is bound and its device is the current one.
+int check_device(lazyev_t* h, const char* call) {
+    if (!h->bound) return fail(h, LAZYEV_ESTATE, "%s before bind", call);
+    int dev = -1;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cudaGetDevice");
+    if (dev != h->device) return fail(h, LAZYEV_ESTATE, "%s needs device %d (the one bound to this handle) to be current, not %d", call, h->device, dev);
+    return LAZYEV_OK;
+}
+
+// The kernels' view of a caller's rows, or EINVAL.
+int rows_view(lazyev_t* h, const char* name, const lazyev_rows_t* r, int heads, int n_tokens, bool output, RowView* out) {
+    if (!r || !r->data) return fail(h, LAZYEV_EINVAL, "%s: null pointer", name);
+    if (r->dtype != LAZYEV_BF16 && r->dtype != LAZYEV_FP16 && r->dtype != LAZYEV_FP32)
+        return fail(h, LAZYEV_EINVAL, "%s: unknown type %d", name, r->dtype);
+    if ((uintptr_t)r->data & 15) return fail(h, LAZYEV_EINVAL, "%s must be 16-byte aligned", name);
+    const long long given[4] = {r->stride_layer, r->stride_batch, r->stride_token, r->stride_head};
+    const int extent[4] = {h->layers, h->batch, n_tokens, heads};
+    const int elems = r->dtype == LAZYEV_FP32 ? 4 : 8;             // of 16 bytes
+    long long stride[4];
+    for (int i = 0; i < 4; ++i) {
+        stride[i] = extent[i] > 1 ? given[i] : 0;
+        if (stride[i] % elems != 0) return fail(h, LAZYEV_EINVAL, "%s: strides must be multiples of 16 bytes", name);
+        if (output && extent[i] > 1 && stride[i] < kHeadDim && stride[i] > -kHeadDim)
+            return fail(h, LAZYEV_EINVAL, "%s: output rows overlap", name);
+    }
+    *out = RowView{r->data, stride[0], stride[1], stride[2], stride[3], r->dtype};
+    return LAZYEV_OK;
+}
+
+RowsArgs rows_args(const lazyev_t* h, int n_tokens, const int32_t* positions, int first_position) {
+    RowsArgs a = {};
+    a.layers = h->layers;
+    a.batch = h->batch;
+    a.q_heads = h->q_heads;
+    a.kv_heads = h->kv_heads;
+    a.n_tokens = n_tokens;
+    a.pairs = h->pairs;
+    a.interleaved = h->interleaved;
+    a.amplitude = h->amplitude;
+    a.eps = h->norm_eps;
+    a.q_weight = h->q_weight;
+    a.k_weight = h->k_weight;
+    a.positions = positions;
+    a.first_position = first_position;
+    a.status = h->st.status;
+    return a;
+}
+
+// Keys and values go into the pages of the next n_tokens slots, as tokens of time ts.
+void rows_to_pages(const lazyev_t* h, int ts, RowsArgs* a) {
+    a->pool = h->pool;
+    a->page_table = h->st.page_table;
+    a->tsm = h->st.tsm;
+    a->pos = h->st.pos;
+    a->pbar = h->st.pbar;
+    a->pages_per_unit = h->pages_per_unit;
+    a->capacity = h->capacity;
+    a->total_pages = h->units * h->pages_per_unit;
+    a->slot = h->n;
+    a->ts = ts;
+    a->pos_first = h->pos_base + h->prefill + h->t;
 }
 
 }  // namespace
@@ -663,6 +791,7 @@ int lazyev_bind(lazyev_t* h, void* kv_pool, void* state, void* scratch, void* cu
     h->stage_hist = (unsigned long long*)(cp + s.off_hist);
     h->h2_table = (double*)(cp + s.off_h2);
     h->h2_table_mode = -1;
+    h->stage_rows = cp + s.off_rows;
 
     // Slots past n are read (and masked) by the decode kernel's last page: they must hold finite values.
     e = cudaMemsetAsync(h->pool, 0, s.kv, h->stream);
@@ -697,7 +826,7 @@ int lazyev_prefill(lazyev_t* h, const void* k, const void* v, int n_tokens) {
     if (h->prefilled) return fail(h, LAZYEV_ESTATE, "prefill called twice");
     if (!k || !v || n_tokens <= 0) return fail(h, LAZYEV_EINVAL, "null pointer or non-positive token count");
     if (n_tokens > h->max_prefill) return fail(h, LAZYEV_ECAPACITY, "prompt of %d tokens exceeds max_prefill = %d", n_tokens, h->max_prefill);
-    cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, INT_MIN, h->stream);
+    cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, INT_MIN, h->pos_base, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "prefill kernel launch");
     h->launches += 1;
     h->prefilled = true;
@@ -709,21 +838,25 @@ int lazyev_prefill(lazyev_t* h, const void* k, const void* v, int n_tokens) {
 
 namespace {
 int host_wait(lazyev_t* h, int allowed);
+int detach(lazyev_t* h);
 }
 
 int lazyev_reset(lazyev_t* h) {
     if (!h) return LAZYEV_EINVAL;
     if (!h->bound) return fail(h, LAZYEV_ESTATE, "reset before bind");
+    if (h->users > 0) return fail(h, LAZYEV_ESTATE, "reset of a handle that others share as their prefix");
     if (h->copy_in) {                       // steps queued through the asynchronous host entry point finish first
         const int rc = host_wait(h, 0);
         if (rc != LAZYEV_OK) return rc;
     }
+    const int rc = detach(h);
+    if (rc != LAZYEV_OK) return rc;
     // Old rows stay in the pool: slots past n are masked, they only have to be finite.  The state arrays
     // are rewritten by the next prompt load and by every append; the device status word is cleared.
     cudaError_t e = cudaMemsetAsync(h->st.status, 0, 64, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "clearing the device status word");
     h->prefilled = false;
-    h->t = h->n = h->prefill = 0;
+    h->t = h->n = h->prefill = h->pos_base = 0;
     h->budget_now = h->budget;
     return LAZYEV_OK;
 }
@@ -732,12 +865,13 @@ int lazyev_prefill_observed(lazyev_t* h, const void* q, const void* k, const voi
     if (!h) return LAZYEV_EINVAL;
     if (!h->bound) return fail(h, LAZYEV_ESTATE, "prefill before bind");
     if (h->prefilled) return fail(h, LAZYEV_ESTATE, "prefill called twice");
+    if (h->shared) return fail(h, LAZYEV_ESTATE, "prefill_observed does not run over an attached prefix");
     if (!q || !k || !v || !out || n_tokens <= 0) return fail(h, LAZYEV_EINVAL, "null pointer or non-positive token count");
     if (n_tokens > h->max_prefill) return fail(h, LAZYEV_ECAPACITY, "prompt of %d tokens exceeds max_prefill = %d", n_tokens, h->max_prefill);
     if (h->prompt_mode == LAZYEV_PROMPT_TILED && (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15))
         return fail(h, LAZYEV_EINVAL, "q, k, v and out must be 16-byte aligned");
     // rows are loaded with TS = their own time j - (P - 1) <= 0 and MRI = 0
-    cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, 1 - n_tokens, h->stream);
+    cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, 1 - n_tokens, 0, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "prefill kernel launch");
     h->launches += 1;
     if (h->prompt_mode == LAZYEV_PROMPT_TILED) {
@@ -859,7 +993,7 @@ int host_wait(lazyev_t* h, int allowed) {
 int lazyev_decode_step_host(lazyev_t* h, const void* q, const void* k_new, const void* v_new, void* out) {
     if (!h) return LAZYEV_EINVAL;
     if (!q || !k_new || !v_new || !out) return fail(h, LAZYEV_EINVAL, "null pointer");
-    if (!h->prefilled) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
+    if (!h->prefilled && !h->shared) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
     int rc = host_streams(h);
     if (rc == LAZYEV_OK) rc = host_wait(h, 0);
     if (rc != LAZYEV_OK) return rc;
@@ -886,7 +1020,7 @@ int lazyev_decode_step_host(lazyev_t* h, const void* q, const void* k_new, const
 int lazyev_decode_step_host_async(lazyev_t* h, const void* q, const void* k_new, const void* v_new, void* out) {
     if (!h) return LAZYEV_EINVAL;
     if (!q || !k_new || !v_new || !out) return fail(h, LAZYEV_EINVAL, "null pointer");
-    if (!h->prefilled) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
+    if (!h->prefilled && !h->shared) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
     int rc = host_streams(h);
     if (rc != LAZYEV_OK) return rc;
     const int slot = (int)(h->host_seq & 1);
@@ -935,6 +1069,7 @@ int lazyev_copy_state(lazyev_t* dst, lazyev_t* src) {
     if (!dst->bound || !src->bound) return fail(dst, LAZYEV_ESTATE, "copy_state needs two bound handles");
     if (!src->prefilled) return fail(dst, LAZYEV_ESTATE, "copy_state from a handle that holds no cache");
     if (dst->prefilled) return fail(dst, LAZYEV_ESTATE, "copy_state into a handle that already holds a cache (reset it first)");
+    if (dst->shared != src->shared) return fail(dst, LAZYEV_ESTATE, "copy_state needs the same prefix attached to both handles, or to neither");
     if (dst->device != src->device || dst->layers != src->layers || dst->batch != src->batch || dst->q_heads != src->q_heads ||
         dst->kv_heads != src->kv_heads || dst->capacity != src->capacity || dst->budget != src->budget ||
         dst->window != src->window || dst->n_recent != src->n_recent || dst->n_initial != src->n_initial)
@@ -956,13 +1091,193 @@ int lazyev_copy_state(lazyev_t* dst, lazyev_t* src) {
     dst->t = src->t;
     dst->n = src->n;
     dst->prefill = src->prefill;
+    dst->pos_base = src->pos_base;
     dst->budget_now = src->budget_now;
+    return LAZYEV_OK;
+}
+
+int lazyev_set_rope(lazyev_t* h, const double* inv_freq, int pairs, int interleaved, float amplitude) {
+    if (!h) return LAZYEV_EINVAL;
+    if (pairs < 0 || pairs > kMaxPairs || pairs % 8 != 0) return fail(h, LAZYEV_EINVAL, "pairs must be a multiple of 8 up to %d", kMaxPairs);
+    if (pairs > 0 && !inv_freq) return fail(h, LAZYEV_EINVAL, "null inv_freq");
+    if (!isfinite(amplitude)) return fail(h, LAZYEV_EINVAL, "the amplitude must be finite");
+    for (int j = 0; j < pairs; ++j)
+        if (!isfinite(inv_freq[j])) return fail(h, LAZYEV_EINVAL, "inv_freq[%d] is not finite", j);
+    for (int j = 0; j < pairs; ++j) h->inv_freq[j] = inv_freq[j];
+    h->pairs = pairs;
+    h->interleaved = interleaved != 0;
+    h->amplitude = amplitude;
+    return LAZYEV_OK;
+}
+
+int lazyev_set_head_norm(lazyev_t* h, const float* q_weight, const float* k_weight, float eps) {
+    if (!h) return LAZYEV_EINVAL;
+    if (((uintptr_t)q_weight | (uintptr_t)k_weight) & 15) return fail(h, LAZYEV_EINVAL, "norm weights must be 16-byte aligned");
+    if ((q_weight || k_weight) && !(eps > 0.f && isfinite(eps))) return fail(h, LAZYEV_EINVAL, "eps must be positive and finite");
+    h->q_weight = q_weight;
+    h->k_weight = k_weight;
+    h->norm_eps = eps;
+    return LAZYEV_OK;
+}
+
+int lazyev_norm_rope(lazyev_t* h, const lazyev_rows_t* q, const lazyev_rows_t* k, int n_tokens, const int32_t* positions,
+                     int first_position, const lazyev_rows_t* q_out, const lazyev_rows_t* k_out) {
+    if (!h) return LAZYEV_EINVAL;
+    int rc = check_device(h, "norm_rope");
+    if (rc != LAZYEV_OK) return rc;
+    if (n_tokens <= 0 || (!q && !k)) return fail(h, LAZYEV_EINVAL, "no rows");
+    RowsArgs a = rows_args(h, n_tokens, positions, first_position);
+    if (q && (rc = rows_view(h, "q", q, h->q_heads, n_tokens, false, &a.q)) != LAZYEV_OK) return rc;
+    if (q && (rc = rows_view(h, "q_out", q_out, h->q_heads, n_tokens, true, &a.q_out)) != LAZYEV_OK) return rc;
+    if (k && (rc = rows_view(h, "k", k, h->kv_heads, n_tokens, false, &a.k)) != LAZYEV_OK) return rc;
+    if (k && (rc = rows_view(h, "k_out", k_out, h->kv_heads, n_tokens, true, &a.k_out)) != LAZYEV_OK) return rc;
+    const cudaError_t e = rows_launch(a, h->inv_freq, h->num_sms, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "norm_rope kernel launch");
+    h->launches += 1;
+    return LAZYEV_OK;
+}
+
+int lazyev_append(lazyev_t* h, const lazyev_rows_t* k, const lazyev_rows_t* v, int n_tokens, const int32_t* positions) {
+    if (!h) return LAZYEV_EINVAL;
+    int rc = check_device(h, "append");
+    if (rc != LAZYEV_OK) return rc;
+    if (h->users > 0) return fail(h, LAZYEV_ESTATE, "append to a handle that others share as their prefix");
+    if (n_tokens <= 0) return fail(h, LAZYEV_EINVAL, "non-positive token count");
+    RowsArgs a = rows_args(h, n_tokens, positions, h->pos_base + h->prefill + h->t);
+    if ((rc = rows_view(h, "k", k, h->kv_heads, n_tokens, false, &a.k)) != LAZYEV_OK) return rc;
+    if ((rc = rows_view(h, "v", v, h->kv_heads, n_tokens, false, &a.v)) != LAZYEV_OK) return rc;
+    if (n_tokens > h->capacity - h->n)
+        return fail(h, LAZYEV_ECAPACITY, "%d tokens after %d exceed the capacity of %d slots per unit", n_tokens, h->n, h->capacity);
+    rows_to_pages(h, h->t, &a);
+    const cudaError_t e = rows_launch(a, h->inv_freq, h->num_sms, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "append kernel launch");
+    h->launches += 1;
+    h->prefilled = true;
+    h->prefill += n_tokens;
+    h->n += n_tokens;
+    return LAZYEV_OK;
+}
+
+int lazyev_decode_step_rows(lazyev_t* h, const lazyev_rows_t* q, const lazyev_rows_t* k, const lazyev_rows_t* v,
+                            const int32_t* positions, void* out) {
+    if (!h) return LAZYEV_EINVAL;
+    int rc = check_device(h, "decode_step_rows");
+    if (rc != LAZYEV_OK) return rc;
+    if (!out) return fail(h, LAZYEV_EINVAL, "null pointer");
+    RowsArgs a = rows_args(h, 1, positions, h->pos_base + h->prefill + h->t);
+    if ((rc = rows_view(h, "q", q, h->q_heads, 1, false, &a.q)) != LAZYEV_OK) return rc;
+    if ((rc = rows_view(h, "k", k, h->kv_heads, 1, false, &a.k)) != LAZYEV_OK) return rc;
+    if ((rc = rows_view(h, "v", v, h->kv_heads, 1, false, &a.v)) != LAZYEV_OK) return rc;
+    if ((rc = check_step(h)) != LAZYEV_OK) return rc;
+    const long long row = kHeadDim, seq = (long long)h->q_heads * row;
+    a.q_out = RowView{h->stage_rows, h->batch * seq, seq, 0, row, kTypeBF16};
+    rows_to_pages(h, h->t + 1, &a);
+    const cudaError_t e = rows_launch(a, h->inv_freq, h->num_sms, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "row kernel launch");
+    h->launches += 1;
+    rc = run_decode(h, h->stage_rows, out, h->n + 1, h->t + 1, nullptr);
+    return rc != LAZYEV_OK ? rc : finish_step(h);
+}
+
+// ---- shared prefix ---------------------------------------------------------------------------------
+namespace {
+
+// Fits the two handles together; the plan of the shared work on success.
+int plan_prefix(lazyev_t* h, const lazyev_t* prefix, PrefixPlan* plan) {
+    if (!h->bound || !prefix->bound) return fail(h, LAZYEV_ESTATE, "a shared prefix needs two bound handles");
+    if (!prefix->prefilled || prefix->n == 0) return fail(h, LAZYEV_ESTATE, "the prefix handle holds no tokens");
+    if (prefix->device != h->device || prefix->layers != h->layers || prefix->q_heads != h->q_heads || prefix->kv_heads != h->kv_heads)
+        return fail(h, LAZYEV_EINVAL, "the prefix needs the same layers, heads and device");
+    if (h->batch % prefix->batch != 0)
+        return fail(h, LAZYEV_EINVAL, "%d sequences do not divide among %d prefixes", h->batch, prefix->batch);
+    *plan = prefix_plan(h->layers, h->batch, prefix->batch, h->kv_heads, h->group, prefix->n, h->num_sms);
+    return LAZYEV_OK;
+}
+
+size_t prefix_o_bytes(const PrefixPlan& p) { return align_up((size_t)p.slots * p.rows * kHeadDim * sizeof(float), 256); }
+
+int detach(lazyev_t* h) {
+    lazyev_t* prefix = h->shared;
+    if (!prefix) return LAZYEV_OK;
+    // what changes the prefix later waits for what reads it now
+    cudaEvent_t done = nullptr;
+    cudaError_t e = cudaEventCreateWithFlags(&done, cudaEventDisableTiming);
+    if (e == cudaSuccess) e = cudaEventRecord(done, h->stream);
+    if (e == cudaSuccess) e = cudaStreamWaitEvent(prefix->stream, done, 0);
+    if (done) cudaEventDestroy(done);
+    prefix->users -= 1;
+    h->shared = nullptr;
+    if (e != cudaSuccess) return cuda_fail(h, e, "detach_prefix");
+    return LAZYEV_OK;
+}
+
+}  // namespace
+
+int lazyev_query_prefix_workspace(const lazyev_t* h, const lazyev_t* prefix, size_t* bytes) {
+    if (!h || !prefix || !bytes) return LAZYEV_EINVAL;
+    PrefixPlan plan;
+    const int rc = plan_prefix(const_cast<lazyev_t*>(h), prefix, &plan);
+    if (rc != LAZYEV_OK) return rc;
+    *bytes = prefix_o_bytes(plan) + (size_t)plan.slots * plan.rows * sizeof(float2);
+    return LAZYEV_OK;
+}
+
+int lazyev_attach_prefix(lazyev_t* h, lazyev_t* prefix, void* workspace) {
+    if (!h) return LAZYEV_EINVAL;
+    if (!prefix || prefix == h) return fail(h, LAZYEV_EINVAL, "the prefix must be another handle");
+    int rc = check_device(h, "attach_prefix");
+    if (rc != LAZYEV_OK) return rc;
+    if (h->shared) return fail(h, LAZYEV_ESTATE, "a prefix is attached already");
+    if (h->users > 0 || prefix->shared) return fail(h, LAZYEV_ESTATE, "a prefix cannot have a prefix of its own");
+    PrefixPlan plan;
+    if ((rc = plan_prefix(h, prefix, &plan)) != LAZYEV_OK) return rc;
+    if (!workspace || ((uintptr_t)workspace & 255)) return fail(h, LAZYEV_EINVAL, "the workspace must be 256-byte aligned");
+    cudaError_t e = prefix_prepare();
+    cudaEvent_t ready = nullptr;
+    // (handles that share it already have seen it cleared)
+    if (e == cudaSuccess && prefix->users == 0) e = clear_tail_launch(geometry(prefix), prefix->pool, prefix->st, prefix->n, prefix->stream);
+    if (e == cudaSuccess) e = cudaEventCreateWithFlags(&ready, cudaEventDisableTiming);
+    if (e == cudaSuccess) e = cudaEventRecord(ready, prefix->stream);
+    if (e == cudaSuccess) e = cudaStreamWaitEvent(h->stream, ready, 0);
+    if (ready) cudaEventDestroy(ready);
+    if (e != cudaSuccess) return cuda_fail(h, e, "attach_prefix");
+    h->shared = prefix;
+    h->prefix_plan = plan;
+    h->prefix_o = (float*)workspace;
+    h->prefix_ml = (float2*)((uint8_t*)workspace + prefix_o_bytes(plan));
+    h->pos_base = prefix->pos_base + prefix->prefill + prefix->t;
+    prefix->users += 1;
+    return LAZYEV_OK;
+}
+
+int lazyev_detach_prefix(lazyev_t* h) {
+    if (!h) return LAZYEV_EINVAL;
+    return detach(h);
+}
+
+int lazyev_attend(lazyev_t* h, const void* q, void* out) {
+    if (!h) return LAZYEV_EINVAL;
+    const int rc = check_device(h, "attend");
+    if (rc != LAZYEV_OK) return rc;
+    if (!q || !out) return fail(h, LAZYEV_EINVAL, "null pointer");
+    if (!h->prefilled && !h->shared) return fail(h, LAZYEV_ESTATE, "attend before prefill");
+    return run_decode(h, q, out, h->n, h->t, nullptr, nullptr, false);
+}
+
+int lazyev_query_state_layout(const lazyev_t* h, size_t* page_table, size_t* ts_mri, size_t* pos, size_t* pbar) {
+    if (!h) return LAZYEV_EINVAL;
+    const Sizes s = sizes_of(h);
+    if (page_table) *page_table = 0;
+    if (ts_mri) *ts_mri = s.off_tsm;
+    if (pos) *pos = s.off_pos;
+    if (pbar) *pbar = s.off_pbar;
     return LAZYEV_OK;
 }
 
 int lazyev_evict(lazyev_t* h, int* evicted) {
     if (!h) return LAZYEV_EINVAL;
     if (!h->prefilled) return fail(h, LAZYEV_ESTATE, "evict before prefill");
+    if (h->users > 0) return fail(h, LAZYEV_ESTATE, "evict on a handle that others share as their prefix");
     return run_evict(h, evicted, h->src, h->first_moved, h->radix_list);
 }
 
@@ -982,6 +1297,7 @@ int lazyev_evict_static(lazyev_t* h, int* evicted) {
     if (!h) return LAZYEV_EINVAL;
     if (evicted) *evicted = 0;
     if (!h->prefilled) return fail(h, LAZYEV_ESTATE, "evict_static before prefill");
+    if (h->users > 0) return fail(h, LAZYEV_ESTATE, "evict_static on a handle that others share as their prefix");
     if (h->units > kStaticMaxUnits || (size_t)h->units * (size_t)h->budget_now > kStaticSrcEntries)
         return fail(h, LAZYEV_ECAPACITY,
                     "evict_static holds %zu source indices for at most %d units; this handle needs %zu for %d units "
@@ -1046,6 +1362,9 @@ int lazyev_get_info(const lazyev_t* h, lazyev_info_t* out) {
     out->launches = h->launches;
     out->evictions = h->evictions;
     out->host_ranges = h->last_host_ranges;
+    out->prefix_tokens = h->shared ? h->shared->n : 0;
+    out->prefix_blocks = h->shared ? h->prefix_plan.blocks : 0;
+    out->next_position = h->pos_base + h->prefill + h->t;
     return LAZYEV_OK;
 }
 
@@ -1235,6 +1554,8 @@ int lazyev_synchronize(lazyev_t* h) {
 
 int lazyev_destroy(lazyev_t* h) {
     if (!h) return LAZYEV_EINVAL;
+    if (h->users > 0) return fail(h, LAZYEV_ESTATE, "destroy of a handle that others share as their prefix");
+    detach(h);
     if (h->copy_in) host_wait(h, 0);        // no copy of ours may still be writing the caller's host buffers
     for (const lazyev::Span& sp : h->pending) {
         cudaEventDestroy(sp.start);

@@ -22,7 +22,7 @@ __global__ void init_state_kernel(Geometry geo, StateView st) {
 
 // One warp per (unit, token): lanes 0..15 move the K row's chunks, lanes 16..31 the V row's.
 __global__ void prefill_kernel(Geometry geo, uint8_t* pool, StateView st, const uint4* __restrict__ k,
-                               const uint4* __restrict__ v, int n_tokens, int ts_first) {
+                               const uint4* __restrict__ v, int n_tokens, int ts_first, int pos_first) {
     const int lane = threadIdx.x & 31;
     const size_t warps = ((size_t)gridDim.x * blockDim.x) >> 5;
     const size_t total = (size_t)geo.units * n_tokens;
@@ -40,7 +40,7 @@ __global__ void prefill_kernel(Geometry geo, uint8_t* pool, StateView st, const 
             // Prompt tokens start at MRI = 0 (Section 4) and TS = 0, or, when the prompt is going to be
             // replayed with tracking, at their own time ts_first + i (the last prompt row is time 0).
             st.tsm[s] = make_int2(ts_first == INT_MIN ? 0 : ts_first + i, 0);
-            st.pos[s] = i;
+            st.pos[s] = pos_first + i;
         }
     }
 }
@@ -65,7 +65,26 @@ __global__ void append_kernel(Geometry geo, uint8_t* pool, StateView st, const u
     }
 }
 
+// One block per unit: zeroes the K and V rows of the slots n .. end of the page in the unit's last page, whatever an
+// earlier sequence left there.  A kernel that multiplies masked rows by zero weights needs them finite.
+__global__ void clear_tail_kernel(Geometry geo, uint8_t* pool, StateView st, int n) {
+    const int u = blockIdx.x;
+    const int32_t pp = st.page_table[(size_t)u * geo.pages_per_unit + n / kPageTokens];
+    if (!in_bounds(pp >= 0 && pp < geo.units * geo.pages_per_unit, st.status)) return;
+    const int first = n % kPageTokens, chunks = (kPageTokens - first) * kChunksPerRow;
+    for (int half = 0; half < 2; ++half) {
+        uint4* rows = reinterpret_cast<uint4*>(page_ptr(pool, pp) + half * kPageHalfBytes + first * kRowBytes);
+        for (int i = threadIdx.x; i < chunks; i += blockDim.x) rows[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
 }  // namespace
+
+cudaError_t clear_tail_launch(const Geometry& geo, uint8_t* pool, StateView st, int n, cudaStream_t stream) {
+    if (n % kPageTokens == 0) return cudaSuccess;
+    clear_tail_kernel<<<geo.units, 256, 0, stream>>>(geo, pool, st, n);
+    return cudaGetLastError();
+}
 
 cudaError_t init_state_launch(const Geometry& geo, StateView st, cudaStream_t stream) {
     init_state_kernel<<<1184, 256, 0, stream>>>(geo, st);
@@ -73,11 +92,11 @@ cudaError_t init_state_launch(const Geometry& geo, StateView st, cudaStream_t st
 }
 
 cudaError_t prefill_launch(const Geometry& geo, uint8_t* pool, StateView st, const void* k, const void* v,
-                           int n_tokens, int ts_first, cudaStream_t stream) {
+                           int n_tokens, int ts_first, int pos_first, cudaStream_t stream) {
     const size_t rows = (size_t)geo.units * n_tokens;
     const int blocks = (int)((rows + 7) / 8 < 148 * 16 ? (rows + 7) / 8 : 148 * 16);
     prefill_kernel<<<blocks, 256, 0, stream>>>(geo, pool, st, reinterpret_cast<const uint4*>(k),
-                                               reinterpret_cast<const uint4*>(v), n_tokens, ts_first);
+                                               reinterpret_cast<const uint4*>(v), n_tokens, ts_first, pos_first);
     return cudaGetLastError();
 }
 

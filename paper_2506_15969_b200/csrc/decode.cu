@@ -70,6 +70,7 @@ struct DecodeParams {
     const uint4* v_new;
     int32_t* pos;
     int append_position;
+    PrefixView prefix;                              // partial sums over a shared prefix, for the kernels with kPrefix
 };
 
 constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the softmax reference by
@@ -104,8 +105,9 @@ __device__ __forceinline__ float ld_rank_f32(const float* local_ptr, uint32_t ra
     return ld_dsmem_f32(map_to_rank(smem_u32(local_ptr), rank));
 }
 
-// NG groups of four consumer warps plus one producer warp.
-template <int NG>
+// NG groups of four consumer warps plus one producer warp.  kPrefix: the softmax of every unit also runs over the
+// tokens of a shared prefix, whose partial sums an earlier launch left in p.prefix.
+template <int NG, bool kPrefix>
 __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const DecodeParams p) {
     constexpr int NW = 4 * NG;
     constexpr int kConsumers = NW * 32;
@@ -378,6 +380,41 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
         };
         if (my_units > 0) load_q(p.unit_begin + cluster_id, qb);
 
+        // The shared prefix: its partial sums (reference, l, O per query row, one set per piece of the prefix) are
+        // what a warp would hold after some of the pages, so the warps of the unit start from them instead of from
+        // nothing -- each from its share -- and the merge at the end of the unit needs to know nothing of them.
+        // The unit's log-sum-exp, hence pbar, covers the prefix like any cached token.
+        auto add_prefix = [&](int u, float& m0, float& m1, float& l0, float& l1, float (&o)[8][4]) {
+            const PrefixPlan& pl = p.prefix.plan;
+            const int hh = u % pl.kv_heads, lb = u / pl.kv_heads;          // lb: (layer, sequence)
+            const int pair = (lb % pl.share) / pl.tile_seqs / 2;
+            const long long x0 = ((long long)(lb / pl.share * pl.kv_heads + hh) * pl.pairs + pair) * pl.key_tiles;
+            const int pieces = prefix_block_of(pl, x0 + pl.key_tiles - 1) - prefix_block_of(pl, x0) + 1;
+            const int n_slots = 2 * pair + 1 < pl.tiles ? pieces : 2 * pieces;
+            for (int s = (int)rank * NW + warp; s < n_slots; s += S * NW) {
+                const long long row = s * pl.rows + (long long)u * G;
+                const float2 none = make_float2(-INFINITY, 0.f);
+                const float2 a0 = h0_on ? p.prefix.ml[row + h0] : none, a1 = h1_on ? p.prefix.ml[row + h1] : none;
+                const bool on0 = a0.x > -INFINITY, on1 = a1.x > -INFINITY;
+                const float* r0 = p.prefix.o + (row + h0) * kHeadDim + g;
+                const float* r1 = r0 + kHeadDim;
+                const float n0 = fmaxf(m0, a0.x), n1 = fmaxf(m1, a1.x);
+                const float c0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
+                const float d0 = on0 ? fast_exp2(a0.x - n0) : 0.f, d1 = on1 ? fast_exp2(a1.x - n1) : 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    o[i][0] = o[i][0] * c0 + (on0 ? r0[16 * i] * d0 : 0.f);
+                    o[i][1] = o[i][1] * c1 + (on1 ? r1[16 * i] * d1 : 0.f);
+                    o[i][2] = o[i][2] * c0 + (on0 ? r0[16 * i + 8] * d0 : 0.f);
+                    o[i][3] = o[i][3] * c1 + (on1 ? r1[16 * i + 8] * d1 : 0.f);
+                }
+                l0 = l0 * c0 + (g == 0 ? a0.y * d0 : 0.f);          // l is a sum over the lanes of a column
+                l1 = l1 * c1 + (g == 0 ? a1.y * d1 : 0.f);
+                m0 = n0;
+                m1 = n1;
+            }
+        };
+
         // Pages belong to the groups in turn (page pc of the block's walk to group pc mod NG, across unit
         // boundaries), and a warp looks at the barriers up to its own next page before it releases the
         // page it holds; the producer refills a stage only after the pages before it were released, so it
@@ -396,6 +433,7 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
             float o[8][4];      // O^T: [m-tile][(dim g, h0), (dim g, h1), (dim g + 8, h0), (dim g + 8, h1)]
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+            if constexpr (kPrefix) add_prefix(u, mref0, mref1, l0, l1, o);
 
             // this group's pages of the unit: j = j0, j0 + NG, ...
             const int j0 = NG == 1 ? 0 : (int)((grp + NG - pc_mod) % NG);
@@ -663,7 +701,7 @@ constexpr int kMaxGroups = 2;
 constexpr int kTmemPages = 128;            // 512 columns / 4 per page
 constexpr size_t kMinSmemBytes = 120 * 1024;
 
-template <int NG>
+template <int NG, bool kPrefix>
 cudaError_t launch_impl(const DecodeParams& p, const DecodePlan& plan, int clusters, cudaStream_t stream,
                         int* max_clusters) {
     cudaLaunchConfig_t cfg = {};
@@ -678,8 +716,8 @@ cudaError_t launch_impl(const DecodeParams& p, const DecodePlan& plan, int clust
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (max_clusters) return cudaOccupancyMaxActiveClusters(max_clusters, decode_kernel<NG>, &cfg);
-    return cudaLaunchKernelEx(&cfg, decode_kernel<NG>, p);
+    if (max_clusters) return cudaOccupancyMaxActiveClusters(max_clusters, decode_kernel<NG, kPrefix>, &cfg);
+    return cudaLaunchKernelEx(&cfg, decode_kernel<NG, kPrefix>, p);
 }
 
 }  // namespace
@@ -734,15 +772,19 @@ int decode_plan(const DecodeConfig& c, int n, int max_smem, int splits, DecodePl
 }
 
 cudaError_t decode_prepare() {
-    cudaError_t e = cudaFuncSetAttribute(decode_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-    if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(decode_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    const void* kernels[4] = {(const void*)decode_kernel<1, false>, (const void*)decode_kernel<2, false>,
+                              (const void*)decode_kernel<1, true>, (const void*)decode_kernel<2, true>};
+    for (const void* k : kernels) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 cudaError_t decode_max_clusters(const DecodePlan& plan, int* clusters) {
     DecodeParams none = {};
-    return plan.groups == 2 ? launch_impl<2>(none, plan, 1, nullptr, clusters)
-                            : launch_impl<1>(none, plan, 1, nullptr, clusters);
+    return plan.groups == 2 ? launch_impl<2, false>(none, plan, 1, nullptr, clusters)
+                            : launch_impl<1, false>(none, plan, 1, nullptr, clusters);
 }
 
 cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clusters, const DecodeArgs& a,
@@ -785,8 +827,12 @@ cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clu
     p.wait_limit_ns = c.wait_limit_ns;
     p.stop_after_pages = c.stop_after_pages;
     p.rounds_before = a.rounds_before;
-    return plan.groups == 2 ? launch_impl<2>(p, plan, clusters, stream, nullptr)
-                            : launch_impl<1>(p, plan, clusters, stream, nullptr);
+    p.prefix = a.prefix;
+    if (a.prefix.ml)
+        return plan.groups == 2 ? launch_impl<2, true>(p, plan, clusters, stream, nullptr)
+                                : launch_impl<1, true>(p, plan, clusters, stream, nullptr);
+    return plan.groups == 2 ? launch_impl<2, false>(p, plan, clusters, stream, nullptr)
+                            : launch_impl<1, false>(p, plan, clusters, stream, nullptr);
 }
 
 }  // namespace lzk

@@ -5,6 +5,48 @@
 
 namespace lzk {
 
+// ---- attention over a shared prefix ------------------------------------------------------------------
+// How the prefix kernel's work is laid out; the decode kernel finds its partial sums by the same arithmetic.
+struct PrefixPlan {
+    int kv_heads, batch;                // of the handle that decodes
+    int share, group;                   // sequences per prefix sequence, query heads per KV head
+    int tile_seqs, tiles, pairs;        // sequences per row tile, row tiles per prefix unit, items (pairs of tiles) per unit
+    int key_tiles;                      // 128-key tiles of the prefix
+    int blocks;
+    int slots;                          // most partial sums of a row
+    long long work;                     // items * key_tiles
+    long long rows;                     // query rows = partial sums per slot
+};
+
+// Block that works on step x of the walk over (item, key tile): block c takes [c work / blocks, (c + 1) work / blocks).
+__host__ __device__ __forceinline__ int prefix_block_of(const PrefixPlan& p, long long x) {
+    return (int)(((x + 1) * p.blocks - 1) / p.work);
+}
+
+struct PrefixView {        // what the decode kernel adds to every unit: ml = null for none
+    PrefixPlan plan;
+    const float* o;        // [slots][rows][128], relative to m
+    const float2* ml;      // [slots][rows]: reference (log2 domain), sum of exp2(x - reference)
+};
+
+struct PrefixArgs {
+    const uint8_t* pool;
+    const int32_t* page_table;
+    int n, pages_per_unit, total_pages; // of the prefix handle
+    int layers;
+    const void* q;
+    float* o;
+    float2* ml;
+    int32_t* status;
+    unsigned long long wait_limit_ns;
+    int stop_after_tiles;
+};
+PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int group, int n, int num_sms);
+cudaError_t prefix_prepare();
+cudaError_t prefix_launch(const PrefixPlan& plan, const PrefixArgs& a, cudaStream_t stream);
+// Zeroes the slots behind the last token in every unit's last page.
+cudaError_t clear_tail_launch(const Geometry& geo, uint8_t* pool, StateView st, int n, cudaStream_t stream);
+
 // ---- decode ------------------------------------------------------------------
 struct DecodeConfig {
     int units, group, pages_per_unit, capacity;
@@ -33,6 +75,7 @@ struct DecodeArgs {
     const void* k_new;            // non-null: the launch also appends the new token (slot n - 1, TS = t, MRI = 0)
     const void* v_new;
     int append_position;
+    PrefixView prefix;            // prefix.ml = null: none
 };
 
 // Deepest ring and the shared-memory layout for n cached tokens and a cluster of `splits` blocks;
@@ -46,10 +89,41 @@ cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clu
 // ---- cache maintenance ---------------------------------------------------------
 cudaError_t init_state_launch(const Geometry& geo, StateView st, cudaStream_t stream);
 // ts_first = INT_MIN: every prompt token starts at TS = 0; otherwise token i starts at TS = ts_first + i.
+// Token i is recorded at position pos_first + i.
 cudaError_t prefill_launch(const Geometry& geo, uint8_t* pool, StateView st, const void* k, const void* v,
-                           int n_tokens, int ts_first, cudaStream_t stream);
+                           int n_tokens, int ts_first, int pos_first, cudaStream_t stream);
 cudaError_t append_launch(const Geometry& geo, uint8_t* pool, StateView st, const void* k_new, const void* v_new,
                           int slot, int t, int position, cudaStream_t stream);
+
+// ---- head rows: norm, rotation, paged append -------------------------------------------------------
+constexpr int kTypeBF16 = 0, kTypeF16 = 1, kTypeF32 = 2;      // LAZYEV_BF16 ...
+constexpr int kMaxPairs = kHeadDim / 2;
+
+struct RowView {           // head rows of 128 contiguous elements; strides in elements
+    const void* data;      // null: no rows of this kind
+    long long stride_layer, stride_batch, stride_token, stride_head;
+    int dtype;
+};
+
+struct RowsArgs {
+    RowView q, k, v, q_out, k_out;      // k_out (and v) only without / with a pool
+    int layers, batch, q_heads, kv_heads, n_tokens;
+    int pairs, interleaved;             // 0 pairs: no rotation
+    float amplitude, eps;
+    const float* q_weight;              // [layers][128]; null: no norm
+    const float* k_weight;
+    const int32_t* positions;           // [batch][n_tokens]; null: first_position + i
+    int first_position;
+    // keys and values into the pages of token slots slot .. slot + n_tokens - 1 (pool = null: keys go to k_out)
+    uint8_t* pool;
+    const int32_t* page_table;
+    int2* tsm;
+    int32_t* pos;
+    float* pbar;
+    int32_t* status;
+    int pages_per_unit, capacity, total_pages, slot, ts, pos_first;
+};
+cudaError_t rows_launch(const RowsArgs& a, const double* inv_freq, int num_sms, cudaStream_t stream);
 
 // ---- prompt pass (causal attention over the prompt with tracking) -----------------------------------
 struct PromptArgs {

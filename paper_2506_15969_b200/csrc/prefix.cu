@@ -1,0 +1,490 @@
+// Attention of a batch over a prefix that its sequences share, computed once for all of them.
+//
+// The prefix is another handle's cache: its units are (layer, prefix sequence, KV head), and `share` sequences of the
+// decoding handle attend to each.  For the share * G query rows of a prefix unit and the prefix's tokens i
+// (Appendix A, Eq. (attn), restricted to the prefix):
+//   x[i] = q . k_i / sqrt(D) * log2 e,   m >= max_i x[i] - 8,   l = sum_i exp2(x[i] - m),   o = sum_i exp2(x[i] - m) v_i
+// (m, l, o) are written as partial sums; the decode kernel starts a unit's softmax over its own tokens from them, so
+// the probabilities it emits are those of the joint softmax.
+//
+// K / V of the prefix are read once per pair of row tiles, 512 bytes per token, where every sequence would read them by
+// itself; 512 flops a byte and 128 rows.  Up to about 300 query rows per prefix unit HBM bounds that, beyond it the
+// exponentials (16 a clock and SM).
+//
+// Structure: persistent blocks, one per SM.  A row tile is 128 accumulator rows = floor(128 / G) sequences x G heads, an
+// item is a prefix unit with two of its row tiles (or its single, or odd last one), and the walk over (item, key tile
+// of 128 tokens) is cut into equal contiguous parts, one per block, so no wave is left half full; a row gets one
+// set of partial sums per block that worked on its item.
+//
+// Two streams of four softmax warps (thread = accumulator row) alternate on the tensor core: with two row tiles a
+// stream has a tile and every key tile; with one, the streams take the key tiles in turn and keep partial sums each.
+//   S = Q K^T (tcgen05.mma, operands in shared memory, accumulator in tensor memory), softmax against a reference that
+//   is raised -- and O rescaled in tensor memory -- only when a logit exceeds it by more than 2^8, P written over S
+//   as two bf16 terms (hi + lo: 16 mantissa bits, as in the other attention kernels here), O += P V with P as the
+//   tensor-memory operand.
+// MMAs of one thread complete in order, and S of a stream's next tile is issued after O += P V of the tile before (they share
+// tensor-memory columns): once S has arrived the warps may rescale O without any further wait.
+//
+// Pages keep 16-byte chunk c of row r at c ^ (r & 7) of every 128-byte half row.  A plain (unswizzled) TMA box of 64 rows x
+// 128 bytes therefore lands as a 128-byte-swizzled operand; a key tile is four boxes from two pages.
+//
+// Warp roles: warps 0-7 softmax and output, warp 8 TMA producer, warp 9 MMA issuer.  All mbarrier waits are bounded.
+#include "internal.h"
+#include "tensor.cuh"
+
+namespace lzk {
+
+namespace {
+
+constexpr int kTile = 128;                         // rows of a row tile, keys of a key tile
+constexpr int kBoxBytes = kTile * 128;             // half an operand: 128 rows x 64 bf16
+constexpr int kOperandBytes = 2 * kBoxBytes;       // a 128 x 128 bf16 operand (32 KiB)
+constexpr int kRing = 5;                           // K and V tiles in flight, in the order they are used
+constexpr int kStreamThreads = 128;
+constexpr int kThreads = 2 * kStreamThreads + 64;
+constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the reference by
+
+constexpr int kOffQ = 0;                           // two row tiles
+constexpr int kOffRing = kOffQ + 2 * kOperandBytes;
+constexpr int kOffMisc = kOffRing + kRing * kOperandBytes;
+constexpr int kSmem = kOffMisc + 1024;
+
+constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;     // per stream: 128 columns of S / P, 128 of O
+
+struct Bars {
+    uint64_t q_full[2], q_empty[2];
+    uint64_t full[kRing], empty[kRing];
+    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t drain;
+};
+
+struct PrefixParams {
+    PrefixPlan plan;
+    const int32_t* page_table;
+    float* o;
+    float2* ml;
+    int32_t* status;
+    int n, pages_per_unit, total_pages;
+    float scale_log2;
+    unsigned long long wait_limit_ns;
+    int stop_after_tiles;
+};
+
+// One block's part of an item: key tiles [k0, k1).
+struct Piece {
+    long long item;
+    int k0, k1;
+    bool both;                                     // two row tiles, a stream each; else one, the key tiles in turn
+    __device__ __forceinline__ int tiles() const { return k1 - k0; }
+    // key tiles of stream s, and the t-th of them
+    __device__ __forceinline__ int stream_tiles(int s) const { return both ? k1 - k0 : (k1 - k0 + 1 - s) >> 1; }
+    __device__ __forceinline__ int key_tile(int s, int t) const { return both ? k0 + t : k0 + 2 * t + s; }
+};
+
+__device__ __forceinline__ Piece piece_at(const PrefixPlan& pl, long long x, long long end) {
+    Piece pc;
+    pc.item = x / pl.key_tiles;
+    pc.k0 = (int)(x - pc.item * pl.key_tiles);
+    pc.k1 = (int)min((long long)pl.key_tiles, pc.k0 + (end - x));
+    pc.both = 2 * (int)(pc.item % pl.pairs) + 1 < pl.tiles;
+    return pc;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PrefixParams p) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Bars* bars = reinterpret_cast<Bars*>(smem + kOffMisc);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffMisc + 512);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const PrefixPlan& pl = p.plan;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars->q_full[i], 1);
+            mbar_init(&bars->q_empty[i], 1);
+            mbar_init(&bars->s_full[i], 1);
+            mbar_init(&bars->p_full[i], 4);
+            mbar_init(&bars->o_full[i], 1);
+        }
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&bars->full[i], 1);
+            mbar_init(&bars->empty[i], 1);
+        }
+        mbar_init(&bars->drain, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    // rows of a row tile that no query row ever fills (128 is no multiple of G): zeros, like all of Q before the first tile
+    for (int i = threadIdx.x; i < 2 * kOperandBytes / 16; i += kThreads)
+        reinterpret_cast<uint4*>(smem + kOffQ)[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async();
+    if (warp == 0) {
+        tmem_alloc(tmem_slot, kTmemCols);
+        tmem_relinquish_alloc_permit();
+    }
+    tmem_fence_before_sync();
+    __syncthreads();
+    tmem_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+    const unsigned long long limit = p.wait_limit_ns;
+    const long long begin = (long long)blockIdx.x * pl.work / pl.blocks, end = ((long long)blockIdx.x + 1) * pl.work / pl.blocks;
+
+    if (warp == 8) {
+        // ------------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            Ring rr, qr;
+            bool ok = true;
+            int k_tiles = 0;
+            const uint32_t q_bytes = (uint32_t)(pl.tile_seqs * pl.group) * 256u;
+            // a K (half = 0) or V (half = 1) tile: 64 rows x 64 elements per box, two pages, both halves of the rows
+            auto load_tile = [&](const int32_t* table, int kt, int half) {
+                const uint32_t st = rr.stage(kRing);
+                ok = wait_bar(&bars->empty[st], rr.parity(kRing) ^ 1u, abort_flag, p.status, limit);
+                if (!ok) return;
+                uint8_t* dst = smem + kOffRing + st * kOperandBytes;
+                mbar_arrive_expect_tx(&bars->full[st], kOperandBytes);
+                const int last = (p.n - 1) / kPageTokens;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    // a tile's second page may lie behind the last one: any page will do, its keys are masked
+                    int32_t pp = table[min(2 * kt + j, last)];
+                    if (pp < 0 || pp >= p.total_pages) {
+                        atomicOr(p.status, kStatusBadIndex);
+                        pp = 0;
+                    }
+                    tma_load_3d(dst + j * (kBoxBytes / 2), &map_kv, 0, half * kPageTokens, pp, &bars->full[st]);
+                    tma_load_3d(dst + kBoxBytes + j * (kBoxBytes / 2), &map_kv, 64, half * kPageTokens, pp, &bars->full[st]);
+                }
+                ++rr.count;
+            };
+            for (long long x = begin; x < end && ok;) {
+                const Piece pc = piece_at(pl, x, end);
+                x += pc.tiles();
+                const long long unit = pc.item / pl.pairs;             // (layer, prefix sequence, head)
+                const int head = (int)(unit % pl.kv_heads), seq0 = (int)(unit / pl.kv_heads) * pl.share;
+                const int tile0 = 2 * (int)(pc.item % pl.pairs);
+                for (int s = 0; s < (pc.both ? 2 : 1) && ok; ++s) {
+                    const uint32_t qs = qr.stage(2);
+                    ok = wait_bar(&bars->q_empty[qs], qr.parity(2) ^ 1u, abort_flag, p.status, limit);
+                    if (!ok) break;
+                    uint8_t* dst = smem + kOffQ + qs * kOperandBytes;
+                    mbar_arrive_expect_tx(&bars->q_full[qs], q_bytes);
+                    const int seq = seq0 + (tile0 + s) * pl.tile_seqs;
+                    tma_load_4d(dst, &map_q, 0, 0, head, seq, &bars->q_full[qs]);
+                    tma_load_4d(dst + kBoxBytes, &map_q, 64, 0, head, seq, &bars->q_full[qs]);
+                    ++qr.count;
+                }
+                const int32_t* table = p.page_table + unit * p.pages_per_unit;
+                const int ahead = pc.both ? 1 : 2, nt = pc.tiles();
+                auto load_k = [&](int j) {
+                    // diagnostics: no copy beyond the first stop_after_tiles K tiles
+                    if (p.stop_after_tiles >= 0 && k_tiles >= p.stop_after_tiles) ok = false;
+                    ++k_tiles;
+                    if (ok) load_tile(table, pc.k0 + j, 0);
+                };
+                for (int j = 0; j < min(ahead, nt) && ok; ++j) load_k(j);
+                for (int j = 0; j < nt && ok; ++j) {
+                    load_tile(table, pc.k0 + j, 1);
+                    if (ok && j + ahead < nt) load_k(j + ahead);
+                }
+            }
+            if (!ok) {      // aborted: let the copies already issued land before the block exits
+                auto drain = [&](uint64_t* full, const Ring& r, uint32_t n) {
+                    const uint32_t last = r.count < n ? r.count : n;
+                    for (uint32_t k = r.count - last; k < r.count; ++k)
+                        wait_bar(&full[k % n], (k / n) & 1u, abort_flag, p.status, limit, false);
+                };
+                drain(bars->full, rr, kRing);
+                drain(bars->q_full, qr, 2);
+            }
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            Ring rr, qr;
+            uint32_t p_uses[2] = {0, 0};
+            bool ok = true;
+            auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+                if (ok) ok = wait_bar(bar, parity, abort_flag, p.status, limit);
+            };
+            auto issue_s = [&](int s, uint32_t q_slot, uint32_t stage) {
+                tmem_fence_after_sync();
+                const uint32_t q_addr = smem_u32(smem + kOffQ + q_slot * kOperandBytes);
+                const uint32_t k_addr = smem_u32(smem + kOffRing + stage * kOperandBytes);
+#pragma unroll
+                for (int s8 = 0; s8 < 8; ++s8) {    // 16 head dimensions per instruction: 32 bytes inside a box row
+                    const uint32_t off = (s8 >> 2) * kBoxBytes + (s8 & 3) * 32;
+                    umma_bf16(tmem_base + kColS + s * 128, smem_desc(q_addr + off, 16, 1024), smem_desc(k_addr + off, 16, 1024),
+                              instr_desc(false), s8 > 0);
+                }
+                umma_commit(&bars->s_full[s]);
+            };
+            auto issue_o = [&](int s, uint32_t stage, bool first) {
+                tmem_fence_after_sync();
+                const uint32_t v_addr = smem_u32(smem + kOffRing + stage * kOperandBytes);
+                const uint32_t p_col = tmem_base + kColS + s * 128, o_col = tmem_base + kColO + s * 128;
+#pragma unroll
+                for (int s8 = 0; s8 < 8; ++s8) {    // 16 keys per instruction; P = hi + lo, two products
+                    const uint64_t v_desc = smem_desc(v_addr + s8 * 2048, kBoxBytes, 1024);
+                    const uint32_t a_col = p_col + (s8 >> 1) * 32 + (s8 & 1) * 8;
+                    umma_bf16_ts(o_col, a_col, v_desc, instr_desc(true), !first || s8 > 0);
+                    umma_bf16_ts(o_col, a_col + 16, v_desc, instr_desc(true), 1u);
+                }
+            };
+            for (long long x = begin; x < end && ok;) {
+                const Piece pc = piece_at(pl, x, end);
+                const int nt = pc.tiles(), streams = pc.both ? 2 : 1;
+                x += nt;
+                uint32_t q_slot[2];
+                for (int s = 0; s < streams; ++s) {
+                    q_slot[s] = qr.stage(2);
+                    wait_on(&bars->q_full[q_slot[s]], qr.parity(2));
+                    ++qr.count;
+                }
+                if (streams == 1) q_slot[1] = q_slot[0];
+                const int ahead = pc.both ? 1 : 2;
+                auto q_done = [&]() {               // the last logits of the piece are issued
+                    for (int s = 0; s < streams; ++s) umma_commit(&bars->q_empty[q_slot[s]]);
+                };
+                const int lead = min(ahead, nt);
+                for (int j = 0; j < lead && ok; ++j) {
+                    const uint32_t st = rr.stage(kRing);
+                    wait_on(&bars->full[st], rr.parity(kRing));
+                    if (!ok) break;
+                    issue_s(pc.both ? 0 : j, q_slot[0], st);
+                    if (pc.both) issue_s(1, q_slot[1], st);
+                    umma_commit(&bars->empty[st]);
+                    ++rr.count;
+                }
+                if (ok && lead == nt) q_done();
+                for (int j = 0; j < nt && ok; ++j) {
+                    const uint32_t v_use = rr.count, k_use = rr.count + 1;
+                    const bool more = j + ahead < nt;
+                    const int s0 = pc.both ? 0 : (j & 1), s1 = pc.both ? 1 : s0;
+                    for (int s = s0; s <= s1 && ok; ++s) {
+                        wait_on(&bars->p_full[s], p_uses[s] & 1u);
+                        ++p_uses[s];
+                        wait_on(&bars->full[v_use % kRing], (v_use / kRing) & 1u);
+                        if (!ok) break;
+                        issue_o(s, v_use % kRing, j < (pc.both ? 1 : 2));
+                        if (s == s1) umma_commit(&bars->empty[v_use % kRing]);
+                        if (more) {
+                            wait_on(&bars->full[k_use % kRing], (k_use / kRing) & 1u);
+                            if (!ok) break;
+                            issue_s(s, q_slot[s], k_use % kRing);
+                            if (s == s1) umma_commit(&bars->empty[k_use % kRing]);
+                        } else {
+                            umma_commit(&bars->o_full[s]);
+                        }
+                    }
+                    rr.count += more ? 2 : 1;
+                    if (ok && more && j + ahead + 1 == nt) q_done();
+                }
+            }
+            // every MMA issued by this thread is complete before tensor memory goes back
+            umma_commit(&bars->drain);
+            wait_bar(&bars->drain, 0, abort_flag, p.status, limit, false);
+        }
+    } else {
+        // ------------------------------------------------------------------ softmax and output
+        const int s = warp >> 2, row = threadIdx.x & 127;
+        const uint32_t lane_base = tmem_base + ((uint32_t)(32 * (warp & 3)) << 16);
+        const uint32_t s_cols = lane_base + kColS + s * 128, o_cols = lane_base + kColO + s * 128;
+        uint32_t s_uses = 0, o_uses = 0;
+        bool dead = false;
+        auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+            const bool gave_up = dead || !wait_bar(bar, parity, abort_flag, p.status, limit);
+            dead = __any_sync(0xffffffffu, gave_up);      // a warp goes on, or leaves, as a whole
+        };
+        for (long long x = begin; x < end && !dead;) {
+            const Piece pc = piece_at(pl, x, end);
+            x += pc.tiles();
+            const int nt = pc.stream_tiles(s);
+            const int tile = 2 * (int)(pc.item % pl.pairs) + (pc.both ? s : 0);
+            const int r = row / pl.group;                              // sequence inside the row tile
+            const int seq = tile * pl.tile_seqs + r;
+            const bool valid = r < pl.tile_seqs && seq < pl.share;
+            const bool warp_on = __any_sync(0xffffffffu, valid);
+            float m = -INFINITY, l = 0.f;
+            for (int t = 0; t < nt; ++t) {
+                wait_on(&bars->s_full[s], s_uses & 1u);
+                if (dead) break;
+                ++s_uses;
+                tmem_fence_after_sync();
+                if (warp_on) {
+                    float v[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(s_cols + 32 * c, v[c]);
+                    tmem_wait_ld();
+                    const int key0 = pc.key_tile(s, t) * kTile;
+                    if (key0 + kTile > p.n) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[c][i] = key0 + 32 * c + i < p.n ? v[c][i] : -INFINITY;
+                    }
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) mx = fmax3(mx, v[c][i], v[c][i + 1]);
+                    mx *= p.scale_log2;
+                    const bool raise = mx > m + kRaiseMargin;
+                    if (__any_sync(0xffffffffu, raise && valid)) {
+                        const float to = fmaxf(m, mx);
+                        const float f = m == to ? 1.f : fast_exp2(m - to);
+                        if (t > 0) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                float o[32];
+                                tmem_ld32(o_cols + 32 * c, o);
+                                tmem_wait_ld();
+                                uint32_t lo16[16], hi16[16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    lo16[i] = __float_as_uint(o[i] * f);
+                                    hi16[i] = __float_as_uint(o[16 + i] * f);
+                                }
+                                tmem_st16(o_cols + 32 * c, lo16);
+                                tmem_st16(o_cols + 32 * c + 16, hi16);
+                            }
+                        }
+                        l *= f;
+                        m = to;
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;      // every logit -inf: all weights are zero
+                    const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), minus2 = pack2(-ref, -ref);
+                    uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t hi[16], lo[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float e0, e1, d0, d1;
+                            unpack2(fma2(pack2(v[c][2 * i], v[c][2 * i + 1]), scale2, minus2), e0, e1);
+                            const uint64_t w = pack2(fast_exp2(e0), fast_exp2(e1));
+                            unpack2(w, e0, e1);
+                            hi[i] = pack_bf16(e0, e1);
+                            unpack2(sub2(w, pack2(bf16_lo_as_float(hi[i]), bf16_hi_as_float(hi[i]))), d0, d1);
+                            lo[i] = pack_bf16(d0, d1);
+                            if (i & 1)
+                                sum1 = add2(sum1, w);
+                            else
+                                sum0 = add2(sum0, w);
+                        }
+                        tmem_st16(s_cols + 32 * c, hi);
+                        tmem_st16(s_cols + 32 * c + 16, lo);
+                    }
+                    float a0, a1;
+                    unpack2(add2(sum0, sum1), a0, a1);
+                    l += a0 + a1;
+                    tmem_wait_st();
+                }
+                tmem_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->p_full[s]);
+            }
+            // ---- the piece's partial sums
+            if (dead) break;
+            const long long item0 = pc.item * pl.key_tiles;
+            const int nth = (int)blockIdx.x - prefix_block_of(pl, item0);
+            const int slot = pc.both ? nth : 2 * nth + s;
+            const long long unit = pc.item / pl.pairs;
+            const long long u = (unit / pl.kv_heads * pl.share + seq) * pl.kv_heads + unit % pl.kv_heads;     // of the decoding handle
+            const long long at = slot * pl.rows + u * pl.group + (row - r * pl.group);
+            if (valid) p.ml[at] = make_float2(m, l);
+            if (nt > 0) {
+                wait_on(&bars->o_full[s], o_uses & 1u);
+                if (dead) break;
+                ++o_uses;
+                tmem_fence_after_sync();
+                if (warp_on) {
+                    float4* dst = reinterpret_cast<float4*>(p.o + at * kHeadDim);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float o[32];
+                        tmem_ld32(o_cols + 32 * c, o);
+                        tmem_wait_ld();
+                        if (valid) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) dst[8 * c + i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        }
+                    }
+                }
+                tmem_fence_before_sync();
+            }
+        }
+    }
+
+    tmem_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) {
+        tmem_fence_after_sync();
+        tmem_dealloc(tmem_base, kTmemCols);
+    }
+}
+
+}  // namespace
+
+PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int group, int n, int num_sms) {
+    PrefixPlan pl;
+    pl.kv_heads = kv_heads;
+    pl.batch = batch;
+    pl.share = batch / prefixes;
+    pl.group = group;
+    pl.tile_seqs = kTile / group < pl.share ? kTile / group : pl.share;
+    pl.tiles = (pl.share + pl.tile_seqs - 1) / pl.tile_seqs;
+    pl.pairs = (pl.tiles + 1) / 2;
+    pl.key_tiles = (n + kTile - 1) / kTile;
+    pl.work = (long long)layers * prefixes * kv_heads * pl.pairs * pl.key_tiles;
+    pl.blocks = (int)(pl.work < num_sms ? pl.work : num_sms);
+    pl.rows = (long long)layers * batch * kv_heads * group;
+    // most blocks that touch one item, and twice that where the streams keep partial sums each
+    const long long per = pl.work / pl.blocks;
+    const long long pieces = (pl.key_tiles + per - 1) / per + 1;
+    const long long most = pieces < pl.blocks ? pieces : pl.blocks;
+    pl.slots = (int)(pl.tiles % 2 ? 2 * most : most);
+    return pl;
+}
+
+cudaError_t prefix_prepare() {
+    return cudaFuncSetAttribute(prefix_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+}
+
+cudaError_t prefix_launch(const PrefixPlan& plan, const PrefixArgs& a, cudaStream_t stream) {
+    CUtensorMap mq, mkv;
+    {
+        // q [layers * batch][kv_heads][G][128]: box = 64 elements x G heads x 1 KV head x tile_seqs sequences, 128-byte swizzle;
+        // sequences behind the last one read as zero, those of the next prefix are rows that nobody looks at
+        const cuuint64_t dims[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)plan.group, (cuuint64_t)plan.kv_heads,
+                                    (cuuint64_t)a.layers * plan.batch};
+        const cuuint64_t strides[3] = {(cuuint64_t)kRowBytes, (cuuint64_t)plan.group * kRowBytes,
+                                       (cuuint64_t)plan.kv_heads * plan.group * kRowBytes};
+        const cuuint32_t box[4] = {64, (cuuint32_t)plan.group, 1, (cuuint32_t)plan.tile_seqs};
+        if (!make_map(&mq, a.q, 4, dims, strides, box)) return cudaErrorInvalidValue;
+    }
+    {
+        // the prefix's pool: [pages][64 K rows, then 64 V rows][128]; the rows are stored swizzled already
+        const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)2 * kPageTokens, (cuuint64_t)a.total_pages};
+        const cuuint64_t strides[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)kPageBytes};
+        const cuuint32_t box[3] = {64, (cuuint32_t)kPageTokens, 1};
+        if (!make_map(&mkv, a.pool, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE)) return cudaErrorInvalidValue;
+    }
+    PrefixParams p;
+    p.plan = plan;
+    p.page_table = a.page_table;
+    p.o = a.o;
+    p.ml = a.ml;
+    p.status = a.status;
+    p.n = a.n;
+    p.pages_per_unit = a.pages_per_unit;
+    p.total_pages = a.total_pages;
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)kHeadDim);
+    p.wait_limit_ns = a.wait_limit_ns;
+    p.stop_after_tiles = a.stop_after_tiles;
+    prefix_kernel<<<plan.blocks, kThreads, kSmem, stream>>>(mq, mkv, p);
+    return cudaGetLastError();
+}
+
+}  // namespace lzk
