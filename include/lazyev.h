@@ -271,7 +271,8 @@ int lazyev_evict(lazyev_t* h, int* evicted);
  * lazyev_prefill() and lazyev_decode_step() take queries and keys that are ready for attention, in the cache's own order.
  * The calls of this section take them as a projection leaves them: strided views, not yet normalised or rotated.
  * All of them need a bound handle whose device is the current one (ESTATE otherwise) and run on its stream; they
- * read the views during the call's kernels only.  (The paper works inside a model that does this; it has no counterpart.)
+ * read the views during the call's kernels only.
+ * The input views of one call are of one type, and so are its output views (EINVAL otherwise).  (The paper works inside a model that does this; it has no counterpart.)
  */
 enum { LAZYEV_BF16 = 0, LAZYEV_FP16 = 1, LAZYEV_FP32 = 2 };
 

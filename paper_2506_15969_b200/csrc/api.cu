@@ -590,6 +590,12 @@ int rows_view(lazyev_t* h, const char* name, const lazyev_rows_t* r, int heads, 
     return LAZYEV_OK;
 }
 
+// One launch reads one type and writes one.
+int same_type(lazyev_t* h, const RowView& x, const RowView& y) {
+    if (x.data && y.data && x.dtype != y.dtype) return fail(h, LAZYEV_EINVAL, "the rows of a call must be of one type (outputs too)");
+    return LAZYEV_OK;
+}
+
 RowsArgs rows_args(const lazyev_t* h, int n_tokens, const int32_t* positions, int first_position) {
     RowsArgs a = {};
     a.layers = h->layers;
@@ -1131,6 +1137,7 @@ int lazyev_norm_rope(lazyev_t* h, const lazyev_rows_t* q, const lazyev_rows_t* k
     if (q && (rc = rows_view(h, "q_out", q_out, h->q_heads, n_tokens, true, &a.q_out)) != LAZYEV_OK) return rc;
     if (k && (rc = rows_view(h, "k", k, h->kv_heads, n_tokens, false, &a.k)) != LAZYEV_OK) return rc;
     if (k && (rc = rows_view(h, "k_out", k_out, h->kv_heads, n_tokens, true, &a.k_out)) != LAZYEV_OK) return rc;
+    if ((rc = same_type(h, a.q, a.k)) != LAZYEV_OK || (rc = same_type(h, a.q_out, a.k_out)) != LAZYEV_OK) return rc;
     const cudaError_t e = rows_launch(a, h->inv_freq, h->num_sms, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "norm_rope kernel launch");
     h->launches += 1;
@@ -1146,6 +1153,7 @@ int lazyev_append(lazyev_t* h, const lazyev_rows_t* k, const lazyev_rows_t* v, i
     RowsArgs a = rows_args(h, n_tokens, positions, h->pos_base + h->prefill + h->t);
     if ((rc = rows_view(h, "k", k, h->kv_heads, n_tokens, false, &a.k)) != LAZYEV_OK) return rc;
     if ((rc = rows_view(h, "v", v, h->kv_heads, n_tokens, false, &a.v)) != LAZYEV_OK) return rc;
+    if ((rc = same_type(h, a.k, a.v)) != LAZYEV_OK) return rc;
     if (n_tokens > h->capacity - h->n)
         return fail(h, LAZYEV_ECAPACITY, "%d tokens after %d exceed the capacity of %d slots per unit", n_tokens, h->n, h->capacity);
     rows_to_pages(h, h->t, &a);
@@ -1168,6 +1176,7 @@ int lazyev_decode_step_rows(lazyev_t* h, const lazyev_rows_t* q, const lazyev_ro
     if ((rc = rows_view(h, "q", q, h->q_heads, 1, false, &a.q)) != LAZYEV_OK) return rc;
     if ((rc = rows_view(h, "k", k, h->kv_heads, 1, false, &a.k)) != LAZYEV_OK) return rc;
     if ((rc = rows_view(h, "v", v, h->kv_heads, 1, false, &a.v)) != LAZYEV_OK) return rc;
+    if ((rc = same_type(h, a.q, a.k)) != LAZYEV_OK || (rc = same_type(h, a.q, a.v)) != LAZYEV_OK) return rc;
     if ((rc = check_step(h)) != LAZYEV_OK) return rc;
     const long long row = kHeadDim, seq = (long long)h->q_heads * row;
     a.q_out = RowView{h->stage_rows, h->batch * seq, seq, 0, row, kTypeBF16};

@@ -106,7 +106,7 @@ struct RowView {           // head rows of 128 contiguous elements; strides in e
 };
 
 struct RowsArgs {
-    RowView q, k, v, q_out, k_out;      // k_out (and v) only without / with a pool
+    RowView q, k, v, q_out, k_out;      // k_out without a pool, v with one; q, k, v of one type, q_out and k_out too
     int layers, batch, q_heads, kv_heads, n_tokens;
     int pairs, interleaved;             // 0 pairs: no rotation
     float amplitude, eps;

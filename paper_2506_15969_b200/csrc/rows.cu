@@ -11,193 +11,389 @@
 // sincospif needs no further reduction.
 //
 // Bound by HBM (a row is read once and written once, 10 flops an element) or, for a few tokens, by launch
-// latency.  A half-warp works on one row, 16 bytes of bf16 per lane; the partner elements of a rotation with
-// pairs (j, j + pairs) are read a second time by their lane (an L1 hit) rather than shuffled.  A warp takes rows
-// of one kind (queries, keys or values) of one token, so that the angles and the weights are computed once and
-// held in registers as two factors per element: z = inv * (x * f + x_partner * g).
+// latency.  At 256 bytes in and out per row an SM has 22 clocks for a row, so what decides is the number of
+// instructions: a half-warp works on one row; each lane holds two groups of four elements chosen so that the partners of
+// a rotation sit in the same lane (no exchange, nothing read twice); angles, weights and signs are folded into four
+// factors per pair that a warp computes once for all the heads of a kind (queries, keys, values) it takes of a token,
+//   z_a = inv (a f_a + b g_a),  z_b = inv (b f_b + a g_b),
+// and the arithmetic runs two elements per instruction.
 #include <cuda_fp16.h>
 
 #include "internal.h"
+#include "tensor.cuh"
 
 namespace lzk {
 
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int kElems = 8;                          // elements of a row per lane
+constexpr int kStages = 4;                         // of a warp's ring of rows in shared memory
+constexpr int kStageBytes = 1024;                  // four rows of 16-bit elements, two of 32-bit ones
 
 struct RowsParams {
     RowsArgs a;
     double turns[kMaxPairs];                       // inv_freq / (2 pi)
-    int groups[3], per_warp[3];                    // per kind (q, k, v): row groups of a token, rows per group
-    int tasks_per_token;
-    long long tasks;
+    uint32_t groups[3], per_warp[3];               // per kind (q, k, v): row groups of a token, rows per group
+    uint32_t joint;                                // one warp takes all rows of a token, kind after kind
+    uint32_t tasks_per_token, row_tasks, tasks;    // warps for rows, then (paged) warps for 32 tokens' state words each
 };
 
-__device__ __forceinline__ void load8(const void* row, int dtype, int c, float (&x)[kElems]) {
-    if (dtype == kTypeF32) {
-        const float4* p = reinterpret_cast<const float4*>(row) + 2 * c;
-        const float4 a = p[0], b = p[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-        return;
+// Four elements as they come from memory, and as they go back.
+template <int kType>
+struct Quad {
+    uint32_t w[kType == kTypeF32 ? 4 : 2];
+    __device__ __forceinline__ void load(uint32_t smem) {
+        if constexpr (kType == kTypeF32)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(smem) : "memory");
+        else
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(smem) : "memory");
     }
-    const uint4 v = reinterpret_cast<const uint4*>(row)[c];
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    __device__ __forceinline__ void unpack(float (&x)[4]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (dtype == kTypeBF16) {
-            x[2 * i] = bf16_lo_as_float(w[i]);
-            x[2 * i + 1] = bf16_hi_as_float(w[i]);
-        } else {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-            x[2 * i] = f.x;
-            x[2 * i + 1] = f.y;
+        for (int i = 0; i < 2; ++i) {
+            if constexpr (kType == kTypeF32) {
+                x[2 * i] = __uint_as_float(w[2 * i]);
+                x[2 * i + 1] = __uint_as_float(w[2 * i + 1]);
+            } else if constexpr (kType == kTypeBF16) {
+                x[2 * i] = bf16_lo_as_float(w[i]);
+                x[2 * i + 1] = bf16_hi_as_float(w[i]);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                x[2 * i] = f.x;
+                x[2 * i + 1] = f.y;
+            }
         }
     }
-}
+};
 
-__device__ __forceinline__ uint4 pack8_bf16(const float (&y)[kElems]) {
-    return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-}
-
-__device__ __forceinline__ void store8(void* row, int dtype, int c, const float (&y)[kElems]) {
-    if (dtype == kTypeF32) {
-        float4* p = reinterpret_cast<float4*>(row) + 2 * c;
-        p[0] = make_float4(y[0], y[1], y[2], y[3]);
-        p[1] = make_float4(y[4], y[5], y[6], y[7]);
-    } else if (dtype == kTypeBF16) {
-        reinterpret_cast<uint4*>(row)[c] = pack8_bf16(y);
+template <int kType>
+__device__ __forceinline__ void store4(uint8_t* p, const float (&x)[4]) {
+    if constexpr (kType == kTypeF32) {
+        *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    } else if constexpr (kType == kTypeBF16) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
     } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __half2 h = __floats2half2_rn(y[2 * i], y[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-        reinterpret_cast<uint4*>(row)[c] = make_uint4(w[0], w[1], w[2], w[3]);
+        const __half2 h0 = __floats2half2_rn(x[0], x[1]), h1 = __floats2half2_rn(x[2], x[3]);
+        *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
     }
 }
 
-__device__ __forceinline__ const uint8_t* row_at(const RowView& v, int l, int b, int i, int head) {
-    return reinterpret_cast<const uint8_t*>(v.data) +
-           (l * v.stride_layer + b * v.stride_batch + i * v.stride_token + head * v.stride_head) * (v.dtype == kTypeF32 ? 4 : 2);
+// Where a warp's rows come from and go to: heads one after the other, this lane's two groups of four elements.
+struct WarpRows {
+    int heads;
+    int src_a, src_b;                               // bytes of the groups in a row of the input
+    uint8_t* dst;                                   // first group of the first head
+    long long dst_step;
+    int dst_b;                                      // bytes from the first group to the second
+    int32_t page;                                   // kPaged: lane h's is head h's; and the byte offsets in a page
+    uint32_t page_a, page_b;
+};
+
+__device__ __forceinline__ void copy16(uint32_t smem, const uint8_t* src, bool on) {     // zeros where `on` is false
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(__cvta_generic_to_global(src)), "r"(on ? 16 : 0) : "memory");
 }
 
-__global__ void __launch_bounds__(kRowThreads) rows_kernel(const __grid_constant__ RowsParams p) {
+struct Factors {
+    uint64_t fa[2], ga[2], fb[2], gb[2];           // two fp32 each
+};
+
+// The rows of a warp go through a ring of asynchronous copies: what limits a plain loop is the latency of its loads, since a
+// warp's factors leave registers for few rows in flight.  A row is copied before it is written (in place).
+template <int kIn>
+struct RowRing {
+    static constexpr int kRowIn = kHeadDim * (kIn == kTypeF32 ? 4 : 2);
+    static constexpr int kRows = kStageBytes / kRowIn;                     // per stage
+    static constexpr int kChunks = kRowIn / 16;
+    uint32_t base, put, get;
+    const uint8_t* src;                             // this lane's first 16-byte chunk of the next stage
+    long long step, far;                            // bytes from stage to stage, to the lane's second chunk
+    int to_fetch;                                   // rows of the segment not fetched yet
+
+    __device__ __forceinline__ void init(uint32_t ring) {
+        const int lane = threadIdx.x & 31;
+        base = ring;
+        put = ring + lane * 16;
+        get = ring + (lane >> 4) * kRowIn;
+        to_fetch = 0;
+    }
+    // The next rows to fetch: one kind's heads.
+    __device__ __forceinline__ void segment(const uint8_t* first, long long row_step, int rows) {
+        const int lane = threadIdx.x & 31, row0 = lane / kChunks, row1 = (lane + 32) / kChunks;
+        src = first + (lane % kChunks) * 16 + row0 * row_step;
+        far = (row1 - row0) * row_step;
+        step = kRows * row_step;
+        to_fetch = rows;
+    }
+    // One stage of the segment (nothing when it is exhausted).
+    __device__ __forceinline__ void fetch() {
+        if (to_fetch > 0) {
+            const int lane = threadIdx.x & 31;
+            copy16(put, src, lane / kChunks < to_fetch);
+            copy16(put + 512, src + far, (lane + 32) / kChunks < to_fetch);
+            src += step;
+            to_fetch -= kRows;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        put = put + kStageBytes < base + kStages * kStageBytes ? put + kStageBytes : base + (threadIdx.x & 31) * 16;
+    }
+    __device__ __forceinline__ void wait() {        // the oldest stage has arrived, and the one before it is read
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();
+    }
+    __device__ __forceinline__ void next() {
+        get = get + kStageBytes < base + kStages * kStageBytes ? get + kStageBytes : get - (kStages - 1) * kStageBytes;
+    }
+};
+
+// Queries or keys.  `refill` fetches the stage that follows those in flight.
+template <int kIn, int kOut, bool kInterleaved, bool kPaged, class Refill>
+__device__ __forceinline__ void turn_rows(const RowsArgs& a, const WarpRows& r, bool norm, bool turns, const Factors& f, RowRing<kIn>& ring,
+                                          Refill refill) {
+    constexpr int kRowIn = RowRing<kIn>::kRowIn, kRows = RowRing<kIn>::kRows, kBatch = kRows / 2;      // rows per half-warp
+    const int half = (threadIdx.x >> 4) & 1;
+    uint8_t* dst = kPaged ? nullptr : r.dst + half * r.dst_step;
+    const float mean = 1.f / kHeadDim;
+    for (int left = r.heads - half; left + half > 0; left -= kRows) {
+        ring.wait();
+        refill();
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            Quad<kIn> qa, qb;
+            qa.load(ring.get + 2 * k * kRowIn + r.src_a);
+            qb.load(ring.get + 2 * k * kRowIn + r.src_b);
+            const int32_t pp = kPaged ? __shfl_sync(0xffffffffu, r.page, r.heads - left + 2 * k) : 0;
+            float xa[4], xb[4];
+            qa.unpack(xa);
+            qb.unpack(xb);
+            uint64_t va[2], vb[2];                  // the pairs' first elements, their second ones
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float* x = i ? xb : xa;
+                va[i] = kInterleaved ? pack2(x[0], x[2]) : pack2(xa[2 * i], xa[2 * i + 1]);
+                vb[i] = kInterleaved ? pack2(x[1], x[3]) : pack2(xb[2 * i], xb[2 * i + 1]);
+            }
+            float inv = 1.f;
+            if (norm) {
+                float s0, s1;
+                unpack2(add2(fma2(va[0], va[0], mul2(va[1], va[1])), fma2(vb[0], vb[0], mul2(vb[1], vb[1]))), s0, s1);
+                float ss = s0 + s1;
+#pragma unroll
+                for (int s = 1; s < 16; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+                inv = rsqrtf(fmaf(ss, mean, a.eps));
+            }
+            const uint64_t inv2 = pack2(inv, inv);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint64_t ua = mul2(va[i], f.fa[i]), ub = mul2(vb[i], f.fb[i]);
+                if (turns) {                        // (elements that stay must not meet others: 0 * inf)
+                    ua = fma2(vb[i], f.ga[i], ua);
+                    ub = fma2(va[i], f.gb[i], ub);
+                }
+                float z0, z1, z2, z3;
+                unpack2(mul2(ua, inv2), z0, z1);
+                unpack2(mul2(ub, inv2), z2, z3);
+                if constexpr (kInterleaved) {
+                    float* x = i ? xb : xa;
+                    x[0] = z0; x[1] = z2; x[2] = z1; x[3] = z3;
+                } else {
+                    xa[2 * i] = z0; xa[2 * i + 1] = z1;
+                    xb[2 * i] = z2; xb[2 * i + 1] = z3;
+                }
+            }
+            if (left > 2 * k) {
+                if constexpr (!kPaged) {
+                    store4<kOut>(dst, xa);
+                    store4<kOut>(dst + r.dst_b, xb);
+                } else if (in_bounds(pp >= 0 && pp < a.total_pages, a.status)) {
+                    uint8_t* page = a.pool + (size_t)pp * kPageBytes;
+                    store4<kTypeBF16>(page + r.page_a, xa);
+                    store4<kTypeBF16>(page + r.page_b, xb);
+                }
+            }
+            if constexpr (!kPaged) dst += 2 * r.dst_step;
+        }
+        ring.next();
+    }
+}
+
+// Values: 16 bytes of bf16 per lane, bits as they are or rounded.  `at`: this lane's byte offset in a page.
+template <int kIn, class Refill>
+__device__ __forceinline__ void copy_rows(const RowsArgs& a, int heads, int32_t page_of, uint32_t at, RowRing<kIn>& ring, Refill refill) {
+    constexpr int kRowIn = RowRing<kIn>::kRowIn, kRows = RowRing<kIn>::kRows, kBatch = kRows / 2;
+    const int half = (threadIdx.x >> 4) & 1, c = threadIdx.x & 15;
+    for (int left = heads - half; left + half > 0; left -= kRows) {
+        ring.wait();
+        refill();
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            uint4 v;
+            const uint32_t from = ring.get + 2 * k * kRowIn + c * (kRowIn / 16);
+            if constexpr (kIn == kTypeBF16) {
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+            } else {
+                Quad<kIn> q0, q1;
+                q0.load(from);
+                q1.load(from + kRowIn / 32);
+                float x[4], y[4];
+                q0.unpack(x);
+                q1.unpack(y);
+                v = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+            }
+            const int32_t pp = __shfl_sync(0xffffffffu, page_of, heads - left + 2 * k);
+            if (left > 2 * k && in_bounds(pp >= 0 && pp < a.total_pages, a.status))
+                *reinterpret_cast<uint4*>(a.pool + (size_t)pp * kPageBytes + at) = v;
+        }
+        ring.next();
+    }
+}
+
+// One input type and one type of the output views per launch; keys and values go to the pages when there is a pool.
+template <int kIn, int kOut, bool kInterleaved>
+__global__ void __launch_bounds__(kRowThreads, kIn == kTypeF32 ? 3 : 3) rows_kernel(const __grid_constant__ RowsParams p) {
+    __shared__ __align__(16) uint8_t rings[kRowThreads / 32][kStages * kStageBytes];
     const RowsArgs& a = p.a;
     const int lane = threadIdx.x & 31, half = lane >> 4, c = lane & 15;
-    const long long task = (long long)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+    const uint32_t task = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
     if (task >= p.tasks) return;
-    const long long tk = task / p.tasks_per_token;
-    int grp = (int)(task - tk * p.tasks_per_token);
-    int kind = 0;                                   // 0: queries, 1: keys, 2: values
-    while (grp >= p.groups[kind]) grp -= p.groups[kind++];
-    const int heads = kind == 0 ? a.q_heads : a.kv_heads;
-    const int i = (int)(tk % a.n_tokens);
-    const int lb = (int)(tk / a.n_tokens), l = lb / a.batch, b = lb % a.batch;
-    const RowView& in = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-    const int head0 = grp * p.per_warp[kind];
-    const int head_end = min(heads, head0 + p.per_warp[kind]);
-
-    // where this lane's elements 8 c .. 8 c + 7 take part in the rotation
-    const bool turns = kind < 2 && 8 * c < 2 * a.pairs;
-    const int shift = turns && !a.interleaved ? (8 * c < a.pairs ? a.pairs / 8 : -(a.pairs / 8)) : 0;   // chunk of the partners
-    float f[kElems], g[kElems];
-#pragma unroll
-    for (int e = 0; e < kElems; ++e) {
-        f[e] = 1.f;
-        g[e] = 0.f;
+    if (task >= p.row_tasks) {
+        // state words of 32 new tokens, unit by unit: active at their own step, MRI = 0 (Section 4)
+        const uint32_t at = (task - p.row_tasks) * 32 + lane, u = at / (uint32_t)a.n_tokens;
+        const int i = (int)(at - u * a.n_tokens);
+        if (u >= (uint32_t)(a.layers * a.batch * a.kv_heads)) return;
+        if (!in_bounds(a.slot + i >= 0 && a.slot + i < a.capacity, a.status)) return;
+        const size_t s = (size_t)u * a.capacity + a.slot + i;
+        a.tsm[s] = make_int2(a.ts, 0);
+        a.pos[s] = a.pos_first + i;
+        a.pbar[s] = 0.f;
+        return;
     }
-    const float* w = kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
+    const uint32_t tk = task / p.tasks_per_token;
+    uint32_t grp = task - tk * p.tasks_per_token;
+    int kind = 0;                                   // 0: queries, 1: keys, 2: values
+    if (!p.joint)
+        while (grp >= p.groups[kind]) grp -= p.groups[kind++];
+    int fetch_kind = kind;
+    if (p.joint) kind = fetch_kind = a.q.data ? 0 : 1;
+    const int last_kind = !p.joint ? kind : a.v.data ? 2 : a.k.data ? 1 : 0;
+    const int lb = (int)(tk / (uint32_t)a.n_tokens), i = (int)(tk - (uint32_t)lb * a.n_tokens);
+    const int l = lb / a.batch, b = lb - l * a.batch;
+    // Groups of four elements: with pairs (j, j + pairs) group c of the first `pairs` elements and its partners, then the
+    // groups that do not rotate two by two; with pairs (2 j, 2 j + 1) two neighbouring groups.
+    const int low = kInterleaved ? 0 : a.pairs / 4;
+    const int qa = c < low ? c : 2 * low + 2 * (c - low), qb = c < low ? c + low : qa + 1;
+    const bool turns = kInterleaved ? 4 * c < a.pairs : c < low;
+
+    // The copies of the first rows run while the angles are computed, and go on from kind to kind without a break.
+    RowRing<kIn> ring;
+    auto heads_of = [&](int k) { return min((k == 0 ? a.q_heads : a.kv_heads) - (int)(grp * p.per_warp[k]), (int)p.per_warp[k]); };
+    auto refill = [&]() {
+        if (ring.to_fetch <= 0 && fetch_kind <= last_kind) {
+            const RowView& in = fetch_kind == 0 ? a.q : fetch_kind == 1 ? a.k : a.v;
+            const long long bytes = kIn == kTypeF32 ? 4 : 2;
+            ring.segment(reinterpret_cast<const uint8_t*>(in.data) +
+                             (l * in.stride_layer + b * in.stride_batch + i * in.stride_token + (int)(grp * p.per_warp[fetch_kind]) * in.stride_head) * bytes,
+                         in.stride_head * bytes, heads_of(fetch_kind));
+            ++fetch_kind;
+        }
+        ring.fetch();
+    };
+    ring.init(smem_u32(rings[threadIdx.x >> 5]));
+#pragma unroll 1
+    for (int st = 0; st < kStages - 1; ++st) refill();
+    // keys and values: where the token's slot is in the pages of its heads (lane h: head h)
+    int32_t page = 0;
+    uint32_t slot_row = 0;
+    if (last_kind > 0 && a.pool != nullptr) {
+        const int slot = a.slot + i, head0 = (int)(grp * p.per_warp[last_kind]);
+        if (!in_bounds(slot >= 0 && slot < a.capacity, a.status)) return;
+        slot_row = slot % kPageTokens;
+        if (lane < heads_of(last_kind)) page = a.page_table[((size_t)lb * a.kv_heads + head0 + lane) * a.pages_per_unit + slot / kPageTokens];
+    }
+    float cv[4] = {1.f, 1.f, 1.f, 1.f}, sv[4] = {};
     if (kind < 2 && a.pairs > 0) {
+        // this lane's pairs are 4 c .. 4 c + 3; the two halves of the warp need the same angles and compute two each
         const double pos = (double)(a.positions ? a.positions[(size_t)b * a.n_tokens + i] : (long long)a.first_position + i);
-        // Every angle is needed by several lanes (both halves of the warp; both partners): each computes two.
         float cs[2], sn[2];
-        const int j0 = a.interleaved ? 4 * c + 2 * half : 8 * (c % max(a.pairs / 8, 1)) + 4 * half + 2 * (shift < 0);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const double t = pos * p.turns[min(j0 + e, kMaxPairs - 1)];
+            const double t = pos * p.turns[4 * c + 2 * half + e];
             sincospif(2.f * (float)(t - rint(t)), &sn[e], &cs[e]);
-            sn[e] *= a.amplitude;
             cs[e] *= a.amplitude;
+            sn[e] *= a.amplitude;
         }
-        if (a.interleaved) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float cv = __shfl_sync(0xffffffffu, cs[e & 1], (e >> 1) * 16 + c);
-                const float sv = __shfl_sync(0xffffffffu, sn[e & 1], (e >> 1) * 16 + c);
-                if (turns) {
-                    f[2 * e] = f[2 * e + 1] = cv;
-                    g[2 * e] = -sv;
-                    g[2 * e + 1] = sv;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < kElems; ++e) {
-                const int k = e >> 1;               // computed by half k / 2, by the lower partner (k even) or the upper one
-                const int src = turns ? (k >> 1) * 16 + c % (a.pairs / 8) + (k & 1) * (a.pairs / 8) : lane;
-                const float cv = __shfl_sync(0xffffffffu, cs[e & 1], src);
-                const float sv = __shfl_sync(0xffffffffu, sn[e & 1], src);
-                if (turns) {
-                    f[e] = cv;
-                    g[e] = shift > 0 ? -sv : sv;
-                }
-            }
-        }
-    }
-    if (w) {
-        w += (size_t)l * kHeadDim;
-#pragma unroll
-        for (int e = 0; e < kElems; ++e) {
-            f[e] *= w[8 * c + e];
-            g[e] *= a.interleaved ? w[8 * c + (e ^ 1)] : w[8 * (c + shift) + e];
+        for (int e = 0; e < 4; ++e) {
+            const float x = __shfl_sync(0xffffffffu, cs[e & 1], (e >> 1) * 16 + c), y = __shfl_sync(0xffffffffu, sn[e & 1], (e >> 1) * 16 + c);
+            cv[e] = turns ? x : 1.f;
+            sv[e] = turns ? y : 0.f;
         }
     }
 
-    for (int head = head0 + half; head < head_end; head += 2) {
-        const uint32_t mask = head - half + 1 < head_end ? 0xffffffffu : 0x0000ffffu;     // an odd row at the end
-        const uint8_t* row = row_at(in, l, b, i, head);
-        float x[kElems], y[kElems];
-        load8(row, in.dtype, c, x);
-        if (a.interleaved || shift == 0) {
-#pragma unroll
-            for (int e = 0; e < kElems; ++e) y[e] = turns ? x[e ^ 1] : 0.f;
-        } else {
-            load8(row, in.dtype, c + shift, y);
+    for (; kind <= last_kind; ++kind) {
+        if (kind == 2) {
+            copy_rows<kIn>(a, heads_of(2), page, kPageHalfBytes + slot_row * kRowBytes + swz_chunk(c, (int)slot_row) * 16, ring, refill);
+            break;
         }
-        float inv = 1.f;
-        if (w) {
-            float ss = 0.f;
-#pragma unroll
-            for (int e = 0; e < kElems; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-            for (int s = 1; s < 16; s <<= 1) ss += __shfl_xor_sync(mask, ss, s);
-            inv = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
-        }
-#pragma unroll
-        for (int e = 0; e < kElems; ++e) x[e] = inv * fmaf(y[e], g[e], x[e] * f[e]);
-        __syncwarp(mask);                           // in place: every lane has read its partner's elements
-        if (kind == 0 || a.pool == nullptr) {
+        constexpr int kInBytes = kIn == kTypeF32 ? 4 : 2, kOutBytes = kOut == kTypeF32 ? 4 : 2;
+        const bool paged = kind > 0 && a.pool != nullptr;
+        WarpRows r;
+        r.heads = heads_of(kind);
+        r.src_a = 4 * qa * kInBytes;
+        r.src_b = 4 * qb * kInBytes;
+        if (!paged) {
             const RowView& out = kind == 0 ? a.q_out : a.k_out;
-            store8(const_cast<uint8_t*>(row_at(out, l, b, i, head)), out.dtype, c, x);
+            r.dst_step = out.stride_head * kOutBytes;
+            r.dst = reinterpret_cast<uint8_t*>(const_cast<void*>(out.data)) +
+                    (l * out.stride_layer + b * out.stride_batch + i * out.stride_token + (int)(grp * p.per_warp[kind]) * out.stride_head + 4 * qa) * kOutBytes;
+            r.dst_b = 4 * (qb - qa) * kOutBytes;
         } else {
-            const size_t u = (size_t)lb * a.kv_heads + head;
-            const int slot = a.slot + i, r = slot % kPageTokens;
-            if (!in_bounds(slot >= 0 && slot < a.capacity, a.status)) continue;
-            const int32_t pp = a.page_table[u * a.pages_per_unit + slot / kPageTokens];
-            if (!in_bounds(pp >= 0 && pp < a.total_pages, a.status)) continue;
-            uint8_t* dst = a.pool + (size_t)pp * kPageBytes + (kind == 1 ? 0 : kPageHalfBytes) + r * kRowBytes;
-            *reinterpret_cast<uint4*>(dst + swz_chunk(c, r) * 16) = pack8_bf16(x);
-            if (kind == 1 && c == 0) {              // a new token: active at its own step, MRI = 0
-                const size_t s = u * a.capacity + slot;
-                a.tsm[s] = make_int2(a.ts, 0);
-                a.pos[s] = a.pos_first + i;
-                a.pbar[s] = 0.f;
+            r.page = page;
+            r.page_a = slot_row * kRowBytes + swz_chunk(qa >> 1, (int)slot_row) * 16 + (qa & 1) * 8;
+            r.page_b = slot_row * kRowBytes + swz_chunk(qb >> 1, (int)slot_row) * 16 + (qb & 1) * 8;
+        }
+        float wa[4] = {1.f, 1.f, 1.f, 1.f}, wb[4] = {1.f, 1.f, 1.f, 1.f};
+        const float* w = kind == 0 ? a.q_weight : a.k_weight;
+        if (w) {
+            const float4 va = reinterpret_cast<const float4*>(w + (size_t)l * kHeadDim)[qa];
+            const float4 vb = reinterpret_cast<const float4*>(w + (size_t)l * kHeadDim)[qb];
+            const float x[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                wa[e] = x[kInterleaved ? 2 * e : e];
+                wb[e] = x[kInterleaved ? 2 * e + 1 : 4 + e];
             }
         }
+        Factors f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            f.fa[e] = pack2(wa[2 * e] * cv[2 * e], wa[2 * e + 1] * cv[2 * e + 1]);
+            f.gb[e] = pack2(wa[2 * e] * sv[2 * e], wa[2 * e + 1] * sv[2 * e + 1]);
+            f.fb[e] = pack2(wb[2 * e] * cv[2 * e], wb[2 * e + 1] * cv[2 * e + 1]);
+            f.ga[e] = pack2(-wb[2 * e] * sv[2 * e], -wb[2 * e + 1] * sv[2 * e + 1]);
+        }
+        if (paged)
+            turn_rows<kIn, kOut, kInterleaved, true>(a, r, w != nullptr, turns, f, ring, refill);
+        else
+            turn_rows<kIn, kOut, kInterleaved, false>(a, r, w != nullptr, turns, f, ring, refill);
     }
+}
+
+template <int kIn, int kOut>
+void launch(const RowsParams& p, uint32_t blocks, cudaStream_t stream) {
+    if (p.a.interleaved)
+        rows_kernel<kIn, kOut, true><<<blocks, kRowThreads, 0, stream>>>(p);
+    else
+        rows_kernel<kIn, kOut, false><<<blocks, kRowThreads, 0, stream>>>(p);
+}
+
+template <int kIn>
+void launch(const RowsParams& p, int out, uint32_t blocks, cudaStream_t stream) {
+    if (out == kTypeF32)
+        launch<kIn, kTypeF32>(p, blocks, stream);
+    else if (out == kTypeF16)
+        launch<kIn, kTypeF16>(p, blocks, stream);
+    else
+        launch<kIn, kTypeBF16>(p, blocks, stream);
 }
 
 }  // namespace
@@ -208,16 +404,37 @@ cudaError_t rows_launch(const RowsArgs& a, const double* inv_freq, int num_sms, 
     for (int j = 0; j < kMaxPairs; ++j) p.turns[j] = j < a.pairs ? inv_freq[j] / 6.283185307179586476925 : 0.0;
     const int heads[3] = {a.q.data ? a.q_heads : 0, a.k.data ? a.kv_heads : 0, a.v.data ? a.kv_heads : 0};
     const long long tokens = (long long)a.layers * a.batch * a.n_tokens;
-    p.tasks_per_token = 0;
+    // Rows per warp: all rows of a token, so that its angles and pages are found once (a warp knows the pages of 32 heads); or,
+    // as long as that leaves SMs without 16 warps, fewer and fewer heads of a kind, two at least (a warp takes two rows at a time).
+    const long long enough = 16ll * num_sms;
+    p.joint = a.kv_heads <= 32 && tokens >= enough;
+    p.tasks_per_token = 1;
     for (int k = 0; k < 3; ++k) {
-        p.per_warp[k] = 2;
-        p.groups[k] = (heads[k] + 1) / 2;
-        p.tasks_per_token += p.groups[k];
+        p.per_warp[k] = heads[k];
+        p.groups[k] = 0;
     }
-    p.tasks = tokens * p.tasks_per_token;
-    const long long blocks = (p.tasks + kRowThreads / 32 - 1) / (kRowThreads / 32);
-    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-    rows_kernel<<<(unsigned)blocks, kRowThreads, 0, stream>>>(p);
+    for (int most = 32; !p.joint; most /= 2) {
+        p.tasks_per_token = 0;
+        for (int k = 0; k < 3; ++k) {
+            p.per_warp[k] = most;
+            p.groups[k] = (heads[k] + most - 1) / most;
+            p.tasks_per_token += p.groups[k];
+        }
+        if (most == 2 || tokens * p.tasks_per_token >= enough) break;
+    }
+    const long long row_tasks = tokens * p.tasks_per_token;
+    const long long state_tasks = a.pool ? (tokens * a.kv_heads + 31) / 32 : 0;
+    if (row_tasks + state_tasks > 0x7fffffffll) return cudaErrorInvalidValue;
+    p.row_tasks = (uint32_t)row_tasks;
+    p.tasks = (uint32_t)(row_tasks + state_tasks);
+    const uint32_t blocks = (p.tasks + kRowThreads / 32 - 1) / (kRowThreads / 32);
+    const int in = a.q.data ? a.q.dtype : a.k.dtype, out = a.q_out.data ? a.q_out.dtype : a.k_out.dtype;
+    if (in == kTypeF32)
+        launch<kTypeF32>(p, out, blocks, stream);
+    else if (in == kTypeF16)
+        launch<kTypeF16>(p, out, blocks, stream);
+    else
+        launch<kTypeBF16>(p, out, blocks, stream);
     return cudaGetLastError();
 }
 
