@@ -1249,11 +1249,13 @@ int lazyev_attach_prefix(lazyev_t* h, lazyev_t* prefix, void* workspace) {
     if (e == cudaSuccess) e = cudaEventRecord(ready, prefix->stream);
     if (e == cudaSuccess) e = cudaStreamWaitEvent(h->stream, ready, 0);
     if (ready) cudaEventDestroy(ready);
+    float2* ml = (float2*)((uint8_t*)workspace + prefix_o_bytes(plan));
+    if (e == cudaSuccess) e = prefix_clear_launch(plan, ml, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "attach_prefix");
     h->shared = prefix;
     h->prefix_plan = plan;
     h->prefix_o = (float*)workspace;
-    h->prefix_ml = (float2*)((uint8_t*)workspace + prefix_o_bytes(plan));
+    h->prefix_ml = ml;
     h->pos_base = prefix->pos_base + prefix->prefill + prefix->t;
     prefix->users += 1;
     return LAZYEV_OK;

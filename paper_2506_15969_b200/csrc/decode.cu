@@ -382,38 +382,78 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
 
         // The shared prefix: its partial sums (reference, l, O per query row, one set per piece of the prefix) are
         // what a warp would hold after some of the pages, so the warps of the unit start from them instead of from
-        // nothing -- each from its share -- and the merge at the end of the unit needs to know nothing of them.
-        // The unit's log-sum-exp, hence pbar, covers the prefix like any cached token.
-        auto add_prefix = [&](int u, float& m0, float& m1, float& l0, float& l1, float (&o)[8][4]) {
-            const PrefixPlan& pl = p.prefix.plan;
-            const int hh = u % pl.kv_heads, lb = u / pl.kv_heads;          // lb: (layer, sequence)
-            const int pair = (lb % pl.share) / pl.tile_seqs / 2;
-            const long long x0 = ((long long)(lb / pl.share * pl.kv_heads + hh) * pl.pairs + pair) * pl.key_tiles;
-            const int pieces = prefix_block_of(pl, x0 + pl.key_tiles - 1) - prefix_block_of(pl, x0) + 1;
-            const int n_slots = 2 * pair + 1 < pl.tiles ? pieces : 2 * pieces;
-            for (int s = (int)rank * NW + warp; s < n_slots; s += S * NW) {
-                const long long row = s * pl.rows + (long long)u * G;
-                const float2 none = make_float2(-INFINITY, 0.f);
-                const float2 a0 = h0_on ? p.prefix.ml[row + h0] : none, a1 = h1_on ? p.prefix.ml[row + h1] : none;
-                const bool on0 = a0.x > -INFINITY, on1 = a1.x > -INFINITY;
-                const float* r0 = p.prefix.o + (row + h0) * kHeadDim + g;
-                const float* r1 = r0 + kHeadDim;
-                const float n0 = fmaxf(m0, a0.x), n1 = fmaxf(m1, a1.x);
-                const float c0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
-                const float d0 = on0 ? fast_exp2(a0.x - n0) : 0.f, d1 = on1 ? fast_exp2(a1.x - n1) : 0.f;
+        // nothing, and the merge at the end of the unit needs to know nothing of them.  Every warp takes its share of
+        // the 128 dimensions of every set (references are common, l is counted once); clustered blocks take the sets in
+        // turn.  The unit's log-sum-exp, hence pbar, covers the prefix like any cached token.  The first sets of the next
+        // unit are fetched while the current one streams (the latency of two dependent loads would be most of a short unit).
+        constexpr int kSets = kPrefix ? 2 : 1, kTiles = 8 / NW;      // m-tiles (16 dimensions) per warp
+        float2 pm0[kSets], pm1[kSets];
+        float po[kSets][kTiles][4];
+        auto load_set = [&](int u, int set, float2& m0, float2& m1, float (&v)[kTiles][4]) {
+            const int s = (int)rank + set * S;
+            m0 = m1 = make_float2(-INFINITY, 0.f);
+            if (s >= p.prefix.plan.slots) return;
+            const long long row = s * p.prefix.plan.rows + (long long)u * G;
+            const float* r0 = p.prefix.o + (row + h0) * kHeadDim + g;
+            if (h0_on) m0 = p.prefix.ml[row + h0];
+            if (h1_on) m1 = p.prefix.ml[row + h1];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    o[i][0] = o[i][0] * c0 + (on0 ? r0[16 * i] * d0 : 0.f);
-                    o[i][1] = o[i][1] * c1 + (on1 ? r1[16 * i] * d1 : 0.f);
-                    o[i][2] = o[i][2] * c0 + (on0 ? r0[16 * i + 8] * d0 : 0.f);
-                    o[i][3] = o[i][3] * c1 + (on1 ? r1[16 * i + 8] * d1 : 0.f);
-                }
-                l0 = l0 * c0 + (g == 0 ? a0.y * d0 : 0.f);          // l is a sum over the lanes of a column
-                l1 = l1 * c1 + (g == 0 ? a1.y * d1 : 0.f);
-                m0 = n0;
-                m1 = n1;
+            for (int i = 0; i < kTiles; ++i) {
+                const int d = 16 * (kTiles * warp + i);
+                v[i][0] = h0_on ? r0[d] : 0.f;
+                v[i][1] = h1_on ? r0[d + kHeadDim] : 0.f;
+                v[i][2] = h0_on ? r0[d + 8] : 0.f;
+                v[i][3] = h1_on ? r0[d + 8 + kHeadDim] : 0.f;
             }
         };
+        auto load_prefix = [&](int u) {
+#pragma unroll
+            for (int k = 0; k < kSets; ++k) load_set(u, k, pm0[k], pm1[k], po[k]);
+        };
+        auto add_set = [&](float2 a0, float2 a1, const float (&v)[kTiles][4], float& m0, float& m1, float& l0, float& l1, float (&o)[kTiles][4]) {
+            const bool on0 = a0.x > -INFINITY, on1 = a1.x > -INFINITY;       // what an absent set's O holds is anything
+            const float n0 = fmaxf(m0, a0.x), n1 = fmaxf(m1, a1.x);
+            const float c0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
+            const float d0 = on0 ? fast_exp2(a0.x - n0) : 0.f, d1 = on1 ? fast_exp2(a1.x - n1) : 0.f;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                o[i][0] = o[i][0] * c0 + (on0 ? v[i][0] * d0 : 0.f);
+                o[i][1] = o[i][1] * c1 + (on1 ? v[i][1] * d1 : 0.f);
+                o[i][2] = o[i][2] * c0 + (on0 ? v[i][2] * d0 : 0.f);
+                o[i][3] = o[i][3] * c1 + (on1 ? v[i][3] * d1 : 0.f);
+            }
+            const bool counts = warp == 0 && g == 0;                         // l is a sum over warps and the lanes of a column
+            l0 = l0 * c0 + (counts ? a0.y * d0 : 0.f);
+            l1 = l1 * c1 + (counts ? a1.y * d1 : 0.f);
+            m0 = n0;
+            m1 = n1;
+        };
+        auto add_prefix = [&](int u, float& m0, float& m1, float& l0, float& l1, float (&o)[8][4]) {
+            float sum[kTiles][4];
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) sum[i][0] = sum[i][1] = sum[i][2] = sum[i][3] = 0.f;
+#pragma unroll
+            for (int k = 0; k < kSets; ++k) add_set(pm0[k], pm1[k], po[k], m0, m1, l0, l1, sum);
+            constexpr int kMore = 6 / kTiles;                                // sets whose loads are in flight together
+            for (int k0 = kSets; (int)rank + k0 * S < p.prefix.plan.slots; k0 += kMore) {
+                float2 a0[kMore], a1[kMore];
+                float v[kMore][kTiles][4];
+#pragma unroll
+                for (int k = 0; k < kMore; ++k) load_set(u, k0 + k, a0[k], a1[k], v[k]);
+#pragma unroll
+                for (int k = 0; k < kMore; ++k) add_set(a0[k], a1[k], v[k], m0, m1, l0, l1, sum);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i / kTiles == warp) {
+                    o[i][0] = sum[i % kTiles][0];
+                    o[i][1] = sum[i % kTiles][1];
+                    o[i][2] = sum[i % kTiles][2];
+                    o[i][3] = sum[i % kTiles][3];
+                }
+        };
+        if constexpr (kPrefix)
+            if (my_units > 0) load_prefix(p.unit_begin + cluster_id);
 
         // Pages belong to the groups in turn (page pc of the block's walk to group pc mod NG, across unit
         // boundaries), and a warp looks at the barriers up to its own next page before it releases the
@@ -433,7 +473,10 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
             float o[8][4];      // O^T: [m-tile][(dim g, h0), (dim g, h1), (dim g + 8, h0), (dim g + 8, h1)]
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-            if constexpr (kPrefix) add_prefix(u, mref0, mref1, l0, l1, o);
+            if constexpr (kPrefix) {
+                add_prefix(u, mref0, mref1, l0, l1, o);
+                if (u + n_clusters < p.unit_end) load_prefix(u + n_clusters);
+            }
 
             // this group's pages of the unit: j = j0, j0 + NG, ...
             const int j0 = NG == 1 ? 0 : (int)((grp + NG - pc_mod) % NG);

@@ -6,7 +6,7 @@
 namespace lzk {
 
 // ---- attention over a shared prefix ------------------------------------------------------------------
-// How the prefix kernel's work is laid out; the decode kernel finds its partial sums by the same arithmetic.
+// How the prefix kernel's work is laid out.
 struct PrefixPlan {
     int kv_heads, batch;                // of the handle that decodes
     int share, group;                   // sequences per prefix sequence, query heads per KV head
@@ -26,7 +26,7 @@ __host__ __device__ __forceinline__ int prefix_block_of(const PrefixPlan& p, lon
 struct PrefixView {        // what the decode kernel adds to every unit: ml = null for none
     PrefixPlan plan;
     const float* o;        // [slots][rows][128], relative to m
-    const float2* ml;      // [slots][rows]: reference (log2 domain), sum of exp2(x - reference)
+    const float2* ml;      // [slots][rows]: reference (log2 domain, -inf: no such partial sum), sum of exp2(x - reference)
 };
 
 struct PrefixArgs {
@@ -43,6 +43,8 @@ struct PrefixArgs {
 };
 PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int group, int n, int num_sms);
 cudaError_t prefix_prepare();
+// Marks every partial sum as absent: a row has up to `slots` of them, and no launch writes those it has not.
+cudaError_t prefix_clear_launch(const PrefixPlan& plan, float2* ml, cudaStream_t stream);
 cudaError_t prefix_launch(const PrefixPlan& plan, const PrefixArgs& a, cudaStream_t stream);
 // Zeroes the slots behind the last token in every unit's last page.
 cudaError_t clear_tail_launch(const Geometry& geo, uint8_t* pool, StateView st, int n, cudaStream_t stream);

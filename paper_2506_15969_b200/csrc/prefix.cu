@@ -16,8 +16,8 @@
 // of 128 tokens) is cut into equal contiguous parts, one per block, so no wave is left half full; a row gets one
 // set of partial sums per block that worked on its item.
 //
-// Two streams of four softmax warps (thread = accumulator row) alternate on the tensor core: with two row tiles a
-// stream has a tile and every key tile; with one, the streams take the key tiles in turn and keep partial sums each.
+// Two streams of eight softmax warps (two threads per accumulator row) alternate on the tensor core: with two row tiles a
+// stream has a tile and every key tile; with one, the streams take the key tiles in turn and join their sums at the end.
 //   S = Q K^T (tcgen05.mma, operands in shared memory, accumulator in tensor memory), softmax against a reference that
 //   is raised -- and O rescaled in tensor memory -- only when a logit exceeds it by more than 2^8, P written over S
 //   as two bf16 terms (hi + lo: 16 mantissa bits, as in the other attention kernels here), O += P V with P as the
@@ -28,7 +28,7 @@
 // Pages keep 16-byte chunk c of row r at c ^ (r & 7) of every 128-byte half row.  A plain (unswizzled) TMA box of 64 rows x
 // 128 bytes therefore lands as a 128-byte-swizzled operand; a key tile is four boxes from two pages.
 //
-// Warp roles: warps 0-7 softmax and output, warp 8 TMA producer, warp 9 MMA issuer.  All mbarrier waits are bounded.
+// Warp roles: warps 0-15 softmax and output, warp 16 TMA producer, warp 17 MMA issuer.  All mbarrier waits are bounded.
 #include "internal.h"
 #include "tensor.cuh"
 
@@ -40,14 +40,15 @@ constexpr int kTile = 128;                         // rows of a row tile, keys o
 constexpr int kBoxBytes = kTile * 128;             // half an operand: 128 rows x 64 bf16
 constexpr int kOperandBytes = 2 * kBoxBytes;       // a 128 x 128 bf16 operand (32 KiB)
 constexpr int kRing = 5;                           // K and V tiles in flight, in the order they are used
-constexpr int kStreamThreads = 128;
-constexpr int kThreads = 2 * kStreamThreads + 64;
+constexpr int kStreamWarps = 8;                    // two warps per 32 accumulator rows, half of the columns each
+constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 1);
 constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the reference by
 
 constexpr int kOffQ = 0;                           // two row tiles
 constexpr int kOffRing = kOffQ + 2 * kOperandBytes;
 constexpr int kOffMisc = kOffRing + kRing * kOperandBytes;
-constexpr int kSmem = kOffMisc + 1024;
+constexpr int kOffExchange = kOffMisc + 1024;      // [2 streams][128 rows][2]: what the two threads of a row tell each other
+constexpr int kSmem = kOffExchange + 2048;
 
 constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;     // per stream: 128 columns of S / P, 128 of O
 
@@ -90,6 +91,27 @@ __device__ __forceinline__ Piece piece_at(const PrefixPlan& pl, long long x, lon
     return pc;
 }
 
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
+                 "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
+// 64 columns of the accumulator times a factor per row.
+__device__ __noinline__ void rescale(uint32_t cols, float f) {
+#pragma unroll 1
+    for (int c = 0; c < 64; c += 16) {
+        float o[16];
+        tmem_ld16(cols + c, o);
+        tmem_wait_ld();
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
+        tmem_st16(cols + c, w);
+    }
+    tmem_wait_st();
+}
+
 __global__ void __launch_bounds__(kThreads, 1)
 prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PrefixParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -104,7 +126,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             mbar_init(&bars->q_full[i], 1);
             mbar_init(&bars->q_empty[i], 1);
             mbar_init(&bars->s_full[i], 1);
-            mbar_init(&bars->p_full[i], 4);
+            mbar_init(&bars->p_full[i], kStreamWarps);
             mbar_init(&bars->o_full[i], 1);
         }
         for (int i = 0; i < kRing; ++i) {
@@ -130,7 +152,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     const unsigned long long limit = p.wait_limit_ns;
     const long long begin = (long long)blockIdx.x * pl.work / pl.blocks, end = ((long long)blockIdx.x + 1) * pl.work / pl.blocks;
 
-    if (warp == 8) {
+    if (warp == kProducer) {
         // ------------------------------------------------------------------ TMA producer
         if (lane == 0) {
             Ring rr, qr;
@@ -199,7 +221,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 drain(bars->q_full, qr, 2);
             }
         }
-    } else if (warp == 9) {
+    } else if (warp == kIssuer) {
         // ------------------------------------------------------------------ MMA issuer
         if (lane == 0) {
             Ring rr, qr;
@@ -288,16 +310,23 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
     } else {
         // ------------------------------------------------------------------ softmax and output
-        const int s = warp >> 2, row = threadIdx.x & 127;
+        // Accumulator row = TMEM lane; the warps w and w + 4 of a stream share 32 rows and take 64 of the 128 columns each (a
+        // row's chain of exponentials is what a stream's turn is made of: two threads halve it).
+        const int s = warp / kStreamWarps, hf = (warp >> 2) & 1, row = 32 * (warp & 3) + lane;
         const uint32_t lane_base = tmem_base + ((uint32_t)(32 * (warp & 3)) << 16);
-        const uint32_t s_cols = lane_base + kColS + s * 128, o_cols = lane_base + kColO + s * 128;
-        uint32_t s_uses = 0, o_uses = 0;
+        const uint32_t s_cols = lane_base + kColS + s * 128 + hf * 64, o_cols = lane_base + kColO + s * 128 + hf * 64;
+        float* mine = reinterpret_cast<float*>(smem + kOffExchange) + (s * kTile + row) * 2 + hf;
+        const float* other = reinterpret_cast<const float*>(smem + kOffExchange) + (s * kTile + row) * 2 + (hf ^ 1);
+        const int pair_bar = 1 + s * 4 + (warp & 3);                   // of the two warps
+        uint32_t s_uses = 0, o_uses[2] = {0, 0};
+        // A warp whose wait gives up goes on through the same loops, so that its partner's barriers get all their threads, but waits
+        // for nothing any more; what it computes means nothing.
         bool dead = false;
         auto wait_on = [&](uint64_t* bar, uint32_t parity) {
             const bool gave_up = dead || !wait_bar(bar, parity, abort_flag, p.status, limit);
-            dead = __any_sync(0xffffffffu, gave_up);      // a warp goes on, or leaves, as a whole
+            dead = __any_sync(0xffffffffu, gave_up);
         };
-        for (long long x = begin; x < end && !dead;) {
+        for (long long x = begin; x < end;) {
             const Piece pc = piece_at(pl, x, end);
             x += pc.tiles();
             const int nt = pc.stream_tiles(s);
@@ -305,51 +334,38 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const int r = row / pl.group;                              // sequence inside the row tile
             const int seq = tile * pl.tile_seqs + r;
             const bool valid = r < pl.tile_seqs && seq < pl.share;
-            const bool warp_on = __any_sync(0xffffffffu, valid);
+            const bool warp_on = __any_sync(0xffffffffu, valid);       // (the same in both warps of the rows)
             float m = -INFINITY, l = 0.f;
             for (int t = 0; t < nt; ++t) {
                 wait_on(&bars->s_full[s], s_uses & 1u);
-                if (dead) break;
                 ++s_uses;
                 tmem_fence_after_sync();
                 if (warp_on) {
-                    float v[4][32];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(s_cols + 32 * c, v[c]);
+                    float v[2][32];
+                    tmem_ld32(s_cols, v[0]);
+                    tmem_ld32(s_cols + 32, v[1]);
                     tmem_wait_ld();
-                    const int key0 = pc.key_tile(s, t) * kTile;
-                    if (key0 + kTile > p.n) {
+                    const int key0 = pc.key_tile(s, t) * kTile + hf * 64;
+                    if (key0 + 64 > p.n) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
+                        for (int c = 0; c < 2; ++c)
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[c][i] = key0 + 32 * c + i < p.n ? v[c][i] : -INFINITY;
                     }
-                    float mx = -INFINITY;
+                    float mx[4] = {v[0][0], v[0][1], v[1][0], v[1][1]};
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) mx = fmax3(mx, v[c][i], v[c][i + 1]);
-                    mx *= p.scale_log2;
-                    const bool raise = mx > m + kRaiseMargin;
-                    if (__any_sync(0xffffffffu, raise && valid)) {
-                        const float to = fmaxf(m, mx);
+                    for (int i = 2; i < 32; i += 2) {
+                        mx[(i >> 1) & 1] = fmax3(mx[(i >> 1) & 1], v[0][i], v[0][i + 1]);
+                        mx[2 + ((i >> 1) & 1)] = fmax3(mx[2 + ((i >> 1) & 1)], v[1][i], v[1][i + 1]);
+                    }
+                    // the row's maximum over both halves; both threads of the row take the same decisions from here on
+                    *mine = fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
+                    named_barrier_sync(pair_bar, 64);
+                    const float top = fmaxf(*mine, *other) * p.scale_log2;
+                    if (__any_sync(0xffffffffu, top > m + kRaiseMargin && valid)) {
+                        const float to = fmaxf(m, top);
                         const float f = m == to ? 1.f : fast_exp2(m - to);
-                        if (t > 0) {
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                float o[32];
-                                tmem_ld32(o_cols + 32 * c, o);
-                                tmem_wait_ld();
-                                uint32_t lo16[16], hi16[16];
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    lo16[i] = __float_as_uint(o[i] * f);
-                                    hi16[i] = __float_as_uint(o[16 + i] * f);
-                                }
-                                tmem_st16(o_cols + 32 * c, lo16);
-                                tmem_st16(o_cols + 32 * c + 16, hi16);
-                            }
-                        }
+                        if (t > 0) rescale(o_cols, f);
                         l *= f;
                         m = to;
                     }
@@ -357,14 +373,16 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), minus2 = pack2(-ref, -ref);
                     uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t hi[16], lo[16];
+                    for (int c = 0; c < 4; ++c) {                      // 16 columns at a time
+                        uint32_t hi[8], lo[8];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
+                        for (int i = 0; i < 8; ++i) {
+                            const float x0 = v[c >> 1][16 * (c & 1) + 2 * i], x1 = v[c >> 1][16 * (c & 1) + 2 * i + 1];
                             float e0, e1, d0, d1;
-                            unpack2(fma2(pack2(v[c][2 * i], v[c][2 * i + 1]), scale2, minus2), e0, e1);
-                            const uint64_t w = pack2(fast_exp2(e0), fast_exp2(e1));
-                            unpack2(w, e0, e1);
+                            unpack2(fma2(pack2(x0, x1), scale2, minus2), e0, e1);
+                            e0 = fast_exp2(e0);
+                            e1 = fast_exp2(e1);
+                            const uint64_t w = pack2(e0, e1);
                             hi[i] = pack_bf16(e0, e1);
                             unpack2(sub2(w, pack2(bf16_lo_as_float(hi[i]), bf16_hi_as_float(hi[i]))), d0, d1);
                             lo[i] = pack_bf16(d0, d1);
@@ -373,8 +391,9 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                             else
                                 sum0 = add2(sum0, w);
                         }
-                        tmem_st16(s_cols + 32 * c, hi);
-                        tmem_st16(s_cols + 32 * c + 16, lo);
+                        // a chunk of 32 keys: 16 columns of hi terms, then 16 of lo terms
+                        tmem_st8(s_cols + 32 * (c >> 1) + 8 * (c & 1), hi);
+                        tmem_st8(s_cols + 32 * (c >> 1) + 16 + 8 * (c & 1), lo);
                     }
                     float a0, a1;
                     unpack2(add2(sum0, sum1), a0, a1);
@@ -386,34 +405,63 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 if (lane == 0) mbar_arrive(&bars->p_full[s]);
             }
             // ---- the piece's partial sums
-            if (dead) break;
-            const long long item0 = pc.item * pl.key_tiles;
-            const int nth = (int)blockIdx.x - prefix_block_of(pl, item0);
-            const int slot = pc.both ? nth : 2 * nth + s;
+            const int nth = (int)blockIdx.x - prefix_block_of(pl, pc.item * pl.key_tiles);
             const long long unit = pc.item / pl.pairs;
             const long long u = (unit / pl.kv_heads * pl.share + seq) * pl.kv_heads + unit % pl.kv_heads;     // of the decoding handle
-            const long long at = slot * pl.rows + u * pl.group + (row - r * pl.group);
-            if (valid) p.ml[at] = make_float2(m, l);
-            if (nt > 0) {
-                wait_on(&bars->o_full[s], o_uses & 1u);
-                if (dead) break;
-                ++o_uses;
-                tmem_fence_after_sync();
-                if (warp_on) {
-                    float4* dst = reinterpret_cast<float4*>(p.o + at * kHeadDim);
+            const long long at = nth * pl.rows + u * pl.group + (row - r * pl.group);
+            // (the other stream's accumulator is needed where both work on the same rows; its phase is known to have begun:
+            // the MMAs of one thread complete in order)
+            const int nt_other = pc.both ? 0 : pc.stream_tiles(s ^ 1);
+            if (nt > 0) wait_on(&bars->o_full[s], o_uses[s] & 1u);
+            if (nt_other > 0) wait_on(&bars->o_full[s ^ 1], o_uses[s ^ 1] & 1u);
+            o_uses[0] += pc.stream_tiles(0) > 0;
+            o_uses[1] += pc.stream_tiles(1) > 0;
+            tmem_fence_after_sync();
+            if (warp_on) {
+                *mine = l;
+                named_barrier_sync(pair_bar, 64);
+                l += *other;
+                named_barrier_sync(pair_bar, 64);
+                float4* dst = reinterpret_cast<float4*>(p.o + at * kHeadDim);
+                if (pc.both) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < 2; ++c) {
                         float o[32];
                         tmem_ld32(o_cols + 32 * c, o);
                         tmem_wait_ld();
                         if (valid) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) dst[8 * c + i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                            for (int i = 0; i < 8; ++i) dst[16 * hf + 8 * c + i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        }
+                    }
+                } else {
+                    // the two streams' sums into one: four threads per row, 32 columns each
+                    *mine = hf ? l : m;
+                    named_barrier_sync(9 + (warp & 3), 128);
+                    const float2* ml = reinterpret_cast<const float2*>(smem + kOffExchange) + row;
+                    const float2 a0 = ml[0], a1 = ml[kTile];
+                    named_barrier_sync(9 + (warp & 3), 128);
+                    m = fmaxf(a0.x, a1.x);
+                    const float f0 = a0.x > -INFINITY ? fast_exp2(a0.x - m) : 0.f, f1 = a1.x > -INFINITY ? fast_exp2(a1.x - m) : 0.f;
+                    l = a0.y * f0 + a1.y * f1;
+                    const int col = 64 * s + 32 * hf;
+#pragma unroll
+                    for (int c = 0; c < 32; c += 16) {
+                        float o0[16], o1[16];
+                        tmem_ld16(lane_base + kColO + col + c, o0);
+                        tmem_ld16(lane_base + kColO + 128 + col + c, o1);
+                        tmem_wait_ld();
+                        if (valid) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o0[i] = o0[i] * f0 + (pc.tiles() > 1 ? o1[i] * f1 : 0.f);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) dst[(col + c) / 4 + i] = make_float4(o0[4 * i], o0[4 * i + 1], o0[4 * i + 2], o0[4 * i + 3]);
                         }
                     }
                 }
-                tmem_fence_before_sync();
             }
+            tmem_fence_before_sync();
+            if (valid && hf == 0 && (pc.both || s == 0)) p.ml[at] = make_float2(m, l);
         }
     }
 
@@ -440,12 +488,26 @@ PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int gr
     pl.work = (long long)layers * prefixes * kv_heads * pl.pairs * pl.key_tiles;
     pl.blocks = (int)(pl.work < num_sms ? pl.work : num_sms);
     pl.rows = (long long)layers * batch * kv_heads * group;
-    // most blocks that touch one item, and twice that where the streams keep partial sums each
+    // most blocks that touch one item
     const long long per = pl.work / pl.blocks;
     const long long pieces = (pl.key_tiles + per - 1) / per + 1;
-    const long long most = pieces < pl.blocks ? pieces : pl.blocks;
-    pl.slots = (int)(pl.tiles % 2 ? 2 * most : most);
+    pl.slots = (int)(pieces < pl.blocks ? pieces : pl.blocks);
     return pl;
+}
+
+namespace {
+
+__global__ void clear_sums_kernel(float2* ml, long long count) {
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < count) ml[i] = make_float2(-INFINITY, 0.f);
+}
+
+}  // namespace
+
+cudaError_t prefix_clear_launch(const PrefixPlan& plan, float2* ml, cudaStream_t stream) {
+    const long long count = plan.slots * plan.rows;
+    clear_sums_kernel<<<(unsigned)((count + 255) / 256), 256, 0, stream>>>(ml, count);
+    return cudaGetLastError();
 }
 
 cudaError_t prefix_prepare() {
