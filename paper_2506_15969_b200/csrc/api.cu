@@ -16,6 +16,7 @@
 
 using namespace lzk;
 
+constexpr int kDensePages = 4;            // own pages per unit up to which a block of a handle with a prefix walks two units at a time
 constexpr int kHostChunks = 3;            // unit ranges the host-buffer entry point pipelines copies over
 
 struct lazyev {
@@ -350,12 +351,14 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
                bool track = true) {
     cudaError_t e = cudaSuccess;
     DecodeConfig c{h->units, h->group, h->pages_per_unit, h->capacity, track ? h->alpha : INFINITY, h->force_splits, h->force_stages, h->force_groups,
-                   h->wait_limit_ns, h->stop_after_pages};
+                   h->wait_limit_ns, h->stop_after_pages, h->shared != nullptr, false};
     // Launch shape, chosen per number of pages in use and cached.  For every cluster size whose logits
     // fit, a small time model gives the time of the rounds of the round-robin walk; the main launch is
     // the size with the least total.  A partly filled last round goes to a second launch with larger
     // clusters when that is faster, so that more SMs share its units.
     const int np = (n + kPageTokens - 1) / kPageTokens;
+    // A unit of few pages is a chain of short dependent steps that leaves an SM idle most of the time.
+    c.dense = h->shared && np <= kDensePages && h->units > h->num_sms && h->force_splits == 0 && h->force_stages == 0 && h->force_groups == 0;
     auto cached = h->plan_cache.find(np);
     if (cached == h->plan_cache.end() || cached->second.forced_splits != h->force_splits ||
         cached->second.forced_stages != h->force_stages || cached->second.forced_groups != h->force_groups) {
@@ -524,7 +527,7 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     h->last_plan = plan;
     h->last_tail_units = shape.tail_units;
     h->last_tail_splits = shape.tail_splits;
-    h->last_grid = clusters * plan.splits;
+    h->last_grid = (clusters + plan.walkers - 1) / plan.walkers * plan.splits;
     return LAZYEV_OK;
 }
 
@@ -1216,6 +1219,7 @@ int detach(lazyev_t* h) {
     if (done) cudaEventDestroy(done);
     prefix->users -= 1;
     h->shared = nullptr;
+    h->plan_cache.clear();                 // launch shapes differ with and without a prefix
     if (e != cudaSuccess) return cuda_fail(h, e, "detach_prefix");
     return LAZYEV_OK;
 }
@@ -1252,6 +1256,7 @@ int lazyev_attach_prefix(lazyev_t* h, lazyev_t* prefix, void* workspace) {
     float2* ml = (float2*)((uint8_t*)workspace + prefix_o_bytes(plan));
     if (e == cudaSuccess) e = prefix_clear_launch(plan, ml, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "attach_prefix");
+    h->plan_cache.clear();
     h->shared = prefix;
     h->prefix_plan = plan;
     h->prefix_o = (float*)workspace;

@@ -48,6 +48,15 @@ struct Xchg {
     float l[kMaxGroup];                   // sum of exp2(x - m)
 };
 
+constexpr int kPrefixSets = 2;            // partial sums of a head that are fetched a unit ahead
+struct PrefixSet {
+    float o[kHeadDim];
+    float2 ml;
+    float2 pad;                           // 16-byte copies
+};
+constexpr int kQRowBytes = kRowBytes + 16;     // query rows in shared memory: a fragment load meets no bank twice
+constexpr int kPrefixBytes = kMaxGroup * (kPrefixSets * (int)sizeof(PrefixSet) + 2 * kQRowBytes);
+
 struct DecodeParams {
     uint8_t* pool;
     const int32_t* page_table;
@@ -60,7 +69,8 @@ struct DecodeParams {
     int n, t;
     float alpha, scale_log2, inv_group;
     int splits, stages, pages_per_cta, logit_stride, tmem_pages, tmem_cols;
-    int off_logits, off_xchg, off_wml, off_slots, off_misc, off_bars;
+    int off_logits, off_xchg, off_wml, off_slots, off_misc, off_prefix, off_bars;
+    int walker_bytes;                               // shared memory of a walker (blocks of two)
     unsigned long long wait_limit_ns;               // a wait that lasts this long is a failure, not a delay
     int stop_after_pages;                           // diagnostics: the producer issues no copy beyond this many (-1: off)
     int rounds_before;                              // rounds of the round-robin walk that earlier launches of this step took
@@ -106,12 +116,19 @@ __device__ __forceinline__ float ld_rank_f32(const float* local_ptr, uint32_t ra
 }
 
 // NG groups of four consumer warps plus one producer warp.  kPrefix: the softmax of every unit also runs over the
-// tokens of a shared prefix, whose partial sums an earlier launch left in p.prefix.
-template <int NG, bool kPrefix>
-__global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const DecodeParams p) {
+// tokens of a shared prefix, whose partial sums an earlier launch left in p.prefix.  kWalkers: two = the
+// block is two blocks in one, each with its own producer, ring, barriers and half of tensor memory, walking units of its own
+// (a unit of few pages is a chain of short dependent steps: two at a time fill the SM better, and two real blocks
+// would have to make do with 128 registers a thread).
+template <int NG, bool kPrefix, int kWalkers>
+__global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel(const DecodeParams p) {
     constexpr int NW = 4 * NG;
     constexpr int kConsumers = NW * 32;
-    extern __shared__ __align__(1024) uint8_t smem[];
+    static_assert(kWalkers == 1 || NG == 1, "");
+    extern __shared__ __align__(1024) uint8_t smem_block[];
+    const int hw_warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int walker = kWalkers > 1 ? hw_warp / (NW + 1) : 0, warp = kWalkers > 1 ? hw_warp % (NW + 1) : hw_warp;
+    uint8_t* smem = smem_block + (kWalkers > 1 ? walker * p.walker_bytes : 0);
     uint8_t* ring = smem;
     float* spill = reinterpret_cast<float*>(smem + p.off_logits);       // logits of the pages beyond tensor memory
     Xchg* xchg = reinterpret_cast<Xchg*>(smem + p.off_xchg);          // [2], alternating per unit
@@ -125,13 +142,13 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + p.off_bars);
     uint64_t* empty = full + p.stages;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int S = p.splits, NS = p.stages, G = p.group, LS = p.logit_stride;
     const bool clustered = S > 1;
     const uint32_t rank = clustered ? cluster_ctarank() : 0u;
-    const int cluster_id = blockIdx.x / S, n_clusters = gridDim.x / S;
+    const int cluster_id = kWalkers > 1 ? blockIdx.x * kWalkers + walker : blockIdx.x / S;
+    const int n_clusters = kWalkers > 1 ? gridDim.x * kWalkers : gridDim.x / S;
 
-    if (threadIdx.x == 0) {
+    if (warp == 0 && lane == 0) {
         for (int i = 0; i < NS; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 4);           // the four warps of the group that owns the page release it
@@ -139,14 +156,15 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 0) {                           // tensor memory for the logits: allocated and freed by warp 0
-        tmem_alloc(tmem_slot, (uint32_t)p.tmem_cols);
+    if (hw_warp == 0) {                        // tensor memory for the logits: allocated and freed by warp 0
+        tmem_alloc(tmem_slot, (uint32_t)(kWalkers * p.tmem_cols));
         tmem_relinquish_alloc_permit();
     }
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
-    const uint32_t tmem_base = *tmem_slot;
+    const uint32_t tmem_base = kWalkers > 1 ? *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(tmem_slot) - walker * p.walker_bytes) + walker * p.tmem_cols
+                                            : *tmem_slot;
     if (clustered) {   // every block of the cluster is resident before any remote access
         cluster_arrive();
         cluster_wait();
@@ -231,8 +249,9 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
         const int g = lane >> 2, qd = lane & 3;
         const int h0 = 2 * qd, h1 = h0 + 1;
         const bool h0_on = h0 < G, h1_on = h1 < G;
-        const int ctid = threadIdx.x;                 // consumer thread id: warps 0..NW-1
-        const int grp = warp >> 2, wq = warp & 3;
+        const int ctid = warp * 32 + lane;            // consumer thread id: warps 0..NW-1
+        const int grp = warp >> 2, wq = hw_warp & 3;  // (a warp reaches the tensor-memory lanes of its number modulo 4)
+        const int consumer_bar = 1 + walker;
         const uint32_t ring_base = smem_u32(ring);
         const uint32_t lrow = lane & 7;
         // ldmatrix row addresses.  K tile (16 tokens x 16 dims) as the A operand: matrices are
@@ -378,82 +397,146 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                 dst[ks][1] = g < G ? *reinterpret_cast<const uint32_t*>(qrow + 16 * ks + 8 + 2 * qd) : 0u;
             }
         };
-        if (my_units > 0) load_q(p.unit_begin + cluster_id, qb);
-
-        // The shared prefix: its partial sums (reference, l, O per query row, one set per piece of the prefix) are
-        // what a warp would hold after some of the pages, so the warps of the unit start from them instead of from
-        // nothing, and the merge at the end of the unit needs to know nothing of them.  Every warp takes its share of
-        // the 128 dimensions of every set (references are common, l is counted once); clustered blocks take the sets in
-        // turn.  The unit's log-sum-exp, hence pbar, covers the prefix like any cached token.  The first sets of the next
-        // unit are fetched while the current one streams (the latency of two dependent loads would be most of a short unit).
-        constexpr int kSets = kPrefix ? 2 : 1, kTiles = 8 / NW;      // m-tiles (16 dimensions) per warp
-        float2 pm0[kSets], pm1[kSets];
-        float po[kSets][kTiles][4];
-        auto load_set = [&](int u, int set, float2& m0, float2& m1, float (&v)[kTiles][4]) {
-            const int s = (int)rank + set * S;
-            m0 = m1 = make_float2(-INFINITY, 0.f);
-            if (s >= p.prefix.plan.slots) return;
-            const long long row = s * p.prefix.plan.rows + (long long)u * G;
-            const float* r0 = p.prefix.o + (row + h0) * kHeadDim + g;
-            if (h0_on) m0 = p.prefix.ml[row + h0];
-            if (h1_on) m1 = p.prefix.ml[row + h1];
+        if (!kPrefix && my_units > 0) load_q(p.unit_begin + cluster_id, qb);
+        // With a prefix there are no registers for the next unit's queries (a spilled load is waited for at once): they come
+        // through two buffers in shared memory, every warp copying some heads.
+        uint8_t* q_s = smem + p.off_prefix + kMaxGroup * kPrefixSets * sizeof(PrefixSet);
+        auto copy_q = [&](int u, int buf) {
+            const int h = warp * (kMaxGroup / NW) + (lane >> 4);            // two heads per warp, or one
+            if (h < G && (NW == 4 || lane < 16))
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(q_s + (buf * kMaxGroup + h) * kQRowBytes) + 16 * (lane & 15)),
+                             "l"(__cvta_generic_to_global(p.q + ((size_t)u * G + h) * kHeadDim + 8 * (lane & 15))) : "memory");
+        };
+        auto read_q = [&](int buf) {
+            const uint8_t* row = q_s + (buf * kMaxGroup + g) * kQRowBytes + 4 * qd;
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-                const int d = 16 * (kTiles * warp + i);
-                v[i][0] = h0_on ? r0[d] : 0.f;
-                v[i][1] = h1_on ? r0[d + kHeadDim] : 0.f;
-                v[i][2] = h0_on ? r0[d + 8] : 0.f;
-                v[i][3] = h1_on ? r0[d + 8 + kHeadDim] : 0.f;
+            for (int ks = 0; ks < 8; ++ks) {
+                qb[ks][0] = g < G ? *reinterpret_cast<const uint32_t*>(row + 32 * ks) : 0u;
+                qb[ks][1] = g < G ? *reinterpret_cast<const uint32_t*>(row + 32 * ks + 16) : 0u;
             }
         };
+
+        // The shared prefix: its partial sums (reference, l, O per query row, one set per piece of the prefix).  A block that owns
+        // its units folds them in when a warp finishes a head (fold_prefix): the first sets are fetched a unit ahead, since two
+        // dependent loads would be a third of the time of a short unit.  Clustered blocks (few units, then many sets)
+        // start from them instead of from nothing (add_prefix): every block of the cluster takes its share of the sets and every
+        // warp its share of the dimensions, with common references and l counted once, and the merge over the cluster
+        // needs to know nothing of it.  Either way the unit's log-sum-exp, hence pbar, covers the prefix like any cached token.
+        constexpr int kHeadsPerWarp = kMaxGroup / NW, kMore = 6;
+        // a warp's heads and their first sets: O, then (reference, l), copied asynchronously (they would not fit the registers)
+        PrefixSet* sets = reinterpret_cast<PrefixSet*>(smem + p.off_prefix) + warp * kHeadsPerWarp * kPrefixSets;
         auto load_prefix = [&](int u) {
 #pragma unroll
-            for (int k = 0; k < kSets; ++k) load_set(u, k, pm0[k], pm1[k], po[k]);
-        };
-        auto add_set = [&](float2 a0, float2 a1, const float (&v)[kTiles][4], float& m0, float& m1, float& l0, float& l1, float (&o)[kTiles][4]) {
-            const bool on0 = a0.x > -INFINITY, on1 = a1.x > -INFINITY;       // what an absent set's O holds is anything
-            const float n0 = fmaxf(m0, a0.x), n1 = fmaxf(m1, a1.x);
-            const float c0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
-            const float d0 = on0 ? fast_exp2(a0.x - n0) : 0.f, d1 = on1 ? fast_exp2(a1.x - n1) : 0.f;
+            for (int hh = 0; hh < kHeadsPerWarp; ++hh)
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-                o[i][0] = o[i][0] * c0 + (on0 ? v[i][0] * d0 : 0.f);
-                o[i][1] = o[i][1] * c1 + (on1 ? v[i][1] * d1 : 0.f);
-                o[i][2] = o[i][2] * c0 + (on0 ? v[i][2] * d0 : 0.f);
-                o[i][3] = o[i][3] * c1 + (on1 ? v[i][3] * d1 : 0.f);
+                for (int s = 0; s < kPrefixSets; ++s) {
+                    const int h = warp * kHeadsPerWarp + hh;
+                    if (h >= G || s >= p.prefix.plan.slots) continue;
+                    const long long row = s * p.prefix.plan.rows + (long long)u * G + h;
+                    PrefixSet* to = sets + hh * kPrefixSets + s;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to->o + 4 * lane)),
+                                 "l"(__cvta_generic_to_global(p.prefix.o + row * kHeadDim + 4 * lane)) : "memory");
+                    if (lane == 0)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(&to->ml)),
+                                     "l"(__cvta_generic_to_global(p.prefix.ml + row)) : "memory");
+                }
+        };
+        auto fold_set = [&](float2 ml, const float (&v)[4], float& m, float& l, float (&acc)[4]) {
+            if (ml.x == -INFINITY) return;          // no such set: what its O holds is anything
+            const float n = fmaxf(m, ml.x), c = m == -INFINITY ? 0.f : fast_exp2(m - n), f = fast_exp2(ml.x - n);
+            m = n;
+            l = l * c + ml.y * f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[k] = acc[k] * c + v[k] * f;
+        };
+        auto fold_prefix = [&](int u, int hh, float& m, float& l, float (&acc)[4]) {
+            float v[4];
+#pragma unroll
+            for (int s = 0; s < kPrefixSets; ++s)
+                if (s < p.prefix.plan.slots) {
+                    const PrefixSet* from = sets + hh * kPrefixSets + s;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = from->o[lane + 32 * k];
+                    fold_set(from->ml, v, m, l, acc);
+                }
+            for (int s0 = kPrefixSets; s0 < p.prefix.plan.slots; s0 += kMore) {
+                float2 ml[kMore];
+                float w[kMore][4];
+#pragma unroll
+                for (int s = 0; s < kMore; ++s) {
+                    ml[s] = make_float2(-INFINITY, 0.f);
+                    if (s0 + s >= p.prefix.plan.slots) continue;
+                    const long long row = (s0 + s) * p.prefix.plan.rows + (long long)u * G + warp * kHeadsPerWarp + hh;
+                    ml[s] = p.prefix.ml[row];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[s][k] = p.prefix.o[row * kHeadDim + lane + 32 * k];
+                }
+#pragma unroll
+                for (int s = 0; s < kMore; ++s) fold_set(ml[s], w[s], m, l, acc);
             }
-            const bool counts = warp == 0 && g == 0;                         // l is a sum over warps and the lanes of a column
-            l0 = l0 * c0 + (counts ? a0.y * d0 : 0.f);
-            l1 = l1 * c1 + (counts ? a1.y * d1 : 0.f);
-            m0 = n0;
-            m1 = n1;
         };
         auto add_prefix = [&](int u, float& m0, float& m1, float& l0, float& l1, float (&o)[8][4]) {
+            constexpr int kTiles = 8 / NW;          // m-tiles (16 dimensions) per warp
             float sum[kTiles][4];
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) sum[i][0] = sum[i][1] = sum[i][2] = sum[i][3] = 0.f;
+            constexpr int kChunk = kMore / kTiles;
+            for (int s0 = (int)rank; s0 < p.prefix.plan.slots; s0 += kChunk * S) {
+                float2 a0[kChunk], a1[kChunk];
+                float v[kChunk][kTiles][4];
 #pragma unroll
-            for (int k = 0; k < kSets; ++k) add_set(pm0[k], pm1[k], po[k], m0, m1, l0, l1, sum);
-            constexpr int kMore = 6 / kTiles;                                // sets whose loads are in flight together
-            for (int k0 = kSets; (int)rank + k0 * S < p.prefix.plan.slots; k0 += kMore) {
-                float2 a0[kMore], a1[kMore];
-                float v[kMore][kTiles][4];
+                for (int k = 0; k < kChunk; ++k) {
+                    const int s = s0 + k * S;
+                    a0[k] = a1[k] = make_float2(-INFINITY, 0.f);
+                    if (s >= p.prefix.plan.slots) continue;
+                    const long long row = s * p.prefix.plan.rows + (long long)u * G;
+                    const float* r0 = p.prefix.o + (row + h0) * kHeadDim + g;
+                    if (h0_on) a0[k] = p.prefix.ml[row + h0];
+                    if (h1_on) a1[k] = p.prefix.ml[row + h1];
 #pragma unroll
-                for (int k = 0; k < kMore; ++k) load_set(u, k0 + k, a0[k], a1[k], v[k]);
+                    for (int i = 0; i < kTiles; ++i) {
+                        const int d = 16 * (kTiles * warp + i);
+                        v[k][i][0] = h0_on ? r0[d] : 0.f;
+                        v[k][i][1] = h1_on ? r0[d + kHeadDim] : 0.f;
+                        v[k][i][2] = h0_on ? r0[d + 8] : 0.f;
+                        v[k][i][3] = h1_on ? r0[d + 8 + kHeadDim] : 0.f;
+                    }
+                }
 #pragma unroll
-                for (int k = 0; k < kMore; ++k) add_set(a0[k], a1[k], v[k], m0, m1, l0, l1, sum);
+                for (int k = 0; k < kChunk; ++k) {
+                    const bool on0 = a0[k].x > -INFINITY, on1 = a1[k].x > -INFINITY;
+                    const float n0 = fmaxf(m0, a0[k].x), n1 = fmaxf(m1, a1[k].x);
+                    const float c0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
+                    const float d0 = on0 ? fast_exp2(a0[k].x - n0) : 0.f, d1 = on1 ? fast_exp2(a1[k].x - n1) : 0.f;
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i) {
+                        sum[i][0] = sum[i][0] * c0 + (on0 ? v[k][i][0] * d0 : 0.f);
+                        sum[i][1] = sum[i][1] * c1 + (on1 ? v[k][i][1] * d1 : 0.f);
+                        sum[i][2] = sum[i][2] * c0 + (on0 ? v[k][i][2] * d0 : 0.f);
+                        sum[i][3] = sum[i][3] * c1 + (on1 ? v[k][i][3] * d1 : 0.f);
+                    }
+                    const bool counts = warp == 0 && g == 0;     // l is a sum over warps and the lanes of a column
+                    l0 = l0 * c0 + (counts ? a0[k].y * d0 : 0.f);
+                    l1 = l1 * c1 + (counts ? a1[k].y * d1 : 0.f);
+                    m0 = n0;
+                    m1 = n1;
+                }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i / kTiles == warp) {
-                    o[i][0] = sum[i % kTiles][0];
-                    o[i][1] = sum[i % kTiles][1];
-                    o[i][2] = sum[i % kTiles][2];
-                    o[i][3] = sum[i % kTiles][3];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[i][e] = sum[i % kTiles][e];
                 }
         };
-        if constexpr (kPrefix)
-            if (my_units > 0) load_prefix(p.unit_begin + cluster_id);
+        if constexpr (kPrefix) {
+            if (my_units > 0) {
+                copy_q(p.unit_begin + cluster_id, 0);
+                if (!clustered) load_prefix(p.unit_begin + cluster_id);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            named_barrier_sync(consumer_bar, kConsumers);
+        }
 
         // Pages belong to the groups in turn (page pc of the block's walk to group pc mod NG, across unit
         // boundaries), and a warp looks at the barriers up to its own next page before it releases the
@@ -463,20 +546,23 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
         // page lies behind the first unit's merge, so that is made sure of here, once.
         if (NG > 1) {
             observe_through((uint32_t)(NG - 1));
-            named_barrier_sync(1, kConsumers);
+            named_barrier_sync(consumer_bar, kConsumers);
         }
 
         for (int u = p.unit_begin + cluster_id; u < p.unit_end; u += n_clusters, ++it) {
             uint32_t qn[8][2] = {};
-            if (u + n_clusters < p.unit_end) load_q(u + n_clusters, qn);
+            if constexpr (kPrefix) {
+                read_q(it & 1);
+                if (u + n_clusters < p.unit_end) copy_q(u + n_clusters, (it + 1) & 1);
+            } else if (u + n_clusters < p.unit_end) {
+                load_q(u + n_clusters, qn);
+            }
             float mref0 = -INFINITY, mref1 = -INFINITY, l0 = 0.f, l1 = 0.f;
             float o[8][4];      // O^T: [m-tile][(dim g, h0), (dim g, h1), (dim g + 8, h0), (dim g + 8, h1)]
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-            if constexpr (kPrefix) {
-                add_prefix(u, mref0, mref1, l0, l1, o);
-                if (u + n_clusters < p.unit_end) load_prefix(u + n_clusters);
-            }
+            if constexpr (kPrefix)
+                if (clustered) add_prefix(u, mref0, mref1, l0, l1, o);
 
             // this group's pages of the unit: j = j0, j0 + NG, ...
             const int j0 = NG == 1 ? 0 : (int)((grp + NG - pc_mod) % NG);
@@ -575,6 +661,7 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
             pc_mod = (pc_mod + npg) % NG;
             st_base = (st_base + (uint32_t)npg) % NS;
 
+            if constexpr (kPrefix) asm volatile("cp.async.wait_all;" ::: "memory");      // the next queries, this unit's sums: shared from the barrier on
             // ---- merge the warps of this block ---------------------------------
             // Every warp leaves its (reference, l) pair and its unscaled O^T in a slot of its own; after
             // one barrier 8 x NW threads turn the references into per-warp scales and the block's
@@ -603,12 +690,11 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                     d1[8] = o[mt][3];
                 }
             }
-            named_barrier_sync(1, kConsumers);
+            named_barrier_sync(consumer_bar, kConsumers);
             if (!clustered) {
                 // One block owns the unit: every warp finishes 8 / NW heads on its own -- the block's
                 // reference, the per-warp scales, l, the log-sum-exp and the normalised output -- so one
                 // more barrier (for the log-sum-exp) ends the unit.
-                constexpr int kHeadsPerWarp = kMaxGroup / NW;
 #pragma unroll
                 for (int hh = 0; hh < kHeadsPerWarp; ++hh) {
                     const int h = warp * kHeadsPerWarp + hh;
@@ -621,6 +707,22 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                         const float mk = wml[k * 16 + h];
                         sc[k] = mk == -INFINITY ? 0.f : fast_exp2(mk - mc);
                         lc += wml[k * 16 + 8 + h] * sc[k];
+                    }
+                    if constexpr (kPrefix) {
+                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                        if (h < G) {
+#pragma unroll
+                            for (int k4 = 0; k4 < kHeadDim / 32; ++k4)
+#pragma unroll
+                                for (int k = 0; k < NW; ++k) acc[k4] += slots[k * (kMaxGroup * kXchgRow) + h * kXchgRow + lane + 32 * k4] * sc[k];
+                            fold_prefix(u, hh, mc, lc, acc);
+                            const float inv = 1.f / lc;
+#pragma unroll
+                            for (int k4 = 0; k4 < kHeadDim / 32; ++k4)
+                                p.out[((size_t)u * G + h) * kHeadDim + lane + 32 * k4] = __float2bfloat16_rn(acc[k4] * inv);
+                        }
+                        if (lane == 0) lse_s[h] = mc + log2f(lc);
+                        continue;
                     }
                     const float inv = 1.f / lc;
                     if (lane == 0) lse_s[h] = mc + log2f(lc);
@@ -635,7 +737,11 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                         }
                     }
                 }
-                named_barrier_sync(1, kConsumers);
+                if constexpr (kPrefix) {
+                    __syncwarp();
+                    if (u + n_clusters < p.unit_end) load_prefix(u + n_clusters);
+                }
+                named_barrier_sync(consumer_bar, kConsumers);
                 lse0 = lse_s[h0];
                 lse1 = lse_s[h1];
                 u_prev = u;
@@ -659,7 +765,7 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                         xb->l[h] = lc;
                     }
                 }
-                named_barrier_sync(1, kConsumers);
+                named_barrier_sync(consumer_bar, kConsumers);
                 for (int e = ctid; e < kMaxGroup * kHeadDim; e += kConsumers) {
                     const int h = e >> 7, d = e & (kHeadDim - 1);
                     float acc = 0.f;
@@ -671,7 +777,7 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                     cluster_arrive();
                     cluster_wait();
                 } else {
-                    named_barrier_sync(1, kConsumers);
+                    named_barrier_sync(consumer_bar, kConsumers);
                 }
 
                 // ---- merge the blocks of the cluster: exact log-sum-exp per head -----
@@ -688,7 +794,7 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                         sc_s[r * kMaxGroup + ctid] = mr == -INFINITY ? 0.f : exp2f(mr - M) / L;
                     }
                 }
-                named_barrier_sync(1, kConsumers);
+                named_barrier_sync(consumer_bar, kConsumers);
                 lse0 = lse_s[h0];
                 lse1 = lse_s[h1];
                 u_prev = u;
@@ -706,10 +812,12 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                     }
                 }
             }
+            if constexpr (!kPrefix) {
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-                qb[ks][0] = qn[ks][0];
-                qb[ks][1] = qn[ks][1];
+                for (int ks = 0; ks < 8; ++ks) {
+                    qb[ks][0] = qn[ks][0];
+                    qb[ks][1] = qn[ks][1];
+                }
             }
             // No barrier here: lse_s and sc_s are rewritten only after the barriers of the next unit's
             // merge, the exchange buffer alternates, and every logit slot is read and rewritten by
@@ -730,9 +838,9 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
     // No block may exit while a peer can still read its shared memory; tensor memory goes back last.
     tmem_fence_before_sync();
     __syncthreads();
-    if (warp == 0) {
+    if (hw_warp == 0) {
         tmem_fence_after_sync();
-        tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
+        tmem_dealloc(tmem_base, (uint32_t)(kWalkers * p.tmem_cols));
     }
     if (clustered) {
         cluster_arrive();
@@ -744,12 +852,19 @@ constexpr int kMaxGroups = 2;
 constexpr int kTmemPages = 128;            // 512 columns / 4 per page
 constexpr size_t kMinSmemBytes = 120 * 1024;
 
-template <int NG, bool kPrefix>
+typedef void (*DecodeKernel)(const DecodeParams);
+
+DecodeKernel kernel_of(const DecodePlan& plan, bool prefix) {
+    if (plan.walkers == 2) return decode_kernel<1, true, 2>;
+    if (prefix) return plan.groups == 2 ? decode_kernel<2, true, 1> : decode_kernel<1, true, 1>;
+    return plan.groups == 2 ? decode_kernel<2, false, 1> : decode_kernel<1, false, 1>;
+}
+
 cudaError_t launch_impl(const DecodeParams& p, const DecodePlan& plan, int clusters, cudaStream_t stream,
                         int* max_clusters) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((max_clusters ? 1 : clusters) * plan.splits, 1, 1);
-    cfg.blockDim = dim3((4 * NG + 1) * 32, 1, 1);
+    cfg.gridDim = dim3(max_clusters ? plan.splits : (clusters + plan.walkers - 1) / plan.walkers * plan.splits, 1, 1);
+    cfg.blockDim = dim3(plan.walkers * (4 * plan.groups + 1) * 32, 1, 1);
     cfg.dynamicSmemBytes = plan.smem_bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -759,8 +874,13 @@ cudaError_t launch_impl(const DecodeParams& p, const DecodePlan& plan, int clust
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (max_clusters) return cudaOccupancyMaxActiveClusters(max_clusters, decode_kernel<NG, kPrefix>, &cfg);
-    return cudaLaunchKernelEx(&cfg, decode_kernel<NG, kPrefix>, p);
+    const DecodeKernel kernel = kernel_of(plan, p.prefix.ml != nullptr);
+    if (max_clusters) {
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(max_clusters, kernel, &cfg);
+        *max_clusters *= plan.walkers;
+        return e;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 }  // namespace
@@ -783,11 +903,14 @@ static size_t layout(const DecodeConfig& c, int np, int s, int ns, DecodePlan* p
     off += 2 * sizeof(Xchg);
     plan->off_wml = (int)off;
     off += 4 * kMaxGroups * 16 * sizeof(float);
-    plan->groups = c.force_groups > 0 ? c.force_groups : 2;
+    plan->walkers = c.dense && s == 1 ? 2 : 1;
+    plan->groups = plan->walkers == 2 ? 1 : c.force_groups > 0 ? c.force_groups : 2;
     plan->off_slots = (int)off;
     off += (size_t)4 * plan->groups * kMaxGroup * kXchgRow * sizeof(float);
     plan->off_misc = (int)off;
     off += 256 * sizeof(float);
+    plan->off_prefix = (int)off;
+    if (c.prefix) off += kPrefixBytes;
     plan->off_bars = (int)off;
     off += 2 * (size_t)ns * sizeof(uint64_t);
     plan->splits = s;
@@ -798,6 +921,8 @@ static size_t layout(const DecodeConfig& c, int np, int s, int ns, DecodePlan* p
     plan->tmem_cols = cols;
     // More than half of an SM's shared memory: one block per SM, so the tensor-memory allocation
     // of one block never waits for another block's.
+    plan->walker_bytes = (int)((off + 127) / 128 * 128);
+    if (plan->walkers == 2) off = 2 * (size_t)plan->walker_bytes;
     if (off < kMinSmemBytes) off = kMinSmemBytes;
     plan->smem_bytes = (int)off;
     return off;
@@ -806,7 +931,11 @@ static size_t layout(const DecodeConfig& c, int np, int s, int ns, DecodePlan* p
 int decode_plan(const DecodeConfig& c, int n, int max_smem, int splits, DecodePlan* plan) {
     const int np = (n + kPageTokens - 1) / kPageTokens;
     constexpr int kMaxStages = 6;
-    const int min_stages = 2;      // a stage per group being worked on      // a stage per group being worked on
+    const int min_stages = 2;      // a stage per group being worked on
+    if (c.dense && splits == 1) {
+        const size_t bytes = layout(c, np, 1, 2, plan);
+        return plan->tmem_cols <= 256 && bytes <= (size_t)max_smem ? 0 : -1;
+    }
     if (c.force_stages > 0)
         return c.force_stages >= min_stages && layout(c, np, splits, c.force_stages, plan) <= (size_t)max_smem ? 0 : -1;
     for (int ns = kMaxStages; ns >= min_stages; --ns)
@@ -815,10 +944,10 @@ int decode_plan(const DecodeConfig& c, int n, int max_smem, int splits, DecodePl
 }
 
 cudaError_t decode_prepare() {
-    const void* kernels[4] = {(const void*)decode_kernel<1, false>, (const void*)decode_kernel<2, false>,
-                              (const void*)decode_kernel<1, true>, (const void*)decode_kernel<2, true>};
-    for (const void* k : kernels) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    const DecodeKernel kernels[5] = {decode_kernel<1, false, 1>, decode_kernel<2, false, 1>, decode_kernel<1, true, 1>,
+                                     decode_kernel<2, true, 1>, decode_kernel<1, true, 2>};
+    for (const DecodeKernel k : kernels) {
+        const cudaError_t e = cudaFuncSetAttribute((const void*)k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -826,8 +955,7 @@ cudaError_t decode_prepare() {
 
 cudaError_t decode_max_clusters(const DecodePlan& plan, int* clusters) {
     DecodeParams none = {};
-    return plan.groups == 2 ? launch_impl<2, false>(none, plan, 1, nullptr, clusters)
-                            : launch_impl<1, false>(none, plan, 1, nullptr, clusters);
+    return launch_impl(none, plan, 1, nullptr, clusters);
 }
 
 cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clusters, const DecodeArgs& a,
@@ -866,16 +994,14 @@ cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clu
     p.off_wml = plan.off_wml;
     p.off_slots = plan.off_slots;
     p.off_misc = plan.off_misc;
+    p.off_prefix = plan.off_prefix;
+    p.walker_bytes = plan.walker_bytes;
     p.off_bars = plan.off_bars;
     p.wait_limit_ns = c.wait_limit_ns;
     p.stop_after_pages = c.stop_after_pages;
     p.rounds_before = a.rounds_before;
     p.prefix = a.prefix;
-    if (a.prefix.ml)
-        return plan.groups == 2 ? launch_impl<2, true>(p, plan, clusters, stream, nullptr)
-                                : launch_impl<1, true>(p, plan, clusters, stream, nullptr);
-    return plan.groups == 2 ? launch_impl<2, false>(p, plan, clusters, stream, nullptr)
-                            : launch_impl<1, false>(p, plan, clusters, stream, nullptr);
+    return launch_impl(p, plan, clusters, stream, nullptr);
 }
 
 }  // namespace lzk

@@ -58,11 +58,15 @@ struct DecodeConfig {
     int force_groups;      // 0 = automatic; groups of four consumer warps per block (1 or 2)
     unsigned long long wait_limit_ns;   // bounded waits give up after this long
     int stop_after_pages;  // diagnostics: -1 = off
+    bool prefix;           // the launches add the partial sums of a shared prefix
+    bool dense;            // two walkers per block where one owns a unit
 };
 
 struct DecodePlan {
+    int walkers;           // unit walks per block (clusters are counted in walks)
+    int walker_bytes;
     int splits, stages, groups, pages_per_cta, logit_stride, tmem_pages, tmem_cols;
-    int off_logits, off_xchg, off_wml, off_slots, off_misc, off_bars, smem_bytes;
+    int off_logits, off_xchg, off_wml, off_slots, off_misc, off_prefix, off_bars, smem_bytes;
 };
 
 struct DecodeArgs {

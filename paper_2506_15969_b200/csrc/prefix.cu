@@ -154,7 +154,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 
     if (warp == kProducer) {
         // ------------------------------------------------------------------ TMA producer
-        if (lane == 0) {
+        if (elect_one()) {
             Ring rr, qr;
             bool ok = true;
             int k_tiles = 0;
@@ -223,91 +223,111 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         }
     } else if (warp == kIssuer) {
         // ------------------------------------------------------------------ MMA issuer
-        if (lane == 0) {
-            Ring rr, qr;
-            uint32_t p_uses[2] = {0, 0};
-            bool ok = true;
-            auto wait_on = [&](uint64_t* bar, uint32_t parity) {
-                if (ok) ok = wait_bar(bar, parity, abort_flag, p.status, limit);
-            };
-            auto issue_s = [&](int s, uint32_t q_slot, uint32_t stage) {
-                tmem_fence_after_sync();
-                const uint32_t q_addr = smem_u32(smem + kOffQ + q_slot * kOperandBytes);
-                const uint32_t k_addr = smem_u32(smem + kOffRing + stage * kOperandBytes);
+        // The whole warp walks the loop (so that descriptors and addresses stay in uniform registers) and one elected lane, the same
+        // every time, issues.  One warp issues for both streams, in turn: that keeps them half a step apart, one at the tensor
+        // core while the other is in its softmax.  (With an issuer each they fall into step and take 1.4 times as long.)
+        uint32_t p_uses[2] = {0, 0}, stage = 0, parity = 0, q_uses = 0;
+        bool ok = true;
+        auto wait_on = [&](uint64_t* bar, uint32_t par) {
+            if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, par, abort_flag, p.status, limit));
+        };
+        auto next_stage = [&]() {                   // the ring is used in the order it is filled
+            if (++stage == kRing) {
+                stage = 0;
+                parity ^= 1u;
+            }
+        };
+        const uint64_t q_desc = smem_desc(smem_u32(smem + kOffQ), 16, 1024), k_desc = smem_desc(smem_u32(smem + kOffRing), 16, 1024);
+        const uint64_t v_desc = smem_desc(smem_u32(smem + kOffRing), kBoxBytes, 1024);
+        constexpr uint32_t kStep = kOperandBytes >> 4;              // from operand to operand, in a descriptor's units
+        // (called by one lane) S of stream s from the K tile in stage st; O of stream s += P V from the V tile in it
+        auto issue_s = [&](int s, uint32_t q_slot, uint32_t st) {
+            const uint64_t a = q_desc + q_slot * kStep, b = k_desc + st * kStep;
 #pragma unroll
-                for (int s8 = 0; s8 < 8; ++s8) {    // 16 head dimensions per instruction: 32 bytes inside a box row
-                    const uint32_t off = (s8 >> 2) * kBoxBytes + (s8 & 3) * 32;
-                    umma_bf16(tmem_base + kColS + s * 128, smem_desc(q_addr + off, 16, 1024), smem_desc(k_addr + off, 16, 1024),
-                              instr_desc(false), s8 > 0);
-                }
-                umma_commit(&bars->s_full[s]);
-            };
-            auto issue_o = [&](int s, uint32_t stage, bool first) {
-                tmem_fence_after_sync();
-                const uint32_t v_addr = smem_u32(smem + kOffRing + stage * kOperandBytes);
-                const uint32_t p_col = tmem_base + kColS + s * 128, o_col = tmem_base + kColO + s * 128;
+            for (int s8 = 0; s8 < 8; ++s8) {        // 16 head dimensions per instruction: 32 bytes inside a box row
+                const uint32_t off = ((s8 >> 2) * kBoxBytes + (s8 & 3) * 32) >> 4;
+                umma_bf16(tmem_base + kColS + s * 128, a + off, b + off, instr_desc(false), s8 > 0);
+            }
+            umma_commit(&bars->s_full[s]);
+        };
+        auto issue_o = [&](int s, uint32_t st, bool first) {
+            const uint64_t b = v_desc + st * kStep;
 #pragma unroll
-                for (int s8 = 0; s8 < 8; ++s8) {    // 16 keys per instruction; P = hi + lo, two products
-                    const uint64_t v_desc = smem_desc(v_addr + s8 * 2048, kBoxBytes, 1024);
-                    const uint32_t a_col = p_col + (s8 >> 1) * 32 + (s8 & 1) * 8;
-                    umma_bf16_ts(o_col, a_col, v_desc, instr_desc(true), !first || s8 > 0);
-                    umma_bf16_ts(o_col, a_col + 16, v_desc, instr_desc(true), 1u);
+            for (int s8 = 0; s8 < 8; ++s8) {        // 16 keys per instruction; P = hi + lo, two products
+                const uint32_t a_col = tmem_base + kColS + s * 128 + (s8 >> 1) * 32 + (s8 & 1) * 8;
+                umma_bf16_ts(tmem_base + kColO + s * 128, a_col, b + s8 * (2048 >> 4), instr_desc(true), !first || s8 > 0);
+                umma_bf16_ts(tmem_base + kColO + s * 128, a_col + 16, b + s8 * (2048 >> 4), instr_desc(true), 1u);
+            }
+        };
+        for (long long x = begin; x < end && ok;) {
+            const Piece pc = piece_at(pl, x, end);
+            const int nt = pc.tiles();
+            x += nt;
+            // Q tiles sit in two slots, used in turn
+            const uint32_t slot0 = q_uses & 1u, slot1 = pc.both ? slot0 ^ 1u : slot0;
+            wait_on(&bars->q_full[slot0], (q_uses >> 1) & 1u);
+            ++q_uses;
+            if (pc.both) {
+                wait_on(&bars->q_full[slot1], (q_uses >> 1) & 1u);
+                ++q_uses;
+            }
+            // Ring: K_0 (streams in turn: K_0, K_1), then V_j, K_(j + ahead) alternately.
+            const int ahead = pc.both ? 1 : 2;
+            for (int j = 0; j < min(ahead, nt); ++j) {
+                wait_on(&bars->full[stage], parity);
+                if (!ok) break;
+                tmem_fence_after_sync();
+                if (elect_one()) {
+                    issue_s(pc.both ? 0 : j, slot0, stage);
+                    if (pc.both) issue_s(1, slot1, stage);
+                    umma_commit(&bars->empty[stage]);
+                    if (j + 1 == nt) {
+                        umma_commit(&bars->q_empty[slot0]);
+                        if (pc.both) umma_commit(&bars->q_empty[slot1]);
+                    }
                 }
-            };
-            for (long long x = begin; x < end && ok;) {
-                const Piece pc = piece_at(pl, x, end);
-                const int nt = pc.tiles(), streams = pc.both ? 2 : 1;
-                x += nt;
-                uint32_t q_slot[2];
-                for (int s = 0; s < streams; ++s) {
-                    q_slot[s] = qr.stage(2);
-                    wait_on(&bars->q_full[q_slot[s]], qr.parity(2));
-                    ++qr.count;
-                }
-                if (streams == 1) q_slot[1] = q_slot[0];
-                const int ahead = pc.both ? 1 : 2;
-                auto q_done = [&]() {               // the last logits of the piece are issued
-                    for (int s = 0; s < streams; ++s) umma_commit(&bars->q_empty[q_slot[s]]);
-                };
-                const int lead = min(ahead, nt);
-                for (int j = 0; j < lead && ok; ++j) {
-                    const uint32_t st = rr.stage(kRing);
-                    wait_on(&bars->full[st], rr.parity(kRing));
+                __syncwarp();
+                next_stage();
+            }
+            for (int j = 0; j < nt && ok; ++j) {
+                const bool more = j + ahead < nt;
+                const uint32_t v_stage = stage, v_parity = parity;
+                next_stage();
+                const uint32_t k_stage = stage, k_parity = parity;
+                if (more) next_stage();
+                const int streams = pc.both ? 2 : 1;
+#pragma unroll 1
+                for (int i = 0; i < streams; ++i) {
+                    const int s = pc.both ? i : (j & 1);
+                    const bool last = i + 1 == streams;
+                    wait_on(&bars->p_full[s], s ? p_uses[1] & 1u : p_uses[0] & 1u);
+                    if (s) ++p_uses[1]; else ++p_uses[0];
+                    if (i == 0) wait_on(&bars->full[v_stage], v_parity);
+                    if (i == 0 && more) wait_on(&bars->full[k_stage], k_parity);
                     if (!ok) break;
-                    issue_s(pc.both ? 0 : j, q_slot[0], st);
-                    if (pc.both) issue_s(1, q_slot[1], st);
-                    umma_commit(&bars->empty[st]);
-                    ++rr.count;
-                }
-                if (ok && lead == nt) q_done();
-                for (int j = 0; j < nt && ok; ++j) {
-                    const uint32_t v_use = rr.count, k_use = rr.count + 1;
-                    const bool more = j + ahead < nt;
-                    const int s0 = pc.both ? 0 : (j & 1), s1 = pc.both ? 1 : s0;
-                    for (int s = s0; s <= s1 && ok; ++s) {
-                        wait_on(&bars->p_full[s], p_uses[s] & 1u);
-                        ++p_uses[s];
-                        wait_on(&bars->full[v_use % kRing], (v_use / kRing) & 1u);
-                        if (!ok) break;
-                        issue_o(s, v_use % kRing, j < (pc.both ? 1 : 2));
-                        if (s == s1) umma_commit(&bars->empty[v_use % kRing]);
+                    tmem_fence_after_sync();
+                    if (elect_one()) {
+                        issue_o(s, v_stage, j < ahead);
+                        if (last) umma_commit(&bars->empty[v_stage]);
                         if (more) {
-                            wait_on(&bars->full[k_use % kRing], (k_use / kRing) & 1u);
-                            if (!ok) break;
-                            issue_s(s, q_slot[s], k_use % kRing);
-                            if (s == s1) umma_commit(&bars->empty[k_use % kRing]);
+                            issue_s(s, s ? slot1 : slot0, k_stage);
+                            if (last) umma_commit(&bars->empty[k_stage]);
+                            if (last && j + ahead + 1 == nt) {                 // the last logits of the piece
+                                umma_commit(&bars->q_empty[slot0]);
+                                if (pc.both) umma_commit(&bars->q_empty[slot1]);
+                            }
                         } else {
                             umma_commit(&bars->o_full[s]);
                         }
                     }
-                    rr.count += more ? 2 : 1;
-                    if (ok && more && j + ahead + 1 == nt) q_done();
+                    __syncwarp();
                 }
             }
-            // every MMA issued by this thread is complete before tensor memory goes back
-            umma_commit(&bars->drain);
-            wait_bar(&bars->drain, 0, abort_flag, p.status, limit, false);
         }
+        // every MMA issued by this warp is complete before tensor memory goes back
+        if (elect_one()) umma_commit(&bars->drain);
+        __syncwarp();
+        wait_bar(&bars->drain, 0, abort_flag, p.status, limit, false);
     } else {
         // ------------------------------------------------------------------ softmax and output
         // Accumulator row = TMEM lane; the warps w and w + 4 of a stream share 32 rows and take 64 of the 128 columns each (a
@@ -318,7 +338,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         float* mine = reinterpret_cast<float*>(smem + kOffExchange) + (s * kTile + row) * 2 + hf;
         const float* other = reinterpret_cast<const float*>(smem + kOffExchange) + (s * kTile + row) * 2 + (hf ^ 1);
         const int pair_bar = 1 + s * 4 + (warp & 3);                   // of the two warps
-        uint32_t s_uses = 0, o_uses[2] = {0, 0};
+        uint32_t s_uses = 0, o_uses = 0;
         // A warp whose wait gives up goes on through the same loops, so that its partner's barriers get all their threads, but waits
         // for nothing any more; what it computes means nothing.
         bool dead = false;
@@ -409,13 +429,10 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const long long unit = pc.item / pl.pairs;
             const long long u = (unit / pl.kv_heads * pl.share + seq) * pl.kv_heads + unit % pl.kv_heads;     // of the decoding handle
             const long long at = nth * pl.rows + u * pl.group + (row - r * pl.group);
-            // (the other stream's accumulator is needed where both work on the same rows; its phase is known to have begun:
-            // the MMAs of one thread complete in order)
-            const int nt_other = pc.both ? 0 : pc.stream_tiles(s ^ 1);
-            if (nt > 0) wait_on(&bars->o_full[s], o_uses[s] & 1u);
-            if (nt_other > 0) wait_on(&bars->o_full[s ^ 1], o_uses[s ^ 1] & 1u);
-            o_uses[0] += pc.stream_tiles(0) > 0;
-            o_uses[1] += pc.stream_tiles(1) > 0;
+            if (nt > 0) {
+                wait_on(&bars->o_full[s], o_uses & 1u);
+                ++o_uses;
+            }
             tmem_fence_after_sync();
             if (warp_on) {
                 *mine = l;
@@ -435,12 +452,14 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                         }
                     }
                 } else {
-                    // the two streams' sums into one: four threads per row, 32 columns each
+                    // The two streams' sums into one: four threads per row, 32 columns each.  (Each stream's warps have waited for
+                    // their own accumulator; the barrier passes that on.)
                     *mine = hf ? l : m;
+                    tmem_fence_before_sync();
                     named_barrier_sync(9 + (warp & 3), 128);
+                    tmem_fence_after_sync();
                     const float2* ml = reinterpret_cast<const float2*>(smem + kOffExchange) + row;
                     const float2 a0 = ml[0], a1 = ml[kTile];
-                    named_barrier_sync(9 + (warp & 3), 128);
                     m = fmaxf(a0.x, a1.x);
                     const float f0 = a0.x > -INFINITY ? fast_exp2(a0.x - m) : 0.f, f1 = a1.x > -INFINITY ? fast_exp2(a1.x - m) : 0.f;
                     l = a0.y * f0 + a1.y * f1;
@@ -458,6 +477,8 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                             for (int i = 0; i < 4; ++i) dst[(col + c) / 4 + i] = make_float4(o0[4 * i], o0[4 * i + 1], o0[4 * i + 2], o0[4 * i + 3]);
                         }
                     }
+                    tmem_fence_before_sync();
+                    named_barrier_sync(9 + (warp & 3), 128);           // all are done with both accumulators and the exchange
                 }
             }
             tmem_fence_before_sync();

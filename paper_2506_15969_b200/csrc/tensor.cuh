@@ -7,6 +7,14 @@
 
 namespace lzk {
 
+// True in one lane of a whole warp.  The compiler knows that at most one lane runs what it guards; behind a comparison with a lane
+// number it wraps every instruction that takes uniform operands (MMA, TMA, commit) in a loop over the active lanes.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on != 0;
+}
+
 // ---- TMA tiles ----------------------------------------------------------------------------------
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
