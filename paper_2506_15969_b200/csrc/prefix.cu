@@ -28,7 +28,7 @@
 // Pages keep 16-byte chunk c of row r at c ^ (r & 7) of every 128-byte half row.  A plain (unswizzled) TMA box of 64 rows x
 // 128 bytes therefore lands as a 128-byte-swizzled operand; a key tile is four boxes from two pages.
 //
-// Warp roles: warps 0-15 softmax and output, warp 16 TMA producer, warp 17 MMA issuer.  All mbarrier waits are bounded.
+// Warp roles: warps 0-15 softmax and output, warp 16 TMA producer, warps 17 and 18 MMA issuers, one per stream.  All mbarrier waits are bounded.
 #include "internal.h"
 #include "tensor.cuh"
 
@@ -41,7 +41,7 @@ constexpr int kBoxBytes = kTile * 128;             // half an operand: 128 rows 
 constexpr int kOperandBytes = 2 * kBoxBytes;       // a 128 x 128 bf16 operand (32 KiB)
 constexpr int kRing = 5;                           // K and V tiles in flight, in the order they are used
 constexpr int kStreamWarps = 8;                    // two warps per 32 accumulator rows, half of the columns each
-constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 1);
+constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 2);      // an issuer per stream
 constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the reference by
 
 constexpr int kOffQ = 0;                           // two row tiles
@@ -55,8 +55,8 @@ constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;     // per stream: 1
 struct Bars {
     uint64_t q_full[2], q_empty[2];
     uint64_t full[kRing], empty[kRing];
-    uint64_t s_full[2], p_full[2], o_full[2];
-    uint64_t drain;
+    uint64_t s_full[2], p_full[2][2], o_full[2];   // [stream]; P comes in two halves
+    uint64_t drain[2];
 };
 
 struct PrefixParams {
@@ -124,16 +124,17 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->q_full[i], 1);
-            mbar_init(&bars->q_empty[i], 1);
+            mbar_init(&bars->q_empty[i], 2);       // (one arrival per stream)
             mbar_init(&bars->s_full[i], 1);
-            mbar_init(&bars->p_full[i], kStreamWarps);
+            for (int h = 0; h < 2; ++h) mbar_init(&bars->p_full[i][h], kStreamWarps);
             mbar_init(&bars->o_full[i], 1);
         }
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&bars->full[i], 1);
-            mbar_init(&bars->empty[i], 1);
+            mbar_init(&bars->empty[i], 2);
         }
-        mbar_init(&bars->drain, 1);
+        mbar_init(&bars->drain[0], 1);
+        mbar_init(&bars->drain[1], 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -221,113 +222,103 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 drain(bars->q_full, qr, 2);
             }
         }
-    } else if (warp == kIssuer) {
-        // ------------------------------------------------------------------ MMA issuer
-        // The whole warp walks the loop (so that descriptors and addresses stay in uniform registers) and one elected lane, the same
-        // every time, issues.  One warp issues for both streams, in turn: that keeps them half a step apart, one at the tensor
-        // core while the other is in its softmax.  (With an issuer each they fall into step and take 1.4 times as long.)
-        uint32_t p_uses[2] = {0, 0}, stage = 0, parity = 0, q_uses = 0;
-        bool ok = true;
-        auto wait_on = [&](uint64_t* bar, uint32_t par) {
-            if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, par, abort_flag, p.status, limit));
+    } else if (warp >= kIssuer) {
+        // ------------------------------------------------------------------ MMA issuers, one warp per stream
+        // A warp walks its loop as a whole (so that descriptors and addresses stay in uniform registers) and one elected lane, the
+        // same every time, issues.  The tensor core queues few instructions and a ready barrier costs 150 clocks to look at, so
+        // with one issuer it idled a third of the time between two streams' turns; two issuers left to themselves
+        // let the streams fall into step (both in the softmax, then both at the tensor core).  So each does its waiting
+        // beforehand and they hand the tensor core to each other turn by turn, which keeps the streams half a step apart.
+        const int s = warp - kIssuer;
+        uint32_t p_uses = 0, uses = 0, q_uses = 0;  // products issued; uses of the K / V ring and of the Q slots by earlier pieces
+        bool ok = true;                             // a warp that gave up goes through the same turns without issuing
+        auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+            if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag, p.status, limit));
         };
-        auto next_stage = [&]() {                   // the ring is used in the order it is filled
-            if (++stage == kRing) {
-                stage = 0;
-                parity ^= 1u;
-            }
+        // Hands a buffer back once the MMAs issued so far are done.  Every buffer expects both streams; one that only this
+        // stream reads gets the other arrival from here.
+        auto release = [&](uint64_t* bar, bool shared) {
+            if (!shared) mbar_arrive(bar);
+            umma_commit(bar);
         };
+        const uint32_t s_col = tmem_base + kColS + s * 128, o_col = tmem_base + kColO + s * 128;
         const uint64_t q_desc = smem_desc(smem_u32(smem + kOffQ), 16, 1024), k_desc = smem_desc(smem_u32(smem + kOffRing), 16, 1024);
         const uint64_t v_desc = smem_desc(smem_u32(smem + kOffRing), kBoxBytes, 1024);
         constexpr uint32_t kStep = kOperandBytes >> 4;              // from operand to operand, in a descriptor's units
-        // (called by one lane) S of stream s from the K tile in stage st; O of stream s += P V from the V tile in it
-        auto issue_s = [&](int s, uint32_t q_slot, uint32_t st) {
-            const uint64_t a = q_desc + q_slot * kStep, b = k_desc + st * kStep;
-#pragma unroll
-            for (int s8 = 0; s8 < 8; ++s8) {        // 16 head dimensions per instruction: 32 bytes inside a box row
-                const uint32_t off = ((s8 >> 2) * kBoxBytes + (s8 & 3) * 32) >> 4;
-                umma_bf16(tmem_base + kColS + s * 128, a + off, b + off, instr_desc(false), s8 > 0);
-            }
-            umma_commit(&bars->s_full[s]);
-        };
-        auto issue_o = [&](int s, uint32_t st, bool first) {
+        // O += P V for the keys of P's half `part`: the first or the second 32 of every 64
+        auto issue_o = [&](uint32_t st, int part, bool first) {
             const uint64_t b = v_desc + st * kStep;
 #pragma unroll
-            for (int s8 = 0; s8 < 8; ++s8) {        // 16 keys per instruction; P = hi + lo, two products
-                const uint32_t a_col = tmem_base + kColS + s * 128 + (s8 >> 1) * 32 + (s8 & 1) * 8;
-                umma_bf16_ts(tmem_base + kColO + s * 128, a_col, b + s8 * (2048 >> 4), instr_desc(true), !first || s8 > 0);
-                umma_bf16_ts(tmem_base + kColO + s * 128, a_col + 16, b + s8 * (2048 >> 4), instr_desc(true), 1u);
+            for (int i = 0; i < 4; ++i) {           // 16 keys per instruction; P = hi + lo, two products
+                const int s8 = (i >> 1) * 4 + part * 2 + (i & 1);
+                const uint32_t a_col = s_col + (s8 >> 1) * 32 + (s8 & 1) * 8;
+                umma_bf16_ts(o_col, a_col, b + s8 * (2048 >> 4), instr_desc(true), !first || i > 0);
+                umma_bf16_ts(o_col, a_col + 16, b + s8 * (2048 >> 4), instr_desc(true), 1u);
             }
         };
-        for (long long x = begin; x < end && ok;) {
+        for (long long x = begin; x < end;) {
             const Piece pc = piece_at(pl, x, end);
-            const int nt = pc.tiles();
+            const int nt = pc.tiles(), mine = pc.stream_tiles(s), step = pc.both ? 1 : 2, turns = pc.both ? 2 * nt : nt;
             x += nt;
-            // Q tiles sit in two slots, used in turn
-            const uint32_t slot0 = q_uses & 1u, slot1 = pc.both ? slot0 ^ 1u : slot0;
-            wait_on(&bars->q_full[slot0], (q_uses >> 1) & 1u);
-            ++q_uses;
-            if (pc.both) {
-                wait_on(&bars->q_full[slot1], (q_uses >> 1) & 1u);
-                ++q_uses;
-            }
-            // Ring: K_0 (streams in turn: K_0, K_1), then V_j, K_(j + ahead) alternately.
-            const int ahead = pc.both ? 1 : 2;
-            for (int j = 0; j < min(ahead, nt); ++j) {
-                wait_on(&bars->full[stage], parity);
-                if (!ok) break;
+            const uint32_t q_use = q_uses + (pc.both ? s : 0), q_slot = q_use & 1u;
+            q_uses += pc.both ? 2 : 1;
+            // The ring holds K_0 (one tile ahead; with alternating streams K_0, K_1), then V_j, K_(j + ahead) in turn.
+            const int ahead = pc.both ? 1 : 2, lead = min(ahead, nt);
+            auto v_use = [&](int j) { return uses + lead + j + min(j, nt - lead); };
+            auto k_use = [&](int j) { return j < ahead ? uses + j : v_use(j - ahead) + 1; };
+            auto issue_s = [&](uint32_t st, bool last) {               // (by one lane) S = Q K^T
+                const uint64_t a = q_desc + q_slot * kStep, b = k_desc + st * kStep;
+#pragma unroll
+                for (int s8 = 0; s8 < 8; ++s8) {    // 16 head dimensions per instruction: 32 bytes inside a box row
+                    const uint32_t off = ((s8 >> 2) * kBoxBytes + (s8 & 3) * 32) >> 4;
+                    umma_bf16(s_col, a + off, b + off, instr_desc(false), s8 > 0);
+                }
+                umma_commit(&bars->s_full[s]);
+                release(&bars->empty[st], pc.both);
+                if (last) release(&bars->q_empty[q_slot], !pc.both);
+            };
+            wait_on(&bars->q_full[q_slot], (q_use >> 1) & 1u);
+            int j = pc.both ? 0 : s;
+            if (mine > 0) {
+                const uint32_t use = k_use(j);
+                wait_on(&bars->full[use % kRing], (use / kRing) & 1u);
                 tmem_fence_after_sync();
-                if (elect_one()) {
-                    issue_s(pc.both ? 0 : j, slot0, stage);
-                    if (pc.both) issue_s(1, slot1, stage);
-                    umma_commit(&bars->empty[stage]);
-                    if (j + 1 == nt) {
-                        umma_commit(&bars->q_empty[slot0]);
-                        if (pc.both) umma_commit(&bars->q_empty[slot1]);
-                    }
+                if (ok && elect_one()) issue_s(use % kRing, mine == 1);
+            } else if (ok && elect_one()) {
+                mbar_arrive(&bars->q_empty[q_slot]);
+            }
+            __syncwarp();
+            for (int t = 0; t < mine; ++t, j += step) {
+                const int turn = 2 * t + s;         // the streams take turns: 0, 1, 0, 1 ..
+                const bool more = t + 1 < mine;
+                const uint32_t vu = v_use(j), vs = vu % kRing, ku = more ? k_use(j + step) : 0u, ks = ku % kRing;
+                wait_on(&bars->full[vs], (vu / kRing) & 1u);
+                if (more) wait_on(&bars->full[ks], (ku / kRing) & 1u);
+                wait_on(&bars->p_full[s][0], p_uses & 1u);
+                if (turn > 0) named_barrier_sync(13 + s, 64);
+                tmem_fence_after_sync();
+                if (ok && elect_one()) issue_o(vs, 0, t == 0);
+                __syncwarp();
+                wait_on(&bars->p_full[s][1], p_uses & 1u);
+                ++p_uses;
+                tmem_fence_after_sync();
+                if (ok && elect_one()) {
+                    issue_o(vs, 1, false);
+                    release(&bars->empty[vs], pc.both);
+                    if (more)
+                        issue_s(ks, t + 2 == mine);
+                    else
+                        umma_commit(&bars->o_full[s]);
                 }
                 __syncwarp();
-                next_stage();
+                if (turn + 1 < turns) asm volatile("bar.arrive %0, %1;" ::"r"(13 + (s ^ 1)), "r"(64) : "memory");
             }
-            for (int j = 0; j < nt && ok; ++j) {
-                const bool more = j + ahead < nt;
-                const uint32_t v_stage = stage, v_parity = parity;
-                next_stage();
-                const uint32_t k_stage = stage, k_parity = parity;
-                if (more) next_stage();
-                const int streams = pc.both ? 2 : 1;
-#pragma unroll 1
-                for (int i = 0; i < streams; ++i) {
-                    const int s = pc.both ? i : (j & 1);
-                    const bool last = i + 1 == streams;
-                    wait_on(&bars->p_full[s], s ? p_uses[1] & 1u : p_uses[0] & 1u);
-                    if (s) ++p_uses[1]; else ++p_uses[0];
-                    if (i == 0) wait_on(&bars->full[v_stage], v_parity);
-                    if (i == 0 && more) wait_on(&bars->full[k_stage], k_parity);
-                    if (!ok) break;
-                    tmem_fence_after_sync();
-                    if (elect_one()) {
-                        issue_o(s, v_stage, j < ahead);
-                        if (last) umma_commit(&bars->empty[v_stage]);
-                        if (more) {
-                            issue_s(s, s ? slot1 : slot0, k_stage);
-                            if (last) umma_commit(&bars->empty[k_stage]);
-                            if (last && j + ahead + 1 == nt) {                 // the last logits of the piece
-                                umma_commit(&bars->q_empty[slot0]);
-                                if (pc.both) umma_commit(&bars->q_empty[slot1]);
-                            }
-                        } else {
-                            umma_commit(&bars->o_full[s]);
-                        }
-                    }
-                    __syncwarp();
-                }
-            }
+            uses += 2 * nt;
         }
         // every MMA issued by this warp is complete before tensor memory goes back
-        if (elect_one()) umma_commit(&bars->drain);
+        if (elect_one()) umma_commit(&bars->drain[s]);
         __syncwarp();
-        wait_bar(&bars->drain, 0, abort_flag, p.status, limit, false);
+        wait_bar(&bars->drain[s], 0, abort_flag, p.status, limit, false);
     } else {
         // ------------------------------------------------------------------ softmax and output
         // Accumulator row = TMEM lane; the warps w and w + 4 of a stream share 32 rows and take 64 of the 128 columns each (a
@@ -394,6 +385,12 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {                      // 16 columns at a time
+                        if (c == 2) {                                  // the first half of P is there: its product may begin
+                            tmem_wait_st();
+                            tmem_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&bars->p_full[s][0]);
+                        }
                         uint32_t hi[8], lo[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -419,10 +416,12 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     unpack2(add2(sum0, sum1), a0, a1);
                     l += a0 + a1;
                     tmem_wait_st();
+                } else if (lane == 0) {
+                    mbar_arrive(&bars->p_full[s][0]);
                 }
                 tmem_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars->p_full[s]);
+                if (lane == 0) mbar_arrive(&bars->p_full[s][1]);
             }
             // ---- the piece's partial sums
             const int nth = (int)blockIdx.x - prefix_block_of(pl, pc.item * pl.key_tiles);
