@@ -438,7 +438,6 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
         prefix.plan = h->prefix_plan;
         prefix.o = h->prefix_o;
         prefix.ml = h->prefix_ml;
-        if (!pipe && (e = run_prefix(h, q)) != cudaSuccess) return cuda_fail(h, e, "prefix kernel launch");
     }
     if (tok && !fuse_append) {
         SpanGuard g(h, kSpanAppend, 0.0);
@@ -446,6 +445,7 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
         if (e != cudaSuccess) return cuda_fail(h, e, "append kernel launch");
         h->launches += 1;
     }
+    if (h->shared && !pipe && (e = run_prefix(h, q)) != cudaSuccess) return cuda_fail(h, e, "prefix kernel launch");
     {
         // algorithmic bytes: every cached K and V row read once, one probability written per token,
         // the queries read and the outputs written
@@ -504,7 +504,8 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
             if (e != cudaSuccess) break;
             // a range of the main walk continues it; the last round's units are a walk of their own
             DecodeArgs a{h->pool, h->st, q, out, n, t, begin[r], count[r], is_tail ? 0 : begin[r] / clusters,
-                         fuse_append ? tok->k : nullptr, fuse_append ? tok->v : nullptr, fuse_append ? tok->position : 0, prefix};
+                         fuse_append ? tok->k : nullptr, fuse_append ? tok->v : nullptr, fuse_append ? tok->position : 0, prefix,
+                         h->shared && !pipe && !fork && r == 0 && !h->profiling};
             const bool beside = is_tail && fork;
             if (e != cudaSuccess) break;
             e = decode_launch(c, is_tail ? tail_plan : plan, is_tail ? count[r] : (clusters < count[r] ? clusters : count[r]), a,

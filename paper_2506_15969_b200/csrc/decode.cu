@@ -530,6 +530,9 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                 }
         };
         if constexpr (kPrefix) {
+            // The launch may begin beside the end of the prefix launch (its own pages and queries come from earlier ones);
+            // from here on that one is complete.
+            asm volatile("griddepcontrol.wait;" ::: "memory");
             if (my_units > 0) {
                 copy_q(p.unit_begin + cluster_id, 0);
                 if (!clustered) load_prefix(p.unit_begin + cluster_id);
@@ -861,19 +864,21 @@ DecodeKernel kernel_of(const DecodePlan& plan, bool prefix) {
 }
 
 cudaError_t launch_impl(const DecodeParams& p, const DecodePlan& plan, int clusters, cudaStream_t stream,
-                        int* max_clusters) {
+                        int* max_clusters, bool behind_prefix = false) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(max_clusters ? plan.splits : (clusters + plan.walkers - 1) / plan.walkers * plan.splits, 1, 1);
     cfg.blockDim = dim3(plan.walkers * (4 * plan.groups + 1) * 32, 1, 1);
     cfg.dynamicSmemBytes = plan.smem_bytes;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = plan.splits;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = behind_prefix ? 2 : 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     const DecodeKernel kernel = kernel_of(plan, p.prefix.ml != nullptr);
     if (max_clusters) {
         const cudaError_t e = cudaOccupancyMaxActiveClusters(max_clusters, kernel, &cfg);
@@ -1001,7 +1006,7 @@ cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clu
     p.stop_after_pages = c.stop_after_pages;
     p.rounds_before = a.rounds_before;
     p.prefix = a.prefix;
-    return launch_impl(p, plan, clusters, stream, nullptr);
+    return launch_impl(p, plan, clusters, stream, nullptr, a.behind_prefix);
 }
 
 }  // namespace lzk

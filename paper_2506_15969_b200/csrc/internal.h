@@ -82,6 +82,7 @@ struct DecodeArgs {
     const void* v_new;
     int append_position;
     PrefixView prefix;            // prefix.ml = null: none
+    bool behind_prefix;           // the prefix launch is right before: begin beside its end
 };
 
 // Deepest ring and the shared-memory layout for n cached tokens and a cluster of `splits` blocks;

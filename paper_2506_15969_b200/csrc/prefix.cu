@@ -150,6 +150,8 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     __syncthreads();
     tmem_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
+    // every block is resident: the decode launch may take the SMs that this one leaves (it waits for the sums itself)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const unsigned long long limit = p.wait_limit_ns;
     const long long begin = (long long)blockIdx.x * pl.work / pl.blocks, end = ((long long)blockIdx.x + 1) * pl.work / pl.blocks;
 
