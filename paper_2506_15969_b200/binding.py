@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -42,9 +43,7 @@ class Profile(C.Structure):
             "append_launches", "decode_launches", "select_launches", "compact_launches")]
 
 
-class Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int), ("stride_layer", C.c_longlong), ("stride_batch", C.c_longlong),
-                ("stride_token", C.c_longlong), ("stride_head", C.c_longlong)]
+_ROWS = struct.Struct("@Pi4xqqqq")        # lazyev_rows_t
 
 
 class Dump(C.Structure):
@@ -83,9 +82,9 @@ _PROTOS = {
     "lazyev_copy_state": [C.c_void_p, C.c_void_p],
     "lazyev_set_rope": [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float],
     "lazyev_set_head_norm": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_float],
-    "lazyev_norm_rope": [C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.c_int, C.c_void_p, C.c_int, C.POINTER(Rows), C.POINTER(Rows)],
-    "lazyev_append": [C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.c_int, C.c_void_p],
-    "lazyev_decode_step_rows": [C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.c_void_p, C.c_void_p],
+    "lazyev_norm_rope": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p],
+    "lazyev_append": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p],
+    "lazyev_decode_step_rows": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
     "lazyev_query_prefix_workspace": [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)],
     "lazyev_attach_prefix": [C.c_void_p, C.c_void_p, C.c_void_p],
     "lazyev_detach_prefix": [C.c_void_p],
@@ -157,6 +156,8 @@ class Engine:
         self._torch = torch
         self._h = C.c_void_p()
         self._norm = self._prefix = None          # tensors and the engine that the handle reads
+        self._views = C.create_string_buffer(4 * _ROWS.size)
+        self._views_at = C.addressof(self._views)
         self._shape = layers, batch, q_heads, kv_heads
         self._check(lib().lazyev_create(C.byref(self._h), layers, q_heads, kv_heads, head_dim, budget, window,
                                         threshold), create=True)
@@ -261,17 +262,19 @@ class Engine:
         """lazyev_copy_state(self, src): this handle becomes a copy of src's cached sequences."""
         self._check(lib().lazyev_copy_state(self._h, src._h))
 
-    def _rows(self, x, heads: int, tokens: int) -> Rows:
-        """A tensor [layers, batch, tokens, heads, 128] (of one token: the dimension may be left out) as the library's view."""
-        shape, stride = x.shape, x.stride()
-        layers, batch = self._shape[:2]
-        if len(shape) == 4 and tokens == 1:
-            shape, stride = (*shape[:2], 1, *shape[2:]), (*stride[:2], 0, *stride[2:])
-        if tuple(shape) != (layers, batch, tokens, heads, 128) or stride[4] != 1:
-            raise ValueError(f"rows must be [{layers}, {batch}, {tokens}, {heads}, 128] with contiguous rows, not {tuple(x.shape)}")
-        if x.device != self._index:
+    def _rows(self, slot: int, x, heads: int, tokens: int) -> int:
+        """A tensor [layers, batch, tokens, heads, 128] (of one token: the dimension may be left out) as a lazyev_rows_t in
+        slot 0..3 of this engine's; returns its address."""
+        stride = x.stride()
+        if x.shape != (self._shape[0], self._shape[1], tokens, heads, 128) or stride[4] != 1:
+            if x.shape != (self._shape[0], self._shape[1], heads, 128) or tokens != 1 or stride[3] != 1:
+                raise ValueError(f"rows must be [{self._shape[0]}, {self._shape[1]}, {tokens}, {heads}, 128] with contiguous rows, "
+                                 f"not {tuple(x.shape)} with strides {stride}")
+            stride = stride[0], stride[1], 0, stride[2]
+        if x.get_device() != self._index.index:
             raise ValueError(f"rows must be on {self._index}, not {x.device}")
-        return Rows(x.data_ptr(), self._types[x.dtype], *stride[:4])
+        _ROWS.pack_into(self._views, slot * _ROWS.size, x.data_ptr(), self._types[x.dtype], stride[0], stride[1], stride[2], stride[3])
+        return self._views_at + slot * _ROWS.size
 
     def _positions(self, positions, tokens: int) -> int:
         if positions is None:
@@ -296,22 +299,25 @@ class Engine:
 
     def norm_rope(self, q, k, q_out, k_out, positions=None, first_position: int = 0) -> None:
         """lazyev_norm_rope: q [layers, batch, tokens, q_heads, 128], k with kv_heads (either may be None), strided as they are."""
-        tokens = (q if q is not None else k).shape[2]
+        tokens = (k if q is None else q).shape[2]
         _, _, hq, hkv = self._shape
-        rows = [None if x is None else self._rows(x, heads, tokens) for x, heads in ((q, hq), (k, hkv), (q_out, hq), (k_out, hkv))]
-        self._check(lib().lazyev_norm_rope(self._h, rows[0], rows[1], tokens, self._positions(positions, tokens), first_position,
-                                           rows[2], rows[3]))
+        qi = qo = ki = ko = 0
+        if q is not None:
+            qi, qo = self._rows(0, q, hq, tokens), self._rows(2, q_out, hq, tokens)
+        if k is not None:
+            ki, ko = self._rows(1, k, hkv, tokens), self._rows(3, k_out, hkv, tokens)
+        self._check(lib().lazyev_norm_rope(self._h, qi, ki, tokens, self._positions(positions, tokens), first_position, qo, ko))
 
     def append(self, k, v, positions=None) -> None:
         """lazyev_append: k, v [layers, batch, tokens, kv_heads, 128], strided as they are."""
         tokens, heads = k.shape[2], self._shape[3]
-        self._check(lib().lazyev_append(self._h, self._rows(k, heads, tokens), self._rows(v, heads, tokens), tokens,
+        self._check(lib().lazyev_append(self._h, self._rows(1, k, heads, tokens), self._rows(2, v, heads, tokens), tokens,
                                         self._positions(positions, tokens)))
 
     def decode_step_rows(self, q, k, v, out, positions=None) -> None:
         """lazyev_decode_step_rows: q, k, v [layers, batch, (1,) heads, 128], strided as they are; out as for decode_step."""
         _, _, hq, hkv = self._shape
-        self._check(lib().lazyev_decode_step_rows(self._h, self._rows(q, hq, 1), self._rows(k, hkv, 1), self._rows(v, hkv, 1),
+        self._check(lib().lazyev_decode_step_rows(self._h, self._rows(0, q, hq, 1), self._rows(1, k, hkv, 1), self._rows(2, v, hkv, 1),
                                                   self._positions(positions, 1), _ptr(out)))
 
     def attach_prefix(self, prefix: "Engine") -> None:

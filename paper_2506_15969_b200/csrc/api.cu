@@ -65,7 +65,7 @@ struct lazyev {
     bool slot_busy[2] = {false, false};
     int last_host_ranges = 0;
     // what the calls that take projected rows do to queries and keys
-    double inv_freq[kMaxPairs] = {0};
+    double turns[kMaxPairs] = {0};         // per position: inv_freq / (2 pi)
     int pairs = 0, interleaved = 0;
     float amplitude = 1.f, norm_eps = 0.f;
     const float* q_weight = nullptr;
@@ -73,6 +73,7 @@ struct lazyev {
     // a prefix shared by this handle's sequences (another handle), and how many handles share this one
     lazyev* shared = nullptr;
     PrefixPlan prefix_plan = {};
+    PrefixPool prefix_pool = {};           // the prefix's pool as the kernel addresses it
     float* prefix_o = nullptr;
     float2* prefix_ml = nullptr;
     int users = 0;
@@ -327,7 +328,7 @@ struct NewToken {
 cudaError_t run_prefix(lazyev_t* h, const void* q) {
     const lazyev_t* src = h->shared;
     PrefixArgs a;
-    a.pool = src->pool;
+    a.pool = &h->prefix_pool;
     a.page_table = src->st.page_table;
     a.n = src->n;
     a.pages_per_unit = src->pages_per_unit;
@@ -1113,7 +1114,7 @@ int lazyev_set_rope(lazyev_t* h, const double* inv_freq, int pairs, int interlea
     if (!isfinite(amplitude)) return fail(h, LAZYEV_EINVAL, "the amplitude must be finite");
     for (int j = 0; j < pairs; ++j)
         if (!isfinite(inv_freq[j])) return fail(h, LAZYEV_EINVAL, "inv_freq[%d] is not finite", j);
-    for (int j = 0; j < pairs; ++j) h->inv_freq[j] = inv_freq[j];
+    for (int j = 0; j < kMaxPairs; ++j) h->turns[j] = j < pairs ? inv_freq[j] / 6.283185307179586476925 : 0.0;
     h->pairs = pairs;
     h->interleaved = interleaved != 0;
     h->amplitude = amplitude;
@@ -1142,7 +1143,7 @@ int lazyev_norm_rope(lazyev_t* h, const lazyev_rows_t* q, const lazyev_rows_t* k
     if (k && (rc = rows_view(h, "k", k, h->kv_heads, n_tokens, false, &a.k)) != LAZYEV_OK) return rc;
     if (k && (rc = rows_view(h, "k_out", k_out, h->kv_heads, n_tokens, true, &a.k_out)) != LAZYEV_OK) return rc;
     if ((rc = same_type(h, a.q, a.k)) != LAZYEV_OK || (rc = same_type(h, a.q_out, a.k_out)) != LAZYEV_OK) return rc;
-    const cudaError_t e = rows_launch(a, h->inv_freq, h->num_sms, h->stream);
+    const cudaError_t e = rows_launch(a, h->turns, h->num_sms, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "norm_rope kernel launch");
     h->launches += 1;
     return LAZYEV_OK;
@@ -1161,7 +1162,7 @@ int lazyev_append(lazyev_t* h, const lazyev_rows_t* k, const lazyev_rows_t* v, i
     if (n_tokens > h->capacity - h->n)
         return fail(h, LAZYEV_ECAPACITY, "%d tokens after %d exceed the capacity of %d slots per unit", n_tokens, h->n, h->capacity);
     rows_to_pages(h, h->t, &a);
-    const cudaError_t e = rows_launch(a, h->inv_freq, h->num_sms, h->stream);
+    const cudaError_t e = rows_launch(a, h->turns, h->num_sms, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "append kernel launch");
     h->launches += 1;
     h->prefilled = true;
@@ -1185,7 +1186,7 @@ int lazyev_decode_step_rows(lazyev_t* h, const lazyev_rows_t* q, const lazyev_ro
     const long long row = kHeadDim, seq = (long long)h->q_heads * row;
     a.q_out = RowView{h->stage_rows, h->batch * seq, seq, 0, row, kTypeBF16};
     rows_to_pages(h, h->t + 1, &a);
-    const cudaError_t e = rows_launch(a, h->inv_freq, h->num_sms, h->stream);
+    const cudaError_t e = rows_launch(a, h->turns, h->num_sms, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "row kernel launch");
     h->launches += 1;
     rc = run_decode(h, h->stage_rows, out, h->n + 1, h->t + 1, nullptr);
@@ -1246,7 +1247,7 @@ int lazyev_attach_prefix(lazyev_t* h, lazyev_t* prefix, void* workspace) {
     PrefixPlan plan;
     if ((rc = plan_prefix(h, prefix, &plan)) != LAZYEV_OK) return rc;
     if (!workspace || ((uintptr_t)workspace & 255)) return fail(h, LAZYEV_EINVAL, "the workspace must be 256-byte aligned");
-    cudaError_t e = prefix_prepare();
+    cudaError_t e = prefix_prepare(prefix->pool, prefix->units * prefix->pages_per_unit, &h->prefix_pool);
     cudaEvent_t ready = nullptr;
     // (handles that share it already have seen it cleared)
     if (e == cudaSuccess && prefix->users == 0) e = clear_tail_launch(geometry(prefix), prefix->pool, prefix->st, prefix->n, prefix->stream);

@@ -29,8 +29,12 @@ struct PrefixView {        // what the decode kernel adds to every unit: ml = nu
     const float2* ml;      // [slots][rows]: reference (log2 domain, -inf: no such partial sum), sum of exp2(x - reference)
 };
 
+struct PrefixPool {
+    unsigned long long map[16];         // a tensor map
+};
+
 struct PrefixArgs {
-    const uint8_t* pool;
+    const PrefixPool* pool;
     const int32_t* page_table;
     int n, pages_per_unit, total_pages; // of the prefix handle
     int layers;
@@ -42,7 +46,7 @@ struct PrefixArgs {
     int stop_after_tiles;
 };
 PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int group, int n, int num_sms);
-cudaError_t prefix_prepare();
+cudaError_t prefix_prepare(const uint8_t* pool, int total_pages, PrefixPool* out);
 // Marks every partial sum as absent: a row has up to `slots` of them, and no launch writes those it has not.
 cudaError_t prefix_clear_launch(const PrefixPlan& plan, float2* ml, cudaStream_t stream);
 cudaError_t prefix_launch(const PrefixPlan& plan, const PrefixArgs& a, cudaStream_t stream);
@@ -130,7 +134,8 @@ struct RowsArgs {
     int32_t* status;
     int pages_per_unit, capacity, total_pages, slot, ts, pos_first;
 };
-cudaError_t rows_launch(const RowsArgs& a, const double* inv_freq, int num_sms, cudaStream_t stream);
+// turns: rotation per position of every pair, in whole turns
+cudaError_t rows_launch(const RowsArgs& a, const double* turns, int num_sms, cudaStream_t stream);
 
 // ---- prompt pass (causal attention over the prompt with tracking) -----------------------------------
 struct PromptArgs {

@@ -29,6 +29,8 @@
 // 128 bytes therefore lands as a 128-byte-swizzled operand; a key tile is four boxes from two pages.
 //
 // Warp roles: warps 0-15 softmax and output, warp 16 TMA producer, warps 17 and 18 MMA issuers, one per stream.  All mbarrier waits are bounded.
+#include <string.h>
+
 #include "internal.h"
 #include "tensor.cuh"
 
@@ -532,7 +534,15 @@ cudaError_t prefix_clear_launch(const PrefixPlan& plan, float2* ml, cudaStream_t
     return cudaGetLastError();
 }
 
-cudaError_t prefix_prepare() {
+cudaError_t prefix_prepare(const uint8_t* pool, int total_pages, PrefixPool* out) {
+    // [pages][64 K rows, then 64 V rows][128]; the rows are stored swizzled already
+    static_assert(sizeof(PrefixPool) == sizeof(CUtensorMap), "");
+    const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)2 * kPageTokens, (cuuint64_t)total_pages};
+    const cuuint64_t strides[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)kPageBytes};
+    const cuuint32_t box[3] = {64, (cuuint32_t)kPageTokens, 1};
+    CUtensorMap map;
+    if (!make_map(&map, pool, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE)) return cudaErrorInvalidValue;
+    memcpy(out, &map, sizeof(map));
     return cudaFuncSetAttribute(prefix_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
 }
 
@@ -548,13 +558,7 @@ cudaError_t prefix_launch(const PrefixPlan& plan, const PrefixArgs& a, cudaStrea
         const cuuint32_t box[4] = {64, (cuuint32_t)plan.group, 1, (cuuint32_t)plan.tile_seqs};
         if (!make_map(&mq, a.q, 4, dims, strides, box)) return cudaErrorInvalidValue;
     }
-    {
-        // the prefix's pool: [pages][64 K rows, then 64 V rows][128]; the rows are stored swizzled already
-        const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)2 * kPageTokens, (cuuint64_t)a.total_pages};
-        const cuuint64_t strides[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)kPageBytes};
-        const cuuint32_t box[3] = {64, (cuuint32_t)kPageTokens, 1};
-        if (!make_map(&mkv, a.pool, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE)) return cudaErrorInvalidValue;
-    }
+    memcpy(&mkv, a.pool, sizeof(mkv));
     PrefixParams p;
     p.plan = plan;
     p.page_table = a.page_table;

@@ -398,10 +398,10 @@ void launch(const RowsParams& p, int out, uint32_t blocks, cudaStream_t stream) 
 
 }  // namespace
 
-cudaError_t rows_launch(const RowsArgs& a, const double* inv_freq, int num_sms, cudaStream_t stream) {
+cudaError_t rows_launch(const RowsArgs& a, const double* turns, int num_sms, cudaStream_t stream) {
     RowsParams p;
     p.a = a;
-    for (int j = 0; j < kMaxPairs; ++j) p.turns[j] = j < a.pairs ? inv_freq[j] / 6.283185307179586476925 : 0.0;
+    for (int j = 0; j < kMaxPairs; ++j) p.turns[j] = turns[j];
     const int heads[3] = {a.q.data ? a.q_heads : 0, a.k.data ? a.kv_heads : 0, a.v.data ? a.kv_heads : 0};
     const long long tokens = (long long)a.layers * a.batch * a.n_tokens;
     // Rows per warp: all rows of a token, so that its angles and pages are found once (a warp knows the pages of 32 heads); or,

@@ -142,8 +142,12 @@ def test_row_calls_refuse_bad_arguments():
     x = torch.zeros(1, 2, 4, 8, D, dtype=torch.bfloat16, device="cuda")
     k = torch.zeros(1, 2, 4, 2, D, dtype=torch.bfloat16, device="cuda")
 
+    class Rows(C.Structure):             # lazyev_rows_t
+        _fields_ = [("data", C.c_void_p), ("dtype", C.c_int), ("stride_layer", C.c_longlong), ("stride_batch", C.c_longlong),
+                    ("stride_token", C.c_longlong), ("stride_head", C.c_longlong)]
+
     def rows(t, **kw):
-        r = e._rows(t, t.shape[3], t.shape[2])
+        r = Rows(t.data_ptr(), binding.BF16, *t.stride()[:4])
         for name, v in kw.items():
             setattr(r, name, v)
         return C.byref(r)
