@@ -1205,6 +1205,7 @@ int plan_prefix(lazyev_t* h, const lazyev_t* prefix, PrefixPlan* plan) {
     if (h->batch % prefix->batch != 0)
         return fail(h, LAZYEV_EINVAL, "%d sequences do not divide among %d prefixes", h->batch, prefix->batch);
     *plan = prefix_plan(h->layers, h->batch, prefix->batch, h->kv_heads, h->group, prefix->n, h->num_sms);
+    if (plan->blocks == 0) return fail(h, LAZYEV_EINVAL, "the shared work of %d prefixes of %d tokens is not supported", prefix->batch, prefix->n);
     return LAZYEV_OK;
 }
 

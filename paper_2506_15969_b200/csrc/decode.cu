@@ -530,13 +530,10 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                 }
         };
         if constexpr (kPrefix) {
-            // The launch may begin beside the end of the prefix launch (its own pages and queries come from earlier ones);
-            // from here on that one is complete.
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            if (my_units > 0) {
-                copy_q(p.unit_begin + cluster_id, 0);
-                if (!clustered) load_prefix(p.unit_begin + cluster_id);
-            }
+            // The launch may begin beside the end of the prefix launch: its own pages and queries come from earlier ones, and only
+            // the sums are waited for, where they are first used.
+            if (clustered) asm volatile("griddepcontrol.wait;" ::: "memory");
+            if (my_units > 0) copy_q(p.unit_begin + cluster_id, 0);
             asm volatile("cp.async.wait_all;" ::: "memory");
             named_barrier_sync(consumer_bar, kConsumers);
         }
@@ -664,7 +661,13 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
             pc_mod = (pc_mod + npg) % NG;
             st_base = (st_base + (uint32_t)npg) % NS;
 
-            if constexpr (kPrefix) asm volatile("cp.async.wait_all;" ::: "memory");      // the next queries, this unit's sums: shared from the barrier on
+            if constexpr (kPrefix) {
+                if (it == 0 && !clustered) {
+                    asm volatile("griddepcontrol.wait;" ::: "memory");
+                    load_prefix(u);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");      // the next queries, this unit's sums: shared from the barrier on
+            }
             // ---- merge the warps of this block ---------------------------------
             // Every warp leaves its (reference, l) pair and its unscaled O^T in a slot of its own; after
             // one barrier 8 x NW threads turn the references into per-warp scales and the block's

@@ -12,15 +12,20 @@ struct PrefixPlan {
     int share, group;                   // sequences per prefix sequence, query heads per KV head
     int tile_seqs, tiles, pairs;        // sequences per row tile, row tiles per prefix unit, items (pairs of tiles) per unit
     int key_tiles;                      // 128-key tiles of the prefix
-    int blocks;
+    int items;                          // prefix units * pairs
+    int blocks;                         // the walk over (item, key tile) is cut into `blocks` contiguous parts:
+    int per, extra;                     // the first `extra` of per + 1 steps, the others of per
     int slots;                          // most partial sums of a row
-    long long work;                     // items * key_tiles
     long long rows;                     // query rows = partial sums per slot
 };
 
-// Block that works on step x of the walk over (item, key tile): block c takes [c work / blocks, (c + 1) work / blocks).
-__host__ __device__ __forceinline__ int prefix_block_of(const PrefixPlan& p, long long x) {
-    return (int)(((x + 1) * p.blocks - 1) / p.work);
+__host__ __device__ __forceinline__ int prefix_begin(const PrefixPlan& p, int block) {
+    return block * p.per + (block < p.extra ? block : p.extra);
+}
+// Block that works on step x.
+__host__ __device__ __forceinline__ int prefix_block_of(const PrefixPlan& p, int x) {
+    const int longer = p.extra * (p.per + 1);
+    return x < longer ? x / (p.per + 1) : p.extra + (x - longer) / p.per;
 }
 
 struct PrefixView {        // what the decode kernel adds to every unit: ml = null for none
@@ -45,6 +50,7 @@ struct PrefixArgs {
     unsigned long long wait_limit_ns;
     int stop_after_tiles;
 };
+// blocks = 0: more steps than an int counts.
 PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int group, int n, int num_sms);
 cudaError_t prefix_prepare(const uint8_t* pool, int total_pages, PrefixPool* out);
 // Marks every partial sum as absent: a row has up to `slots` of them, and no launch writes those it has not.

@@ -75,8 +75,7 @@ struct PrefixParams {
 
 // One block's part of an item: key tiles [k0, k1).
 struct Piece {
-    long long item;
-    int k0, k1;
+    int item, k0, k1;
     bool both;                                     // two row tiles, a stream each; else one, the key tiles in turn
     __device__ __forceinline__ int tiles() const { return k1 - k0; }
     // key tiles of stream s, and the t-th of them
@@ -84,12 +83,12 @@ struct Piece {
     __device__ __forceinline__ int key_tile(int s, int t) const { return both ? k0 + t : k0 + 2 * t + s; }
 };
 
-__device__ __forceinline__ Piece piece_at(const PrefixPlan& pl, long long x, long long end) {
+__device__ __forceinline__ Piece piece_at(const PrefixPlan& pl, int x, int end) {
     Piece pc;
     pc.item = x / pl.key_tiles;
-    pc.k0 = (int)(x - pc.item * pl.key_tiles);
-    pc.k1 = (int)min((long long)pl.key_tiles, pc.k0 + (end - x));
-    pc.both = 2 * (int)(pc.item % pl.pairs) + 1 < pl.tiles;
+    pc.k0 = x - pc.item * pl.key_tiles;
+    pc.k1 = min(pl.key_tiles, pc.k0 + (end - x));
+    pc.both = 2 * (pc.item % pl.pairs) + 1 < pl.tiles;
     return pc;
 }
 
@@ -114,6 +113,30 @@ __device__ __noinline__ void rescale(uint32_t cols, float f) {
     tmem_wait_st();
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+
+// A unit's page numbers, 32 at a time in the lanes of a warp.
+struct PageList {
+    const int32_t* table;
+    int last, first;                               // last page of the unit; first page of those in the lanes
+    int32_t entry;
+    __device__ __forceinline__ void open(const int32_t* t, int last_page, int page) {
+        table = t;
+        last = last_page;
+        first = page;
+    }
+    __device__ __forceinline__ void fetch(int page) {
+        first = page;
+        entry = table[min(page + (int)(threadIdx.x & 31), last)];
+    }
+    __device__ __forceinline__ int32_t at(int page) {      // pages are asked for in ascending order
+        if (page >= first + 32) fetch(page);
+        return __shfl_sync(0xffffffffu, entry, page - first);
+    }
+};
+
 __global__ void __launch_bounds__(kThreads, 1)
 prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PrefixParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -122,7 +145,20 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const PrefixPlan& pl = p.plan;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int begin = prefix_begin(pl, blockIdx.x), end = prefix_begin(pl, blockIdx.x + 1);
 
+    // the producer's first page numbers, asked for before everything else
+    PageList k_pages, v_pages;
+    if (warp == kProducer) {
+        if (lane == 0) {
+            prefetch_map(&map_q);
+            prefetch_map(&map_kv);
+        }
+        const Piece pc = piece_at(pl, begin, end);
+        k_pages.open(p.page_table + (long long)(pc.item / pl.pairs) * p.pages_per_unit, (p.n - 1) / kPageTokens, 2 * pc.k0);
+        k_pages.fetch(2 * pc.k0);
+        v_pages = k_pages;
+    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->q_full[i], 1);
@@ -155,76 +191,83 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     // every block is resident: the decode launch may take the SMs that this one leaves (it waits for the sums itself)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const unsigned long long limit = p.wait_limit_ns;
-    const long long begin = (long long)blockIdx.x * pl.work / pl.blocks, end = ((long long)blockIdx.x + 1) * pl.work / pl.blocks;
 
     if (warp == kProducer) {
         // ------------------------------------------------------------------ TMA producer
-        if (elect_one()) {
-            Ring rr, qr;
-            bool ok = true;
-            int k_tiles = 0;
-            const uint32_t q_bytes = (uint32_t)(pl.tile_seqs * pl.group) * 256u;
-            // a K (half = 0) or V (half = 1) tile: 64 rows x 64 elements per box, two pages, both halves of the rows
-            auto load_tile = [&](const int32_t* table, int kt, int half) {
-                const uint32_t st = rr.stage(kRing);
-                ok = wait_bar(&bars->empty[st], rr.parity(kRing) ^ 1u, abort_flag, p.status, limit);
-                if (!ok) return;
-                uint8_t* dst = smem + kOffRing + st * kOperandBytes;
+        // (the whole warp: the lanes keep 32 page numbers, one elected lane issues the copies)
+        Ring rr, qr;
+        bool ok = true;
+        int k_tiles = 0;
+        const uint32_t q_bytes = (uint32_t)(pl.tile_seqs * pl.group) * 256u;
+        auto wait_on = [&](uint64_t* bar, uint32_t parity) { ok = __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag, p.status, limit)); };
+        // a K (half = 0) or V (half = 1) tile: 64 rows x 64 elements per box, two pages, both halves of the rows
+        auto load_tile = [&](PageList& pages, int kt, int half) {
+            // (a tile's second page may lie behind the last one: any page will do, its keys are masked)
+            int32_t p0 = pages.at(2 * kt), p1 = pages.at(2 * kt + 1);
+            if (p0 < 0 || p0 >= p.total_pages || p1 < 0 || p1 >= p.total_pages) {
+                if (lane == 0) atomicOr(p.status, kStatusBadIndex);
+                p0 = p1 = 0;
+            }
+            const uint32_t st = rr.stage(kRing);
+            wait_on(&bars->empty[st], rr.parity(kRing) ^ 1u);
+            if (!ok) return;
+            uint8_t* dst = smem + kOffRing + st * kOperandBytes;
+            if (elect_one()) {
                 mbar_arrive_expect_tx(&bars->full[st], kOperandBytes);
-                const int last = (p.n - 1) / kPageTokens;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    // a tile's second page may lie behind the last one: any page will do, its keys are masked
-                    int32_t pp = table[min(2 * kt + j, last)];
-                    if (pp < 0 || pp >= p.total_pages) {
-                        atomicOr(p.status, kStatusBadIndex);
-                        pp = 0;
-                    }
-                    tma_load_3d(dst + j * (kBoxBytes / 2), &map_kv, 0, half * kPageTokens, pp, &bars->full[st]);
-                    tma_load_3d(dst + kBoxBytes + j * (kBoxBytes / 2), &map_kv, 64, half * kPageTokens, pp, &bars->full[st]);
-                }
-                ++rr.count;
-            };
-            for (long long x = begin; x < end && ok;) {
-                const Piece pc = piece_at(pl, x, end);
-                x += pc.tiles();
-                const long long unit = pc.item / pl.pairs;             // (layer, prefix sequence, head)
-                const int head = (int)(unit % pl.kv_heads), seq0 = (int)(unit / pl.kv_heads) * pl.share;
-                const int tile0 = 2 * (int)(pc.item % pl.pairs);
-                for (int s = 0; s < (pc.both ? 2 : 1) && ok; ++s) {
-                    const uint32_t qs = qr.stage(2);
-                    ok = wait_bar(&bars->q_empty[qs], qr.parity(2) ^ 1u, abort_flag, p.status, limit);
-                    if (!ok) break;
-                    uint8_t* dst = smem + kOffQ + qs * kOperandBytes;
+                tma_load_3d(dst, &map_kv, 0, half * kPageTokens, p0, &bars->full[st]);
+                tma_load_3d(dst + kBoxBytes / 2, &map_kv, 0, half * kPageTokens, p1, &bars->full[st]);
+                tma_load_3d(dst + kBoxBytes, &map_kv, 64, half * kPageTokens, p0, &bars->full[st]);
+                tma_load_3d(dst + kBoxBytes + kBoxBytes / 2, &map_kv, 64, half * kPageTokens, p1, &bars->full[st]);
+            }
+            __syncwarp();
+            ++rr.count;
+        };
+        for (int x = begin; x < end && ok;) {
+            const Piece pc = piece_at(pl, x, end);
+            const int unit = pc.item / pl.pairs;                       // (layer, prefix sequence, head)
+            const int head = unit % pl.kv_heads, seq0 = unit / pl.kv_heads * pl.share;
+            const int tile0 = 2 * (pc.item % pl.pairs);
+            if (x != begin) {
+                k_pages.open(p.page_table + (long long)unit * p.pages_per_unit, (p.n - 1) / kPageTokens, 2 * pc.k0);
+                k_pages.fetch(2 * pc.k0);
+                v_pages = k_pages;
+            }
+            x += pc.tiles();
+            for (int s = 0; s < (pc.both ? 2 : 1) && ok; ++s) {
+                const uint32_t qs = qr.stage(2);
+                wait_on(&bars->q_empty[qs], qr.parity(2) ^ 1u);
+                if (!ok) break;
+                uint8_t* dst = smem + kOffQ + qs * kOperandBytes;
+                const int seq = seq0 + (tile0 + s) * pl.tile_seqs;
+                if (elect_one()) {
                     mbar_arrive_expect_tx(&bars->q_full[qs], q_bytes);
-                    const int seq = seq0 + (tile0 + s) * pl.tile_seqs;
                     tma_load_4d(dst, &map_q, 0, 0, head, seq, &bars->q_full[qs]);
                     tma_load_4d(dst + kBoxBytes, &map_q, 64, 0, head, seq, &bars->q_full[qs]);
-                    ++qr.count;
                 }
-                const int32_t* table = p.page_table + unit * p.pages_per_unit;
-                const int ahead = pc.both ? 1 : 2, nt = pc.tiles();
-                auto load_k = [&](int j) {
-                    // diagnostics: no copy beyond the first stop_after_tiles K tiles
-                    if (p.stop_after_tiles >= 0 && k_tiles >= p.stop_after_tiles) ok = false;
-                    ++k_tiles;
-                    if (ok) load_tile(table, pc.k0 + j, 0);
-                };
-                for (int j = 0; j < min(ahead, nt) && ok; ++j) load_k(j);
-                for (int j = 0; j < nt && ok; ++j) {
-                    load_tile(table, pc.k0 + j, 1);
-                    if (ok && j + ahead < nt) load_k(j + ahead);
-                }
+                __syncwarp();
+                ++qr.count;
             }
-            if (!ok) {      // aborted: let the copies already issued land before the block exits
-                auto drain = [&](uint64_t* full, const Ring& r, uint32_t n) {
-                    const uint32_t last = r.count < n ? r.count : n;
-                    for (uint32_t k = r.count - last; k < r.count; ++k)
-                        wait_bar(&full[k % n], (k / n) & 1u, abort_flag, p.status, limit, false);
-                };
-                drain(bars->full, rr, kRing);
-                drain(bars->q_full, qr, 2);
+            const int ahead = pc.both ? 1 : 2, nt = pc.tiles();
+            auto load_k = [&](int j) {
+                // diagnostics: no copy beyond the first stop_after_tiles K tiles
+                if (p.stop_after_tiles >= 0 && k_tiles >= p.stop_after_tiles) ok = false;
+                ++k_tiles;
+                if (ok) load_tile(k_pages, pc.k0 + j, 0);
+            };
+            for (int j = 0; j < min(ahead, nt) && ok; ++j) load_k(j);
+            for (int j = 0; j < nt && ok; ++j) {
+                load_tile(v_pages, pc.k0 + j, 1);
+                if (ok && j + ahead < nt) load_k(j + ahead);
             }
+        }
+        if (!ok) {      // aborted: let the copies already issued land before the block exits
+            auto drain = [&](uint64_t* full, const Ring& r, uint32_t n) {
+                const uint32_t last = r.count < n ? r.count : n;
+                for (uint32_t k = r.count - last; k < r.count; ++k)
+                    wait_bar(&full[k % n], (k / n) & 1u, abort_flag, p.status, limit, false);
+            };
+            drain(bars->full, rr, kRing);
+            drain(bars->q_full, qr, 2);
         }
     } else if (warp >= kIssuer) {
         // ------------------------------------------------------------------ MMA issuers, one warp per stream
@@ -260,7 +303,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 umma_bf16_ts(o_col, a_col + 16, b + s8 * (2048 >> 4), instr_desc(true), 1u);
             }
         };
-        for (long long x = begin; x < end;) {
+        for (int x = begin; x < end;) {
             const Piece pc = piece_at(pl, x, end);
             const int nt = pc.tiles(), mine = pc.stream_tiles(s), step = pc.both ? 1 : 2, turns = pc.both ? 2 * nt : nt;
             x += nt;
@@ -341,11 +384,11 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const bool gave_up = dead || !wait_bar(bar, parity, abort_flag, p.status, limit);
             dead = __any_sync(0xffffffffu, gave_up);
         };
-        for (long long x = begin; x < end;) {
+        for (int x = begin; x < end;) {
             const Piece pc = piece_at(pl, x, end);
             x += pc.tiles();
             const int nt = pc.stream_tiles(s);
-            const int tile = 2 * (int)(pc.item % pl.pairs) + (pc.both ? s : 0);
+            const int tile = 2 * (pc.item % pl.pairs) + (pc.both ? s : 0);
             const int r = row / pl.group;                              // sequence inside the row tile
             const int seq = tile * pl.tile_seqs + r;
             const bool valid = r < pl.tile_seqs && seq < pl.share;
@@ -428,10 +471,9 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 if (lane == 0) mbar_arrive(&bars->p_full[s][1]);
             }
             // ---- the piece's partial sums
-            const int nth = (int)blockIdx.x - prefix_block_of(pl, pc.item * pl.key_tiles);
-            const long long unit = pc.item / pl.pairs;
-            const long long u = (unit / pl.kv_heads * pl.share + seq) * pl.kv_heads + unit % pl.kv_heads;     // of the decoding handle
-            const long long at = nth * pl.rows + u * pl.group + (row - r * pl.group);
+            const int nth = (int)blockIdx.x - prefix_block_of(pl, pc.item * pl.key_tiles), unit = pc.item / pl.pairs;
+            const int u = (unit / pl.kv_heads * pl.share + seq) * pl.kv_heads + unit % pl.kv_heads;     // of the decoding handle
+            const long long at = nth * pl.rows + (long long)u * pl.group + (row - r * pl.group);
             if (nt > 0) {
                 wait_on(&bars->o_full[s], o_uses & 1u);
                 ++o_uses;
@@ -509,13 +551,16 @@ PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int gr
     pl.tiles = (pl.share + pl.tile_seqs - 1) / pl.tile_seqs;
     pl.pairs = (pl.tiles + 1) / 2;
     pl.key_tiles = (n + kTile - 1) / kTile;
-    pl.work = (long long)layers * prefixes * kv_heads * pl.pairs * pl.key_tiles;
-    pl.blocks = (int)(pl.work < num_sms ? pl.work : num_sms);
     pl.rows = (long long)layers * batch * kv_heads * group;
+    const long long items = (long long)layers * prefixes * kv_heads * pl.pairs, work = items * pl.key_tiles;
+    pl.items = (int)items;
+    pl.blocks = work > 0x40000000 ? 0 : (int)(work < num_sms ? work : num_sms);
+    if (pl.blocks == 0) return pl;
+    pl.per = (int)(work / pl.blocks);
+    pl.extra = (int)(work % pl.blocks);
     // most blocks that touch one item
-    const long long per = pl.work / pl.blocks;
-    const long long pieces = (pl.key_tiles + per - 1) / per + 1;
-    pl.slots = (int)(pieces < pl.blocks ? pieces : pl.blocks);
+    const int pieces = (pl.key_tiles + pl.per - 1) / pl.per + 1;
+    pl.slots = pieces < pl.blocks ? pieces : pl.blocks;
     return pl;
 }
 
