@@ -26,9 +26,9 @@ namespace lzk {
 
 namespace {
 
-constexpr int kRowThreads = 256;
-constexpr int kStages = 4;                         // of a warp's ring of rows in shared memory
-constexpr int kStageBytes = 1024;                  // four rows of 16-bit elements, two of 32-bit ones
+constexpr int kRowThreads = 128;
+constexpr int kStages = 3;                         // of a warp's ring of rows in shared memory
+constexpr int kStageBytes = 2048;                  // eight rows of 16-bit elements, four of 32-bit ones
 
 struct RowsParams {
     RowsArgs a;
@@ -106,7 +106,7 @@ struct RowRing {
     static constexpr int kChunks = kRowIn / 16;
     uint32_t base, put, get;
     const uint8_t* src;                             // this lane's first 16-byte chunk of the next stage
-    long long step, far;                            // bytes from stage to stage, to the lane's second chunk
+    long long step;                                 // bytes from one of the lane's chunks to the next
     int to_fetch;                                   // rows of the segment not fetched yet
 
     __device__ __forceinline__ void init(uint32_t ring) {
@@ -118,19 +118,20 @@ struct RowRing {
     }
     // The next rows to fetch: one kind's heads.
     __device__ __forceinline__ void segment(const uint8_t* first, long long row_step, int rows) {
-        const int lane = threadIdx.x & 31, row0 = lane / kChunks, row1 = (lane + 32) / kChunks;
-        src = first + (lane % kChunks) * 16 + row0 * row_step;
-        far = (row1 - row0) * row_step;
-        step = kRows * row_step;
+        const int lane = threadIdx.x & 31;
+        src = first + (lane % kChunks) * 16 + lane / kChunks * row_step;
+        step = 32 / kChunks * row_step;
         to_fetch = rows;
     }
     // One stage of the segment (nothing when it is exhausted).
     __device__ __forceinline__ void fetch() {
         if (to_fetch > 0) {
-            const int lane = threadIdx.x & 31;
-            copy16(put, src, lane / kChunks < to_fetch);
-            copy16(put + 512, src + far, (lane + 32) / kChunks < to_fetch);
-            src += step;
+            const int row = (threadIdx.x & 31) / kChunks;
+#pragma unroll
+            for (int i = 0; i < kStageBytes / 512; ++i) {
+                copy16(put + 512 * i, src, row + i * (32 / kChunks) < to_fetch);
+                src += step;
+            }
             to_fetch -= kRows;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -249,10 +250,16 @@ __device__ __forceinline__ void copy_rows(const RowsArgs& a, int heads, int32_t 
 
 // One input type and one type of the output views per launch; keys and values go to the pages when there is a pool.
 template <int kIn, int kOut, bool kInterleaved>
-__global__ void __launch_bounds__(kRowThreads, kIn == kTypeF32 ? 3 : 3) rows_kernel(const __grid_constant__ RowsParams p) {
+__global__ void __launch_bounds__(kRowThreads, 6) rows_kernel(const __grid_constant__ RowsParams p) {
     __shared__ __align__(16) uint8_t rings[kRowThreads / 32][kStages * kStageBytes];
     const RowsArgs& a = p.a;
     const int lane = threadIdx.x & 31, half = lane >> 4, c = lane & 15;
+    // (indexed by the lane, a parameter is read one address at a time)
+    __shared__ double turns_s[kMaxPairs];
+    if (a.pairs > 0) {
+        if (threadIdx.x < kMaxPairs) turns_s[threadIdx.x] = p.turns[threadIdx.x];
+        __syncthreads();
+    }
     const uint32_t task = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
     if (task >= p.tasks) return;
     if (task >= p.row_tasks) {
@@ -316,8 +323,13 @@ __global__ void __launch_bounds__(kRowThreads, kIn == kTypeF32 ? 3 : 3) rows_ker
         float cs[2], sn[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const double t = pos * p.turns[4 * c + 2 * half + e];
-            sincospif(2.f * (float)(t - rint(t)), &sn[e], &cs[e]);
+            const double t = pos * turns_s[4 * c + 2 * half + e];
+            const float turn = (float)(t - rint(t));                   // -1/2 .. 1/2
+            // For 16-bit results the hardware's sine and cosine will do: 2^-20.5 off at most, 2^-9 of a rounding step.
+            if (kOut == kTypeF32)
+                sincospif(2.f * turn, &sn[e], &cs[e]);
+            else
+                __sincosf(6.283185307f * turn, &sn[e], &cs[e]);
             cs[e] *= a.amplitude;
             sn[e] *= a.amplitude;
         }
