@@ -308,7 +308,8 @@ int lazyev_set_head_norm(lazyev_t* h, const float* q_weight, const float* k_weig
 /*
  * Norm and rotation of queries and / or keys, in one pass: rows of n_tokens tokens of every sequence and layer, q with
  * q_heads heads, k with kv_heads (either pair may be NULL).  Arithmetic in float32, one rounding to the output's
- * type; any of the three types on either side.  Output views may equal the input's (in place).  positions: device
+ * type; any of the three types on either side.  An output view may equal its own input's (in place: data, type and
+ * strides); apart from that no output may overlap an input.  positions: device
  * int32 [batch][n_tokens], or NULL for first_position + i.  Nothing in the cache is read or changed.
  * Errors: EINVAL (views, n_tokens <= 0, no rows at all), ESTATE, ECUDA.
  */
