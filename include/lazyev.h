@@ -365,6 +365,9 @@ int lazyev_detach_prefix(lazyev_t* h);
  * Attention of one query row per head over everything cached -- the attached prefix and the own tokens -- without a new
  * token: for the tokens that lazyev_append() loaded last, or to ask again.  q, out as for lazyev_decode_step().  The
  * probabilities of the own tokens are stored as by a decode step; TS, MRI, t and n do not change.
+ * It may be captured into a CUDA graph, like lazyev_norm_rope(), and replayed for other queries in the same buffer while the
+ * cache and its prefix stay as they were at capture.  Calls on one handle share its scratch, state and prefix
+ * workspace, replays of its graphs too: order them.
  * Errors: EINVAL (null; q not 16-byte aligned while a prefix is attached), ESTATE (nothing cached), ECUDA.
  */
 int lazyev_attend(lazyev_t* h, const void* q, void* out);

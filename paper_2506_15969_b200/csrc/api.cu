@@ -76,7 +76,7 @@ struct lazyev {
     PrefixPool prefix_pool = {};           // the prefix's pool as the kernel addresses it
     float* prefix_o = nullptr;
     float2* prefix_ml = nullptr;
-    int users = 0;
+    std::atomic<int> users{0};             // (its users may live on threads of their own)
     // progress
     int t = 0, n = 0, prefill = 0;
     int pos_base = 0;                      // position of the first own token: the prefix's next one
@@ -766,12 +766,13 @@ int lazyev_bind(lazyev_t* h, void* kv_pool, void* state, void* scratch, void* cu
         return fail(h, LAZYEV_EINVAL, "device regions must be 256-byte aligned");
     cudaError_t e = cudaGetDevice(&h->device);
     if (e != cudaSuccess) return cuda_fail(h, e, "cudaGetDevice");
-    cudaDeviceProp prop;
-    e = cudaGetDeviceProperties(&prop, h->device);
-    if (e != cudaSuccess) return cuda_fail(h, e, "cudaGetDeviceProperties");
-    if (prop.major != 10) return fail(h, LAZYEV_ECUDA, "this library is built for sm_100a only (device is sm_%d%d)", prop.major, prop.minor);
-    h->num_sms = prop.multiProcessorCount;
-    h->max_smem = (int)prop.sharedMemPerBlockOptin;
+    int major = 0, minor = 0;              // (single attributes: the whole property record takes milliseconds to fill)
+    e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->max_smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, h->device);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cudaDeviceGetAttribute");
+    if (major != 10) return fail(h, LAZYEV_ECUDA, "this library is built for sm_100a only (device is sm_%d%d)", major, minor);
     if ((e = decode_prepare()) != cudaSuccess) return cuda_fail(h, e, "decode kernel set-up");
     if ((e = select_prepare()) != cudaSuccess) return cuda_fail(h, e, "select kernel set-up");
 
@@ -1214,12 +1215,16 @@ size_t prefix_o_bytes(const PrefixPlan& p) { return align_up((size_t)p.slots * p
 int detach(lazyev_t* h) {
     lazyev_t* prefix = h->shared;
     if (!prefix) return LAZYEV_OK;
-    // what changes the prefix later waits for what reads it now
+    // what changes the prefix later waits for what reads it now (an event belongs to the device that is current)
+    int dev = -1;
     cudaEvent_t done = nullptr;
-    cudaError_t e = cudaEventCreateWithFlags(&done, cudaEventDisableTiming);
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev != h->device) e = cudaSetDevice(h->device);
+    if (e == cudaSuccess) e = cudaEventCreateWithFlags(&done, cudaEventDisableTiming);
     if (e == cudaSuccess) e = cudaEventRecord(done, h->stream);
     if (e == cudaSuccess) e = cudaStreamWaitEvent(prefix->stream, done, 0);
     if (done) cudaEventDestroy(done);
+    if (dev >= 0 && dev != h->device) cudaSetDevice(dev);
     prefix->users -= 1;
     h->shared = nullptr;
     h->plan_cache.clear();                 // launch shapes differ with and without a prefix

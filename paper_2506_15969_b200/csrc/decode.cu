@@ -599,6 +599,14 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                 if (tok0 + base + 16 > p.n) {                    // only the unit's last page can be ragged
                     if (tok0 + base + g >= p.n) x00 = x01 = -INFINITY;
                     if (tok0 + base + g + 8 >= p.n) x10 = x11 = -INFINITY;
+                    // What an earlier sequence left in the slots past n may be NaN or infinite, and its weight of zero does not
+                    // make it vanish: this warp's V rows past n become zeros (in shared memory).
+                    const int first = min(16, max(0, p.n - tok0 - base));
+                    for (int e = lane; e < (16 - first) * kChunksPerRow; e += 32)
+                        *reinterpret_cast<uint4*>(smem + stage * kPageBytes + kPageHalfBytes +
+                                                  (tok_off + first) * kRowBytes + e * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    fence_proxy_async();      // the stage's next page is written through the async proxy
+                    __syncwarp();
                 }
                 store_logits(j, x00, x01, x10, x11);
 

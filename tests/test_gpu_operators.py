@@ -43,7 +43,9 @@ def freqs(pairs, base=1e4):
 
 def engine(layers, q_heads, kv_heads, batch, tokens, window=1, threshold=2.0, **kw):
     """An engine that holds `tokens` tokens and a few more per unit and evicts nothing on its own account."""
-    return binding.Engine(layers, q_heads, kv_heads, D, tokens + window + 1, window, threshold, batch=batch, **kw)
+    e = binding.Engine(layers, q_heads, kv_heads, D, tokens + window + 1, window, threshold, batch=batch, **kw)
+    e.set_auto_evict(False)
+    return e
 
 
 def rows_ref(x, weight, eps, positions, inv_freq, interleaved=False, amplitude=1.0):
@@ -102,6 +104,77 @@ def test_norm_rope_against_64_bits(layers, batch, tokens, hq, hkv, pairs, interl
     for got, x, w in ((qo, q, qw), (ko, k, kw)):
         ref, size = rows_ref(x, w, 1e-5, at, f, interleaved, 1.25)
         assert_rows(got, ref, size, dout)
+
+
+@pytest.mark.parametrize("tokens,hq,hkv,pairs,interleaved,dtype", [
+    (1301, 10, 5, 64, False, torch.bfloat16),    # a warp per token, rows that do not fill a stage
+    (650, 21, 3, 16, True, torch.float16),
+    (1200, 3, 3, 40, False, torch.float32),
+    (40, 41, 41, 64, False, torch.bfloat16),     # more KV heads than a warp keeps pages of
+    (700, 35, 35, 32, True, torch.float32),
+])
+def test_norm_rope_and_append_of_many_tokens(tokens, hq, hkv, pairs, interleaved, dtype):
+    g = gen(tokens)
+    L, B = 1, 2
+    e = engine(L, hq, hkv, B, tokens)
+    e.set_page_table(np.random.RandomState(1).permutation(e.info().units * e.info().pages_per_unit))
+    qkv = randn(g, L, B, tokens, hq + 2 * hkv, D).to(dtype)
+    q, k, v = qkv[..., :hq, :], qkv[..., hq:hq + hkv, :], qkv[..., hq + hkv:, :]
+    f = freqs(pairs)
+    e.set_rope(f, interleaved=interleaved)
+    w = torch.rand(L, D, generator=g, device="cuda") + 0.5
+    e.set_head_norm(w, w, 1e-6)
+    pos = torch.randint(0, 100000, (B, tokens), generator=g, device="cuda", dtype=torch.int32)
+    at = [p.cpu().numpy() for p in pos]
+    ref_q, ref_k = rows_ref(q, w, 1e-6, at, f, interleaved), rows_ref(k, w, 1e-6, at, f, interleaved)
+    for out in (torch.bfloat16, dtype):
+        qo, ko = torch.empty(q.shape, dtype=out, device="cuda"), torch.empty(k.shape, dtype=out, device="cuda")
+        e.norm_rope(q, k, qo, ko, positions=pos)
+        q1, k1 = torch.empty_like(qo), torch.empty_like(ko)
+        e.norm_rope(q, None, q1, None, positions=pos)
+        e.norm_rope(None, k, None, k1, positions=pos)
+        e.synchronize()
+        assert_rows(qo, *ref_q, out)
+        assert_rows(ko, *ref_k, out)
+        assert torch.equal(qo, q1) and torch.equal(ko, k1)
+    e.append(k, v, positions=pos)
+    d = e.dump_state(kv=True)
+    gk = orc.bf16_bits_to_f64(d["k"]).reshape(L, B, hkv, tokens, D).transpose(0, 1, 3, 2, 4)
+    assert_rows(torch.from_numpy(gk.copy()), *ref_k, torch.bfloat16)
+    gv = orc.bf16_bits_to_f64(d["v"]).reshape(L, B, hkv, tokens, D).transpose(0, 1, 3, 2, 4)
+    assert np.array_equal(gv, f64(v.to(torch.bfloat16)))
+    assert np.array_equal(d["pos"][0], np.arange(tokens))               # the cache's own order, whatever the keys turn by
+    # in place, queries and keys in one call
+    e.norm_rope(q, k, q, k, positions=pos)
+    e.synchronize()
+    assert_rows(q, *ref_q, dtype)
+    assert_rows(k, *ref_k, dtype)
+
+
+def test_rows_more_than_four_gigabytes_apart():
+    """Strides and pages behind 32-bit offsets: two sequences whose rows lie 4.8 GB apart, pages at the end of a pool of 9 GB."""
+    g = gen(6)
+    Hq, Hkv, T = 4, 2, 70
+    flat = torch.empty(2 ** 31 + 2 ** 28, dtype=torch.bfloat16, device="cuda")
+    n = T * (Hq + 2 * Hkv) * D
+    x = flat.as_strided((1, 2, T, Hq + 2 * Hkv, D), (0, flat.numel() - n, (Hq + 2 * Hkv) * D, D, 1))
+    x.copy_(randn(g, *x.shape))
+    e = binding.Engine(1, Hq, Hkv, D, 2 ** 22, 64, 2.0, batch=2)
+    inf = e.info()
+    assert inf.units * inf.pages_per_unit * 32768 > 2 ** 32
+    e.set_page_table(np.arange(inf.units * inf.pages_per_unit)[::-1].copy())
+    f = freqs(64)
+    e.set_rope(f)
+    qo = torch.empty(1, 2, T, Hq, D, dtype=torch.bfloat16, device="cuda")
+    e.norm_rope(x[..., :Hq, :], None, qo, None)
+    e.append(x[..., Hq:Hq + Hkv, :], x[..., Hq + Hkv:, :])
+    d = e.dump_state(kv=True)
+    assert_rows(qo, *rows_ref(x[..., :Hq, :], None, 0, [np.arange(T)] * 2, f), torch.bfloat16)
+    ref, size = rows_ref(x[..., Hq:Hq + Hkv, :], None, 0, [np.arange(T)] * 2, f)
+    gk = orc.bf16_bits_to_f64(d["k"]).reshape(1, 2, Hkv, T, D).transpose(0, 1, 3, 2, 4)
+    assert_rows(torch.from_numpy(gk.copy()), ref, size, torch.bfloat16)
+    gv = orc.bf16_bits_to_f64(d["v"]).reshape(1, 2, Hkv, T, D).transpose(0, 1, 3, 2, 4)
+    assert np.array_equal(gv, f64(x[..., Hq + Hkv:, :]))
 
 
 def test_norm_rope_positions_views_and_in_place():
@@ -608,13 +681,14 @@ def test_captured_and_replayed():
             assert_attend(got, own.state_views()["pbar"][:, :n], *attend_ref(got_q[:, :, 0], *kv))
 
 
-@pytest.mark.parametrize("N,limits", [(4000, (0,)), (60000, (1, 3))])     # blocks have one key tile each / six and more
-def test_a_prefix_launch_that_starves_reports_and_recovers(N, limits):
+@pytest.mark.parametrize("L,N,limits", [(1, 4000, (0,)), (1, 60000, (1, 3)),     # blocks have one key tile each / six and more
+                                        (4, 300, (1,))])                          # two unit walks per decode block
+def test_a_prefix_launch_that_starves_reports_and_recovers(L, N, limits):
     """The producer of the prefix kernel stops after some key tiles: bounded waits run out, the status word tells, and
     after a reset the handle works again."""
     g = gen(16)
-    pre, own, *kv = prefixed(g, 1, 40, 1, 8, 1, N, 100)
-    q = randn(g, 1, 40, 8, D)
+    pre, own, *kv = prefixed(g, L, 40, 1, 8, 1, N, 100)
+    q = randn(g, L, 40, 8, D)
     out = torch.empty_like(q)
     own.set_wait_limit(0.002)
     for tiles in limits:
@@ -629,6 +703,74 @@ def test_a_prefix_launch_that_starves_reports_and_recovers(N, limits):
         own.prefill(kv[2], kv[3])
     own.set_wait_limit(2.0)
     check_attend(own, q, *kv)
+
+
+def test_prefix_pages_behind_four_gigabytes():
+    g = gen(21)
+    L, B, Hq, Hkv, N, n = 1, 3, 8, 4, 500, 10
+    pre = binding.Engine(L, Hq, Hkv, D, 2 ** 22, 64, 2.0, batch=1)        # 65 537 pages per unit
+    own = engine(L, Hq, Hkv, B, n)
+    inf = pre.info()
+    assert inf.units * inf.pages_per_unit * 32768 > 2 ** 32
+    pre.set_page_table(np.arange(inf.units * inf.pages_per_unit)[::-1].copy())
+    kp, vp = randn(g, L, 1, Hkv, N, D), randn(g, L, 1, Hkv, N, D)
+    ko, vo = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    pre.prefill(kp, vp)
+    own.attach_prefix(pre)
+    own.prefill(ko, vo)
+    check_attend(own, randn(g, L, B, Hq, D), kp, vp, ko, vo)
+
+
+def test_stale_slots_of_the_own_cache_hold_no_poison():
+    """NaN and infinite rows of an earlier sequence in the slots behind the last token: append, attend, decode and the prompt's
+    replay see nothing of them, with and without a prefix."""
+    g = gen(22)
+    L, B, Hq, Hkv, N = 1, 5, 8, 2, 100
+    kp, vp = randn(g, L, 1, Hkv, N, D), randn(g, L, 1, Hkv, N, D)
+    pre = engine(L, Hq, Hkv, 1, N)
+    pre.prefill(kp, vp)
+    none = kp[:, :, :, :0].expand(L, B, Hkv, 0, D)
+    for shared in (False, True):
+        e = engine(L, Hq, Hkv, B, 200)
+        bad = torch.full((L, B, Hkv, 200, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        bad[..., 64:, :] = float("-inf")
+        e.prefill(bad, bad)
+        for n in (1, 7, 16, 63, 64, 65, 130):
+            e.reset()
+            if shared:
+                e.attach_prefix(pre)
+            k, v = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+            e.append(k.transpose(2, 3), v.transpose(2, 3))
+            q, out = randn(g, L, B, Hq, D), torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+            pk, pv = (kp, vp) if shared else (none, none)
+            check_attend(e, q, pk, pv, k, v)
+            kn, vn = randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+            e.decode_step(q, kn, vn, out)
+            e.synchronize()
+            ref = attend_ref(q, pk, pv, torch.cat((k, kn.unsqueeze(3)), 3), torch.cat((v, vn.unsqueeze(3)), 3))
+            assert_attend(out, e.state_views()["pbar"][:, :n + 1], *ref)
+
+
+def test_decoding_starts_with_no_own_token():
+    g = gen(23)
+    L, B, Hq, Hkv, N = 2, 6, 14, 2, 129
+    pre, own, kp, vp, ko, vo = prefixed(g, L, B, 2, Hq, Hkv, N, 0)
+    ks, vs = [], []
+    for step in range(3):
+        q, kn, vn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+        ks.append(kn), vs.append(vn)
+        out = torch.empty_like(q)
+        if step < 2:
+            own.decode_step(q, kn, vn, out)
+        else:
+            own.decode_step_rows(q, kn, vn, out)
+        own.synchronize()
+        assert_attend(out, own.state_views()["pbar"][:, :step + 1], *attend_ref(q, kp, vp, torch.stack(ks, 3), torch.stack(vs, 3)))
+        if step == 0:
+            with pytest.raises(binding.LazyEvError):
+                own.prefill(ko, vo)                            # it holds tokens now
+    d = own.dump_state()
+    assert np.array_equal(d["pos"][0], N + np.arange(3)) and np.array_equal(d["ts"][0], [1, 2, 3])
 
 
 # ---- together ------------------------------------------------------------------------------------------------------------
