@@ -16,7 +16,7 @@
 
 using namespace lzk;
 
-constexpr int kDensePages = 4;            // own pages per unit up to which a block of a handle with a prefix walks two units at a time
+constexpr int kShortUnitsPerSm = 2;       // units per SM from which short own caches behind a prefix get a warp each
 constexpr int kHostChunks = 3;            // unit ranges the host-buffer entry point pipelines copies over
 
 struct lazyev {
@@ -352,17 +352,18 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
                bool track = true) {
     cudaError_t e = cudaSuccess;
     DecodeConfig c{h->units, h->group, h->pages_per_unit, h->capacity, track ? h->alpha : INFINITY, h->force_splits, h->force_stages, h->force_groups,
-                   h->wait_limit_ns, h->stop_after_pages, h->shared != nullptr, false};
+                   h->wait_limit_ns, h->stop_after_pages, h->shared != nullptr};
     // Launch shape, chosen per number of pages in use and cached.  For every cluster size whose logits
     // fit, a small time model gives the time of the rounds of the round-robin walk; the main launch is
     // the size with the least total.  A partly filled last round goes to a second launch with larger
     // clusters when that is faster, so that more SMs share its units.
     const int np = (n + kPageTokens - 1) / kPageTokens;
-    // A unit of few pages is a chain of short dependent steps that leaves an SM idle most of the time.
-    c.dense = h->shared && np <= kDensePages && h->units > h->num_sms && h->force_splits == 0 && h->force_stages == 0 && h->force_groups == 0;
+    // Short own caches behind a prefix: one launch with a warp per unit, where there are enough units for it.
+    const bool brief = h->shared && n <= kShortTokens && h->units >= kShortUnitsPerSm * h->num_sms && h->force_splits == 0 &&
+                       h->force_stages == 0 && h->force_groups == 0;
     auto cached = h->plan_cache.find(np);
-    if (cached == h->plan_cache.end() || cached->second.forced_splits != h->force_splits ||
-        cached->second.forced_stages != h->force_stages || cached->second.forced_groups != h->force_groups) {
+    if (!brief && (cached == h->plan_cache.end() || cached->second.forced_splits != h->force_splits ||
+        cached->second.forced_stages != h->force_stages || cached->second.forced_groups != h->force_groups)) {
         lazyev::Shape best;
         best.forced_splits = h->force_splits;
         best.forced_stages = h->force_stages;
@@ -423,16 +424,20 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
         if (best_time < 0) return fail(h, LAZYEV_EINVAL, "no decode launch shape fits %d tokens per unit in shared memory", n);
         cached = h->plan_cache.insert_or_assign(np, best).first;
     }
-    const lazyev::Shape shape = cached->second;
-    DecodePlan plan;
-    if (decode_plan(c, n, h->max_smem, shape.splits, &plan) != 0)
+    lazyev::Shape shape;                    // (brief: one walk over all units)
+    shape.clusters = h->units;
+    if (!brief) shape = cached->second;
+    DecodePlan plan = {};
+    if (brief)
+        plan.splits = plan.groups = 1;
+    else if (decode_plan(c, n, h->max_smem, shape.splits, &plan) != 0)
         return fail(h, LAZYEV_EINVAL, "no decode launch shape fits %d tokens per unit in shared memory", n);
     DecodePlan tail_plan = {};
     if (shape.tail_units > 0 && decode_plan(c, n, h->max_smem, shape.tail_splits, &tail_plan) != 0)
         return fail(h, LAZYEV_EINVAL, "no decode launch shape fits %d tokens per unit in shared memory", n);
     const int main_units = h->units - shape.tail_units;
     const int clusters = shape.clusters < main_units ? shape.clusters : main_units;
-    const bool fuse_append = tok && h->fuse_append && shape.tail_units == 0 && main_units <= clusters;
+    const bool fuse_append = tok && h->fuse_append && !brief && shape.tail_units == 0 && main_units <= clusters;
     PrefixView prefix = {};
     if (h->shared) {
         if ((uintptr_t)q & 15) return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned while a prefix is attached");
@@ -509,7 +514,10 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
                          h->shared && !pipe && !fork && r == 0 && !h->profiling};
             const bool beside = is_tail && fork;
             if (e != cudaSuccess) break;
-            e = decode_launch(c, is_tail ? tail_plan : plan, is_tail ? count[r] : (clusters < count[r] ? clusters : count[r]), a,
+            if (brief)
+                e = decode_short_launch(c, a, h->num_sms, h->stream);
+            else
+                e = decode_launch(c, is_tail ? tail_plan : plan, is_tail ? count[r] : (clusters < count[r] ? clusters : count[r]), a,
                               beside ? h->tail_stream : h->stream);
             h->launches += 1;
             if (beside && e == cudaSuccess) {
@@ -529,7 +537,7 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     h->last_plan = plan;
     h->last_tail_units = shape.tail_units;
     h->last_tail_splits = shape.tail_splits;
-    h->last_grid = (clusters + plan.walkers - 1) / plan.walkers * plan.splits;
+    h->last_grid = brief ? decode_short_blocks(h->units, h->num_sms) : clusters * plan.splits;
     return LAZYEV_OK;
 }
 
@@ -774,6 +782,7 @@ int lazyev_bind(lazyev_t* h, void* kv_pool, void* state, void* scratch, void* cu
     if (e != cudaSuccess) return cuda_fail(h, e, "cudaDeviceGetAttribute");
     if (major != 10) return fail(h, LAZYEV_ECUDA, "this library is built for sm_100a only (device is sm_%d%d)", major, minor);
     if ((e = decode_prepare()) != cudaSuccess) return cuda_fail(h, e, "decode kernel set-up");
+    if ((e = decode_short_prepare()) != cudaSuccess) return cuda_fail(h, e, "decode kernel set-up");
     if ((e = select_prepare()) != cudaSuccess) return cuda_fail(h, e, "select kernel set-up");
 
     const Sizes s = sizes_of(h);

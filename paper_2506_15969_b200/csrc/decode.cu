@@ -70,7 +70,6 @@ struct DecodeParams {
     float alpha, scale_log2, inv_group;
     int splits, stages, pages_per_cta, logit_stride, tmem_pages, tmem_cols;
     int off_logits, off_xchg, off_wml, off_slots, off_misc, off_prefix, off_bars;
-    int walker_bytes;                               // shared memory of a walker (blocks of two)
     unsigned long long wait_limit_ns;               // a wait that lasts this long is a failure, not a delay
     int stop_after_pages;                           // diagnostics: the producer issues no copy beyond this many (-1: off)
     int rounds_before;                              // rounds of the round-robin walk that earlier launches of this step took
@@ -116,19 +115,12 @@ __device__ __forceinline__ float ld_rank_f32(const float* local_ptr, uint32_t ra
 }
 
 // NG groups of four consumer warps plus one producer warp.  kPrefix: the softmax of every unit also runs over the
-// tokens of a shared prefix, whose partial sums an earlier launch left in p.prefix.  kWalkers: two = the
-// block is two blocks in one, each with its own producer, ring, barriers and half of tensor memory, walking units of its own
-// (a unit of few pages is a chain of short dependent steps: two at a time fill the SM better, and two real blocks
-// would have to make do with 128 registers a thread).
-template <int NG, bool kPrefix, int kWalkers>
-__global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel(const DecodeParams p) {
+// tokens of a shared prefix, whose partial sums an earlier launch left in p.prefix.
+template <int NG, bool kPrefix>
+__global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const DecodeParams p) {
     constexpr int NW = 4 * NG;
     constexpr int kConsumers = NW * 32;
-    static_assert(kWalkers == 1 || NG == 1, "");
-    extern __shared__ __align__(1024) uint8_t smem_block[];
-    const int hw_warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int walker = kWalkers > 1 ? hw_warp / (NW + 1) : 0, warp = kWalkers > 1 ? hw_warp % (NW + 1) : hw_warp;
-    uint8_t* smem = smem_block + (kWalkers > 1 ? walker * p.walker_bytes : 0);
+    extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* ring = smem;
     float* spill = reinterpret_cast<float*>(smem + p.off_logits);       // logits of the pages beyond tensor memory
     Xchg* xchg = reinterpret_cast<Xchg*>(smem + p.off_xchg);          // [2], alternating per unit
@@ -142,13 +134,13 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + p.off_bars);
     uint64_t* empty = full + p.stages;
 
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int S = p.splits, NS = p.stages, G = p.group, LS = p.logit_stride;
     const bool clustered = S > 1;
     const uint32_t rank = clustered ? cluster_ctarank() : 0u;
-    const int cluster_id = kWalkers > 1 ? blockIdx.x * kWalkers + walker : blockIdx.x / S;
-    const int n_clusters = kWalkers > 1 ? gridDim.x * kWalkers : gridDim.x / S;
+    const int cluster_id = blockIdx.x / S, n_clusters = gridDim.x / S;
 
-    if (warp == 0 && lane == 0) {
+    if (threadIdx.x == 0) {
         for (int i = 0; i < NS; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 4);           // the four warps of the group that owns the page release it
@@ -156,15 +148,14 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (hw_warp == 0) {                        // tensor memory for the logits: allocated and freed by warp 0
-        tmem_alloc(tmem_slot, (uint32_t)(kWalkers * p.tmem_cols));
+    if (warp == 0) {                           // tensor memory for the logits: allocated and freed by warp 0
+        tmem_alloc(tmem_slot, (uint32_t)p.tmem_cols);
         tmem_relinquish_alloc_permit();
     }
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
-    const uint32_t tmem_base = kWalkers > 1 ? *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(tmem_slot) - walker * p.walker_bytes) + walker * p.tmem_cols
-                                            : *tmem_slot;
+    const uint32_t tmem_base = *tmem_slot;
     if (clustered) {   // every block of the cluster is resident before any remote access
         cluster_arrive();
         cluster_wait();
@@ -249,9 +240,8 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
         const int g = lane >> 2, qd = lane & 3;
         const int h0 = 2 * qd, h1 = h0 + 1;
         const bool h0_on = h0 < G, h1_on = h1 < G;
-        const int ctid = warp * 32 + lane;            // consumer thread id: warps 0..NW-1
-        const int grp = warp >> 2, wq = hw_warp & 3;  // (a warp reaches the tensor-memory lanes of its number modulo 4)
-        const int consumer_bar = 1 + walker;
+        const int ctid = threadIdx.x;                 // consumer thread id: warps 0..NW-1
+        const int grp = warp >> 2, wq = warp & 3;
         const uint32_t ring_base = smem_u32(ring);
         const uint32_t lrow = lane & 7;
         // ldmatrix row addresses.  K tile (16 tokens x 16 dims) as the A operand: matrices are
@@ -535,7 +525,7 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
             if (clustered) asm volatile("griddepcontrol.wait;" ::: "memory");
             if (my_units > 0) copy_q(p.unit_begin + cluster_id, 0);
             asm volatile("cp.async.wait_all;" ::: "memory");
-            named_barrier_sync(consumer_bar, kConsumers);
+            named_barrier_sync(1, kConsumers);
         }
 
         // Pages belong to the groups in turn (page pc of the block's walk to group pc mod NG, across unit
@@ -546,7 +536,7 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
         // page lies behind the first unit's merge, so that is made sure of here, once.
         if (NG > 1) {
             observe_through((uint32_t)(NG - 1));
-            named_barrier_sync(consumer_bar, kConsumers);
+            named_barrier_sync(1, kConsumers);
         }
 
         for (int u = p.unit_begin + cluster_id; u < p.unit_end; u += n_clusters, ++it) {
@@ -704,7 +694,7 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                     d1[8] = o[mt][3];
                 }
             }
-            named_barrier_sync(consumer_bar, kConsumers);
+            named_barrier_sync(1, kConsumers);
             if (!clustered) {
                 // One block owns the unit: every warp finishes 8 / NW heads on its own -- the block's
                 // reference, the per-warp scales, l, the log-sum-exp and the normalised output -- so one
@@ -755,7 +745,7 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                     __syncwarp();
                     if (u + n_clusters < p.unit_end) load_prefix(u + n_clusters);
                 }
-                named_barrier_sync(consumer_bar, kConsumers);
+                named_barrier_sync(1, kConsumers);
                 lse0 = lse_s[h0];
                 lse1 = lse_s[h1];
                 u_prev = u;
@@ -779,7 +769,7 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                         xb->l[h] = lc;
                     }
                 }
-                named_barrier_sync(consumer_bar, kConsumers);
+                named_barrier_sync(1, kConsumers);
                 for (int e = ctid; e < kMaxGroup * kHeadDim; e += kConsumers) {
                     const int h = e >> 7, d = e & (kHeadDim - 1);
                     float acc = 0.f;
@@ -791,7 +781,7 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                     cluster_arrive();
                     cluster_wait();
                 } else {
-                    named_barrier_sync(consumer_bar, kConsumers);
+                    named_barrier_sync(1, kConsumers);
                 }
 
                 // ---- merge the blocks of the cluster: exact log-sum-exp per head -----
@@ -808,7 +798,7 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
                         sc_s[r * kMaxGroup + ctid] = mr == -INFINITY ? 0.f : exp2f(mr - M) / L;
                     }
                 }
-                named_barrier_sync(consumer_bar, kConsumers);
+                named_barrier_sync(1, kConsumers);
                 lse0 = lse_s[h0];
                 lse1 = lse_s[h1];
                 u_prev = u;
@@ -852,9 +842,9 @@ __global__ void __launch_bounds__(kWalkers * (4 * NG + 1) * 32, 1) decode_kernel
     // No block may exit while a peer can still read its shared memory; tensor memory goes back last.
     tmem_fence_before_sync();
     __syncthreads();
-    if (hw_warp == 0) {
+    if (warp == 0) {
         tmem_fence_after_sync();
-        tmem_dealloc(tmem_base, (uint32_t)(kWalkers * p.tmem_cols));
+        tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
     }
     if (clustered) {
         cluster_arrive();
@@ -869,16 +859,15 @@ constexpr size_t kMinSmemBytes = 120 * 1024;
 typedef void (*DecodeKernel)(const DecodeParams);
 
 DecodeKernel kernel_of(const DecodePlan& plan, bool prefix) {
-    if (plan.walkers == 2) return decode_kernel<1, true, 2>;
-    if (prefix) return plan.groups == 2 ? decode_kernel<2, true, 1> : decode_kernel<1, true, 1>;
-    return plan.groups == 2 ? decode_kernel<2, false, 1> : decode_kernel<1, false, 1>;
+    if (prefix) return plan.groups == 2 ? decode_kernel<2, true> : decode_kernel<1, true>;
+    return plan.groups == 2 ? decode_kernel<2, false> : decode_kernel<1, false>;
 }
 
 cudaError_t launch_impl(const DecodeParams& p, const DecodePlan& plan, int clusters, cudaStream_t stream,
                         int* max_clusters, bool behind_prefix = false) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(max_clusters ? plan.splits : (clusters + plan.walkers - 1) / plan.walkers * plan.splits, 1, 1);
-    cfg.blockDim = dim3(plan.walkers * (4 * plan.groups + 1) * 32, 1, 1);
+    cfg.gridDim = dim3((max_clusters ? 1 : clusters) * plan.splits, 1, 1);
+    cfg.blockDim = dim3((4 * plan.groups + 1) * 32, 1, 1);
     cfg.dynamicSmemBytes = plan.smem_bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -891,11 +880,7 @@ cudaError_t launch_impl(const DecodeParams& p, const DecodePlan& plan, int clust
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     const DecodeKernel kernel = kernel_of(plan, p.prefix.ml != nullptr);
-    if (max_clusters) {
-        const cudaError_t e = cudaOccupancyMaxActiveClusters(max_clusters, kernel, &cfg);
-        *max_clusters *= plan.walkers;
-        return e;
-    }
+    if (max_clusters) return cudaOccupancyMaxActiveClusters(max_clusters, kernel, &cfg);
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
@@ -919,8 +904,7 @@ static size_t layout(const DecodeConfig& c, int np, int s, int ns, DecodePlan* p
     off += 2 * sizeof(Xchg);
     plan->off_wml = (int)off;
     off += 4 * kMaxGroups * 16 * sizeof(float);
-    plan->walkers = c.dense && s == 1 ? 2 : 1;
-    plan->groups = plan->walkers == 2 ? 1 : c.force_groups > 0 ? c.force_groups : 2;
+    plan->groups = c.force_groups > 0 ? c.force_groups : 2;
     plan->off_slots = (int)off;
     off += (size_t)4 * plan->groups * kMaxGroup * kXchgRow * sizeof(float);
     plan->off_misc = (int)off;
@@ -937,8 +921,6 @@ static size_t layout(const DecodeConfig& c, int np, int s, int ns, DecodePlan* p
     plan->tmem_cols = cols;
     // More than half of an SM's shared memory: one block per SM, so the tensor-memory allocation
     // of one block never waits for another block's.
-    plan->walker_bytes = (int)((off + 127) / 128 * 128);
-    if (plan->walkers == 2) off = 2 * (size_t)plan->walker_bytes;
     if (off < kMinSmemBytes) off = kMinSmemBytes;
     plan->smem_bytes = (int)off;
     return off;
@@ -948,10 +930,6 @@ int decode_plan(const DecodeConfig& c, int n, int max_smem, int splits, DecodePl
     const int np = (n + kPageTokens - 1) / kPageTokens;
     constexpr int kMaxStages = 6;
     const int min_stages = 2;      // a stage per group being worked on
-    if (c.dense && splits == 1) {
-        const size_t bytes = layout(c, np, 1, 2, plan);
-        return plan->tmem_cols <= 256 && bytes <= (size_t)max_smem ? 0 : -1;
-    }
     if (c.force_stages > 0)
         return c.force_stages >= min_stages && layout(c, np, splits, c.force_stages, plan) <= (size_t)max_smem ? 0 : -1;
     for (int ns = kMaxStages; ns >= min_stages; --ns)
@@ -960,8 +938,7 @@ int decode_plan(const DecodeConfig& c, int n, int max_smem, int splits, DecodePl
 }
 
 cudaError_t decode_prepare() {
-    const DecodeKernel kernels[5] = {decode_kernel<1, false, 1>, decode_kernel<2, false, 1>, decode_kernel<1, true, 1>,
-                                     decode_kernel<2, true, 1>, decode_kernel<1, true, 2>};
+    const DecodeKernel kernels[4] = {decode_kernel<1, false>, decode_kernel<2, false>, decode_kernel<1, true>, decode_kernel<2, true>};
     for (const DecodeKernel k : kernels) {
         const cudaError_t e = cudaFuncSetAttribute((const void*)k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
         if (e != cudaSuccess) return e;
@@ -1011,7 +988,6 @@ cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clu
     p.off_slots = plan.off_slots;
     p.off_misc = plan.off_misc;
     p.off_prefix = plan.off_prefix;
-    p.walker_bytes = plan.walker_bytes;
     p.off_bars = plan.off_bars;
     p.wait_limit_ns = c.wait_limit_ns;
     p.stop_after_pages = c.stop_after_pages;

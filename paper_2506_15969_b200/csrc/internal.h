@@ -69,12 +69,9 @@ struct DecodeConfig {
     unsigned long long wait_limit_ns;   // bounded waits give up after this long
     int stop_after_pages;  // diagnostics: -1 = off
     bool prefix;           // the launches add the partial sums of a shared prefix
-    bool dense;            // two walkers per block where one owns a unit
 };
 
 struct DecodePlan {
-    int walkers;           // unit walks per block (clusters are counted in walks)
-    int walker_bytes;
     int splits, stages, groups, pages_per_cta, logit_stride, tmem_pages, tmem_cols;
     int off_logits, off_xchg, off_wml, off_slots, off_misc, off_prefix, off_bars, smem_bytes;
 };
@@ -102,6 +99,12 @@ cudaError_t decode_prepare();
 cudaError_t decode_max_clusters(const DecodePlan& plan, int* clusters);
 cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clusters, const DecodeArgs& a,
                           cudaStream_t stream);
+
+// Short units behind a shared prefix: a warp per unit (a.prefix set, a.n <= kShortTokens, no append inside).
+constexpr int kShortTokens = 256;
+cudaError_t decode_short_prepare();
+int decode_short_blocks(int units, int num_sms);
+cudaError_t decode_short_launch(const DecodeConfig& c, const DecodeArgs& a, int num_sms, cudaStream_t stream);
 
 // ---- cache maintenance ---------------------------------------------------------
 cudaError_t init_state_launch(const Geometry& geo, StateView st, cudaStream_t stream);

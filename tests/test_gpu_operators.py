@@ -400,6 +400,15 @@ def check_attend(own, q, kp, vp, ko, vo):
     (28, 32, 2, 28, 4, 300, 10),        # more items than blocks
     (5, 1, 1, 12, 2, 200, 700),         # own tokens longer than the prefix, no sharing
     (1, 260, 1, 4, 4, 513, 0),
+    (4, 40, 1, 8, 4, 200, 0),           # many units with short own caches: a warp each
+    (4, 40, 2, 16, 2, 200, 1),
+    (4, 40, 1, 28, 4, 1000, 16),
+    (4, 75, 1, 5, 1, 5000, 17),         # many partial sums per row
+    (16, 40, 1, 12, 2, 70, 65),
+    (16, 40, 1, 7, 7, 70, 240),
+    (16, 40, 1, 6, 2, 70, 255),
+    (30, 45, 1, 40, 8, 70, 256),        # several units per warp
+    (30, 45, 3, 9, 3, 70, 257),         # one token too long for it
 ])
 def test_attend_against_64_bits(L, B, P, Hq, Hkv, N, n):
     g = gen(N * 7 + n)
@@ -584,11 +593,11 @@ def test_step_entry_points_agree_with_a_prefix():
             assert np.array_equal(want[f], got[f]), (name, f)
 
 
-@pytest.mark.parametrize("L,ranges", [(14, 1), (28, 3)])       # 1792 units are 7 rounds of the walk, 3584 are 13
-def test_wide_host_step_with_a_prefix(L, ranges):
+@pytest.mark.parametrize("n,ranges", [(64, 1), (300, 3)])       # short own caches are one launch, longer ones a walk of 13 rounds
+def test_wide_host_step_with_a_prefix(n, ranges):
     """More units than blocks: the host-buffer step runs in unit ranges, the prefix launch once for all of them."""
     g = gen(12)
-    B, Hq, Hkv, N, n = 32, 28, 4, 200, 64
+    L, B, Hq, Hkv, N = 14, 32, 28, 4, 200
     pre, own, *kv = prefixed(g, L, B, 1, Hq, Hkv, N, n)
     twin = engine(L, Hq, Hkv, B, n)
     twin.attach_prefix(pre)
@@ -682,7 +691,7 @@ def test_captured_and_replayed():
 
 
 @pytest.mark.parametrize("L,N,limits", [(1, 4000, (0,)), (1, 60000, (1, 3)),     # blocks have one key tile each / six and more
-                                        (4, 300, (1,))])                          # two unit walks per decode block
+                                        (16, 300, (1,))])                         # a warp per unit in the decode launch
 def test_a_prefix_launch_that_starves_reports_and_recovers(L, N, limits):
     """The producer of the prefix kernel stops after some key tiles: bounded waits run out, the status word tells, and
     after a reset the handle works again."""
