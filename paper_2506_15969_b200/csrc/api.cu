@@ -16,7 +16,7 @@
 
 using namespace lzk;
 
-constexpr int kShortUnitsPerSm = 2;       // units per SM from which short own caches behind a prefix get a warp each
+constexpr int kShortUnitsPerSm = 3;       // units per SM from which short own caches behind a prefix get a warp each
 constexpr int kHostChunks = 3;            // unit ranges the host-buffer entry point pipelines copies over
 
 struct lazyev {

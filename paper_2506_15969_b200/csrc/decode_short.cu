@@ -1,13 +1,15 @@
 // Decode attention over short own caches behind a shared prefix: a warp per cache unit.
 //
 // Same mathematics as decode.cu (Appendix A, Eq. (attn), over the prefix's tokens and the own ones; pbar and Eq. (1) for the own
-// ones), for units of at most 256 own tokens -- sequences that have just begun to answer.  Such a unit is a chain of short
+// ones), for units of at most 384 own tokens -- sequences that have just begun to answer.  Such a unit is a chain of short
 // dependent steps: a block of nine warps on it spends its time in barriers and merges (4900 clocks for 64 tokens, of which 1400
 // would stream them).  Here every warp walks units of its own: it fetches its tiles of 16 tokens (4 KiB of K, 4 KiB of V) itself
 // through a three-stage ring, keeps all heads' O^T in registers, adds the prefix's partial sums to it in the same layout, and
 // meets no other warp between the start and the end of the launch.  Eight units per SM are in flight.
 //
-// Bound by HBM for many units (512 bytes a token); for few by the latency of one unit.
+// Bound by HBM for many units (512 bytes a token); for few by the latency of one unit.  Measured on B200, with a prefix of 64 tokens
+// (both launches): 4096 units of 256 tokens 108 us against 126 us with a block per unit, 1792 of 64 tokens 29 against 50;
+// 3584 units of 512 tokens 174 against 172, 256 units of 256 tokens 31 against 23: hence the limits on tokens and units.
 #include "internal.h"
 
 namespace lzk {
@@ -23,7 +25,8 @@ constexpr int kMaxTiles = kShortTokens / kTileTokens;
 constexpr int kSets = 2;                                        // partial sums of the prefix fetched while the unit streams
 constexpr int kOffBars = kWarps * kRing * kTileBytes;
 constexpr int kSmem = kOffBars + kWarps * kRing * 8 + 64;
-constexpr uint32_t kTmemCols = 2 * 4 * kMaxTiles;               // four columns per tile; warps w and w + 4 share lanes
+constexpr uint32_t kTmemCols = 256;                             // four columns per tile; warps w and w + 4 share lanes
+static_assert(2 * 4 * kMaxTiles <= kTmemCols, "");
 constexpr float kRaiseMargin = 8.f;
 
 struct ShortParams {

@@ -401,14 +401,15 @@ def check_attend(own, q, kp, vp, ko, vo):
     (5, 1, 1, 12, 2, 200, 700),         # own tokens longer than the prefix, no sharing
     (1, 260, 1, 4, 4, 513, 0),
     (4, 40, 1, 8, 4, 200, 0),           # many units with short own caches: a warp each
-    (4, 40, 2, 16, 2, 200, 1),
+    (6, 40, 2, 16, 2, 200, 1),
     (4, 40, 1, 28, 4, 1000, 16),
-    (4, 75, 1, 5, 1, 5000, 17),         # many partial sums per row
+    (4, 150, 1, 5, 1, 5000, 17),        # many partial sums per row
     (16, 40, 1, 12, 2, 70, 65),
     (16, 40, 1, 7, 7, 70, 240),
     (16, 40, 1, 6, 2, 70, 255),
-    (30, 45, 1, 40, 8, 70, 256),        # several units per warp
-    (30, 45, 3, 9, 3, 70, 257),         # one token too long for it
+    (30, 45, 1, 40, 8, 70, 383),        # several units per warp
+    (30, 45, 1, 3, 1, 70, 384),
+    (30, 45, 3, 9, 3, 70, 385),         # one token too long for it
 ])
 def test_attend_against_64_bits(L, B, P, Hq, Hkv, N, n):
     g = gen(N * 7 + n)
@@ -593,7 +594,7 @@ def test_step_entry_points_agree_with_a_prefix():
             assert np.array_equal(want[f], got[f]), (name, f)
 
 
-@pytest.mark.parametrize("n,ranges", [(64, 1), (300, 3)])       # short own caches are one launch, longer ones a walk of 13 rounds
+@pytest.mark.parametrize("n,ranges", [(64, 1), (400, 3)])       # short own caches are one launch, longer ones a walk of 13 rounds
 def test_wide_host_step_with_a_prefix(n, ranges):
     """More units than blocks: the host-buffer step runs in unit ranges, the prefix launch once for all of them."""
     g = gen(12)
