@@ -479,7 +479,7 @@ int lazyev_dump_state(lazyev_t* h, lazyev_dump_t* dump);
  * (unit_begin = 0, unit_count = units) with pos, ts, mri, k and v set (host arrays laid out
  * as dump_state writes them, row stride snap->capacity; pbar optional, score ignored) and
  * its n and t; `prefill` is the prompt length of the original run (positions of new tokens
- * continue from prefill + t).  The handle may have another capacity than the one the
+ * continue from prefill + t; behind an attached prefix, attached before, prefill may be 0 and counts own tokens only).  The handle may have another capacity than the one the
  * snapshot came from as long as n fits.  Decoding then continues exactly as the original
  * handle would have.  Synchronises the stream; a slow path (one host-to-device copy per page).
  * Errors: EINVAL (partial snapshot, sizes), ESTATE (not bound, or already holds a cache), ECUDA.
@@ -515,6 +515,7 @@ int lazyev_mri_quantile(lazyev_t* h, int unit_begin, int unit_count, double frac
  *             one float probability written per token, queries read, outputs written
  *   select  : units * (8 * candidates + 4 * budget)       -- TS, MRI read; source list written
  *   compact : moved rows * (2 * (512 + 12) + 4)           -- rows and their state read and written
+ * (Prefix and row launches are not among them.)
  * lazyev_get_profile() synchronises the stream; reset != 0 clears the sums.
  */
 typedef struct lazyev_profile {

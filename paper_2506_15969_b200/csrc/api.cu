@@ -344,9 +344,9 @@ cudaError_t run_prefix(lazyev_t* h, const void* q) {
     return prefix_launch(h->prefix_plan, a, h->stream);
 }
 
-// The decode launches of one step: attention of q over the shared prefix, if there is one, and the first n cached
-// tokens of every unit with tracking (unless `track` is false) at time t.  `tok` (may be null) is the token to append at slot n - 1 first: as a launch of
-// its own, or -- when every block of the decode launch takes exactly one unit, the launch-latency-sized
+// The decode launches of one step: attention of q over the shared prefix, if there is one, and the first n cached tokens of
+// every unit with tracking (unless `track` is false) at time t.  `tok` (may be null) is the token to append at slot n - 1 first: as
+// a launch of its own, or -- when every block of the decode launch takes exactly one unit, the launch-latency-sized
 // problems -- inside the decode launch.
 int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPipe* pipe, const NewToken* tok = nullptr,
                bool track = true) {
@@ -362,8 +362,9 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     const bool brief = h->shared && n <= kShortTokens && h->units >= kShortUnitsPerSm * h->num_sms && h->force_splits == 0 &&
                        h->force_stages == 0 && h->force_groups == 0;
     auto cached = h->plan_cache.find(np);
-    if (!brief && (cached == h->plan_cache.end() || cached->second.forced_splits != h->force_splits ||
-        cached->second.forced_stages != h->force_stages || cached->second.forced_groups != h->force_groups)) {
+    const bool planned = cached != h->plan_cache.end() && cached->second.forced_splits == h->force_splits &&
+                         cached->second.forced_stages == h->force_stages && cached->second.forced_groups == h->force_groups;
+    if (!planned && !brief) {
         lazyev::Shape best;
         best.forced_splits = h->force_splits;
         best.forced_stages = h->force_stages;
@@ -1476,7 +1477,8 @@ int lazyev_load_state(lazyev_t* h, const lazyev_dump_t* d, int prefill) {
     if (h->prefilled) return fail(h, LAZYEV_ESTATE, "load_state on a handle that already holds a cache");
     if (d->unit_begin != 0 || d->unit_count != h->units) return fail(h, LAZYEV_EINVAL, "the snapshot must cover all %d units", h->units);
     if (!d->pos || !d->ts || !d->mri || !d->k || !d->v) return fail(h, LAZYEV_EINVAL, "pos, ts, mri, k and v are required");
-    if (d->n <= 0 || d->n > h->capacity || d->capacity < d->n || d->t < 0 || prefill <= 0)
+    // (sequences behind a shared prefix may have begun with no prompt of their own)
+    if (d->n <= 0 || d->n > h->capacity || d->capacity < d->n || d->t < 0 || prefill < 0 || (prefill == 0 && !h->shared))
         return fail(h, LAZYEV_EINVAL, "snapshot sizes out of range (n = %d, capacity here = %d)", d->n, h->capacity);
     const size_t scap = (size_t)d->capacity, width = (size_t)d->n * 4;
     cudaError_t e = cudaMemcpy2DAsync(h->st.pos, (size_t)h->capacity * 4, d->pos, scap * 4, width, h->units, cudaMemcpyHostToDevice, h->stream);

@@ -474,6 +474,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             const int nth = (int)blockIdx.x - prefix_block_of(pl, pc.item * pl.key_tiles), unit = pc.item / pl.pairs;
             const int u = (unit / pl.kv_heads * pl.share + seq) * pl.kv_heads + unit % pl.kv_heads;     // of the decoding handle
             const long long at = nth * pl.rows + (long long)u * pl.group + (row - r * pl.group);
+            const bool writes = valid && in_bounds(nth >= 0 && nth < pl.slots && at >= 0 && at < pl.slots * pl.rows, p.status);
             if (nt > 0) {
                 wait_on(&bars->o_full[s], o_uses & 1u);
                 ++o_uses;
@@ -491,7 +492,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                         float o[32];
                         tmem_ld32(o_cols + 32 * c, o);
                         tmem_wait_ld();
-                        if (valid) {
+                        if (writes) {
 #pragma unroll
                             for (int i = 0; i < 8; ++i) dst[16 * hf + 8 * c + i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                         }
@@ -515,7 +516,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                         tmem_ld16(lane_base + kColO + col + c, o0);
                         tmem_ld16(lane_base + kColO + 128 + col + c, o1);
                         tmem_wait_ld();
-                        if (valid) {
+                        if (writes) {
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o0[i] = o0[i] * f0 + (pc.tiles() > 1 ? o1[i] * f1 : 0.f);
 #pragma unroll
@@ -527,7 +528,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 }
             }
             tmem_fence_before_sync();
-            if (valid && hf == 0 && (pc.both || s == 0)) p.ml[at] = make_float2(m, l);
+            if (writes && hf == 0 && (pc.both || s == 0)) p.ml[at] = make_float2(m, l);
         }
     }
 

@@ -15,7 +15,7 @@
 // instructions: a half-warp works on one row; each lane holds two groups of four elements chosen so that the partners of
 // a rotation sit in the same lane (no exchange, nothing read twice); angles, weights and signs are folded into four
 // factors per pair that a warp computes once for all the heads of a kind (queries, keys, values) it takes of a token,
-//   z_a = inv (a f_a + b g_a),  z_b = inv (b f_b + a g_b),
+//   z_a = (inv a) f_a + (inv b) g_a,  z_b = (inv b) f_b + (inv a) g_b,
 // and the arithmetic runs two elements per instruction.
 //
 // Measured on B200 (copy bandwidth 6.54 TB/s): 32768 tokens of 40 + 8 bf16 heads 128 us, 6.3 TB/s; 131072 tokens of 8 key and
@@ -188,14 +188,15 @@ __device__ __forceinline__ void turn_rows(const RowsArgs& a, const WarpRows& r, 
             const uint64_t inv2 = pack2(inv, inv);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                uint64_t ua = mul2(va[i], f.fa[i]), ub = mul2(vb[i], f.fb[i]);
+                const uint64_t ya = mul2(va[i], inv2), yb = mul2(vb[i], inv2);
+                uint64_t ua = mul2(ya, f.fa[i]), ub = mul2(yb, f.fb[i]);
                 if (turns) {                        // (elements that stay must not meet others: 0 * inf)
-                    ua = fma2(vb[i], f.ga[i], ua);
-                    ub = fma2(va[i], f.gb[i], ub);
+                    ua = fma2(yb, f.ga[i], ua);
+                    ub = fma2(ya, f.gb[i], ub);
                 }
                 float z0, z1, z2, z3;
-                unpack2(mul2(ua, inv2), z0, z1);
-                unpack2(mul2(ub, inv2), z2, z3);
+                unpack2(ua, z0, z1);
+                unpack2(ub, z2, z3);
                 if constexpr (kInterleaved) {
                     float* x = i ? xb : xa;
                     x[0] = z0; x[1] = z2; x[2] = z1; x[3] = z3;

@@ -783,6 +783,65 @@ def test_decoding_starts_with_no_own_token():
     assert np.array_equal(d["pos"][0], N + np.arange(3)) and np.array_equal(d["ts"][0], [1, 2, 3])
 
 
+def test_resume_behind_a_prefix():
+    """A snapshot of sequences that began with no prompt of their own goes into another handle behind the same prefix."""
+    g = gen(24)
+    L, B, Hq, Hkv, N = 1, 4, 8, 2, 90
+    pre, a, *_ = prefixed(g, L, B, 1, Hq, Hkv, N, 0)
+    out = torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    for _ in range(5):
+        a.decode_step(randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D), out)
+    snap = a.dump_state(kv=True)
+    b = engine(L, Hq, Hkv, B, 5)
+    with pytest.raises(binding.LazyEvError):
+        b.load_state(snap, 0)                                  # without a prefix there has to be a prompt
+    b.attach_prefix(pre)
+    b.load_state(snap, 0)
+    assert b.info().next_position == a.info().next_position == N + 5
+    q, kn, vn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+    out2 = torch.empty_like(out)
+    a.decode_step(q, kn, vn, out)
+    b.decode_step(q, kn, vn, out2)
+    x, y = a.dump_state(kv=True), b.dump_state(kv=True)
+    assert torch.equal(out, out2)
+    for name in ("pos", "ts", "mri", "pbar", "k", "v"):
+        assert np.array_equal(x[name], y[name]), name
+
+
+def test_rows_of_extreme_size():
+    """Zero rows, rows near the largest and smallest bf16, and a row with an infinity: the norm's factor meets the elements first,
+    as in the formula in 32 bits, and rows do not touch each other."""
+    e = engine(1, 4, 4, 1, 1)
+    e.set_rope(freqs(64))
+    w = torch.full((1, D), 1.5, device="cuda")
+    e.set_head_norm(w, None, 1e-6)
+    x = torch.ones(1, 1, 1, 4, D, dtype=torch.bfloat16, device="cuda")
+    x[..., 0, :], x[..., 1, :], x[..., 2, :] = 0.0, 1e18, 1e-30
+    x[..., 3, 7] = float("inf")
+    out = torch.empty_like(x)
+    e.norm_rope(x, None, out, None, first_position=3)
+    e.synchronize()
+    finite = x[..., :3, :]
+    ref, size = rows_ref(finite, w, 1e-6, [[3]], freqs(64))
+    assert_rows(out[..., :3, :], ref, size, torch.bfloat16)
+    assert not bool(torch.isfinite(out[..., 3, 7]).any())
+
+
+def test_range_checked_build():
+    """The same tests through the build whose kernels check every slot, page and work index."""
+    import os
+    import subprocess
+    import sys
+    if binding.debug_bounds_requested():
+        pytest.skip("already inside the range-checked run")
+    res = subprocess.run([sys.executable, "-m", "pytest", os.path.abspath(__file__), "-q", "-x", "-m", "gpu", "-k",
+                          "64_bits or chunks or many_tokens or rise or poison or serving or clusters or entry_points"],
+                         env=dict(os.environ, LAZYEV_DEBUG_BOUNDS="1"), capture_output=True, text=True,
+                         cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert res.returncode == 0, res.stdout[-3000:] + res.stderr[-2000:]
+    assert " passed" in res.stdout and "failed" not in res.stdout
+
+
 # ---- together ------------------------------------------------------------------------------------------------------------
 
 def test_serving_run_from_projections_to_evictions():
