@@ -4,7 +4,7 @@
 // ones), for units of at most 384 own tokens -- sequences that have just begun to answer.  Such a unit is a chain of short
 // dependent steps: a block of nine warps on it spends its time in barriers and merges (4900 clocks for 64 tokens, of which 1400
 // would stream them).  Here every warp walks units of its own: it fetches its tiles of 16 tokens (4 KiB of K, 4 KiB of V) itself
-// through a three-stage ring, keeps all heads' O^T in registers, adds the prefix's partial sums to it in the same layout, and
+// through a ring, keeps all heads' O^T in registers, adds the prefix's partial sums to it in the same layout, and
 // meets no other warp between the start and the end of the launch.  Eight units per SM are in flight.
 //
 // Bound by HBM for many units (512 bytes a token); for few by the latency of one unit.  Measured on B200, with a prefix of 64 tokens
@@ -20,10 +20,14 @@ constexpr int kWarps = 8;
 constexpr int kTileTokens = 16;
 constexpr int kTileHalf = kTileTokens * kRowBytes;              // K or V of a tile: 4 KiB
 constexpr int kTileBytes = 2 * kTileHalf;
-constexpr int kRing = 3;
+constexpr int kRing = 2;
 constexpr int kMaxTiles = kShortTokens / kTileTokens;
 constexpr int kSets = 2;                                        // partial sums of the prefix fetched while the unit streams
-constexpr int kOffBars = kWarps * kRing * kTileBytes;
+constexpr int kSumRow = kHeadDim * 4 + 16;                      // a partial sum's O: a fragment read meets no bank twice
+constexpr int kQRow = kRowBytes + 16;
+// of a warp: the ring, the next unit's queries, the unit's first partial sums
+constexpr int kOffQ = kRing * kTileBytes, kOffSums = kOffQ + kMaxGroup * kQRow, kWarpBytes = kOffSums + kSets * kMaxGroup * kSumRow;
+constexpr int kOffBars = kWarps * kWarpBytes;
 constexpr int kSmem = kOffBars + kWarps * kRing * 8 + 64;
 constexpr uint32_t kTmemCols = 256;                             // four columns per tile; warps w and w + 4 share lanes
 static_assert(2 * 4 * kMaxTiles <= kTmemCols, "");
@@ -63,17 +67,20 @@ __device__ __forceinline__ bool wait_tile(uint64_t* bar, uint32_t parity, int32_
     return true;
 }
 
-// One set of the prefix's partial sums in the layout of the O^T fragments: heads h0, h1; dimensions 16 i + g, 16 i + g + 8.
-struct SumSet {
-    float2 ml0, ml1;
-    float v[8][4];
-};
+__device__ __forceinline__ void copy16(uint32_t smem, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(__cvta_generic_to_global(src)) : "memory");
+}
+// This warp's copies have arrived, for all its lanes.
+__device__ __forceinline__ void copies_done() {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+}
 
 __global__ void __launch_bounds__(kWarps * 32, 1) decode_short_kernel(const __grid_constant__ ShortParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffBars + kWarps * kRing * 8);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint8_t* ring = smem + warp * kRing * kTileBytes;
+    uint8_t* ring = smem + warp * kWarpBytes;
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + kOffBars) + warp * kRing;
     if (lane == 0) {
         for (int i = 0; i < kRing; ++i) mbar_init(&full[i], 1);
@@ -133,40 +140,41 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_short_kernel(const __gr
     const uint32_t k_term = ((lane >> 4) ^ lrow) << 4, v_term = (((lane >> 3) & 1) ^ lrow) << 4;
     const uint32_t ring_base = smem_u32(ring);
 
-    uint32_t qb[8][2], qn[8][2];
-    auto load_q = [&](int u, uint32_t (&dst)[8][2]) {
-        const __nv_bfloat16* row = p.q + ((size_t)u * G + g) * kHeadDim + 2 * qd;
+    // Queries and partial sums come as whole rows through shared memory (in fragment layout their loads would touch eight
+    // sectors each, 80 of them per unit).
+    const uint32_t q_s = ring_base + kOffQ, sums_s = ring_base + kOffSums;
+    uint32_t qb[8][2];
+    auto copy_q = [&](int u) {
+        for (int h = lane >> 4; h < G; h += 2)
+            copy16(q_s + h * kQRow + 16 * (lane & 15), p.q + ((size_t)u * G + h) * kHeadDim + 8 * (lane & 15));
+    };
+    auto read_q = [&]() {                      // Q as the B operand: rows are heads, two 16-dimension steps per instruction
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-            dst[ks][0] = g < G ? *reinterpret_cast<const uint32_t*>(row + 16 * ks) : 0u;
-            dst[ks][1] = g < G ? *reinterpret_cast<const uint32_t*>(row + 16 * ks + 8) : 0u;
+        for (int ks = 0; ks < 8; ks += 2)
+            ldmatrix_x4(qb[ks][0], qb[ks][1], qb[ks + 1][0], qb[ks + 1][1], q_s + (lane & 7) * kQRow + 32 * ks + 16 * (lane >> 3));
+    };
+    float2 ml[kSets];                          // lane h: head h's (reference, l) of the sets
+    auto copy_sets = [&](int u, int s0) {
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) {
+            ml[k] = make_float2(-INFINITY, 0.f);
+            if (s0 + k >= p.prefix.plan.slots) continue;
+            const long long row = (s0 + k) * p.prefix.plan.rows + (long long)u * G;
+            if (lane < G) ml[k] = p.prefix.ml[row + lane];
+            for (int h = 0; h < G; ++h) copy16(sums_s + (k * kMaxGroup + h) * kSumRow + 16 * lane, p.prefix.o + (row + h) * kHeadDim + 4 * lane);
         }
     };
-    auto load_set = [&](int u, int s, SumSet& set) {
-        set.ml0 = set.ml1 = make_float2(-INFINITY, 0.f);
-        if (s >= p.prefix.plan.slots) return;
-        const long long row = s * p.prefix.plan.rows + (long long)u * G + h0;
-        const float* o = p.prefix.o + row * kHeadDim + g;
-        if (h0_on) set.ml0 = p.prefix.ml[row];
-        if (h1_on) set.ml1 = p.prefix.ml[row + 1];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            set.v[i][0] = h0_on ? o[16 * i] : 0.f;
-            set.v[i][1] = h1_on ? o[16 * i + kHeadDim] : 0.f;
-            set.v[i][2] = h0_on ? o[16 * i + 8] : 0.f;
-            set.v[i][3] = h1_on ? o[16 * i + 8 + kHeadDim] : 0.f;
-        }
-    };
-    if (walker < p.units) load_q(walker, qb);
+    for (int h = G; h < kMaxGroup; ++h)        // rows of heads that are not there
+        if (lane < 16) *reinterpret_cast<uint4*>(ring + kOffQ + h * kQRow + 16 * lane) = make_uint4(0u, 0u, 0u, 0u);
+    if (walker < p.units) copy_q(walker);
+    copies_done();
 
     bool first = true, alive = true;
     for (int u = walker; u < p.units && alive; u += walkers) {
-        SumSet sets[kSets];
-        if (!first) {
-#pragma unroll
-            for (int s = 0; s < kSets; ++s) load_set(u, s, sets[s]);
-        }
-        if (u + walkers < p.units) load_q(u + walkers, qn);
+        read_q();
+        __syncwarp();
+        if (u + walkers < p.units) copy_q(u + walkers);
+        if (!first) copy_sets(u, 0);
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float o[8][4];
 #pragma unroll
@@ -255,8 +263,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_short_kernel(const __gr
         // ones); its sums are waited for here, once.
         if (first) {
             asm volatile("griddepcontrol.wait;" ::: "memory");
-#pragma unroll
-            for (int s = 0; s < kSets; ++s) load_set(u, s, sets[s]);
+            copy_sets(u, 0);
             first = false;
         }
 #pragma unroll
@@ -264,30 +271,33 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_short_kernel(const __gr
             l0 += __shfl_xor_sync(0xffffffffu, l0, s);
             l1 += __shfl_xor_sync(0xffffffffu, l1, s);
         }
-        auto add = [&](const SumSet& set) {
-            const bool on0 = set.ml0.x > -INFINITY, on1 = set.ml1.x > -INFINITY;       // what an absent set's O holds is anything
-            const float n0 = fmaxf(m0, set.ml0.x), n1 = fmaxf(m1, set.ml1.x);
-            const float c0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
-            const float d0 = on0 ? fast_exp2(set.ml0.x - n0) : 0.f, d1 = on1 ? fast_exp2(set.ml1.x - n1) : 0.f;
+        for (int s = 0;; s += kSets) {
+            copies_done();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                o[i][0] = o[i][0] * c0 + (on0 ? set.v[i][0] * d0 : 0.f);
-                o[i][1] = o[i][1] * c1 + (on1 ? set.v[i][1] * d1 : 0.f);
-                o[i][2] = o[i][2] * c0 + (on0 ? set.v[i][2] * d0 : 0.f);
-                o[i][3] = o[i][3] * c1 + (on1 ? set.v[i][3] * d1 : 0.f);
+            for (int k = 0; k < kSets; ++k) {
+                const float a0 = __shfl_sync(0xffffffffu, ml[k].x, h0), a1 = __shfl_sync(0xffffffffu, ml[k].x, h1);
+                const float b0 = __shfl_sync(0xffffffffu, ml[k].y, h0), b1 = __shfl_sync(0xffffffffu, ml[k].y, h1);
+                const bool on0 = a0 > -INFINITY, on1 = a1 > -INFINITY;       // what an absent set's O holds is anything
+                const float n0 = fmaxf(m0, a0), n1 = fmaxf(m1, a1);
+                const float c0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), c1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
+                const float d0 = on0 ? fast_exp2(a0 - n0) : 0.f, d1 = on1 ? fast_exp2(a1 - n1) : 0.f;
+                const float* v0 = reinterpret_cast<const float*>(ring + kOffSums + (k * kMaxGroup + h0) * kSumRow) + g;
+                const float* v1 = v0 + kSumRow / 4;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    o[i][0] = o[i][0] * c0 + (on0 ? v0[16 * i] * d0 : 0.f);
+                    o[i][1] = o[i][1] * c1 + (on1 ? v1[16 * i] * d1 : 0.f);
+                    o[i][2] = o[i][2] * c0 + (on0 ? v0[16 * i + 8] * d0 : 0.f);
+                    o[i][3] = o[i][3] * c1 + (on1 ? v1[16 * i + 8] * d1 : 0.f);
+                }
+                l0 = l0 * c0 + b0 * d0;
+                l1 = l1 * c1 + b1 * d1;
+                m0 = n0;
+                m1 = n1;
             }
-            l0 = l0 * c0 + set.ml0.y * d0;
-            l1 = l1 * c1 + set.ml1.y * d1;
-            m0 = n0;
-            m1 = n1;
-        };
-#pragma unroll
-        for (int s = 0; s < kSets; ++s) add(sets[s]);
-        for (int s = kSets; s < p.prefix.plan.slots; s += kSets) {
-#pragma unroll
-            for (int k = 0; k < kSets; ++k) load_set(u, s + k, sets[k]);
-#pragma unroll
-            for (int k = 0; k < kSets; ++k) add(sets[k]);
+            __syncwarp();
+            if (s + kSets >= p.prefix.plan.slots) break;
+            copy_sets(u, s + kSets);
         }
 
         // ---- output: (dimension, head) fragments turned into rows of two dimensions per lane
@@ -332,11 +342,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_short_kernel(const __gr
                     }
                 }
             }
-        }
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-            qb[ks][0] = qn[ks][0];
-            qb[ks][1] = qn[ks][1];
         }
     }
     // a warp that gave up: the tiles in flight land before the block exits
