@@ -16,7 +16,8 @@
 
 using namespace lzk;
 
-constexpr int kShortUnitsPerSm = 3;       // units per SM from which short own caches behind a prefix get a warp each
+// Units per SM from which own caches of n tokens behind a prefix get a warp each (measured pairs: decode_short.cu).
+constexpr int short_units_per_sm(int n) { return n <= 128 ? 3 : 4; }
 constexpr int kHostChunks = 3;            // unit ranges the host-buffer entry point pipelines copies over
 
 struct lazyev {
@@ -359,7 +360,7 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     // clusters when that is faster, so that more SMs share its units.
     const int np = (n + kPageTokens - 1) / kPageTokens;
     // Short own caches behind a prefix: one launch with a warp per unit, where there are enough units for it.
-    const bool brief = h->shared && n <= kShortTokens && h->units >= kShortUnitsPerSm * h->num_sms && h->force_splits == 0 &&
+    const bool brief = h->shared && n <= kShortTokens && h->units >= short_units_per_sm(n) * h->num_sms && h->force_splits == 0 &&
                        h->force_stages == 0 && h->force_groups == 0;
     auto cached = h->plan_cache.find(np);
     const bool planned = cached != h->plan_cache.end() && cached->second.forced_splits == h->force_splits &&

@@ -2,14 +2,21 @@
 //
 // Same mathematics as decode.cu (Appendix A, Eq. (attn), over the prefix's tokens and the own ones; pbar and Eq. (1) for the own
 // ones), for units of at most 384 own tokens -- sequences that have just begun to answer.  Such a unit is a chain of short
-// dependent steps: a block of nine warps on it spends its time in barriers and merges (4900 clocks for 64 tokens, of which 1400
-// would stream them).  Here every warp walks units of its own: it fetches its tiles of 16 tokens (4 KiB of K, 4 KiB of V) itself
+// dependent steps: a block of nine warps on it spends its time in barriers and merges (896 units take 33 us whether they hold
+// 1 token or 64).  Here every warp walks units of its own: it fetches its tiles of 16 tokens (4 KiB of K, 4 KiB of V) itself
 // through a ring, keeps all heads' O^T in registers, adds the prefix's partial sums to it in the same layout, and
-// meets no other warp between the start and the end of the launch.  Eight units per SM are in flight.
+// meets no other warp between the start and the end of the launch.  Eight units per SM are in flight.  Queries and partial
+// sums come through shared memory as whole rows: 165 registers; read in fragment layout from global memory 231.
 //
-// Bound by HBM for many units (512 bytes a token); for few by the latency of one unit.  Measured on B200, with a prefix of 64 tokens
-// (both launches): 4096 units of 256 tokens 108 us against 126 us with a block per unit, 1792 of 64 tokens 29 against 50;
-// 3584 units of 512 tokens 174 against 172, 256 units of 256 tokens 31 against 23: hence the limits on tokens and units.
+// Bound by HBM for many units (512 bytes a token); for few by the latency of one unit.  Measured on B200, both launches behind a
+// prefix of 64 tokens, a warp per unit / a block per unit, us:
+//   own tokens            64            256           384           512
+//    448 units       20.8 / 24.9   30.9 / 28.9   37.1 / 33.0
+//    608 units       22.7 / 28.9   31.1 / 33.9   39.4 / 41.4
+//   3584 units                     95.0 / 112    132 / 142     173 / 172
+//   4096 units       45.4 / 90.5   107 / 126     147 / 158
+// With 320 units the two are level at 64 tokens (20.4 / 20.8) and the block is ahead at 128 (22.9 / 20.8).
+// Hence: at most 384 tokens, three units per SM up to 128 tokens and four beyond.
 #include "internal.h"
 
 namespace lzk {
