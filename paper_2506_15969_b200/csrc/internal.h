@@ -12,7 +12,6 @@ struct PrefixPlan {
     int share, group;                   // sequences per prefix sequence, query heads per KV head
     int tile_seqs, tiles, pairs;        // sequences per row tile, row tiles per prefix unit, items (pairs of tiles) per unit
     int key_tiles;                      // 128-key tiles of the prefix
-    int items;                          // prefix units * pairs
     int blocks;                         // the walk over (item, key tile) is cut into `blocks` contiguous parts:
     int per, extra;                     // the first `extra` of per + 1 steps, the others of per
     int slots;                          // most partial sums of a row

@@ -8,8 +8,11 @@
 // the probabilities it emits are those of the joint softmax.
 //
 // K / V of the prefix are read once per pair of row tiles, 512 bytes per token, where every sequence would read them by
-// itself; 512 flops a byte and 128 rows.  Up to about 300 query rows per prefix unit HBM bounds that, beyond it the
-// exponentials (16 a clock and SM).
+// itself.  Few rows: HBM, behind a part that does not grow with the prefix; many rows: the tensor core
+// (S, and P V twice) and the softmax between its products.  Measured on B200, this kernel under a profiler: 8 KV heads,
+// 65521 tokens, 64 rows, 269 MB read, 53.8 us, tensor pipe 47 % busy; 4 layers x 8 KV heads, 8192 tokens, 640 rows, 125 us,
+// tensor pipe 64 %, issue slots 43 %.  P as one bf16 term took the second case (whole call, then 187 us) to 174 us; it leaves P 8
+// mantissa bits where the framework's other attention kernels keep 16, and is not used.
 //
 // Structure: persistent blocks, one per SM.  A row tile is 128 accumulator rows = floor(128 / G) sequences x G heads, an
 // item is a prefix unit with two of its row tiles (or its single, or odd last one), and the walk over (item, key tile
@@ -554,7 +557,6 @@ PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int gr
     pl.key_tiles = (n + kTile - 1) / kTile;
     pl.rows = (long long)layers * batch * kv_heads * group;
     const long long items = (long long)layers * prefixes * kv_heads * pl.pairs, work = items * pl.key_tiles;
-    pl.items = (int)items;
     pl.blocks = work > 0x40000000 ? 0 : (int)(work < num_sms ? work : num_sms);
     if (pl.blocks == 0) return pl;
     pl.per = (int)(work / pl.blocks);
