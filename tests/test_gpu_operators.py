@@ -410,6 +410,10 @@ def check_attend(own, q, kp, vp, ko, vo):
     (30, 45, 1, 40, 8, 70, 383),        # several units per warp
     (30, 45, 1, 3, 1, 70, 384),
     (30, 45, 3, 9, 3, 70, 385),         # one token too long for it
+    (1, 56, 1, 32, 8, 64, 128),         # three units per SM: a warp each up to here,
+    (1, 56, 1, 32, 8, 64, 129),         # a block each from here
+    (1, 73, 1, 32, 8, 64, 129),         # just below and at four units per SM
+    (1, 74, 1, 32, 8, 64, 129),
 ])
 def test_attend_against_64_bits(L, B, P, Hq, Hkv, N, n):
     g = gen(N * 7 + n)
