@@ -278,10 +278,14 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         // same every time, issues.  The tensor core queues few instructions and a ready barrier costs 150 clocks to look at, so
         // with one issuer it idled a third of the time between two streams' turns; two issuers left to themselves
         // let the streams fall into step (both in the softmax, then both at the tensor core).  So each does its waiting
-        // beforehand and they hand the tensor core to each other turn by turn, which keeps the streams half a step apart.
+        // beforehand and they hand the tensor core to each other turn by turn, which keeps the streams half a step apart.  The turns
+        // go on from piece to piece: stream 0 takes a piece's first turn behind the last one of the piece before, whoever had
+        // that.  So neither warp is ever more than one turn ahead, and no barrier sees the same warp arrive twice in a phase -- the
+        // barriers have no time limit, and what ends every wait on them is that both warps walk all their turns.
         const int s = warp - kIssuer;
         uint32_t p_uses = 0, uses = 0, q_uses = 0;  // products issued; uses of the K / V ring and of the Q slots by earlier pieces
         bool ok = true;                             // a warp that gave up goes through the same turns without issuing
+        bool behind = false;                        // the piece before ended with the other stream's turn (stream 0 looks)
         auto wait_on = [&](uint64_t* bar, uint32_t parity) {
             if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag, p.status, limit));
         };
@@ -345,7 +349,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 wait_on(&bars->full[vs], (vu / kRing) & 1u);
                 if (more) wait_on(&bars->full[ks], (ku / kRing) & 1u);
                 wait_on(&bars->p_full[s][0], p_uses & 1u);
-                if (turn > 0) named_barrier_sync(13 + s, 64);
+                if (turn > 0 || behind) named_barrier_sync(13 + s, 64);
                 tmem_fence_after_sync();
                 if (ok && elect_one()) issue_o(vs, 0, t == 0);
                 __syncwarp();
@@ -361,8 +365,9 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                         umma_commit(&bars->o_full[s]);
                 }
                 __syncwarp();
-                if (turn + 1 < turns) asm volatile("bar.arrive %0, %1;" ::"r"(13 + (s ^ 1)), "r"(64) : "memory");
+                if (turn + 1 < turns || (s == 1 && x < end)) asm volatile("bar.arrive %0, %1;" ::"r"(13 + (s ^ 1)), "r"(64) : "memory");
             }
+            behind = (turns & 1) == 0;
             uses += 2 * nt;
         }
         // every MMA issued by this warp is complete before tensor memory goes back
