@@ -432,7 +432,10 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                 }
         };
         auto fold_set = [&](float2 ml, const float (&v)[4], float& m, float& l, float (&acc)[4]) {
-            if (ml.x == -INFINITY) return;          // no such set: what its O holds is anything
+            if (ml.x == -INFINITY) {                // no such set, and what its O holds is anything: l is zero -- or its logits
+                l += ml.y;                          // were all NaN, and so is l
+                return;
+            }
             const float n = fmaxf(m, ml.x), c = m == -INFINITY ? 0.f : fast_exp2(m - n), f = fast_exp2(ml.x - n);
             m = n;
             l = l * c + ml.y * f;
@@ -763,7 +766,7 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
 #pragma unroll
                         for (int k = 0; k < NW; ++k) {
                             const float mk = wml[k * 16 + h];
-                            lc += mk == -INFINITY ? 0.f : wml[k * 16 + 8 + h] * fast_exp2(mk - mc);
+                            lc += wml[k * 16 + 8 + h] * (mk == -INFINITY ? 0.f : fast_exp2(mk - mc));      // (NaN logits alone leave -inf and NaN)
                         }
                         xb->m[h] = mc;
                         xb->l[h] = lc;
@@ -790,12 +793,12 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                     for (int r = 0; r < S; ++r) M = fmaxf(M, ld_rank_f32(&xb->m[ctid], r, clustered));
                     for (int r = 0; r < S; ++r) {
                         const float mr = ld_rank_f32(&xb->m[ctid], r, clustered);
-                        L += mr == -INFINITY ? 0.f : ld_rank_f32(&xb->l[ctid], r, clustered) * exp2f(mr - M);
+                        L += ld_rank_f32(&xb->l[ctid], r, clustered) * (mr == -INFINITY ? 0.f : exp2f(mr - M));
                     }
                     lse_s[ctid] = M + log2f(L);
                     for (int r = 0; r < S; ++r) {
                         const float mr = ld_rank_f32(&xb->m[ctid], r, clustered);
-                        sc_s[r * kMaxGroup + ctid] = mr == -INFINITY ? 0.f : exp2f(mr - M) / L;
+                        sc_s[r * kMaxGroup + ctid] = (mr == -INFINITY ? 0.f : exp2f(mr - M)) / L;
                     }
                 }
                 named_barrier_sync(1, kConsumers);

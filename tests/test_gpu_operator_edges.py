@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2506_15969_b200 import binding
-from tests.test_gpu_operators import D, check_attend, engine, gen, prefixed, randn
+from tests.test_gpu_operators import D, assert_attend, attend_ref, check_attend, engine, gen, prefixed, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,58 @@ def test_many_short_pieces_repeat_exactly():
             own.attend(q, out)
         own.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("L,B,Hq,Hkv,N,n,splits", [
+    (1, 4, 8, 2, 40, 5, 1),                # a block per unit
+    (1, 4, 8, 2, 300, 0, 1),
+    (1, 4, 8, 2, 3000, 700, 1),
+    (1, 4, 8, 2, 3000, 700, 3),            # clusters
+    (1, 4, 8, 2, 300, 5, 2),               # a block of the cluster has no own token
+    (1, 4, 8, 2, 300, 0, 2),
+    (1, 40, 8, 2, 700, 20, 0),
+    (16, 40, 12, 2, 70, 65, 0),            # a warp per unit
+])
+@pytest.mark.parametrize("where", ["prefix", "piece", "second", "own"])
+def test_nan_logits_do_not_vanish(L, B, Hq, Hkv, N, n, splits, where):
+    """Keys of one KV head that give NaN logits: its heads' outputs and probabilities are NaN, whichever launch joins the parts
+    (a part without any finite logit is not an absent one), and the other heads' are as ever."""
+    if where == "own":
+        n = max(n, 16)
+    g = gen(N + n)
+    kp, ko = randn(g, L, 1, Hkv, N, D), randn(g, L, B, Hkv, n, D)
+    if where == "own":
+        ko[:, :, 0, :16] = float("nan")    # all of a warp's tokens
+    else:
+        first, last = {"prefix": (0, N), "piece": (0, 128), "second": (N // 256 * 128, N // 256 * 128 + 128)}[where]
+        kp[:, :, 0, first:last] = float("nan")
+    pre, own, kp, vp, ko, vo = prefixed(g, L, B, 1, Hq, Hkv, N, n, kp=kp, ko=ko)
+    if splits:
+        own.set_splits(splits)
+    q, out = randn(g, L, B, Hq, D), torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    own.attend(q, out)
+    own.synchronize()
+    G = Hq // Hkv
+    pbar = own.state_views()["pbar"].view(L, B, Hkv, -1)[..., :n]
+    assert bool(torch.isnan(out[:, :, :G]).all()) and bool(torch.isnan(pbar[:, :, 0]).all())
+    ref, size, ref_pbar = attend_ref(q, kp, vp, ko, vo)
+    assert_attend(out[:, :, G:], pbar[:, :, 1:], ref[:, :, G:], size[:, :, G:], ref_pbar[:, :, 1:])
+
+
+@pytest.mark.parametrize("splits,n", [(1, 40), (2, 40), (1, 600), (3, 600)])
+def test_nan_logits_do_not_vanish_without_a_prefix(splits, n):
+    g = gen(31)
+    L, B, Hq, Hkv = 1, 3, 8, 2
+    k, v = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    k[:, :, 0, 16:32] = float("nan")
+    e = engine(L, Hq, Hkv, B, n)
+    e.prefill(k, v)
+    e.set_splits(splits)
+    q, out = randn(g, L, B, Hq, D), torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    e.attend(q, out)
+    e.synchronize()
+    pbar = e.state_views()["pbar"].view(L, B, Hkv, -1)[..., :n]
+    assert bool(torch.isnan(out[:, :, :4]).all()) and bool(torch.isnan(pbar[:, :, 0]).all())
+    none = k[:, :1, :, :0]
+    ref, size, ref_pbar = attend_ref(q, none, none, k, v)
+    assert_attend(out[:, :, 4:], pbar[:, :, 1:], ref[:, :, 4:], size[:, :, 4:], ref_pbar[:, :, 1:])
