@@ -368,6 +368,7 @@ int lazyev_detach_prefix(lazyev_t* h);
  * It may be captured into a CUDA graph, like lazyev_norm_rope(), and replayed for other queries in the same buffer while the
  * cache and its prefix stay as they were at capture.  Calls on one handle share its scratch, state and prefix
  * workspace, replays of its graphs too: order them.
+ * out needs its elements' alignment only (at a multiple of 4 bytes many short sequences behind a prefix are faster).
  * Errors: EINVAL (null; q not 16-byte aligned while a prefix is attached), ESTATE (nothing cached), ECUDA.
  */
 int lazyev_attend(lazyev_t* h, const void* q, void* out);

@@ -359,9 +359,10 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     // the size with the least total.  A partly filled last round goes to a second launch with larger
     // clusters when that is faster, so that more SMs share its units.
     const int np = (n + kPageTokens - 1) / kPageTokens;
-    // Short own caches behind a prefix: one launch with a warp per unit, where there are enough units for it.
+    // Short own caches behind a prefix: one launch with a warp per unit, where there are enough units for it.  It stores two
+    // elements of `out` at a time, the block-per-unit kernel single ones: an `out` at an odd element goes there.
     const bool brief = h->shared && n <= kShortTokens && h->units >= short_units_per_sm(n) * h->num_sms && h->force_splits == 0 &&
-                       h->force_stages == 0 && h->force_groups == 0;
+                       h->force_stages == 0 && h->force_groups == 0 && ((uintptr_t)out & 3) == 0;
     auto cached = h->plan_cache.find(np);
     const bool planned = cached != h->plan_cache.end() && cached->second.forced_splits == h->force_splits &&
                          cached->second.forced_stages == h->force_stages && cached->second.forced_groups == h->force_groups;

@@ -113,3 +113,23 @@ def test_nan_logits_do_not_vanish_without_a_prefix(splits, n):
     none = k[:, :1, :, :0]
     ref, size, ref_pbar = attend_ref(q, none, none, k, v)
     assert_attend(out[:, :, 4:], pbar[:, :, 1:], ref[:, :, 4:], size[:, :, 4:], ref_pbar[:, :, 1:])
+
+
+@pytest.mark.parametrize("L,B,n,splits", [(16, 40, 65, 0), (1, 5, 65, 1), (1, 5, 700, 3)])      # enough units for a warp each; blocks; clusters
+def test_out_at_any_element(L, B, n, splits):
+    """`out` needs no alignment beyond its elements': the launch that stores pairs is not taken for an odd one."""
+    g = gen(50 + n)
+    Hq, Hkv, N = 12, 2, 70
+    pre, own, *kv = prefixed(g, L, B, 1, Hq, Hkv, N, n)
+    own.set_splits(splits)
+    q, kn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D)
+    for at in (0, 1, 2, 3, 8):
+        buf = torch.full((q.numel() + 16,), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = buf[at:at + q.numel()].view(q.shape)
+        own.attend(q, out)
+        own.synchronize()
+        assert_attend(out, own.state_views()["pbar"][:, :n], *attend_ref(q, *kv))
+        assert bool((buf[:at] == 7).all()) and bool((buf[at + q.numel():] == 7).all())
+    own.decode_step(q, kn, kn, torch.empty(q.numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view(q.shape))
+    own.synchronize()
+    assert own.info().n == n + 1
