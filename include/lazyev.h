@@ -13,6 +13,8 @@
  *   - "device pointer" arguments are contiguous arrays in the memory of the GPU
  *     that was current at lazyev_bind(); activations are bfloat16 (raw 16-bit
  *     patterns), head_dim = 128 elements per row.
+ *     Keys and values (k, v, k_new, v_new) are 16-byte aligned, queries 4-byte (16-byte where a call says so),
+ *     outputs as their elements: EINVAL otherwise.
  *   - The caller owns all device memory and the CUDA stream.  The library
  *     allocates no device memory at all; it owns only the host-side handle and a
  *     few internal CUDA streams and events (a low-priority stream for the second
@@ -368,8 +370,8 @@ int lazyev_detach_prefix(lazyev_t* h);
  * It may be captured into a CUDA graph, like lazyev_norm_rope(), and replayed for other queries in the same buffer while the
  * cache and its prefix stay as they were at capture.  Calls on one handle share its scratch, state and prefix
  * workspace, replays of its graphs too: order them.
- * out needs its elements' alignment only (at a multiple of 4 bytes many short sequences behind a prefix are faster).
- * Errors: EINVAL (null; q not 16-byte aligned while a prefix is attached), ESTATE (nothing cached), ECUDA.
+ * (At a multiple of 4 bytes of out many short sequences behind a prefix are faster.)
+ * Errors: EINVAL (null; misaligned, q not 16-byte aligned while a prefix is attached), ESTATE (nothing cached), ECUDA.
  */
 int lazyev_attend(lazyev_t* h, const void* q, void* out);
 

@@ -351,6 +351,9 @@ cudaError_t run_prefix(lazyev_t* h, const void* q) {
 // problems -- inside the decode launch.
 int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPipe* pipe, const NewToken* tok = nullptr,
                bool track = true) {
+    // (the kernels load pairs of elements of q, or tiles of it over a prefix, and store single elements of out)
+    if (h->shared && ((uintptr_t)q & 15)) return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned while a prefix is attached");
+    if (((uintptr_t)q & 3) || ((uintptr_t)out & 1)) return fail(h, LAZYEV_EINVAL, "q must be 4-byte aligned, out 2-byte aligned");
     cudaError_t e = cudaSuccess;
     DecodeConfig c{h->units, h->group, h->pages_per_unit, h->capacity, track ? h->alpha : INFINITY, h->force_splits, h->force_stages, h->force_groups,
                    h->wait_limit_ns, h->stop_after_pages, h->shared != nullptr};
@@ -443,7 +446,6 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     const bool fuse_append = tok && h->fuse_append && !brief && shape.tail_units == 0 && main_units <= clusters;
     PrefixView prefix = {};
     if (h->shared) {
-        if ((uintptr_t)q & 15) return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned while a prefix is attached");
         prefix.plan = h->prefix_plan;
         prefix.o = h->prefix_o;
         prefix.ml = h->prefix_ml;
@@ -570,6 +572,7 @@ int finish_step(lazyev_t* h) {
 int run_step(lazyev_t* h, const void* q, const void* k_new, const void* v_new, void* out, const HostPipe* pipe = nullptr) {
     int rc = check_step(h);
     if (rc != LAZYEV_OK) return rc;
+    if (((uintptr_t)k_new | (uintptr_t)v_new) & 15) return fail(h, LAZYEV_EINVAL, "k_new and v_new must be 16-byte aligned");
     const NewToken tok{k_new, v_new, h->pos_base + h->prefill + h->t};
     rc = run_decode(h, q, out, h->n + 1, h->t + 1, pipe, &tok);
     return rc != LAZYEV_OK ? rc : finish_step(h);
@@ -850,6 +853,7 @@ int lazyev_prefill(lazyev_t* h, const void* k, const void* v, int n_tokens) {
     if (h->prefilled) return fail(h, LAZYEV_ESTATE, "prefill called twice");
     if (!k || !v || n_tokens <= 0) return fail(h, LAZYEV_EINVAL, "null pointer or non-positive token count");
     if (n_tokens > h->max_prefill) return fail(h, LAZYEV_ECAPACITY, "prompt of %d tokens exceeds max_prefill = %d", n_tokens, h->max_prefill);
+    if (((uintptr_t)k | (uintptr_t)v) & 15) return fail(h, LAZYEV_EINVAL, "k and v must be 16-byte aligned");
     cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, INT_MIN, h->pos_base, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "prefill kernel launch");
     h->launches += 1;
@@ -894,6 +898,8 @@ int lazyev_prefill_observed(lazyev_t* h, const void* q, const void* k, const voi
     if (n_tokens > h->max_prefill) return fail(h, LAZYEV_ECAPACITY, "prompt of %d tokens exceeds max_prefill = %d", n_tokens, h->max_prefill);
     if (h->prompt_mode == LAZYEV_PROMPT_TILED && (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15))
         return fail(h, LAZYEV_EINVAL, "q, k, v and out must be 16-byte aligned");
+    if ((((uintptr_t)k | (uintptr_t)v) & 15) || ((uintptr_t)q & 3) || ((uintptr_t)out & 1))
+        return fail(h, LAZYEV_EINVAL, "k and v must be 16-byte aligned, q 4-byte and out 2-byte aligned");
     // rows are loaded with TS = their own time j - (P - 1) <= 0 and MRI = 0
     cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, 1 - n_tokens, 0, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "prefill kernel launch");
@@ -1190,6 +1196,7 @@ int lazyev_decode_step_rows(lazyev_t* h, const lazyev_rows_t* q, const lazyev_ro
     int rc = check_device(h, "decode_step_rows");
     if (rc != LAZYEV_OK) return rc;
     if (!out) return fail(h, LAZYEV_EINVAL, "null pointer");
+    if ((uintptr_t)out & 1) return fail(h, LAZYEV_EINVAL, "out must be 2-byte aligned");
     RowsArgs a = rows_args(h, 1, positions, h->pos_base + h->prefill + h->t);
     if ((rc = rows_view(h, "q", q, h->q_heads, 1, false, &a.q)) != LAZYEV_OK) return rc;
     if ((rc = rows_view(h, "k", k, h->kv_heads, 1, false, &a.k)) != LAZYEV_OK) return rc;

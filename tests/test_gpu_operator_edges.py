@@ -133,3 +133,39 @@ def test_out_at_any_element(L, B, n, splits):
     own.decode_step(q, kn, kn, torch.empty(q.numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view(q.shape))
     own.synchronize()
     assert own.info().n == n + 1
+
+
+def test_misaligned_rows_are_refused():
+    """What the kernels load as pairs or 16-byte chunks is refused at an odd element, before anything is queued."""
+    g = gen(56)
+    L, B, Hq, Hkv, n = 1, 2, 8, 2, 6
+    odd = lambda x: torch.cat((x.flatten()[:1], x.flatten()))[1:].view(x.shape)      # noqa: E731
+    k, q, kn = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D)
+    out = torch.empty_like(q)
+    rows_q, rows_out = randn(g, n, L, B, Hq, D), torch.empty(n, L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    e = engine(L, Hq, Hkv, B, n)
+
+    def refused(f, *args):
+        with pytest.raises(binding.LazyEvError) as err:
+            f(*args)
+        assert err.value.code == binding.EINVAL and "aligned" in str(err.value)
+
+    launches = e.info().launches
+    refused(e.prefill, odd(k), k)
+    refused(e.prefill, k, odd(k))
+    for mode in (binding.PROMPT_REPLAY, binding.PROMPT_TILED):
+        e.set_prompt_mode(mode)
+        refused(e.prefill_observed, rows_q, odd(k), k, rows_out)
+        refused(e.prefill_observed, odd(rows_q), k, k, rows_out)
+    assert e.info().launches == launches and e.info().n == 0
+    e.prefill(k, k)
+    launches = e.info().launches
+    refused(e.attend, odd(q), out)
+    refused(e.decode_step, odd(q), kn, kn, out)
+    refused(e.decode_step, q, odd(kn), kn, out)
+    refused(e.decode_step, q, kn, odd(kn), out)
+    lib = binding.lib()
+    assert lib.lazyev_attend(e._h, q.data_ptr(), out.data_ptr() + 1) == binding.EINVAL
+    assert e.info().launches == launches and e.info().n == n and e.info().t == 0
+    e.decode_step(q, kn, kn, odd(out))
+    e.synchronize()
