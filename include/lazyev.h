@@ -360,7 +360,8 @@ int lazyev_decode_step_rows(lazyev_t* h, const lazyev_rows_t* q, const lazyev_ro
 int lazyev_query_prefix_workspace(const lazyev_t* h, const lazyev_t* prefix, size_t* bytes);
 int lazyev_attach_prefix(lazyev_t* h, lazyev_t* prefix, void* workspace);
 /* Ends the sharing (0 when there was none): this handle's attention covers its own tokens only from here on, and work
- * queued on the prefix's stream later waits for what is queued here.  Errors: ECUDA. */
+ * queued on the prefix's stream later waits for what is queued here.  Own tokens keep their positions and the next ones follow
+ * them; a handle that holds none starts at position 0 again.  Errors: ECUDA. */
 int lazyev_detach_prefix(lazyev_t* h);
 
 /*

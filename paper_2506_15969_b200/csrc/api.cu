@@ -1246,6 +1246,7 @@ int detach(lazyev_t* h) {
     if (dev >= 0 && dev != h->device) cudaSetDevice(dev);
     prefix->users -= 1;
     h->shared = nullptr;
+    if (!h->prefilled) h->pos_base = 0;    // no token has a position after the prefix's: an empty handle again
     h->plan_cache.clear();                 // launch shapes differ with and without a prefix
     if (e != cudaSuccess) return cuda_fail(h, e, "detach_prefix");
     return LAZYEV_OK;

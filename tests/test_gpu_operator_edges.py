@@ -1,6 +1,7 @@
 """Row and prefix calls where they can go wrong between their parts: time-outs in blocks with many short pieces of work, values
 that must not vanish between two launches, memory on another stream than its own, calls that are refused.  Tolerances are those of
 test_gpu_operators.py."""
+import numpy as np
 import pytest
 import torch
 
@@ -169,3 +170,39 @@ def test_misaligned_rows_are_refused():
     assert e.info().launches == launches and e.info().n == n and e.info().t == 0
     e.decode_step(q, kn, kn, odd(out))
     e.synchronize()
+
+
+def test_positions_after_a_detach_with_no_own_token():
+    """A handle that let its prefix go before it held a token is an empty handle: prompts start at position 0 again, in every form."""
+    g = gen(32)
+    L, B, Hq, Hkv, N, n = 1, 2, 8, 2, 90, 20
+    k, v = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    q, kn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D)
+    out = torch.empty_like(q)
+    whole = engine(L, Hq, Hkv, B, n)
+    whole.prefill(k, v)
+    whole.decode_step(q, kn, kn, out)
+    snap = whole.dump_state(kv=True)
+    for load in ("prefill", "observed", "append", "state"):
+        pre, own = engine(L, Hq, Hkv, 1, N), engine(L, Hq, Hkv, B, n)
+        pre.append(*(randn(g, L, 1, N, Hkv, D) for _ in range(2)))
+        own.attach_prefix(pre)
+        assert own.info().next_position == N
+        own.detach_prefix()
+        assert own.info().next_position == 0
+        if load == "prefill":
+            own.prefill(k, v)
+        elif load == "observed":
+            own.prefill_observed(randn(g, n, L, B, Hq, D), k, v, torch.empty(n, L, B, Hq, D, dtype=torch.bfloat16, device="cuda"))
+        elif load == "append":
+            own.append(k.transpose(2, 3), v.transpose(2, 3))
+        else:
+            own.load_state(snap, n)
+        if load != "state":
+            own.decode_step(q, kn, kn, out)
+        assert np.array_equal(own.dump_state()["pos"], np.tile(np.arange(n + 1), (L * B * Hkv, 1))), load
+        assert own.info().next_position == n + 1
+    # with own tokens the positions stay
+    pre, own, *_ = prefixed(g, L, B, 1, Hq, Hkv, N, 5)
+    own.detach_prefix()
+    assert own.info().next_position == N + 5
