@@ -324,8 +324,8 @@ class Engine:
         """lazyev_attach_prefix; the workspace is allocated here and the prefix kept alive while it is attached."""
         n = C.c_size_t()
         self._check(lib().lazyev_query_prefix_workspace(self._h, prefix._h, C.byref(n)))
-        workspace = self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device)
-        workspace.record_stream(self.stream)
+        with self._torch.cuda.stream(self.stream):      # (a block of the current stream's may still be written there)
+            workspace = self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device)
         self._check(lib().lazyev_attach_prefix(self._h, prefix._h, workspace.data_ptr()))
         self._prefix = prefix, workspace
 

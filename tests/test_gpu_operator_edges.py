@@ -1,6 +1,8 @@
 """Row and prefix calls where they can go wrong between their parts: time-outs in blocks with many short pieces of work, values
 that must not vanish between two launches, memory on another stream than its own, calls that are refused.  Tolerances are those of
 test_gpu_operators.py."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -206,3 +208,31 @@ def test_positions_after_a_detach_with_no_own_token():
     pre, own, *_ = prefixed(g, L, B, 1, Hq, Hkv, N, 5)
     own.detach_prefix()
     assert own.info().next_position == N + 5
+
+
+def test_the_workspace_belongs_to_the_engines_stream():
+    """Work that is still queued on the current stream may write a block that was just freed there; the prefix's workspace, used on the
+    engine's stream, must not be that block."""
+    g = gen(33)
+    L, B, Hq, Hkv, N, n = 1, 8, 32, 8, 3000, 10
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        pre, own, *kv = prefixed(g, L, B, 1, Hq, Hkv, N, n)
+    q, out = randn(g, L, B, Hq, D), torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    size = C.c_size_t()
+    assert binding.lib().lazyev_query_prefix_workspace(own._h, pre._h, C.byref(size)) == binding.OK
+    own.detach_prefix()
+    torch.cuda.synchronize()
+    xs = [torch.zeros(size.value // 4, dtype=torch.float32, device="cuda").fill_(1.0) for _ in range(12)]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    for x in xs:
+        x.fill_(3.0)                       # partial sums that look present
+    keep = xs[1::2]                        # (the free blocks between them are of just that size)
+    del x, xs
+    own.attach_prefix(pre)
+    torch.cuda.synchronize()
+    own.attend(q, out)
+    own.synchronize()
+    assert_attend(out, own.state_views()["pbar"][:, :n], *attend_ref(q, *kv))
+    del keep
