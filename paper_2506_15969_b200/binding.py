@@ -172,10 +172,13 @@ class Engine:
         self._types = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
         with torch.cuda.device(self.device):
             self._index = torch.device("cuda", torch.cuda.current_device())
-            self.kv_pool = torch.empty(kv.value, dtype=torch.uint8, device=self.device)
-            self.state = torch.empty(st.value, dtype=torch.uint8, device=self.device)
-            self.scratch = torch.empty(sc.value, dtype=torch.uint8, device=self.device)
             self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+            # The memory is the stream's: nothing queued elsewhere still writes it, and nothing elsewhere gets it before what is
+            # queued here is done.
+            with torch.cuda.stream(self.stream):
+                self.kv_pool = torch.empty(kv.value, dtype=torch.uint8, device=self.device)
+                self.state = torch.empty(st.value, dtype=torch.uint8, device=self.device)
+                self.scratch = torch.empty(sc.value, dtype=torch.uint8, device=self.device)
             self._check(lib().lazyev_bind(self._h, self.kv_pool.data_ptr(), self.state.data_ptr(),
                                           self.scratch.data_ptr(), self.stream.cuda_stream))
 

@@ -236,3 +236,39 @@ def test_the_workspace_belongs_to_the_engines_stream():
     own.synchronize()
     assert_attend(out, own.state_views()["pbar"][:, :n], *attend_ref(q, *kv))
     del keep
+
+
+def test_the_engines_memory_belongs_to_its_stream():
+    """Nothing queued on the current stream may still write the pool of an engine that was just made for another stream, and nothing
+    there may get the pool of one that was just closed while that stream still reads it."""
+    g = gen(34)
+    L, B, Hq, Hkv, n = 1, 4, 8, 2, 4000
+    k, v, q = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D), randn(g, L, B, Hq, D)
+    out = torch.empty_like(q)
+    none = k[:, :1, :, :0]
+    want = attend_ref(q, none, none, k, v)
+    s = torch.cuda.Stream()
+    size = engine(L, Hq, Hkv, B, n, stream=s).kv_pool.numel()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    x = torch.empty(size, dtype=torch.uint8, device="cuda").fill_(0)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    x.fill_(64)
+    del x
+    e = engine(L, Hq, Hkv, B, n, stream=s)
+    e.prefill(k, v)
+    torch.cuda.synchronize()
+    e.attend(q, out)
+    e.synchronize()
+    assert_attend(out, e.state_views()["pbar"][:, :n], *want)
+    out.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    e.attend(q, out)
+    del e
+    y = torch.full((size,), 64, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert bool(((out.double() - want[0]).abs() <= 2.0 ** -8 * want[0].abs() + 2.0 ** -13 * want[1]).all())
+    del y
