@@ -589,6 +589,42 @@ int check_device(lazyev_t* h, const char* call) {
     return LAZYEV_OK;
 }
 
+// Do two different rows of an output view share elements?  Rows overlap when their distance, a sum of (difference of indices) x
+// stride over the dimensions, is below a row's length.  Dimensions come by falling stride, and of each only the differences
+// are looked at that the later ones can still bring near zero: one, in a view whose dimensions nest.
+bool rows_meet(const long long* stride, const long long* extent, int dims, long long at, bool apart) {
+    if (dims == 0) return apart && at < kHeadDim && at > -kHeadDim;
+    long long reach = kHeadDim - 1;
+    for (int i = 1; i < dims; ++i) reach += (extent[i] - 1) * stride[i];
+    // d with |at + d * stride| <= reach
+    if (stride[0] == 0) return true;
+    long long first = (-reach - at) / stride[0] - 1, last = (reach - at) / stride[0] + 1;
+    if (first < 1 - extent[0]) first = 1 - extent[0];
+    if (last > extent[0] - 1) last = extent[0] - 1;
+    for (long long d = first; d <= last; ++d) {
+        const long long to = at + d * stride[0];
+        if (to <= reach && to >= -reach && rows_meet(stride + 1, extent + 1, dims - 1, to, apart || d != 0)) return true;
+    }
+    return false;
+}
+
+bool output_overlaps(const long long* stride, const int* extent) {
+    long long by[4], n[4];
+    int dims = 0;
+    for (int i = 0; i < 4; ++i) {
+        if (extent[i] <= 1) continue;
+        const long long s = stride[i] < 0 ? -stride[i] : stride[i];     // (differences have both signs)
+        int at = dims++;
+        for (; at > 0 && by[at - 1] < s; --at) {
+            by[at] = by[at - 1];
+            n[at] = n[at - 1];
+        }
+        by[at] = s;
+        n[at] = extent[i];
+    }
+    return dims > 0 && rows_meet(by, n, dims, 0, false);
+}
+
 // The kernels' view of a caller's rows, or EINVAL.
 int rows_view(lazyev_t* h, const char* name, const lazyev_rows_t* r, int heads, int n_tokens, bool output, RowView* out) {
     if (!r || !r->data) return fail(h, LAZYEV_EINVAL, "%s: null pointer", name);
@@ -602,9 +638,8 @@ int rows_view(lazyev_t* h, const char* name, const lazyev_rows_t* r, int heads, 
     for (int i = 0; i < 4; ++i) {
         stride[i] = extent[i] > 1 ? given[i] : 0;
         if (stride[i] % elems != 0) return fail(h, LAZYEV_EINVAL, "%s: strides must be multiples of 16 bytes", name);
-        if (output && extent[i] > 1 && stride[i] < kHeadDim && stride[i] > -kHeadDim)
-            return fail(h, LAZYEV_EINVAL, "%s: output rows overlap", name);
     }
+    if (output && output_overlaps(stride, extent)) return fail(h, LAZYEV_EINVAL, "%s: output rows overlap", name);
     *out = RowView{r->data, stride[0], stride[1], stride[2], stride[3], r->dtype};
     return LAZYEV_OK;
 }

@@ -272,3 +272,31 @@ def test_the_engines_memory_belongs_to_its_stream():
     torch.cuda.synchronize()
     assert bool(((out.double() - want[0]).abs() <= 2.0 ** -8 * want[0].abs() + 2.0 ** -13 * want[1]).all())
     del y
+
+
+def test_outputs_whose_dimensions_collide_are_refused():
+    g = gen(35)
+    e = engine(1, 8, 2, 2, 10)
+    lib = binding.lib()
+    x = randn(g, 1, 2, 4, 8, D)
+    pool = torch.empty(1 << 16, dtype=torch.bfloat16, device="cuda")
+
+    def call(batch, token, head, first=0):
+        v = binding._ROWS.pack(x.data_ptr(), binding.BF16, *x.stride()[:4])
+        o = binding._ROWS.pack(pool.data_ptr() + 2 * first, binding.BF16, 0, batch, token, head)
+        a, b = C.create_string_buffer(v), C.create_string_buffer(o)
+        return lib.lazyev_norm_rope(e._h, C.addressof(a), None, 4, None, 0, C.addressof(b), None)
+
+    # (2 sequences, 4 tokens, 8 heads)
+    for batch, token, head in ((4096, 128, 128), (4096, 1024, 1024), (128, 256, 256), (1024, 1024, 128), (3968, 1024, 128), (512, 1024, 128),
+                               (1024, -1024, 128), (640, 128, 512), (4096, 1016, 128),
+                               (4096, 1032, 128)):       # (the last token ends at 4120)
+        assert call(batch, token, head, 8192) == binding.EINVAL, (batch, token, head)
+        assert "overlap" in lib.lazyev_last_error(e._h).decode()
+    for batch, token, head in ((4096, 1024, 128), (128, 2048, 256), (512, 128, 1024), (4128, 1032, 128), (-4096, -1024, 128), (128, 8192, 384),
+                               (1152, 256, 2304), (128, 768, 3200)):
+        pool.zero_()
+        assert call(batch, token, head, 32768) == binding.OK, (batch, token, head)
+        e.synchronize()
+        assert torch.equal(pool.as_strided(x.shape[1:], (batch, token, head, 1), 32768) if min(batch, token, head) > 0 else
+                           pool.as_strided(x.shape[1:], (-batch, -token, head, 1), 32768 + batch + 3 * token).flip(0).flip(1), x[0])
