@@ -231,6 +231,7 @@ class Engine:
 
     def reset(self) -> None:
         self._check(lib().lazyev_reset(self._h))
+        self._prefix = None                      # (detached, as by detach_prefix)
 
     def set_prompt_mode(self, mode: int) -> None:
         self._check(lib().lazyev_set_prompt_mode(self._h, mode))
@@ -334,6 +335,8 @@ class Engine:
 
     def detach_prefix(self) -> None:
         self._check(lib().lazyev_detach_prefix(self._h))
+        # (what is queued still reads both; their streams get the memory back behind it)
+        self._prefix = None
 
     def attend(self, q, out) -> None:
         """lazyev_attend: q, out as for decode_step."""

@@ -2,6 +2,8 @@
 that must not vanish between two launches, memory on another stream than its own, calls that are refused.  Tolerances are those of
 test_gpu_operators.py."""
 import ctypes as C
+import gc
+import weakref
 
 import numpy as np
 import pytest
@@ -300,3 +302,32 @@ def test_outputs_whose_dimensions_collide_are_refused():
         e.synchronize()
         assert torch.equal(pool.as_strided(x.shape[1:], (batch, token, head, 1), 32768) if min(batch, token, head) > 0 else
                            pool.as_strided(x.shape[1:], (-batch, -token, head, 1), 32768 + batch + 3 * token).flip(0).flip(1), x[0])
+
+
+@pytest.mark.parametrize("how", ["detach_prefix", "reset"])
+def test_a_prefix_let_go_is_not_kept(how):
+    g = gen(36)
+    L, B, Hq, Hkv, N, n = 1, 8, 8, 2, 2000, 10
+    kp, vp = randn(g, L, 1, Hkv, N, D), randn(g, L, 1, Hkv, N, D)
+    k, v, q = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D), randn(g, L, B, Hq, D)
+    out = torch.empty_like(q)
+    s0, s1 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    pre, own = engine(L, Hq, Hkv, 1, N, stream=s0), engine(L, Hq, Hkv, B, n, stream=s1)
+    pre.prefill(kp, vp)
+    own.attach_prefix(pre)
+    own.prefill(k, v)
+    size, there = pre.kv_pool.numel(), weakref.ref(pre)
+    with torch.cuda.stream(s1):
+        torch.cuda._sleep(200_000_000)
+    own.attend(q, out)
+    getattr(own, how)()
+    del pre
+    gc.collect()
+    assert there() is None
+    with torch.cuda.stream(s0):            # its memory comes back behind what still reads it
+        y = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    ref, bound, _ = attend_ref(q, kp, vp, k, v)
+    assert bool(((out.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -13 * bound).all())
+    del y
