@@ -300,7 +300,7 @@ typedef struct lazyev_rows {
 int lazyev_set_rope(lazyev_t* h, const double* inv_freq, int pairs, int interleaved, float amplitude);
 
 /*
- * RMS norm of every query and key head before the rotation: y = x * rsqrt(mean(x^2) + eps) * w.  q_weight, k_weight:
+ * RMS norm of every query and key head before the rotation: y = x * rsqrt(mean(x^2) + eps) * w, for finite rows of any size.  q_weight, k_weight:
  * device pointers, float32 [layers][128], 16-byte aligned, read by every later call of this section (they stay the
  * caller's and must stay valid); NULL for either: that side is not normalised.  Errors: EINVAL (misaligned, eps not
  * positive and finite while a weight is given).

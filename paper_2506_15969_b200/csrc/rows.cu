@@ -19,8 +19,11 @@
 // and the arithmetic runs two elements per instruction.
 //
 // Measured on B200 (copy bandwidth 6.54 TB/s): 32768 tokens of 40 + 8 bf16 heads 128 us, 6.3 TB/s; 131072 tokens of 8 key and
-// 8 value heads into pages 179 us, 6.1 TB/s; one token 3.6 us.
+// 8 value heads into pages 183 us, 5.9 TB/s; one token 3.6 us.  Looking for rows whose squares overflow is 2 us of the 183 (a
+// vote per stage; a vote per row 3).
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "internal.h"
 #include "tensor.cuh"
@@ -149,6 +152,16 @@ struct RowRing {
     }
 };
 
+// Over the 16 lanes of a row.
+__device__ __forceinline__ float sum_of_squares(const uint64_t (&va)[2], const uint64_t (&vb)[2]) {
+    float s0, s1;
+    unpack2(add2(fma2(va[0], va[0], mul2(va[1], va[1])), fma2(vb[0], vb[0], mul2(vb[1], vb[1]))), s0, s1);
+    float ss = s0 + s1;
+#pragma unroll
+    for (int s = 1; s < 16; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
+    return ss;
+}
+
 // Queries or keys.  `refill` fetches the stage that follows those in flight.
 template <int kIn, int kOut, bool kInterleaved, bool kPaged, class Refill>
 __device__ __forceinline__ void turn_rows(const RowsArgs& a, const WarpRows& r, bool norm, bool turns, const Factors& f, RowRing<kIn>& ring,
@@ -157,65 +170,84 @@ __device__ __forceinline__ void turn_rows(const RowsArgs& a, const WarpRows& r, 
     const int half = (threadIdx.x >> 4) & 1;
     uint8_t* dst = kPaged ? nullptr : r.dst + half * r.dst_step;
     const float mean = 1.f / kHeadDim;
+    // Row k of this half-warp's in the stage; its sum of squares.  kLarge: squares of elements from 1.6e18 on do not fit fp32, but
+    // those of a row times 2^-70 do, and its norm is 2^-70 of the row's.
+    auto turn_row = [&](int k, int left, uint8_t* to, auto large) {
+        constexpr bool kLarge = decltype(large)::value;
+        Quad<kIn> qa, qb;
+        qa.load(ring.get + 2 * k * kRowIn + r.src_a);
+        qb.load(ring.get + 2 * k * kRowIn + r.src_b);
+        const int32_t pp = kPaged ? __shfl_sync(0xffffffffu, r.page, r.heads - left + 2 * k) : 0;
+        float xa[4], xb[4];
+        qa.unpack(xa);
+        qb.unpack(xb);
+        uint64_t va[2], vb[2];                      // the pairs' first elements, their second ones
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float* x = i ? xb : xa;
+            va[i] = kInterleaved ? pack2(x[0], x[2]) : pack2(xa[2 * i], xa[2 * i + 1]);
+            vb[i] = kInterleaved ? pack2(x[1], x[3]) : pack2(xb[2 * i], xb[2 * i + 1]);
+        }
+        float inv = 1.f, ss = 0.f;
+        if (norm) {
+            ss = sum_of_squares(va, vb);
+            float eps = a.eps;
+            if (kLarge) {
+                const float scale = ss == INFINITY ? 0x1p-70f : 1.f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    va[i] = mul2(va[i], pack2(scale, scale));
+                    vb[i] = mul2(vb[i], pack2(scale, scale));
+                }
+                ss = sum_of_squares(va, vb);
+                eps = eps * scale * scale;
+            }
+            inv = rsqrtf(fmaf(ss, mean, eps));
+        }
+        const uint64_t inv2 = pack2(inv, inv);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint64_t ya = mul2(va[i], inv2), yb = mul2(vb[i], inv2);
+            uint64_t ua = mul2(ya, f.fa[i]), ub = mul2(yb, f.fb[i]);
+            if (turns) {                            // (elements that stay must not meet others: 0 * inf)
+                ua = fma2(yb, f.ga[i], ua);
+                ub = fma2(ya, f.gb[i], ub);
+            }
+            float z0, z1, z2, z3;
+            unpack2(ua, z0, z1);
+            unpack2(ub, z2, z3);
+            if constexpr (kInterleaved) {
+                float* x = i ? xb : xa;
+                x[0] = z0; x[1] = z2; x[2] = z1; x[3] = z3;
+            } else {
+                xa[2 * i] = z0; xa[2 * i + 1] = z1;
+                xb[2 * i] = z2; xb[2 * i + 1] = z3;
+            }
+        }
+        if (left > 2 * k) {
+            if constexpr (!kPaged) {
+                store4<kOut>(to, xa);
+                store4<kOut>(to + r.dst_b, xb);
+            } else if (in_bounds(pp >= 0 && pp < a.total_pages, a.status)) {
+                uint8_t* page = a.pool + (size_t)pp * kPageBytes;
+                store4<kTypeBF16>(page + r.page_a, xa);
+                store4<kTypeBF16>(page + r.page_b, xb);
+            }
+        }
+        return ss;
+    };
     for (int left = r.heads - half; left + half > 0; left -= kRows) {
         ring.wait();
         refill();
+        float top = 0.f;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            Quad<kIn> qa, qb;
-            qa.load(ring.get + 2 * k * kRowIn + r.src_a);
-            qb.load(ring.get + 2 * k * kRowIn + r.src_b);
-            const int32_t pp = kPaged ? __shfl_sync(0xffffffffu, r.page, r.heads - left + 2 * k) : 0;
-            float xa[4], xb[4];
-            qa.unpack(xa);
-            qb.unpack(xb);
-            uint64_t va[2], vb[2];                  // the pairs' first elements, their second ones
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float* x = i ? xb : xa;
-                va[i] = kInterleaved ? pack2(x[0], x[2]) : pack2(xa[2 * i], xa[2 * i + 1]);
-                vb[i] = kInterleaved ? pack2(x[1], x[3]) : pack2(xb[2 * i], xb[2 * i + 1]);
-            }
-            float inv = 1.f;
-            if (norm) {
-                float s0, s1;
-                unpack2(add2(fma2(va[0], va[0], mul2(va[1], va[1])), fma2(vb[0], vb[0], mul2(vb[1], vb[1]))), s0, s1);
-                float ss = s0 + s1;
-#pragma unroll
-                for (int s = 1; s < 16; s <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, s);
-                inv = rsqrtf(fmaf(ss, mean, a.eps));
-            }
-            const uint64_t inv2 = pack2(inv, inv);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint64_t ya = mul2(va[i], inv2), yb = mul2(vb[i], inv2);
-                uint64_t ua = mul2(ya, f.fa[i]), ub = mul2(yb, f.fb[i]);
-                if (turns) {                        // (elements that stay must not meet others: 0 * inf)
-                    ua = fma2(yb, f.ga[i], ua);
-                    ub = fma2(ya, f.gb[i], ub);
-                }
-                float z0, z1, z2, z3;
-                unpack2(ua, z0, z1);
-                unpack2(ub, z2, z3);
-                if constexpr (kInterleaved) {
-                    float* x = i ? xb : xa;
-                    x[0] = z0; x[1] = z2; x[2] = z1; x[3] = z3;
-                } else {
-                    xa[2 * i] = z0; xa[2 * i + 1] = z1;
-                    xb[2 * i] = z2; xb[2 * i + 1] = z3;
-                }
-            }
-            if (left > 2 * k) {
-                if constexpr (!kPaged) {
-                    store4<kOut>(dst, xa);
-                    store4<kOut>(dst + r.dst_b, xb);
-                } else if (in_bounds(pp >= 0 && pp < a.total_pages, a.status)) {
-                    uint8_t* page = a.pool + (size_t)pp * kPageBytes;
-                    store4<kTypeBF16>(page + r.page_a, xa);
-                    store4<kTypeBF16>(page + r.page_b, xb);
-                }
-            }
+            top = fmaxf(top, turn_row(k, left, dst, std::false_type{}));
             if constexpr (!kPaged) dst += 2 * r.dst_step;
+        }
+        if (norm && __any_sync(0xffffffffu, top == INFINITY)) {      // the stage once more (a branch per row would keep rows from overlapping)
+#pragma unroll 1
+            for (int k = 0; k < kBatch; ++k) turn_row(k, left, kPaged ? nullptr : dst + 2 * (k - kBatch) * r.dst_step, std::true_type{});
         }
         ring.next();
     }

@@ -10,7 +10,8 @@ import pytest
 import torch
 
 from paper_2506_15969_b200 import binding
-from tests.test_gpu_operators import D, assert_attend, attend_ref, check_attend, engine, gen, prefixed, randn
+from tests.test_gpu_operators import (D, assert_attend, assert_rows, attend_ref, check_attend, engine, freqs, gen, prefixed,
+                                      randn, rows_ref)
 
 pytestmark = pytest.mark.gpu
 
@@ -331,3 +332,35 @@ def test_a_prefix_let_go_is_not_kept(how):
     ref, bound, _ = attend_ref(q, kp, vp, k, v)
     assert bool(((out.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -13 * bound).all())
     del y
+
+
+@pytest.mark.parametrize("dtype,sizes", [(torch.bfloat16, [1.0, 1e18, 2e18, 1e19, 1e25, 1e38, 3e38]),
+                                         (torch.float32, [1e-3, 1e18, 3e18, 1e20, 1e30, 3e37, 1e38])])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_norm_of_rows_whose_squares_overflow(dtype, sizes, interleaved):
+    """Finite rows of any size have a norm: the squares of elements from 1.6e18 on, 128 of them, do not fit fp32."""
+    g = gen(37)
+    H = len(sizes)
+    e = engine(1, H, H, 1, 1)
+    e.set_rope(freqs(64), interleaved=interleaved)
+    w = torch.rand(1, D, generator=g, device="cuda") + 0.5
+    e.set_head_norm(w, w, 1e-6)
+    unit = torch.rand(1, 1, 40, H, D, generator=g, device="cuda", dtype=torch.float64) * 2 - 1
+    x = (unit * torch.tensor(sizes, device="cuda", dtype=torch.float64)[:, None]).to(dtype)
+    assert bool(torch.isfinite(x).all())
+    for tokens in (1, 40):
+        q, k = x[:, :, :tokens], x[:, :, :tokens].flip(3)
+        for to in (torch.bfloat16, torch.float32):
+            qo, ko = torch.empty(q.shape, dtype=to, device="cuda"), torch.empty(k.shape, dtype=to, device="cuda")
+            e.norm_rope(q, k, qo, ko)
+            e.synchronize()
+            for got, rows in ((qo, q), (ko, k)):
+                assert_rows(got, *rows_ref(rows, w, 1e-6, [np.arange(tokens)], freqs(64), interleaved), to)
+    # a row with an infinity is NaN there and zero elsewhere in its pairs' formula; its neighbours do not notice
+    x[0, 0, 0, 1, 5] = float("inf")
+    q, qo = x[:, :, :1], torch.empty(1, 1, 1, H, D, dtype=dtype, device="cuda")
+    e.norm_rope(q, None, qo, None)
+    e.synchronize()
+    assert not bool(torch.isfinite(qo[..., 1, 5]).any())
+    rest = [h for h in range(H) if h != 1]
+    assert_rows(qo[..., rest, :], *rows_ref(q[..., rest, :], w, 1e-6, [np.arange(1)], freqs(64), interleaved), dtype)
