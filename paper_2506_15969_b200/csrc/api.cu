@@ -1058,8 +1058,8 @@ int host_wait(lazyev_t* h, int allowed) {
 int lazyev_decode_step_host(lazyev_t* h, const void* q, const void* k_new, const void* v_new, void* out) {
     if (!h) return LAZYEV_EINVAL;
     if (!q || !k_new || !v_new || !out) return fail(h, LAZYEV_EINVAL, "null pointer");
-    if (!h->prefilled && !h->shared) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
-    int rc = host_streams(h);
+    int rc = check_step(h);                 // (before any copy is queued)
+    if (rc == LAZYEV_OK) rc = host_streams(h);
     if (rc == LAZYEV_OK) rc = host_wait(h, 0);
     if (rc != LAZYEV_OK) return rc;
     // The copy streams start after everything queued on the bound stream so far (an earlier step's
@@ -1085,8 +1085,8 @@ int lazyev_decode_step_host(lazyev_t* h, const void* q, const void* k_new, const
 int lazyev_decode_step_host_async(lazyev_t* h, const void* q, const void* k_new, const void* v_new, void* out) {
     if (!h) return LAZYEV_EINVAL;
     if (!q || !k_new || !v_new || !out) return fail(h, LAZYEV_EINVAL, "null pointer");
-    if (!h->prefilled && !h->shared) return fail(h, LAZYEV_ESTATE, "decode_step before prefill");
-    int rc = host_streams(h);
+    int rc = check_step(h);                 // (before any copy is queued)
+    if (rc == LAZYEV_OK) rc = host_streams(h);
     if (rc != LAZYEV_OK) return rc;
     const int slot = (int)(h->host_seq & 1);
     // The slot's previous step (two steps back) must be complete before its staging buffers are
@@ -1111,7 +1111,10 @@ int lazyev_decode_step_host_async(lazyev_t* h, const void* q, const void* k_new,
     if (e == cudaSuccess) e = cudaStreamWaitEvent(h->stream, h->ev_in[0], 0);
     if (e != cudaSuccess) return cuda_fail(h, e, "host-to-device copy");
     rc = run_step(h, h->stage_q[slot], h->stage_k[slot], h->stage_v[slot], h->stage_out[slot]);
-    if (rc != LAZYEV_OK) return rc;      // found before anything was queued (see lazyev_decode_step)
+    if (rc != LAZYEV_OK) {                  // (no copy is left in flight on the caller's buffers)
+        cudaStreamSynchronize(h->copy_in);
+        return rc;
+    }
     e = cudaEventRecord(h->ev_done[0], h->stream);
     if (e == cudaSuccess) e = cudaStreamWaitEvent(h->copy_out, h->ev_done[0], 0);
     if (e == cudaSuccess) e = cudaMemcpyAsync(out, h->stage_out[slot], qbytes, cudaMemcpyDeviceToHost, h->copy_out);

@@ -364,3 +364,22 @@ def test_norm_of_rows_whose_squares_overflow(dtype, sizes, interleaved):
     assert not bool(torch.isfinite(qo[..., 1, 5]).any())
     rest = [h for h in range(H) if h != 1]
     assert_rows(qo[..., rest, :], *rows_ref(q[..., rest, :], w, 1e-6, [np.arange(1)], freqs(64), interleaved), dtype)
+
+
+def test_a_host_step_that_is_refused_copies_nothing():
+    g = gen(38)
+    pre, own, *_ = prefixed(g, 1, 4, 1, 8, 2, 30, 5)
+    full = binding.Engine(1, 8, 2, D, 62, 1, 2.0)
+    full.set_auto_evict(False)
+    full.append(randn(g, 1, 1, 64, 2, D), randn(g, 1, 1, 64, 2, D))
+    host = [torch.randn(1, 1, h, D).to(torch.bfloat16).pin_memory() for h in (8, 2, 2, 8)]
+    for e, code in ((pre, binding.ESTATE), (full, binding.ECAPACITY)):
+        e.synchronize()
+        before = e.scratch.clone()
+        for step in (e.decode_step_host, e.decode_step_host_async):
+            with pytest.raises(binding.LazyEvError) as err:
+                step(*host)
+            assert err.value.code == code
+        e.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(e.scratch, before)
