@@ -191,8 +191,9 @@ int lazyev_set_wait_limit(lazyev_t* h, double seconds);
  * limit and flag the device status word.  Nothing faults: the kernel ends by itself, and the
  * outputs and statistics of that step are undefined (lazyev_reset() before the handle is used
  * again).  Honoured by launches with one block per unit (lazyev_set_splits(h, 1)); -1 = off.
- * The tiled prompt kernel of lazyev_prefill_observed() honours it too: the thread that feeds a
- * block's ring of key tiles issues no copy beyond its first `pages` key tiles, with the same outcome.
+ * The tiled prompt kernel of lazyev_prefill_observed() and the kernel over a shared prefix honour it too: the thread that feeds a
+ * block's ring of key tiles issues no copy beyond its first `pages` key tiles (of 128 keys); and so does the decode launch with a
+ * warp per unit, by the pages' worth of tokens of a warp.  The outcome is the same.
  */
 int lazyev_debug_starve_page_ring(lazyev_t* h, int pages);
 
@@ -425,6 +426,7 @@ typedef struct lazyev_info {
     int splits;          /* blocks per unit used by the last decode launch   */
     int stages;          /* pipeline stages used by the last decode launch   */
     int groups;          /* consumer warp groups used by the last decode launch */
+                         /* (many units with short own caches behind a prefix, a warp per unit: splits = groups = 1, stages per warp) */
     int tail_units;      /* units of a partly filled last round, given to a second launch (0 = none) */
     int tail_splits;     /* blocks per unit in that second launch                  */
     int grid;            /* blocks launched by the last decode launch        */

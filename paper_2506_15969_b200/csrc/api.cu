@@ -435,7 +435,7 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
     if (!brief) shape = cached->second;
     DecodePlan plan = {};
     if (brief)
-        plan.splits = plan.groups = 1;
+        plan = decode_short_plan();
     else if (decode_plan(c, n, h->max_smem, shape.splits, &plan) != 0)
         return fail(h, LAZYEV_EINVAL, "no decode launch shape fits %d tokens per unit in shared memory", n);
     DecodePlan tail_plan = {};

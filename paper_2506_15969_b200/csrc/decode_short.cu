@@ -368,6 +368,14 @@ cudaError_t decode_short_prepare() {
     return cudaFuncSetAttribute(decode_short_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
 }
 
+DecodePlan decode_short_plan() {
+    DecodePlan plan = {};
+    plan.splits = plan.groups = 1;
+    plan.stages = kRing;
+    plan.smem_bytes = kSmem;
+    return plan;
+}
+
 int decode_short_blocks(int units, int num_sms) {
     return units < num_sms ? units : num_sms;
 }

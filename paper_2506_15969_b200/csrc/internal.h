@@ -102,6 +102,7 @@ cudaError_t decode_launch(const DecodeConfig& c, const DecodePlan& plan, int clu
 // Short units behind a shared prefix: a warp per unit (a.prefix set, a.n <= kShortTokens, no append inside).
 constexpr int kShortTokens = 384;
 cudaError_t decode_short_prepare();
+DecodePlan decode_short_plan();        // what lazyev_get_info() reports of such a launch
 int decode_short_blocks(int units, int num_sms);
 cudaError_t decode_short_launch(const DecodeConfig& c, const DecodeArgs& a, int num_sms, cudaStream_t stream);
 

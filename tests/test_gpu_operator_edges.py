@@ -383,3 +383,11 @@ def test_a_host_step_that_is_refused_copies_nothing():
         e.synchronize()
         torch.cuda.synchronize()
         assert torch.equal(e.scratch, before)
+
+
+def test_info_of_a_warp_per_unit_launch():
+    g = gen(39)
+    pre, own, *kv = prefixed(g, 16, 40, 1, 12, 2, 70, 65)
+    check_attend(own, randn(g, 16, 40, 12, D), *kv)
+    inf = own.info()
+    assert inf.splits == 1 and inf.grid > 0 and inf.stages >= 1 and inf.smem_bytes > 100 * 1024 and inf.tail_units == 0
