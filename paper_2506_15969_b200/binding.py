@@ -269,6 +269,8 @@ class Engine:
     def _rows(self, slot: int, x, heads: int, tokens: int) -> int:
         """A tensor [layers, batch, tokens, heads, 128] (of one token: the dimension may be left out) as a lazyev_rows_t in
         slot 0..3 of this engine's; returns its address."""
+        if x is None or x.dtype not in self._types:
+            raise ValueError(f"rows must be a bfloat16, float16 or float32 tensor, not {None if x is None else x.dtype}")
         stride = x.stride()
         if x.shape != (self._shape[0], self._shape[1], tokens, heads, 128) or stride[4] != 1:
             if x.shape != (self._shape[0], self._shape[1], heads, 128) or tokens != 1 or stride[3] != 1:
@@ -279,6 +281,15 @@ class Engine:
             raise ValueError(f"rows must be on {self._index}, not {x.device}")
         _ROWS.pack_into(self._views, slot * _ROWS.size, x.data_ptr(), self._types[x.dtype], stride[0], stride[1], stride[2], stride[3])
         return self._views_at + slot * _ROWS.size
+
+    def _queries(self, x, name: str) -> int:
+        """A tensor like the q or out of decode_step: [layers, batch, q_heads, 128], or as many elements in that order."""
+        layers, batch, q_heads, _ = self._shape
+        if (x.dtype != self._torch.bfloat16 or x.device != self._index or not x.is_contiguous()
+                or x.numel() != layers * batch * q_heads * 128):
+            raise ValueError(f"{name} must be contiguous bfloat16 [{layers}, {batch}, {q_heads}, 128] on {self._index}, "
+                             f"not {x.dtype} {tuple(x.shape)} on {x.device}")
+        return x.data_ptr()
 
     def _positions(self, positions, tokens: int) -> int:
         if positions is None:
@@ -296,13 +307,16 @@ class Engine:
     def set_head_norm(self, q_weight, k_weight, eps: float) -> None:
         """lazyev_set_head_norm: float32 CUDA tensors [layers, 128], or None for no norm on that side."""
         for w in (q_weight, k_weight):
-            if w is not None and (w.dtype != self._torch.float32 or w.device != self._index or tuple(w.shape) != (self._shape[0], 128)):
-                raise ValueError(f"norm weights must be float32 [{self._shape[0]}, 128] on {self._index}")
+            if w is not None and (w.dtype != self._torch.float32 or w.device != self._index or tuple(w.shape) != (self._shape[0], 128)
+                                  or not w.is_contiguous()):
+                raise ValueError(f"norm weights must be contiguous float32 [{self._shape[0]}, 128] on {self._index}")
         self._check(lib().lazyev_set_head_norm(self._h, _ptr(q_weight), _ptr(k_weight), eps))
         self._norm = q_weight, k_weight
 
     def norm_rope(self, q, k, q_out, k_out, positions=None, first_position: int = 0) -> None:
         """lazyev_norm_rope: q [layers, batch, tokens, q_heads, 128], k with kv_heads (either may be None), strided as they are."""
+        if q is None and k is None:
+            raise ValueError("no rows")
         tokens = (k if q is None else q).shape[2]
         _, _, hq, hkv = self._shape
         qi = qo = ki = ko = 0
@@ -322,7 +336,7 @@ class Engine:
         """lazyev_decode_step_rows: q, k, v [layers, batch, (1,) heads, 128], strided as they are; out as for decode_step."""
         _, _, hq, hkv = self._shape
         self._check(lib().lazyev_decode_step_rows(self._h, self._rows(0, q, hq, 1), self._rows(1, k, hkv, 1), self._rows(2, v, hkv, 1),
-                                                  self._positions(positions, 1), _ptr(out)))
+                                                  self._positions(positions, 1), self._queries(out, "out")))
 
     def attach_prefix(self, prefix: "Engine") -> None:
         """lazyev_attach_prefix; the workspace is allocated here and the prefix kept alive while it is attached."""
@@ -340,7 +354,7 @@ class Engine:
 
     def attend(self, q, out) -> None:
         """lazyev_attend: q, out as for decode_step."""
-        self._check(lib().lazyev_attend(self._h, _ptr(q), _ptr(out)))
+        self._check(lib().lazyev_attend(self._h, self._queries(q, "q"), self._queries(out, "out")))
 
     def state_views(self) -> dict:
         """Views of the live device memory (valid while the engine is): pages [pages, 2 (K, V), 64, 128] bf16 in the

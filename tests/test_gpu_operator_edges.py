@@ -391,3 +391,26 @@ def test_info_of_a_warp_per_unit_launch():
     check_attend(own, randn(g, 16, 40, 12, D), *kv)
     inf = own.info()
     assert inf.splits == 1 and inf.grid > 0 and inf.stages >= 1 and inf.smem_bytes > 100 * 1024 and inf.tail_units == 0
+
+
+def test_binding_refuses_what_does_not_fit():
+    g = gen(40)
+    L, B, Hq, Hkv = 1, 2, 8, 2
+    e = engine(L, Hq, Hkv, B, 10)
+    q, k = randn(g, L, B, 4, Hq, D), randn(g, L, B, 4, Hkv, D)
+    e.append(k, k)
+    q1, out = q[:, :, 0].contiguous(), torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    twice = torch.empty(2 * L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    bad = [lambda: e.norm_rope(q.double(), None, q, None), lambda: e.append(k.double(), k.double()), lambda: e.norm_rope(q, None, None, None),
+           lambda: e.norm_rope(None, k, None, None), lambda: e.norm_rope(None, None, None, None), lambda: e.append(k, None),
+           lambda: e.set_head_norm(torch.ones(L, 2 * D, device="cuda")[:, ::2], None, 1e-6),
+           lambda: e.attend(q1.float(), out), lambda: e.attend(q1, out.float()), lambda: e.attend(twice, out), lambda: e.attend(q1, twice),
+           lambda: e.attend(twice.view(L, B, 2 * Hq, D)[:, :, ::2], out), lambda: e.decode_step_rows(q[:, :, :1], k[:, :, :1], k[:, :, :1], out.float()),
+           lambda: e.decode_step_rows(q[:, :, :1], k[:, :, :1], k[:, :, :1], twice), lambda: e.attend(q1.cpu(), out),
+           lambda: e.attend(q1, out.cpu()), lambda: e.decode_step_rows(q[:, :, :1], k[:, :, :1], k[:, :, :1], out[:, :1])]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+        assert e.info().n == 4 and e.info().t == 0, i
+    e.attend(q[:, :, :1].contiguous(), out)      # one token, its dimension there
+    e.synchronize()
