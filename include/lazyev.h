@@ -352,6 +352,7 @@ int lazyev_decode_step_rows(lazyev_t* h, const lazyev_rows_t* q, const lazyev_ro
  * protected: they are neither tracked nor evicted.  A handle with a prefix may be decoded with no own token
  * yet.  Own tokens appended from now on get the positions after the prefix's.
  *   workspace : device memory of lazyev_query_prefix_workspace() bytes, 256-byte aligned, for as long as the prefix is attached
+ *               (of one handle; the size holds for these two handles whatever number of tokens the prefix comes to hold)
  * While it is attached the prefix must not change: lazyev_decode_step*(), _append(), _evict*(), _reset() and _destroy() on
  * it answer ESTATE.  It may serve several handles at once, on their own streams; the attached handle is ordered after
  * everything queued on the prefix's stream.  The slots behind the prefix's last token are zeroed.  lazyev_reset() detaches, and so does lazyev_destroy().

@@ -1297,6 +1297,8 @@ int lazyev_query_prefix_workspace(const lazyev_t* h, const lazyev_t* prefix, siz
     PrefixPlan plan;
     const int rc = plan_prefix(const_cast<lazyev_t*>(h), prefix, &plan);
     if (rc != LAZYEV_OK) return rc;
+    // enough whatever the prefix comes to hold: a caller may ask once and attach later
+    plan.slots = prefix_most_slots(h->layers, h->batch, prefix->batch, h->kv_heads, h->group, prefix->capacity, h->num_sms);
     *bytes = prefix_o_bytes(plan) + (size_t)plan.slots * plan.rows * sizeof(float2);
     return LAZYEV_OK;
 }

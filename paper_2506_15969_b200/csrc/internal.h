@@ -51,6 +51,8 @@ struct PrefixArgs {
 };
 // blocks = 0: more steps than an int counts.
 PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int group, int n, int num_sms);
+// The most slots of a plan for up to `capacity` tokens (they do not grow with n alone: a longer prefix may have fewer).
+int prefix_most_slots(int layers, int batch, int prefixes, int kv_heads, int group, int capacity, int num_sms);
 cudaError_t prefix_prepare(const uint8_t* pool, int total_pages, PrefixPool* out);
 // Marks every partial sum as absent: a row has up to `slots` of them, and no launch writes those it has not.
 cudaError_t prefix_clear_launch(const PrefixPlan& plan, float2* ml, cudaStream_t stream);

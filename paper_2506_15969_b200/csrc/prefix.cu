@@ -561,6 +561,7 @@ PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int gr
     pl.pairs = (pl.tiles + 1) / 2;
     pl.key_tiles = (n + kTile - 1) / kTile;
     pl.rows = (long long)layers * batch * kv_heads * group;
+    pl.slots = 0;
     const long long items = (long long)layers * prefixes * kv_heads * pl.pairs, work = items * pl.key_tiles;
     pl.blocks = work > 0x40000000 ? 0 : (int)(work < num_sms ? work : num_sms);
     if (pl.blocks == 0) return pl;
@@ -570,6 +571,15 @@ PrefixPlan prefix_plan(int layers, int batch, int prefixes, int kv_heads, int gr
     const int pieces = (pl.key_tiles + pl.per - 1) / pl.per + 1;
     pl.slots = pieces < pl.blocks ? pieces : pl.blocks;
     return pl;
+}
+
+int prefix_most_slots(int layers, int batch, int prefixes, int kv_heads, int group, int capacity, int num_sms) {
+    int most = 0;
+    for (int n = kTile; n < capacity + kTile; n += kTile) {
+        const int slots = prefix_plan(layers, batch, prefixes, kv_heads, group, n < capacity ? n : capacity, num_sms).slots;
+        if (slots > most) most = slots;
+    }
+    return most;
 }
 
 namespace {

@@ -414,3 +414,43 @@ def test_binding_refuses_what_does_not_fit():
         assert e.info().n == 4 and e.info().t == 0, i
     e.attend(q[:, :, :1].contiguous(), out)      # one token, its dimension there
     e.synchronize()
+
+
+def test_the_workspace_fits_whatever_the_prefix_comes_to_hold():
+    """The size that is asked for once holds for every length of that prefix."""
+    g = gen(41)
+    for L, B, Hq, Hkv, cap in ((1, 16, 32, 8, 6000), (1, 4, 8, 1, 3000), (4, 8, 8, 2, 5000)):
+        pre, own = engine(L, Hq, Hkv, 1, cap), engine(L, Hq, Hkv, B, 2)
+        lib, size, first = binding.lib(), C.c_size_t(), None
+        at = 0
+        for n in (1, 129, 1000, 2305, 2500, cap):
+            k = randn(g, L, 1, n - at, Hkv, D) if n > at else None
+            if k is None:
+                continue
+            pre.append(k, k)
+            at = n
+            assert lib.lazyev_query_prefix_workspace(own._h, pre._h, C.byref(size)) == binding.OK
+            first = first or size.value
+            assert size.value == first, (n, size.value, first)
+
+
+def test_a_workspace_asked_for_early():
+    """A workspace of the size that was answered for one token, attached after the prefix has grown: nothing is written behind it."""
+    g = gen(42)
+    L, B, Hq, Hkv, n, cap = 1, 16, 32, 8, 5, 4608                  # 36 key tiles of 8 units: as many parts as there can be
+    pre, own = engine(L, Hq, Hkv, 1, cap), engine(L, Hq, Hkv, B, n)
+    ko, vo = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    own.prefill(ko, vo)
+    kp, vp = randn(g, L, 1, Hkv, cap, D), randn(g, L, 1, Hkv, cap, D)
+    pre.append(kp[..., :1, :].transpose(2, 3), vp[..., :1, :].transpose(2, 3))
+    lib, size = binding.lib(), C.c_size_t()
+    assert lib.lazyev_query_prefix_workspace(own._h, pre._h, C.byref(size)) == binding.OK
+    space = torch.full((size.value + (1 << 20),), 171, dtype=torch.uint8, device="cuda")
+    pre.append(kp[..., 1:, :].transpose(2, 3), vp[..., 1:, :].transpose(2, 3))
+    need = C.c_size_t()
+    assert lib.lazyev_query_prefix_workspace(own._h, pre._h, C.byref(need)) == binding.OK and need.value <= size.value
+    assert lib.lazyev_attach_prefix(own._h, pre._h, space.data_ptr()) == binding.OK
+    check_attend(own, randn(g, L, B, Hq, D), kp, vp, ko, vo)
+    assert bool((space[size.value:] == 171).all())
+    own.detach_prefix()
+    own.synchronize()
