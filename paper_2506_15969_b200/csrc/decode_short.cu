@@ -351,9 +351,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_short_kernel(const __gr
             }
         }
     }
-    // a warp that gave up: the tiles in flight land before the block exits
-    if (!alive && lane == 0)
-        for (uint32_t k = used; k < fetched; ++k) wait_tile(&full[k % kRing], (k / kRing) & 1u, p.status, p.wait_limit_ns);
+    // A warp that gave up: what it has in flight lands before the block exits, and the launch does not end before the prefix launch
+    // does (work queued behind it may write what that one still reads).
+    if (!alive) {
+        if (first) asm volatile("griddepcontrol.wait;" ::: "memory");
+        copies_done();
+        if (lane == 0)
+            for (uint32_t k = used; k < fetched; ++k) wait_tile(&full[k % kRing], (k / kRing) & 1u, p.status, p.wait_limit_ns);
+    }
     tmem_fence_before_sync();
     __syncthreads();
     if (warp == 0) {

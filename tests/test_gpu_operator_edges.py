@@ -454,3 +454,29 @@ def test_a_workspace_asked_for_early():
     assert bool((space[size.value:] == 171).all())
     own.detach_prefix()
     own.synchronize()
+
+
+def test_work_behind_a_launch_that_gave_up():
+    """A warp-per-unit launch that gives up ends behind the prefix launch: the prefix is let go, emptied and filled anew right behind it."""
+    g = gen(57)
+    L, B, Hq, Hkv, N, n = 16, 40, 12, 2, 700, 65
+    pre, own, kp, vp, ko, vo = prefixed(g, L, B, 1, Hq, Hkv, N, n)
+    q = randn(g, L, B, Hq, D)
+    out = torch.empty_like(q)
+    for pages in (0, 1, 0):
+        own.set_wait_limit(1e-4)
+        own.debug_starve_page_ring(pages)
+        own.attend(q, out)
+        own.detach_prefix()
+        pre.reset()
+        kp, vp = randn(g, L, 1, Hkv, N, D), randn(g, L, 1, Hkv, N, D)
+        pre.prefill(kp, vp)
+        with pytest.raises(binding.LazyEvError):
+            own.synchronize()
+        pre.synchronize()
+        own.set_wait_limit(2.0)
+        own.debug_starve_page_ring(-1)
+        own.reset()
+        own.attach_prefix(pre)
+        own.prefill(ko, vo)
+        check_attend(own, q, kp, vp, ko, vo)
