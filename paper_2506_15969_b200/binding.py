@@ -311,6 +311,9 @@ class Engine:
                                   or not w.is_contiguous()):
                 raise ValueError(f"norm weights must be contiguous float32 [{self._shape[0]}, 128] on {self._index}")
         self._check(lib().lazyev_set_head_norm(self._h, _ptr(q_weight), _ptr(k_weight), eps))
+        for w in (q_weight, k_weight):
+            if w is not None:
+                w.record_stream(self.stream)     # (queued work may outlive the engine's interest in them)
         self._norm = q_weight, k_weight
 
     def norm_rope(self, q, k, q_out, k_out, positions=None, first_position: int = 0) -> None:

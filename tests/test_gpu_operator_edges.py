@@ -480,3 +480,31 @@ def test_work_behind_a_launch_that_gave_up():
         own.attach_prefix(pre)
         own.prefill(ko, vo)
         check_attend(own, q, kp, vp, ko, vo)
+
+
+@pytest.mark.parametrize("how", ["replaced", "closed"])
+def test_norm_weights_outlive_the_work_that_reads_them(how):
+    """Weights made on another stream, let go while the engine's stream has yet to read them: their memory is not given away before."""
+    g = gen(58)
+    L, H = 2, 4
+    s = torch.cuda.Stream()
+    e = engine(L, H, H, 1, 1, stream=s)
+    x = randn(g, L, 1, 50, H, D)
+    out = torch.empty_like(x)
+    w = torch.rand(L, D, generator=g, device="cuda") + 0.5
+    want = rows_ref(x, w, 1e-6, [np.arange(50)], [])
+    torch.full((L, D), 9.0, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    e.set_head_norm(w, None, 1e-6)
+    e.norm_rope(x, None, out, None)
+    if how == "replaced":
+        e.set_head_norm(None, None, 0.0)
+    else:
+        del e
+    del w
+    others = [torch.full((L, D), 9.0, device="cuda") for _ in range(20)]
+    torch.cuda.synchronize()
+    assert_rows(out, *want, torch.bfloat16)
+    del others
