@@ -9,13 +9,21 @@
 // sums come through shared memory as whole rows: 165 registers; read in fragment layout from global memory 231.
 //
 // Bound by HBM for many units (512 bytes a token); for few by the latency of one unit.  Measured on B200, both launches behind a
-// prefix of 64 tokens, a warp per unit / a block per unit, us:
-//   own tokens            64            256           384           512
-//    448 units       20.8 / 24.9   30.9 / 28.9   37.1 / 33.0
-//    608 units       22.7 / 28.9   31.1 / 33.9   39.4 / 41.4
-//   3584 units                     95.0 / 112    132 / 142     173 / 172
-//   4096 units       45.4 / 90.5   107 / 126     147 / 158
-// With 320 units the two are level at 64 tokens (20.4 / 20.8) and the block is ahead at 128 (22.9 / 20.8).
+// prefix of 64 tokens, 16 query and 4 KV heads, caches in turn that L2 does not hold together; a warp per unit / a block per unit, us:
+//   own tokens       64            128           256           384
+//    448 units   22.7 / 26.8   25.0 / 27.0
+//    608 units   22.7 / 28.9   25.9 / 30.0   32.9 / 35.0   39.7 / 40.9
+//   1184 units   24.6 / 39.1   28.8 / 41.1   41.0 / 51.1   53.3 / 59.4
+//   1200 units   24.8 / 39.1   29.5 / 41.2   45.2 / 50.7   62.4 / 61.4
+//   1500 units   28.8 / 44.4   36.5 / 46.8   54.3 / 57.6   72.2 / 71.9
+//   1800 units   28.9 / 49.4   36.9 / 51.6   55.5 / 65.7   74.1 / 81.3
+//   2368 units   30.9 / 59.6   41.1 / 62.8   64.2 / 80.1   86.5 / 99.3
+//   2400 units   31.3 / 59.8   41.6 / 62.6   68.6 / 80.2   97.7 / 101
+//   3584 units   39.1 / 80.0   55.2 / 84.2   90.2 / 110     131 / 139
+//   4096 units   43.1 / 88.6   62.6 / 94.3    103 / 124     143 / 156
+// The walk is fixed, 1184 warps: just beyond a whole round (1200 to 1500 units, 2400) its last one is nearly empty, and with 384 tokens the
+// two are level there.  With 8 KV heads: 448 units 30.9 / 28.9 at 256 tokens and 37.1 / 33.0 at 384, 3584 units 173 / 172 at 512;
+// 320 units level at 64 tokens (20.4 / 20.8), the block ahead at 128 (22.9 / 20.8).
 // Hence: at most 384 tokens, three units per SM up to 128 tokens and four beyond.
 #include "internal.h"
 
