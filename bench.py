@@ -40,8 +40,8 @@ FALLBACK_HBM_GBS = 6650.0
 # units x tokens, so a full launch is scaled by its algorithmic bytes.  Valid only for the kernel
 # sources it was taken on.
 NCU_DECODE_CAPTURE = {
-    "traffic_per_algorithmic_byte": 1.0072,
-    "sha256": {"decode.cu": "d503c2c87321f96c31e2e309b6839b3a37a429614323ee1bb163f2251c1c05a9",
+    "traffic_per_algorithmic_byte": 1.0075,
+    "sha256": {"decode.cu": "4bc95d881ebfb025b0d6259913fbd34084200929dde79d3d22ddadd6feb7272a",
                "common.cuh": "38bde61410b93126cf44ed1a98971cc365c31108efb5043fc9500d293d16e3f1"},
 }
 

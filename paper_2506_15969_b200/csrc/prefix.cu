@@ -10,14 +10,16 @@
 // K / V of the prefix are read once per pair of row tiles, 512 bytes per token, where every sequence would read them by
 // itself.  Few rows: HBM, behind a part that does not grow with the prefix; many rows: the tensor core
 // (S, and P V twice) and the softmax between its products.  Measured on B200, this kernel under a profiler: 8 KV heads,
-// 65521 tokens, 64 rows, 269 MB read, 53.8 us, tensor pipe 47 % busy; 4 layers x 8 KV heads, 8192 tokens, 640 rows, 125 us,
-// tensor pipe 64 %, issue slots 43 %.  P as one bf16 term took the second case (whole call, then 187 us) to 174 us; it leaves P 8
+// 65521 tokens, 64 rows, 269 MB read, 54.3 us, tensor pipe 44 % busy; 4 layers x 8 KV heads, 8192 tokens, 640 rows, 125 us,
+// tensor pipe 64 %, issue slots 43 %.  Of the second case's tensor work a sixth is on empty rows: a tile holds whole sequences, 25 of
+// 5 heads, and 128 of them fill five tiles and 3 sequences of a sixth.  P as one bf16 term took the second case (whole call, then 187 us) to 174 us; it leaves P 8
 // mantissa bits where the framework's other attention kernels keep 16, and is not used.
 //
 // Structure: persistent blocks, one per SM.  A row tile is 128 accumulator rows = floor(128 / G) sequences x G heads, an
 // item is a prefix unit with two of its row tiles (or its single, or odd last one), and the walk over (item, key tile
-// of 128 tokens) is cut into equal contiguous parts, one per block, so no wave is left half full; a row gets one
-// set of partial sums per block that worked on its item.
+// of 128 tokens) is cut into equal contiguous parts, one per block, so no wave is left half full (a step of a single row tile counts
+// like one of a pair, though it costs the tensor core half: with an odd number of tiles the blocks on pairs end last); a row gets
+// one set of partial sums per block that worked on its item.
 //
 // Two streams of eight softmax warps (two threads per accumulator row) alternate on the tensor core: with two row tiles a
 // stream has a tile and every key tile; with one, the streams take the key tiles in turn and join their sums at the end.

@@ -27,7 +27,7 @@ def test_a_prefix_launch_that_starves_among_short_pieces(share, Hq, Hkv, N, limi
     """Every block walks several short pieces when its key tiles stop coming: whichever warp gives up first, all of them come to the
     end of their walk within the wait limit, the status word tells, and the handle works again after a reset."""
     g = gen(share * N)
-    L, P = 12, 4
+    L, P = 11, 4
     B = P * share
     pre, own, *kv = prefixed(g, L, B, P, Hq, Hkv, N, 5)
     assert L * P * Hkv > 2 * 148           # units of the prefix: more than two pieces per block
@@ -53,7 +53,7 @@ def test_a_prefix_launch_that_starves_among_short_pieces(share, Hq, Hkv, N, limi
 
 def test_many_short_pieces_repeat_exactly():
     """Walks of every kind of piece, back to back: right, and the same bits in every run."""
-    for i, (L, P, share, Hq, Hkv, N) in enumerate([(12, 4, 32, 64, 8, 100), (12, 4, 40, 64, 8, 130), (12, 4, 8, 64, 8, 300),
+    for i, (L, P, share, Hq, Hkv, N) in enumerate([(11, 4, 32, 64, 8, 100), (11, 4, 40, 64, 8, 130), (11, 4, 8, 64, 8, 300),
                                                    (9, 3, 20, 56, 8, 500), (28, 2, 16, 28, 4, 2048)]):
         g = gen(40 + i)
         pre, own, *kv = prefixed(g, L, P * share, P, Hq, Hkv, N, 3)
