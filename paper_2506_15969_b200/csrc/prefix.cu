@@ -265,15 +265,14 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 if (ok && j + ahead < nt) load_k(j + ahead);
             }
         }
-        if (!ok) {      // aborted: let the copies already issued land before the block exits
-            auto drain = [&](uint64_t* full, const Ring& r, uint32_t n) {
-                const uint32_t last = r.count < n ? r.count : n;
-                for (uint32_t k = r.count - last; k < r.count; ++k)
-                    wait_bar(&full[k % n], (k / n) & 1u, abort_flag, p.status, limit, false);
-            };
-            drain(bars->full, rr, kRing);
-            drain(bars->q_full, qr, 2);
-        }
+        // the copies already issued land before the block exits, whoever gives up and when
+        auto drain = [&](uint64_t* full, const Ring& r, uint32_t n) {
+            const uint32_t last = r.count < n ? r.count : n;
+            for (uint32_t k = r.count - last; k < r.count; ++k)
+                wait_bar(&full[k % n], (k / n) & 1u, abort_flag, p.status, limit, false);
+        };
+        drain(bars->full, rr, kRing);
+        drain(bars->q_full, qr, 2);
     } else if (warp >= kIssuer) {
         // ------------------------------------------------------------------ MMA issuers, one warp per stream
         // A warp walks its loop as a whole (so that descriptors and addresses stay in uniform registers) and one elected lane, the
@@ -291,11 +290,20 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
         auto wait_on = [&](uint64_t* bar, uint32_t parity) {
             if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag, p.status, limit));
         };
-        // Hands a buffer back once the MMAs issued so far are done.  Every buffer expects both streams; one that only this
-        // stream reads gets the other arrival from here.
-        auto release = [&](uint64_t* bar, bool shared) {
-            if (!shared) mbar_arrive(bar);
-            umma_commit(bar);
+        // Every buffer expects both streams: it is handed back by a commit, once the MMAs issued so far are done, or at once by a
+        // stream that does not read it.  A wait for a phase of a barrier means something only to a warp that saw the phase before:
+        // a page may come in long after the pages asked for behind it, and a warp that only looked at its own uses of the ring
+        // took a stage for full that still waited for an earlier use's load.  So each warp looks at all uses, in order, and hands
+        // back those of the other stream; the producer cannot lap a warp that has yet to look.
+        uint32_t seen = 0;                          // uses of the ring that this warp has looked at
+        auto look_at = [&](uint32_t uses_to, bool reads_last) {
+            for (; seen < uses_to; ++seen) {
+                const uint32_t st = seen % kRing;
+                wait_on(&bars->full[st], (seen / kRing) & 1u);
+                if (reads_last && seen + 1 == uses_to) continue;
+                if (ok && elect_one()) mbar_arrive(&bars->empty[st]);
+                __syncwarp();
+            }
         };
         const uint32_t s_col = tmem_base + kColS + s * 128, o_col = tmem_base + kColO + s * 128;
         const uint64_t q_desc = smem_desc(smem_u32(smem + kOffQ), 16, 1024), k_desc = smem_desc(smem_u32(smem + kOffRing), 16, 1024);
@@ -330,14 +338,17 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                     umma_bf16(s_col, a + off, b + off, instr_desc(false), s8 > 0);
                 }
                 umma_commit(&bars->s_full[s]);
-                release(&bars->empty[st], pc.both);
-                if (last) release(&bars->q_empty[q_slot], !pc.both);
+                umma_commit(&bars->empty[st]);
+                if (last) {                         // (Q of two row tiles: each stream reads its own, and answers for the other)
+                    if (pc.both) mbar_arrive(&bars->q_empty[q_slot]);
+                    umma_commit(&bars->q_empty[q_slot]);
+                }
             };
             wait_on(&bars->q_full[q_slot], (q_use >> 1) & 1u);
             int j = pc.both ? 0 : s;
             if (mine > 0) {
                 const uint32_t use = k_use(j);
-                wait_on(&bars->full[use % kRing], (use / kRing) & 1u);
+                look_at(use + 1, true);
                 tmem_fence_after_sync();
                 if (ok && elect_one()) issue_s(use % kRing, mine == 1);
             } else if (ok && elect_one()) {
@@ -348,8 +359,8 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 const int turn = 2 * t + s;         // the streams take turns: 0, 1, 0, 1 ..
                 const bool more = t + 1 < mine;
                 const uint32_t vu = v_use(j), vs = vu % kRing, ku = more ? k_use(j + step) : 0u, ks = ku % kRing;
-                wait_on(&bars->full[vs], (vu / kRing) & 1u);
-                if (more) wait_on(&bars->full[ks], (ku / kRing) & 1u);
+                look_at(vu + 1, true);
+                if (more) look_at(ku + 1, true);
                 wait_on(&bars->p_full[s][0], p_uses & 1u);
                 if (turn > 0 || behind) named_barrier_sync(13 + s, 64);
                 tmem_fence_after_sync();
@@ -360,7 +371,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_fence_after_sync();
                 if (ok && elect_one()) {
                     issue_o(vs, 1, false);
-                    release(&bars->empty[vs], pc.both);
+                    umma_commit(&bars->empty[vs]);
                     if (more)
                         issue_s(ks, t + 2 == mine);
                     else
@@ -371,6 +382,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             }
             behind = (turns & 1) == 0;
             uses += 2 * nt;
+            look_at(uses, false);                   // (the other stream's last ones)
         }
         // every MMA issued by this warp is complete before tensor memory goes back
         if (elect_one()) umma_commit(&bars->drain[s]);

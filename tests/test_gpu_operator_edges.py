@@ -508,3 +508,36 @@ def test_norm_weights_outlive_the_work_that_reads_them(how):
     torch.cuda.synchronize()
     assert_rows(out, *want, torch.bfloat16)
     del others
+
+
+@pytest.mark.parametrize("L,P,share,Hq,Hkv,N,n", [
+    (12, 3, 1, 24, 8, 2497, 2),            # one row tile: several pieces of many key tiles per block, of odd and even numbers
+    (3, 2, 4, 28, 4, 9001, 5),
+    (1, 1, 16, 32, 8, 40000, 30),
+    (2, 1, 40, 16, 2, 20000, 3),           # two row tiles and a single one in turn
+])
+def test_prefix_pages_scattered_over_a_large_pool(L, P, share, Hq, Hkv, N, n):
+    """Pages far apart, in random order, in a pool of some GB: loads come in out of order, and every stage of the ring is used only
+    when its own load is there.  The same bits in every run, and right."""
+    g = gen(N)
+    B = P * share
+    units = L * P * Hkv
+    capacity = max(N + 64, 2 ** 32 // (512 * units))
+    pre = binding.Engine(L, Hq, Hkv, D, capacity, 64, 2.0, batch=P)
+    inf = pre.info()
+    pre.set_page_table(np.random.RandomState(N).permutation(inf.units * inf.pages_per_unit))
+    kp, vp = randn(g, L, P, Hkv, N, D), randn(g, L, P, Hkv, N, D)
+    pre.prefill(kp, vp)
+    own = engine(L, Hq, Hkv, B, n)
+    own.attach_prefix(pre)
+    ko, vo = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    own.prefill(ko, vo)
+    q = randn(g, L, B, Hq, D)
+    want = check_attend(own, q, kp, vp, ko, vo)
+    out, flush = torch.empty_like(q), torch.empty(2 ** 28, dtype=torch.uint8, device="cuda")
+    for i in range(100):
+        out.zero_()
+        flush.fill_(i)                     # (neither pages nor their translations are near)
+        own.attend(q, out)
+        assert torch.equal(out, want), i
+    own.synchronize()
