@@ -172,10 +172,10 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
         // ------------------------------------------------------------ producer
         uint32_t pc = 0, stage = 0, parity = 1;     // parity of the "empty" phase that frees the stage
         int it = 0;
-        bool stopped = false;
+        bool stopped = false, alive = true;         // (a warp whose wait gave up arms and fetches nothing any more)
         for (int u = p.unit_begin + cluster_id; u < p.unit_end && !stopped; u += n_clusters, ++it) {
             const int32_t* pt = p.page_table + (size_t)u * p.pages_per_unit + pg0;
-            for (int base = 0; base < npg && !stopped; base += 32) {
+            for (int base = 0; base < npg && !stopped && alive; base += 32) {
                 const int cnt = min(32, npg - base);
                 const int32_t entry = lane < cnt ? pt[base + lane] : 0;
                 for (int j = 0; j < cnt; ++j, ++pc) {
@@ -186,7 +186,12 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
                         break;
                     }
                     int32_t pp = __shfl_sync(0xffffffffu, entry, j);
-                    if (pc >= (uint32_t)NS) wait_phase(&empty[stage], parity, abort_flag, p.status, p.wait_limit_ns);
+                    // A stage that was not handed back, or that consumers handed back after one had given up, may still wait for its
+                    // load: arming it again would be an error.  (Consumers that wait for the prefix launch hand nothing back until
+                    // that one has ended or given up.)
+                    if (pc >= (uint32_t)NS)
+                        alive = __all_sync(0xffffffffu, wait_phase(&empty[stage], parity, abort_flag, p.status, p.wait_limit_ns) && !*abort_flag);
+                    if (!alive) break;
                     if (pp < 0 || pp >= p.total_pages) {
                         if (lane == 0) atomicOr(p.status, kStatusBadIndex);
                         pp = 0;
@@ -228,11 +233,10 @@ __global__ void __launch_bounds__((4 * NG + 1) * 32, 1) decode_kernel(const Deco
             }
         }
         if (clustered && it > 0) cluster_wait();
-        if (*abort_flag || stopped) {   // consumers stopped waiting: let the copies in flight land before the block exits
-            const uint32_t last = pc < (uint32_t)NS ? pc : (uint32_t)NS;
-            for (uint32_t k = pc - last; k < pc; ++k)
-                wait_phase(&full[k % NS], (k / NS) & 1, abort_flag, p.status, p.wait_limit_ns, false);
-        }
+        // the copies in flight land before the block exits, whoever gives up and when
+        const uint32_t last = pc < (uint32_t)NS ? pc : (uint32_t)NS;
+        for (uint32_t k = pc - last; k < pc; ++k)
+            wait_phase(&full[k % NS], (k / NS) & 1, abort_flag, p.status, p.wait_limit_ns, false);
     } else {
         // ------------------------------------------------------------ consumers
         // Fragment coordinates of this lane: row g (and g + 8), column pair 2 qd, 2 qd + 1.

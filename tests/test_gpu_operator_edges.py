@@ -541,3 +541,33 @@ def test_prefix_pages_scattered_over_a_large_pool(L, P, share, Hq, Hkv, N, n):
         own.attend(q, out)
         assert torch.equal(out, want), i
     own.synchronize()
+
+
+@pytest.mark.parametrize("splits,n", [(2, 9000), (1, 3000), (8, 9000)])
+def test_long_own_caches_behind_a_prefix_launch_that_gives_up(splits, n):
+    """The decode launch begins beside a prefix launch of few blocks that only ends by its time-out, and its blocks have more pages to
+    stream than their rings hold: all of it ends, the status word tells, and the handle works again."""
+    g = gen(59)
+    L, B, Hq, Hkv, N = 1, 2, 8, 1, 12800
+    pre, own, *kv = prefixed(g, L, B, 1, Hq, Hkv, N, n)
+    assert own.info().prefix_blocks == 100
+    own.set_splits(splits)
+    q = randn(g, L, B, Hq, D)
+    want = check_attend(own, q, *kv)
+    assert own.info().splits == splits
+    out = torch.empty_like(q)
+    for limit in (0.002, 0.0005):
+        own.set_wait_limit(limit)
+        own.debug_starve_page_ring(0)
+        own.attend(q, out)
+        with pytest.raises(binding.LazyEvError) as err:
+            own.synchronize()
+        assert err.value.code == binding.EDEVICE
+        own.debug_starve_page_ring(-1)
+        own.set_wait_limit(2.0)
+        own.reset()
+        own.attach_prefix(pre)
+        own.prefill(kv[2], kv[3])
+        own.attend(q, out)
+        own.synchronize()
+        assert torch.equal(out, want)
