@@ -40,8 +40,8 @@ FALLBACK_HBM_GBS = 6650.0
 # units x tokens, so a full launch is scaled by its algorithmic bytes.  Valid only for the kernel
 # sources it was taken on.
 NCU_DECODE_CAPTURE = {
-    "traffic_per_algorithmic_byte": 1.0075,
-    "sha256": {"decode.cu": "4bc95d881ebfb025b0d6259913fbd34084200929dde79d3d22ddadd6feb7272a",
+    "traffic_per_algorithmic_byte": 1.0072,
+    "sha256": {"decode.cu": "07f7d866a95aa761e7cc961fc03fa1bf381a386abc3d3e5a363ae6db81d3c61a",
                "common.cuh": "38bde61410b93126cf44ed1a98971cc365c31108efb5043fc9500d293d16e3f1"},
 }
 

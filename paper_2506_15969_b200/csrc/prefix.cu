@@ -10,7 +10,7 @@
 // K / V of the prefix are read once per pair of row tiles, 512 bytes per token, where every sequence would read them by
 // itself.  Few rows: HBM, behind a part that does not grow with the prefix; many rows: the tensor core
 // (S, and P V twice) and the softmax between its products.  Measured on B200, this kernel under a profiler: 8 KV heads,
-// 65521 tokens, 64 rows, 269 MB read, 54.3 us, tensor pipe 44 % busy; 4 layers x 8 KV heads, 8192 tokens, 640 rows, 125 us,
+// 65521 tokens, 64 rows, 269 MB read, 54.8 us, tensor pipe 47 % busy; 4 layers x 8 KV heads, 8192 tokens, 640 rows, 127 us,
 // tensor pipe 64 %, issue slots 43 %.  Of the second case's tensor work a sixth is on empty rows: a tile holds whole sequences, 25 of
 // 5 heads, and 128 of them fill five tiles and 3 sequences of a sixth.  P as one bf16 term took the second case (whole call, then 187 us) to 174 us; it leaves P 8
 // mantissa bits where the framework's other attention kernels keep 16, and is not used.
