@@ -63,8 +63,9 @@ enum {
     LAZYEV_SCORE_H1_PLUS_H2 = 0,            /* Eq. (2) as printed */
     LAZYEV_SCORE_H1_ONLY = 1,               /* ablation: without the H2-score */
     LAZYEV_SCORE_H2_ONLY = 2,               /* ablation: without the H1-score */
-    LAZYEV_SCORE_H1_PLUS_H2_DECREASING = 3  /* Eq. (2) with H2 = 2 sigma(-(MRI - 1)): falls with MRI, as Section 4's
+    LAZYEV_SCORE_H1_PLUS_H2_DECREASING = 3, /* Eq. (2) with H2 = 2 sigma(-(MRI - 1)): falls with MRI, as Section 4's
                                                prose and the appendix on the score's formulation require */
+    LAZYEV_SCORE_WEIGHT = 4                 /* the attention weight a token has received (lazyev_set_weights), not of the paper */
 };
 
 /*
@@ -92,7 +93,19 @@ int lazyev_set_max_prefill(lazyev_t* h, int n_tokens);
 int lazyev_set_budget(lazyev_t* h, int budget_now);
 /* on != 0: lazyev_decode_step() runs the eviction itself when one is due (default). */
 int lazyev_set_auto_evict(lazyev_t* h, int on);
+/* EINVAL for LAZYEV_SCORE_WEIGHT on a handle without weights. */
 int lazyev_set_score_mode(lazyev_t* h, int mode);
+/*
+ * on != 0: the handle keeps for every cached token the attention weight that it has received, a float32 per slot (4 bytes more of
+ * state; lazyev_query_weights_layout).  It is 0 when a token comes with a prompt or an append.  Every decode step adds the
+ * token's probability (averaged over the query heads of its group, and behind a prefix that of the joint softmax); a chunk sets
+ * or adds its own when asked (lazyev_attend_chunk); lazyev_attend(), lazyev_attend_sparse() and the observation of
+ * lazyev_prefill_observed() change none.  Evictions move the weights with their tokens.  With
+ * lazyev_set_score_mode(LAZYEV_SCORE_WEIGHT) they select by it: the heaviest tokens stay, ties to the more recent, what is
+ * no number before any; the budget, the window and the protected tokens are as ever, and there is no limit on the number of candidates.
+ * Errors: ESTATE after bind, EINVAL (off while it is the score).
+ */
+int lazyev_set_weights(lazyev_t* h, int on);
 /* Number of thread blocks (one cluster) that share one unit in the decode
  * kernel: 0 = choose automatically, else 1..8. */
 int lazyev_set_splits(lazyev_t* h, int splits);
@@ -378,6 +391,70 @@ int lazyev_detach_prefix(lazyev_t* h);
  */
 int lazyev_attend(lazyev_t* h, const void* q, void* out);
 
+/* ---- A whole cache at once ---------------------------------------------------------------------------
+ * (The paper has no counterpart of this section: prompts in chunks, drafted tokens checked together, selection by accumulated
+ * weight and attention over selected blocks are what a server does around its method.)
+ */
+enum { LAZYEV_WEIGHTS_OFF = 0, LAZYEV_WEIGHTS_SET = 1, LAZYEV_WEIGHTS_ADD = 2 };
+
+/*
+ * Causal attention of the last n_tokens cached tokens (1 <= n_tokens <= n; lazyev_append() has loaded their keys and values) with
+ * their own queries: token i of the chunk sees the attached prefix, the tokens before the chunk and the chunk's tokens up to itself:
+ *   out_i = softmax(q_i [K_prefix, K_{0 .. n - n_tokens + i}]^T / sqrt(128)) [V_prefix; V]
+ *   q       : views of q_heads heads (normalised and rotated already: lazyev_norm_rope), bfloat16, strides positive and below 2^38
+ *   out     : views of q_heads heads, any of the three types; may not overlap q
+ *   weights : LAZYEV_WEIGHTS_OFF; _SET or _ADD: the weight of every own token i becomes, or grows by,
+ *             1 / G sum over the chunk's rows that see it of their probabilities of i (a second pass over the keys)
+ *   workspace : device memory of lazyev_query_chunk_workspace() bytes for these n_tokens (or more) and use of the weights, 256-byte aligned,
+ *             used during the call's kernels only
+ * Nothing else changes: probabilities, TS, MRI, t and n stay.  The logits, the softmax and its sums are float32; the weights of the
+ * value product are bfloat16 (single tokens: lazyev_attend() keeps 16 bits of them).  A key or value that a row does not see does
+ * not touch it, whatever it holds.  Any number of tokens, also where a decode step has no launch shape for so long a cache.
+ * It may be captured into a CUDA graph and replayed for other queries in the same buffers while the cache and its
+ * prefix stay as they were at capture.  Calls on one handle share its scratch: order them, replays too.
+ * Errors: EINVAL (views, types, n_tokens, misaligned workspace), ESTATE (weights asked of a handle that keeps none), ECUDA.
+ */
+int lazyev_query_chunk_workspace(const lazyev_t* h, int n_tokens, int weights, size_t* bytes);
+int lazyev_attend_chunk(lazyev_t* h, const lazyev_rows_t* q, int n_tokens, const lazyev_rows_t* out, int weights, void* workspace);
+
+/*
+ * Evicts now, whatever the step: every unit is cut to `keep` tokens (n_recent + n_initial < keep <= the create-time budget) by the
+ * handle's score mode and protection, as by lazyev_evict(), in place (dst NULL or h itself), or into `dst`: another bound
+ * handle of the same layers, batch, heads and device, without a cache, and with the same prefix attached or none, whose own capacity,
+ * budget and score may differ -- a long prompt is read in one large cache and goes on in a small one.  Then h stays as it is, and dst
+ * continues at h's t and next position with K, V, TS, MRI, positions and (where both keep them, else zeros) weights of the kept
+ * tokens, ordered after what is queued on h's stream and asynchronous on its own; h's later work waits for it.  A cache of
+ * at most `keep` tokens stays whole, or is copied whole.
+ * Errors: EINVAL (keep; other shapes; more than 25 600 unprotected tokens with a score of the paper's), ESTATE (no cache; dst holds one, is not
+ * bound or has another prefix; in place on a shared prefix), ECAPACITY (dst is too small), ECUDA.  They are found before anything is queued.
+ */
+int lazyev_evict_to(lazyev_t* h, int keep, lazyev_t* dst, int* evicted);
+
+/*
+ * Attention of one query row per head over a selection of the own tokens, and over the whole attached prefix.  A block is a page of
+ * 64 slots.  For every block before the newest its keys' bounds are kept, high[d] and low[d], and a unit's score of it is
+ *   s = sum over the group's heads g and dimensions d of max(q_g[d] high[d], q_g[d] low[d]),
+ * which no key between the bounds exceeds with its logits summed over the heads; it is taken in 64 bits.  The blocks - 1 best (ties to
+ * the older, what is no number first) and the newest block are read, all of them when there are no more:
+ *   out = softmax(q [K_prefix, K_selected]^T / sqrt(128)) [V_prefix; V_selected]
+ *   q, out   : as for lazyev_decode_step(), q 16-byte aligned
+ *   selected : device int32 [units][blocks], or NULL: the selected blocks in ascending order, -1 behind the last
+ * Nothing in the cache changes (the stored probabilities neither).  Bounds that are missing are made first: those of blocks that have filled since
+ * the last call, all of them after a prompt load or an eviction.  lazyev_index_blocks() makes them beforehand, and again from
+ * first_block on for a caller that has written to the pages itself.
+ * The workspace, device memory of *bytes bytes, 256-byte aligned, is the caller's and must stay valid while it is set (NULL ends that);
+ * the bounds lie in it from *bounds on: bf16 [units][pages_per_unit][2 (high, low)][128].
+ * Capture and ordering as for lazyev_attend_chunk(); a graph makes the bounds that were missing at its capture at every replay.
+ * Errors: EINVAL (null, misaligned, blocks <= 0), ESTATE (no workspace, no own token), ECUDA.
+ */
+int lazyev_query_block_workspace(const lazyev_t* h, size_t* bytes, size_t* bounds);
+int lazyev_set_block_workspace(lazyev_t* h, void* workspace);
+int lazyev_index_blocks(lazyev_t* h, int first_block);
+int lazyev_attend_sparse(lazyev_t* h, const void* q, int blocks, void* out, int32_t* selected);
+
+/* Byte offset of the weights inside the bound state region, float32 [units][capacity].  ESTATE for a handle that keeps none. */
+int lazyev_query_weights_layout(const lazyev_t* h, size_t* weights);
+
 /* Byte offsets inside the bound state region, for code that reads it on the device: the page table, int32 [units][pages_per_unit];
  * (TS, MRI), int32 pairs; positions, int32; probabilities, float32; all [units][capacity].  Any pointer may be NULL. */
 int lazyev_query_state_layout(const lazyev_t* h, size_t* page_table, size_t* ts_mri, size_t* pos, size_t* pbar);
@@ -462,7 +539,7 @@ int lazyev_get_counters(lazyev_t* h, lazyev_counters_t* out);
  * fills unit_begin / unit_count and the host pointers it wants (NULL = skip);
  * arrays are [unit_count][capacity] (k, v: [unit_count][capacity][head_dim],
  * de-swizzled bf16 bits), valid in the first `n` slots of each unit.
- * `score` receives Eq. (2) evaluated now, at step t, for every cached token.
+ * `score` receives Eq. (2) evaluated now, at step t, for every cached token (with LAZYEV_SCORE_WEIGHT: its weight).
  * `device_status` is the kernels' status word (0 = healthy).
  */
 typedef struct lazyev_dump {
@@ -484,7 +561,8 @@ int lazyev_dump_state(lazyev_t* h, lazyev_dump_t* dump);
  * no counterpart, its method keeps no state beyond TS and MRI of Eq. (1) and the cache).
  * Valid on a bound handle instead of lazyev_prefill().  `snap` must cover all units
  * (unit_begin = 0, unit_count = units) with pos, ts, mri, k and v set (host arrays laid out
- * as dump_state writes them, row stride snap->capacity; pbar optional, score ignored) and
+ * as dump_state writes them, row stride snap->capacity; pbar optional; score ignored, except that
+ * with LAZYEV_SCORE_WEIGHT it gives the weights, which are else 0) and
  * its n and t; `prefill` is the prompt length of the original run (positions of new tokens
  * continue from prefill + t; behind an attached prefix, attached before, prefill may be 0 and counts own tokens only).  The handle may have another capacity than the one the
  * snapshot came from as long as n fits.  Decoding then continues exactly as the original

@@ -17,7 +17,8 @@ import numpy as np
 from . import build as _build
 
 OK, EINVAL, ESTATE, ECAPACITY, EDEVICE, ECUDA = 0, -1, -2, -3, -4, -5
-SCORE_H1_PLUS_H2, SCORE_H1_ONLY, SCORE_H2_ONLY, SCORE_H1_PLUS_H2_DECREASING = 0, 1, 2, 3
+SCORE_H1_PLUS_H2, SCORE_H1_ONLY, SCORE_H2_ONLY, SCORE_H1_PLUS_H2_DECREASING, SCORE_WEIGHT = 0, 1, 2, 3, 4
+WEIGHTS_OFF, WEIGHTS_SET, WEIGHTS_ADD = 0, 1, 2
 PROMPT_TILED, PROMPT_REPLAY = 0, 1
 BF16, FP16, FP32 = 0, 1, 2
 
@@ -61,6 +62,7 @@ _PROTOS = {
     "lazyev_set_budget": [C.c_void_p, C.c_int],
     "lazyev_set_auto_evict": [C.c_void_p, C.c_int],
     "lazyev_set_score_mode": [C.c_void_p, C.c_int],
+    "lazyev_set_weights": [C.c_void_p, C.c_int],
     "lazyev_set_splits": [C.c_void_p, C.c_int],
     "lazyev_set_stages": [C.c_void_p, C.c_int],
     "lazyev_set_groups": [C.c_void_p, C.c_int],
@@ -90,6 +92,14 @@ _PROTOS = {
     "lazyev_detach_prefix": [C.c_void_p],
     "lazyev_attend": [C.c_void_p, C.c_void_p, C.c_void_p],
     "lazyev_query_state_layout": [C.c_void_p, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+    "lazyev_query_weights_layout": [C.c_void_p, C.POINTER(C.c_size_t)],
+    "lazyev_query_chunk_workspace": [C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_size_t)],
+    "lazyev_attend_chunk": [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p],
+    "lazyev_evict_to": [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_int)],
+    "lazyev_query_block_workspace": [C.c_void_p, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+    "lazyev_set_block_workspace": [C.c_void_p, C.c_void_p],
+    "lazyev_index_blocks": [C.c_void_p, C.c_int],
+    "lazyev_attend_sparse": [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p],
     "lazyev_evict": [C.c_void_p, C.POINTER(C.c_int)],
     "lazyev_evict_static": [C.c_void_p, C.POINTER(C.c_int)],
     "lazyev_get_info": [C.c_void_p, C.POINTER(Info)],
@@ -151,11 +161,14 @@ class Engine:
 
     def __init__(self, layers: int, q_heads: int, kv_heads: int, head_dim: int, budget: int, window: int,
                  threshold: float, batch: int = 1, n_recent: Optional[int] = None, n_initial: int = 0,
-                 max_prefill: Optional[int] = None, device="cuda", stream=None):
+                 max_prefill: Optional[int] = None, device="cuda", stream=None, weights: bool = False):
         import torch
         self._torch = torch
         self._h = C.c_void_p()
         self._norm = self._prefix = None          # tensors and the engine that the handle reads
+        self._chunk_space, self._chunk_room = [], {}      # workspaces of attend_chunk; the bytes that a number of tokens takes
+        self._block_space = None
+        self._weights = weights
         self._views = C.create_string_buffer(4 * _ROWS.size)
         self._views_at = C.addressof(self._views)
         self._shape = layers, batch, q_heads, kv_heads
@@ -166,6 +179,8 @@ class Engine:
             self._check(lib().lazyev_set_protect(self._h, window if n_recent is None else n_recent, n_initial))
         if max_prefill is not None:
             self._check(lib().lazyev_set_max_prefill(self._h, max_prefill))
+        if weights:
+            self._check(lib().lazyev_set_weights(self._h, 1))
         kv, st, sc = C.c_size_t(), C.c_size_t(), C.c_size_t()
         self._check(lib().lazyev_query_sizes(self._h, C.byref(kv), C.byref(st), C.byref(sc)))
         self.device = torch.device(device)
@@ -359,9 +374,69 @@ class Engine:
         """lazyev_attend: q, out as for decode_step."""
         self._check(lib().lazyev_attend(self._h, self._queries(q, "q"), self._queries(out, "out")))
 
+    def reserve_chunk(self, tokens: int, weights: int = WEIGHTS_OFF) -> None:
+        """The workspace of attend_chunk for up to `tokens` tokens.  attend_chunk makes room by itself; a caller that captures it into a
+        graph without having called it at this size before reserves it beforehand.  Earlier ones stay (graphs may use them)."""
+        n = C.c_size_t()
+        self._check(lib().lazyev_query_chunk_workspace(self._h, tokens, weights, C.byref(n)))
+        self._chunk_room[tokens, weights] = n.value
+        if not self._chunk_space or self._chunk_space[-1].numel() < n.value:
+            with self._torch.cuda.stream(self.stream):
+                self._chunk_space.append(self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device))
+
+    def attend_chunk(self, q, out, weights: int = WEIGHTS_OFF) -> None:
+        """lazyev_attend_chunk of the last q.shape[2] cached tokens: q, out [layers, batch, tokens, q_heads, 128], strided as they are."""
+        if q is None or q.dim() != 5:
+            raise ValueError(f"q must be [layers, batch, tokens, q_heads, 128], not {None if q is None else tuple(q.shape)}")
+        tokens, heads = q.shape[2], self._shape[2]
+        qi, oi = self._rows(0, q, heads, tokens), self._rows(2, out, heads, tokens)
+        space = 0
+        if tokens > 0:
+            room = self._chunk_room.get((tokens, weights))
+            if room is None or not self._chunk_space or self._chunk_space[-1].numel() < room:
+                self.reserve_chunk(tokens, weights)
+            space = self._chunk_space[-1].data_ptr()
+        self._check(lib().lazyev_attend_chunk(self._h, qi, tokens, oi, weights, space))
+
+    def evict_to(self, keep: int, dst: Optional["Engine"] = None) -> int:
+        """lazyev_evict_to: cut this cache to `keep` tokens per unit now, in place or into another engine; tokens removed."""
+        n = C.c_int()
+        self._check(lib().lazyev_evict_to(self._h, keep, None if dst is None else dst._h, C.byref(n)))
+        return n.value
+
+    def _blocks(self):
+        if self._block_space is None:
+            n = C.c_size_t()
+            self._check(lib().lazyev_query_block_workspace(self._h, C.byref(n), None))
+            with self._torch.cuda.stream(self.stream):
+                space = self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device)
+            self._check(lib().lazyev_set_block_workspace(self._h, space.data_ptr()))
+            self._block_space = space
+        return self._block_space
+
+    def index_blocks(self, first_block: Optional[int] = None) -> None:
+        """lazyev_index_blocks: the bounds of blocks that have none yet, or of all from first_block on."""
+        self._blocks()
+        self._check(lib().lazyev_index_blocks(self._h, 2 ** 31 - 1 if first_block is None else first_block))
+
+    def block_bounds(self):
+        """A view of the bounds [units, pages_per_unit, 2 (high, low), 128] bf16; the newest block has none."""
+        inf = self.info()
+        size = inf.units * inf.pages_per_unit * 512
+        return self._blocks()[:size].view(self._torch.bfloat16).view(inf.units, inf.pages_per_unit, 2, 128)
+
+    def attend_sparse(self, q, out, blocks: int, selected=None) -> None:
+        """lazyev_attend_sparse: q, out as for decode_step; selected: int32 [units, blocks] to receive the blocks that were read."""
+        self._blocks()
+        qi, oi = self._queries(q, "q"), self._queries(out, "out")
+        if selected is not None and (selected.dtype != self._torch.int32 or selected.device != self._index or not selected.is_contiguous()
+                                     or selected.numel() != self._shape[0] * self._shape[1] * self._shape[3] * blocks):
+            raise ValueError(f"selected must be contiguous int32 [units, {blocks}] on {self._index}")
+        self._check(lib().lazyev_attend_sparse(self._h, qi, blocks, oi, _ptr(selected)))
+
     def state_views(self) -> dict:
         """Views of the live device memory (valid while the engine is): pages [pages, 2 (K, V), 64, 128] bf16 in the
-        stored order, page_table [units, pages_per_unit], and per unit and slot ts_mri [.., 2], pos and pbar."""
+        stored order, page_table [units, pages_per_unit], and per unit and slot ts_mri [.., 2], pos and pbar, and weights where they are kept."""
         t, inf, off = self._torch, self.info(), [C.c_size_t() for _ in range(4)]
         self._check(lib().lazyev_query_state_layout(self._h, *(C.byref(o) for o in off)))
 
@@ -370,9 +445,14 @@ class Engine:
             return self.state[o.value:o.value + n].view(dtype).view(*shape)
 
         u, cap = inf.units, inf.capacity
-        return {"pages": self.kv_pool.view(t.bfloat16).view(-1, 2, 64, 128),
-                "page_table": view(off[0], t.int32, u, inf.pages_per_unit), "ts_mri": view(off[1], t.int32, u, cap, 2),
-                "pos": view(off[2], t.int32, u, cap), "pbar": view(off[3], t.float32, u, cap)}
+        views = {"pages": self.kv_pool.view(t.bfloat16).view(-1, 2, 64, 128),
+                 "page_table": view(off[0], t.int32, u, inf.pages_per_unit), "ts_mri": view(off[1], t.int32, u, cap, 2),
+                 "pos": view(off[2], t.int32, u, cap), "pbar": view(off[3], t.float32, u, cap)}
+        if self._weights:
+            at = C.c_size_t()
+            self._check(lib().lazyev_query_weights_layout(self._h, C.byref(at)))
+            views["weights"] = view(at, t.float32, u, cap)
+        return views
 
     def evict(self) -> int:
         n = C.c_int()
@@ -391,7 +471,7 @@ class Engine:
         cnt, n = snap["pos"].shape
         d = Dump(unit_begin=0, unit_count=cnt, t=snap["t"], n=n, capacity=n)
         keep = {}
-        for name, dt in (("pos", np.int32), ("ts", np.int32), ("mri", np.int32), ("pbar", np.float32),
+        for name, dt in (("pos", np.int32), ("ts", np.int32), ("mri", np.int32), ("pbar", np.float32), ("score", np.float64),
                          ("k", np.uint16), ("v", np.uint16)):
             if name in snap:
                 keep[name] = np.ascontiguousarray(snap[name], dtype=dt)

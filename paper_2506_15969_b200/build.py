@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblazyev.so")
 LIB_DEBUG = os.path.join(HERE, "liblazyev_debug.so")     # the same sources with -DLAZYEV_DEBUG_BOUNDS
 SOURCES = ["api.cu", "decode.cu", "cache_ops.cu", "evict.cu", "prompt.cu", "rows.cu",
-           "prefix.cu", "decode_short.cu"]
+           "prefix.cu", "decode_short.cu", "chunk.cu", "weigh.cu", "keep.cu", "blocks.cu"]
 
 
 def _nvcc() -> str:

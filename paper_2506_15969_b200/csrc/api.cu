@@ -51,6 +51,13 @@ struct lazyev {
     double* stage_score = nullptr;
     unsigned long long* stage_hist = nullptr;
     uint8_t* stage_rows = nullptr;         // queries of lazyev_decode_step_rows(), normalised and rotated
+    // the weights that tokens receive (lazyev_set_weights), and what the calls on a whole cache keep
+    int weights_on = 0;
+    float* weights = nullptr;              // [units][capacity], behind the status word in the state region
+    int32_t* counters = nullptr;           // scratch of the chunk kernels, zero between launches: [2][kChunkCounters]
+    PrefixPool own_pool = {};              // the own pool as the chunk kernels address it
+    uint8_t* block_space = nullptr;        // lazyev_set_block_workspace()
+    int indexed = 0;                       // blocks, from the first on, whose bounds are in it
     double* h2_table = nullptr;            // H2 term per MRI value (scratch), valid for h2_table_mode
     int h2_table_mode = -1;
     // host-buffer entry point: copy streams and events, created at its first call
@@ -132,8 +139,8 @@ void derive(lazyev_t* h) {
 
 struct Sizes {
     size_t kv, state, scratch;
-    size_t off_tsm, off_pos, off_pbar, off_status;                                  // inside state
-    size_t off_first, off_rlist, off_q, off_k, off_v, off_out, off_score, off_hist, off_h2, off_rows;    // inside scratch
+    size_t off_tsm, off_pos, off_pbar, off_status, off_weights;                     // inside state
+    size_t off_first, off_rlist, off_q, off_k, off_v, off_out, off_score, off_hist, off_h2, off_rows, off_counters;    // inside scratch
 };
 
 Sizes sizes_of(const lazyev_t* h) {
@@ -149,6 +156,8 @@ Sizes sizes_of(const lazyev_t* h) {
     off += align_up(slots * 4, 256);
     s.off_status = off;
     off += 256;
+    s.off_weights = off;
+    if (h->weights_on) off += align_up(slots * 4, 256);
     s.state = off;
     off = align_up((size_t)h->units * h->budget * sizeof(int32_t), 256);
     s.off_first = off;
@@ -173,6 +182,8 @@ Sizes sizes_of(const lazyev_t* h) {
     off += align_up((size_t)kH2TableEntries * sizeof(double), 256);
     s.off_rows = off;
     off += align_up(qbytes, 256);
+    s.off_counters = off;
+    off += 2 * kChunkCounters * sizeof(int32_t);
     s.scratch = off;
     return s;
 }
@@ -244,30 +255,29 @@ int collect_profile(lazyev_t* h) {
 // Candidates of an eviction over n cached tokens, or -1 when the select kernel cannot hold them.
 int candidates_of(const lazyev_t* h, int n) {
     const int ncand = n - h->n_recent - h->n_initial;
-    if (ncand <= 0 || select_smem_bytes(ncand) > 200 * 1024) return -1;
+    if (ncand <= 0 || (h->score_mode != LAZYEV_SCORE_WEIGHT && select_smem_bytes(ncand) > 200 * 1024)) return -1;
     return ncand;
 }
 
 bool evict_due_at(const lazyev_t* h, int t, int n) { return t != 0 && t % h->window == 0 && n > h->budget_now; }
 
-// The lagged eviction of Section 4 at the current step, if one is due.  `src` and `first_moved` are
-// the work lists of the select and compact kernels: the bound scratch region's or the library's own.
-int run_evict(lazyev_t* h, int* evicted, int32_t* src, int32_t* first_moved, int32_t* radix_list) {
-    if (evicted) *evicted = 0;
-    if (!evict_due_at(h, h->t, h->n)) return LAZYEV_OK;
+// Which tokens stay when every unit is cut to `keep` of its h->n tokens: the select launches, into the work lists `src` and
+// `first_moved`, the bound scratch region's or the library's own.
+int run_select(lazyev_t* h, int keep, int32_t* src, int32_t* first_moved, int32_t* radix_list, EvictArgs* args) {
     const int ncand = candidates_of(h, h->n);
     if (ncand < 0)
         return fail(h, LAZYEV_EINVAL, "eviction over %d candidates is not supported", h->n - h->n_recent - h->n_initial);
     cudaError_t e;
-    if (h->h2_table_mode != h->score_mode) {      // the H2 term per MRI value, in the variant the mode selects
+    const bool by_weight = h->score_mode == LAZYEV_SCORE_WEIGHT;
+    if (!by_weight && h->h2_table_mode != h->score_mode) {      // the H2 term per MRI value, in the variant the mode selects
         e = h2_table_launch(h->score_mode, kH2TableEntries, h->h2_table, h->stream);
         if (e != cudaSuccess) return cuda_fail(h, e, "H2 table launch");
         h->h2_table_mode = h->score_mode;
         h->launches += 1;
     }
-    EvictArgs a;
+    EvictArgs& a = *args;
     a.n = h->n;
-    a.budget = h->budget_now;
+    a.budget = keep;
     a.n_recent = h->n_recent;
     a.n_initial = h->n_initial;
     a.t = h->t;
@@ -280,21 +290,37 @@ int run_evict(lazyev_t* h, int* evicted, int32_t* src, int32_t* first_moved, int
     a.radix_count = radix_list + h->units;
     const Geometry geo = geometry(h);
     {
-        // algorithmic bytes: TS and MRI of every candidate read, the source list written
-        SpanGuard g(h, kSpanSelect, (double)h->units * (8.0 * ncand + 4.0 * a.budget));
-        e = select_launch(geo, h->st, a, h->num_sms, h->stream);
+        // algorithmic bytes: TS and MRI (the weight) of every candidate read, the source list written
+        SpanGuard g(h, kSpanSelect, (double)h->units * ((by_weight ? 4.0 : 8.0) * ncand + 4.0 * a.budget));
+        e = by_weight ? weigh_select_launch(geo, h->st, h->weights, a, h->stream) : select_launch(geo, h->st, a, h->num_sms, h->stream);
     }
     if (e != cudaSuccess) return cuda_fail(h, e, "select kernel launch");
-    h->launches += 1;        // the selection is two launches
+    h->launches += by_weight ? 1 : 2;        // (the selection by score is two launches)
+    return LAZYEV_OK;
+}
+
+// Cuts every unit to its `keep` < h->n best tokens, in place.
+int run_cut(lazyev_t* h, int keep, int* evicted, int32_t* src, int32_t* first_moved, int32_t* radix_list) {
+    EvictArgs a;
+    const int rc = run_select(h, keep, src, first_moved, radix_list, &a);
+    if (rc != LAZYEV_OK) return rc;
+    const Geometry geo = geometry(h);
+    cudaError_t e;
     {
         SpanGuard g(h, kSpanCompact, 0.0);
         e = compact_launch(geo, h->pool, h->st, a, h->stream);
     }
     if (e != cudaSuccess) return cuda_fail(h, e, "compact kernel launch");
-    h->launches += 2;
+    h->launches += 1;
+    if (h->weights) {
+        e = compact_weights_launch(geo, h->weights, a, h->stream);
+        if (e != cudaSuccess) return cuda_fail(h, e, "weight compaction launch");
+        h->launches += 1;
+    }
+    h->indexed = 0;                          // (the blocks hold other tokens now)
     h->evictions += 1;
-    if (evicted) *evicted = h->n - h->budget_now;
-    h->n = h->budget_now;
+    if (evicted) *evicted = h->n - keep;
+    h->n = keep;
     if (h->profiling) {
         // rows that actually moved: every destination from the first evicted slot on
         std::vector<int32_t> first(h->units);
@@ -308,6 +334,19 @@ int run_evict(lazyev_t* h, int* evicted, int32_t* src, int32_t* first_moved, int
         h->prof.compact_rows += rows;
     }
     return LAZYEV_OK;
+}
+
+// The lagged eviction of Section 4 at the current step, if one is due.
+int run_evict(lazyev_t* h, int* evicted, int32_t* src, int32_t* first_moved, int32_t* radix_list) {
+    if (evicted) *evicted = 0;
+    if (!evict_due_at(h, h->t, h->n)) return LAZYEV_OK;
+    return run_cut(h, h->budget_now, evicted, src, first_moved, radix_list);
+}
+
+// A new sequence's tokens [slot, slot + count) have received nothing yet.
+cudaError_t clear_weights(lazyev_t* h, int slot, int count) {
+    if (!h->weights || count <= 0) return cudaSuccess;
+    return cudaMemset2DAsync(h->weights + slot, (size_t)h->capacity * sizeof(float), 0, (size_t)count * sizeof(float), h->units, h->stream);
 }
 
 // Host side of a pipelined step: queries come from and outputs go to host memory in unit ranges, on
@@ -349,8 +388,9 @@ cudaError_t run_prefix(lazyev_t* h, const void* q) {
 // every unit with tracking (unless `track` is false) at time t.  `tok` (may be null) is the token to append at slot n - 1 first: as
 // a launch of its own, or -- when every block of the decode launch takes exactly one unit, the launch-latency-sized
 // problems -- inside the decode launch.
+// `view` (may be null) stands for the handle's own state: other pages, another place for the probabilities.
 int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPipe* pipe, const NewToken* tok = nullptr,
-               bool track = true) {
+               bool track = true, const StateView* view = nullptr) {
     // (the kernels load pairs of elements of q, or tiles of it over a prefix, and store single elements of out)
     if (h->shared && ((uintptr_t)q & 15)) return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned while a prefix is attached");
     if (((uintptr_t)q & 3) || ((uintptr_t)out & 1)) return fail(h, LAZYEV_EINVAL, "q must be 4-byte aligned, out 2-byte aligned");
@@ -514,7 +554,7 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
             if (pipe) e = cudaStreamWaitEvent(h->stream, h->ev_in[r], 0);
             if (e != cudaSuccess) break;
             // a range of the main walk continues it; the last round's units are a walk of their own
-            DecodeArgs a{h->pool, h->st, q, out, n, t, begin[r], count[r], is_tail ? 0 : begin[r] / clusters,
+            DecodeArgs a{h->pool, view ? *view : h->st, q, out, n, t, begin[r], count[r], is_tail ? 0 : begin[r] / clusters,
                          fuse_append ? tok->k : nullptr, fuse_append ? tok->v : nullptr, fuse_append ? tok->position : 0, prefix,
                          h->shared && !pipe && !fork && r == 0 && !h->profiling};
             const bool beside = is_tail && fork;
@@ -565,6 +605,11 @@ int finish_step(lazyev_t* h) {
     h->t += 1;
     h->n += 1;
     h->prefilled = true;                    // (a handle with a prefix may start with no own token)
+    if (h->weights) {
+        const cudaError_t e = step_weights_launch(geometry(h), h->weights, h->st.pbar, h->n, h->stream);
+        if (e != cudaSuccess) return cuda_fail(h, e, "weight kernel launch");
+        h->launches += 1;
+    }
     if (h->auto_evict) return run_evict(h, nullptr, h->src, h->first_moved, h->radix_list);
     return LAZYEV_OK;
 }
@@ -772,8 +817,17 @@ int lazyev_set_auto_evict(lazyev_t* h, int on) {
 
 int lazyev_set_score_mode(lazyev_t* h, int mode) {
     if (!h) return LAZYEV_EINVAL;
-    if (mode < 0 || mode > 3) return fail(h, LAZYEV_EINVAL, "unknown score mode %d", mode);
+    if (mode < 0 || mode > LAZYEV_SCORE_WEIGHT) return fail(h, LAZYEV_EINVAL, "unknown score mode %d", mode);
+    if (mode == LAZYEV_SCORE_WEIGHT && !h->weights_on) return fail(h, LAZYEV_EINVAL, "selection by weight needs lazyev_set_weights()");
     h->score_mode = mode;
+    return LAZYEV_OK;
+}
+
+int lazyev_set_weights(lazyev_t* h, int on) {
+    if (!h) return LAZYEV_EINVAL;
+    if (h->bound) return fail(h, LAZYEV_ESTATE, "set_weights after bind");
+    if (!on && h->score_mode == LAZYEV_SCORE_WEIGHT) return fail(h, LAZYEV_EINVAL, "selection by weight needs the weights");
+    h->weights_on = on != 0;
     return LAZYEV_OK;
 }
 
@@ -825,6 +879,9 @@ int lazyev_bind(lazyev_t* h, void* kv_pool, void* state, void* scratch, void* cu
     if ((e = decode_prepare()) != cudaSuccess) return cuda_fail(h, e, "decode kernel set-up");
     if ((e = decode_short_prepare()) != cudaSuccess) return cuda_fail(h, e, "decode kernel set-up");
     if ((e = select_prepare()) != cudaSuccess) return cuda_fail(h, e, "select kernel set-up");
+    if ((e = chunk_prepare()) != cudaSuccess) return cuda_fail(h, e, "chunk kernel set-up");
+    if ((e = weigh_prepare()) != cudaSuccess) return cuda_fail(h, e, "weight kernel set-up");
+    if ((e = keep_prepare()) != cudaSuccess) return cuda_fail(h, e, "select kernel set-up");
 
     const Sizes s = sizes_of(h);
     h->stream = (cudaStream_t)cuda_stream;
@@ -854,9 +911,14 @@ int lazyev_bind(lazyev_t* h, void* kv_pool, void* state, void* scratch, void* cu
     h->h2_table = (double*)(cp + s.off_h2);
     h->h2_table_mode = -1;
     h->stage_rows = cp + s.off_rows;
+    h->counters = (int32_t*)(cp + s.off_counters);
+    if (h->weights_on) h->weights = (float*)(sp + s.off_weights);
+    if ((e = prefix_prepare(h->pool, h->units * h->pages_per_unit, &h->own_pool)) != cudaSuccess) return cuda_fail(h, e, "tensor map of the pool");
 
     // Slots past n are read (and masked) by the decode kernel's last page: they must hold finite values.
     e = cudaMemsetAsync(h->pool, 0, s.kv, h->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(h->counters, 0, 2 * kChunkCounters * sizeof(int32_t), h->stream);
+    if (e == cudaSuccess && h->weights) e = cudaMemsetAsync(h->weights, 0, s.state - s.off_weights, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "clearing the KV pool");
     e = init_state_launch(geometry(h), h->st, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "state initialisation launch");
@@ -890,6 +952,7 @@ int lazyev_prefill(lazyev_t* h, const void* k, const void* v, int n_tokens) {
     if (n_tokens > h->max_prefill) return fail(h, LAZYEV_ECAPACITY, "prompt of %d tokens exceeds max_prefill = %d", n_tokens, h->max_prefill);
     if (((uintptr_t)k | (uintptr_t)v) & 15) return fail(h, LAZYEV_EINVAL, "k and v must be 16-byte aligned");
     cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, INT_MIN, h->pos_base, h->stream);
+    if (e == cudaSuccess) e = clear_weights(h, 0, n_tokens);
     if (e != cudaSuccess) return cuda_fail(h, e, "prefill kernel launch");
     h->launches += 1;
     h->prefilled = true;
@@ -917,7 +980,9 @@ int lazyev_reset(lazyev_t* h) {
     // Old rows stay in the pool: slots past n are masked, they only have to be finite.  The state arrays
     // are rewritten by the next prompt load and by every append; the device status word is cleared.
     cudaError_t e = cudaMemsetAsync(h->st.status, 0, 64, h->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(h->counters, 0, 2 * kChunkCounters * sizeof(int32_t), h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "clearing the device status word");
+    h->indexed = 0;
     h->prefilled = false;
     h->t = h->n = h->prefill = h->pos_base = 0;
     h->budget_now = h->budget;
@@ -937,6 +1002,7 @@ int lazyev_prefill_observed(lazyev_t* h, const void* q, const void* k, const voi
         return fail(h, LAZYEV_EINVAL, "k and v must be 16-byte aligned, q 4-byte and out 2-byte aligned");
     // rows are loaded with TS = their own time j - (P - 1) <= 0 and MRI = 0
     cudaError_t e = prefill_launch(geometry(h), h->pool, h->st, k, v, n_tokens, 1 - n_tokens, 0, h->stream);
+    if (e == cudaSuccess) e = clear_weights(h, 0, n_tokens);
     if (e != cudaSuccess) return cuda_fail(h, e, "prefill kernel launch");
     h->launches += 1;
     if (h->prompt_mode == LAZYEV_PROMPT_TILED) {
@@ -1140,7 +1206,7 @@ int lazyev_copy_state(lazyev_t* dst, lazyev_t* src) {
     if (dst->shared != src->shared) return fail(dst, LAZYEV_ESTATE, "copy_state needs the same prefix attached to both handles, or to neither");
     if (dst->device != src->device || dst->layers != src->layers || dst->batch != src->batch || dst->q_heads != src->q_heads ||
         dst->kv_heads != src->kv_heads || dst->capacity != src->capacity || dst->budget != src->budget ||
-        dst->window != src->window || dst->n_recent != src->n_recent || dst->n_initial != src->n_initial)
+        dst->window != src->window || dst->n_recent != src->n_recent || dst->n_initial != src->n_initial || dst->weights_on != src->weights_on)
         return fail(dst, LAZYEV_EINVAL, "copy_state needs two handles of the same configuration on the same device");
     const Sizes sz = sizes_of(src);
     cudaEvent_t ready = nullptr;
@@ -1161,6 +1227,7 @@ int lazyev_copy_state(lazyev_t* dst, lazyev_t* src) {
     dst->prefill = src->prefill;
     dst->pos_base = src->pos_base;
     dst->budget_now = src->budget_now;
+    dst->indexed = 0;
     return LAZYEV_OK;
 }
 
@@ -1219,7 +1286,8 @@ int lazyev_append(lazyev_t* h, const lazyev_rows_t* k, const lazyev_rows_t* v, i
     if (n_tokens > h->capacity - h->n)
         return fail(h, LAZYEV_ECAPACITY, "%d tokens after %d exceed the capacity of %d slots per unit", n_tokens, h->n, h->capacity);
     rows_to_pages(h, h->t, &a);
-    const cudaError_t e = rows_launch(a, h->turns, h->num_sms, h->stream);
+    cudaError_t e = rows_launch(a, h->turns, h->num_sms, h->stream);
+    if (e == cudaSuccess) e = clear_weights(h, h->n, n_tokens);
     if (e != cudaSuccess) return cuda_fail(h, e, "append kernel launch");
     h->launches += 1;
     h->prefilled = true;
@@ -1358,6 +1426,268 @@ int lazyev_query_state_layout(const lazyev_t* h, size_t* page_table, size_t* ts_
     return LAZYEV_OK;
 }
 
+int lazyev_query_weights_layout(const lazyev_t* h, size_t* weights) {
+    if (!h || !weights) return LAZYEV_EINVAL;
+    if (!h->weights_on) return LAZYEV_ESTATE;
+    *weights = sizes_of(h).off_weights;
+    return LAZYEV_OK;
+}
+
+// ---- a chunk of tokens ---------------------------------------------------------------------------------
+namespace {
+
+struct ChunkSpace {
+    size_t ml, sums, norms, bytes;         // offsets inside the workspace (the shared items' sums come first)
+};
+
+ChunkSpace chunk_space(const lazyev_t* h, int n_tokens, int weights) {
+    ChunkSpace s;
+    s.ml = chunk_ml_offset(h->num_sms);
+    s.sums = align_up(chunk_sums_bytes(h->num_sms), 256);
+    s.norms = s.sums;
+    if (weights != LAZYEV_WEIGHTS_OFF) s.norms += align_up(weigh_sums_bytes(h->num_sms), 256);
+    s.bytes = s.norms;
+    if (weights != LAZYEV_WEIGHTS_OFF) {
+        const ChunkPlan plan = chunk_plan(h->layers, h->batch, h->kv_heads, h->group, n_tokens, n_tokens, 0, 1, h->num_sms);
+        s.bytes += (size_t)h->units * plan.tiles * 2 * 128 * sizeof(float);
+    }
+    return s;
+}
+
+}  // namespace
+
+int lazyev_query_chunk_workspace(const lazyev_t* h, int n_tokens, int weights, size_t* bytes) {
+    if (!h || !bytes) return LAZYEV_EINVAL;
+    lazyev_t* w = const_cast<lazyev_t*>(h);
+    if (!h->bound) return fail(w, LAZYEV_ESTATE, "query_chunk_workspace before bind");
+    if (n_tokens <= 0 || n_tokens > h->capacity) return fail(w, LAZYEV_EINVAL, "a chunk has 1 to %d tokens", h->capacity);
+    if (weights < LAZYEV_WEIGHTS_OFF || weights > LAZYEV_WEIGHTS_ADD) return fail(w, LAZYEV_EINVAL, "unknown use of the weights %d", weights);
+    *bytes = chunk_space(h, n_tokens, weights).bytes;
+    return LAZYEV_OK;
+}
+
+int lazyev_attend_chunk(lazyev_t* h, const lazyev_rows_t* q, int n_tokens, const lazyev_rows_t* out, int weights, void* workspace) {
+    if (!h) return LAZYEV_EINVAL;
+    int rc = check_device(h, "attend_chunk");
+    if (rc != LAZYEV_OK) return rc;
+    if (weights < LAZYEV_WEIGHTS_OFF || weights > LAZYEV_WEIGHTS_ADD) return fail(h, LAZYEV_EINVAL, "unknown use of the weights %d", weights);
+    if (weights != LAZYEV_WEIGHTS_OFF && !h->weights) return fail(h, LAZYEV_ESTATE, "this handle keeps no weights (lazyev_set_weights)");
+    if (n_tokens <= 0 || n_tokens > h->n) return fail(h, LAZYEV_EINVAL, "a chunk is the last 1 to %d cached tokens, not %d", h->n, n_tokens);
+    ChunkArgs a = {};
+    if ((rc = rows_view(h, "q", q, h->q_heads, n_tokens, false, &a.q)) != LAZYEV_OK) return rc;
+    if ((rc = rows_view(h, "out", out, h->q_heads, n_tokens, true, &a.out)) != LAZYEV_OK) return rc;
+    if (a.q.dtype != kTypeBF16) return fail(h, LAZYEV_EINVAL, "q must be bfloat16");
+    const long long strides[4] = {a.q.stride_layer, a.q.stride_batch, a.q.stride_token, a.q.stride_head};
+    const int extent[4] = {h->layers, h->batch, n_tokens, h->q_heads};
+    for (int i = 0; i < 4; ++i)
+        if (extent[i] > 1 && (strides[i] <= 0 || strides[i] >= (1ll << 38))) return fail(h, LAZYEV_EINVAL, "q: strides must be positive and below 2^38");
+    if (!workspace || ((uintptr_t)workspace & 255)) return fail(h, LAZYEV_EINVAL, "the workspace must be 256-byte aligned");
+    const lazyev_t* pre = h->shared;
+    const ChunkPlan plan = chunk_plan(h->layers, h->batch, h->kv_heads, h->group, h->n, n_tokens, pre ? pre->n : 0, pre ? h->batch / pre->batch : 1, h->num_sms);
+    const WeighPlan wplan = weigh_plan(plan, h->num_sms);
+    if (plan.blocks == 0 || wplan.blocks == 0) return fail(h, LAZYEV_EINVAL, "a chunk of %d tokens over %d is not supported", n_tokens, h->n);
+    PrefixPool q_map;
+    if (!chunk_query_map(plan, a.q, &q_map)) return fail(h, LAZYEV_EINVAL, "q: no tensor map has these strides");
+    const ChunkSpace space = chunk_space(h, n_tokens, weights);
+    uint8_t* ws = (uint8_t*)workspace;
+    a.pool = &h->own_pool;
+    a.prefix_pool = pre ? &h->prefix_pool : nullptr;
+    a.pages = h->pool;
+    a.prefix_pages = pre ? pre->pool : nullptr;
+    a.page_table = h->st.page_table;
+    a.prefix_table = pre ? pre->st.page_table : nullptr;
+    a.pages_per_unit = h->pages_per_unit;
+    a.total_pages = h->units * h->pages_per_unit;
+    a.prefix_pages_per_unit = pre ? pre->pages_per_unit : 0;
+    a.prefix_total_pages = pre ? pre->units * pre->pages_per_unit : 0;
+    a.q_map = &q_map;
+    a.o = (float*)ws;
+    a.ml = (float2*)(ws + space.ml);
+    a.counters = h->counters;
+    a.norms = weights != LAZYEV_WEIGHTS_OFF ? (float*)(ws + space.norms) : nullptr;
+    a.status = h->st.status;
+    a.wait_limit_ns = h->wait_limit_ns;
+    a.stop_after_tiles = h->stop_after_pages;
+    cudaError_t e = chunk_launch(plan, a, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "chunk kernel launch");
+    h->launches += 1;
+    if (weights == LAZYEV_WEIGHTS_OFF) return LAZYEV_OK;
+    WeighArgs w = {};
+    w.pool = &h->own_pool;
+    w.q_map = &q_map;
+    w.page_table = h->st.page_table;
+    w.pages_per_unit = h->pages_per_unit;
+    w.total_pages = a.total_pages;
+    w.capacity = h->capacity;
+    w.norms = a.norms;
+    w.weights = h->weights;
+    w.add = weights == LAZYEV_WEIGHTS_ADD;
+    w.sums = (float*)(ws + space.sums);
+    w.counters = h->counters + kChunkCounters;
+    w.status = h->st.status;
+    w.wait_limit_ns = h->wait_limit_ns;
+    w.stop_after_tiles = h->stop_after_pages;
+    e = weigh_launch(wplan, plan, w, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "weight kernel launch");
+    h->launches += 1;
+    return LAZYEV_OK;
+}
+
+// ---- selected blocks -----------------------------------------------------------------------------------
+namespace {
+
+struct BlockSpace {
+    size_t keys, table, pbar, bytes;       // offsets (the bounds come first)
+};
+
+BlockSpace block_space(const lazyev_t* h) {
+    const size_t pages = (size_t)h->units * h->pages_per_unit;
+    BlockSpace s;
+    s.keys = align_up(pages * 2 * kRowBytes, 256);
+    s.table = s.keys + align_up(pages * sizeof(unsigned long long), 256);
+    s.pbar = s.table + align_up(pages * sizeof(int32_t), 256);
+    s.bytes = s.pbar + align_up((size_t)h->units * h->capacity * sizeof(float), 256);
+    return s;
+}
+
+BlocksArgs blocks_args(const lazyev_t* h) {
+    const BlockSpace s = block_space(h);
+    BlocksArgs a = {};
+    a.geo = geometry(h);
+    a.pool = h->pool;
+    a.page_table = h->st.page_table;
+    a.bounds = h->block_space;
+    a.keys = (unsigned long long*)(h->block_space + s.keys);
+    a.table = (int32_t*)(h->block_space + s.table);
+    a.status = h->st.status;
+    return a;
+}
+
+// Bounds of the blocks from `first` on, as far as they are not there yet.
+int run_index(lazyev_t* h, int first) {
+    const int last = h->n > 0 ? (h->n - 1) / kPageTokens : 0;      // the newest block has none
+    if (first > h->indexed) first = h->indexed;
+    if (first >= last) return LAZYEV_OK;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(h->stream, &capture);
+    if (e == cudaSuccess) e = bounds_launch(blocks_args(h), first, last - first, h->num_sms, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "bounds kernel launch");
+    h->launches += 1;
+    if (capture == cudaStreamCaptureStatusNone) h->indexed = last;  // (a graph makes them whenever it is replayed)
+    return LAZYEV_OK;
+}
+
+}  // namespace
+
+int lazyev_query_block_workspace(const lazyev_t* h, size_t* bytes, size_t* bounds) {
+    if (!h || !bytes) return LAZYEV_EINVAL;
+    *bytes = block_space(h).bytes;
+    if (bounds) *bounds = 0;
+    return LAZYEV_OK;
+}
+
+int lazyev_set_block_workspace(lazyev_t* h, void* workspace) {
+    if (!h) return LAZYEV_EINVAL;
+    if (!h->bound) return fail(h, LAZYEV_ESTATE, "set_block_workspace before bind");
+    if ((uintptr_t)workspace & 255) return fail(h, LAZYEV_EINVAL, "the workspace must be 256-byte aligned");
+    h->block_space = (uint8_t*)workspace;
+    h->indexed = 0;
+    return LAZYEV_OK;
+}
+
+int lazyev_index_blocks(lazyev_t* h, int first_block) {
+    if (!h) return LAZYEV_EINVAL;
+    const int rc = check_device(h, "index_blocks");
+    if (rc != LAZYEV_OK) return rc;
+    if (!h->block_space) return fail(h, LAZYEV_ESTATE, "no block workspace (lazyev_set_block_workspace)");
+    if (first_block < 0) return fail(h, LAZYEV_EINVAL, "blocks are counted from 0");
+    return run_index(h, first_block);
+}
+
+int lazyev_attend_sparse(lazyev_t* h, const void* q, int blocks, void* out, int32_t* selected) {
+    if (!h) return LAZYEV_EINVAL;
+    int rc = check_device(h, "attend_sparse");
+    if (rc != LAZYEV_OK) return rc;
+    if (!q || !out || blocks <= 0) return fail(h, LAZYEV_EINVAL, "null pointer or non-positive number of blocks");
+    if (((uintptr_t)q & 15) || ((uintptr_t)out & 1) || ((uintptr_t)selected & 3))
+        return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned, out 2-byte and selected 4-byte aligned");
+    if (!h->block_space) return fail(h, LAZYEV_ESTATE, "no block workspace (lazyev_set_block_workspace)");
+    if (!h->prefilled || h->n == 0) return fail(h, LAZYEV_ESTATE, "attend_sparse with no own token cached");
+    if ((rc = run_index(h, h->indexed)) != LAZYEV_OK) return rc;
+    const int last = (h->n - 1) / kPageTokens, picked = blocks - 1 < last ? blocks - 1 : last;
+    BlocksArgs a = blocks_args(h);
+    a.q = q;
+    a.selected = selected;
+    const cudaError_t e = pick_launch(a, last, picked, blocks, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "block selection launch");
+    h->launches += picked > 0 && picked < last ? 2 : 1;
+    StateView view = h->st;
+    view.page_table = a.table;
+    view.pbar = (float*)(h->block_space + block_space(h).pbar);
+    return run_decode(h, q, out, picked * kPageTokens + h->n - last * kPageTokens, h->t, nullptr, nullptr, false, &view);
+}
+
+int lazyev_evict_to(lazyev_t* h, int keep, lazyev_t* dst, int* evicted) {
+    if (!h) return LAZYEV_EINVAL;
+    if (evicted) *evicted = 0;
+    int rc = check_device(h, "evict_to");
+    if (rc != LAZYEV_OK) return rc;
+    if (!h->prefilled || h->n == 0) return fail(h, LAZYEV_ESTATE, "evict_to before prefill");
+    if (keep <= h->n_recent + h->n_initial || keep > h->budget)
+        return fail(h, LAZYEV_EINVAL, "keep must be in (n_recent + n_initial, budget]");
+    const bool all = h->n <= keep;
+    if (!all && candidates_of(h, h->n) < 0)
+        return fail(h, LAZYEV_EINVAL, "eviction over %d candidates is not supported", h->n - h->n_recent - h->n_initial);
+    if (!dst || dst == h) {
+        if (h->users > 0) return fail(h, LAZYEV_ESTATE, "evict_to on a handle that others share as their prefix");
+        return all ? LAZYEV_OK : run_cut(h, keep, evicted, h->src, h->first_moved, h->radix_list);
+    }
+    const int kept = all ? h->n : keep;
+    if (!dst->bound) return fail(h, LAZYEV_ESTATE, "evict_to into a handle that is not bound");
+    if (dst->device != h->device || dst->layers != h->layers || dst->batch != h->batch || dst->q_heads != h->q_heads || dst->kv_heads != h->kv_heads)
+        return fail(h, LAZYEV_EINVAL, "evict_to needs a handle of the same layers, batch, heads and device");
+    if (dst->prefilled) return fail(h, LAZYEV_ESTATE, "evict_to into a handle that already holds a cache (reset it first)");
+    if (dst->shared != h->shared) return fail(h, LAZYEV_ESTATE, "evict_to needs the same prefix attached to both handles, or to neither");
+    if (kept > dst->capacity) return fail(h, LAZYEV_ECAPACITY, "%d tokens exceed the capacity of %d slots per unit", kept, dst->capacity);
+    EvictArgs sel = {};
+    if (!all && (rc = run_select(h, keep, h->src, h->first_moved, h->radix_list, &sel)) != LAZYEV_OK) return rc;
+    KeepArgs a = {};
+    a.from_geo = geometry(h);
+    a.to_geo = geometry(dst);
+    a.from = h->st;
+    a.to = dst->st;
+    a.from_pool = h->pool;
+    a.to_pool = dst->pool;
+    a.from_weights = h->weights;
+    a.to_weights = dst->weights;
+    a.src = all ? nullptr : h->src;
+    a.keep = kept;
+    a.n = h->n;
+    cudaEvent_t ready = nullptr;
+    cudaError_t e = cudaSuccess;
+    if (dst->stream != h->stream) {          // (as in copy_state: the rows move on dst's stream, and h's later work waits for that)
+        e = cudaEventCreateWithFlags(&ready, cudaEventDisableTiming);
+        if (e == cudaSuccess) e = cudaEventRecord(ready, h->stream);
+        if (e == cudaSuccess) e = cudaStreamWaitEvent(dst->stream, ready, 0);
+    }
+    if (e == cudaSuccess) e = keep_launch(a, dst->stream);
+    if (dst->stream != h->stream) {
+        if (e == cudaSuccess) e = cudaEventRecord(ready, dst->stream);
+        if (e == cudaSuccess) e = cudaStreamWaitEvent(h->stream, ready, 0);
+        if (ready) cudaEventDestroy(ready);
+    }
+    if (e != cudaSuccess) return cuda_fail(h, e, "evict_to");
+    dst->launches += 1;
+    dst->prefilled = true;
+    dst->t = h->t;
+    dst->n = kept;
+    dst->prefill = h->prefill;
+    dst->pos_base = h->pos_base;
+    dst->indexed = 0;
+    if (evicted) *evicted = h->n - kept;
+    return LAZYEV_OK;
+}
+
 int lazyev_evict(lazyev_t* h, int* evicted) {
     if (!h) return LAZYEV_EINVAL;
     if (!h->prefilled) return fail(h, LAZYEV_ESTATE, "evict before prefill");
@@ -1481,7 +1811,9 @@ int lazyev_dump_state(lazyev_t* h, lazyev_dump_t* d) {
         const Geometry geo = geometry(h);
         for (int u0 = 0; u0 < d->unit_count; u0 += kScoreStageUnits) {
             const int cnt = d->unit_count - u0 < kScoreStageUnits ? d->unit_count - u0 : kScoreStageUnits;
-            e = score_launch(geo, h->st, d->unit_begin + u0, cnt, h->n, h->t, h->score_mode, h->stage_score, h->stream);
+            e = h->score_mode == LAZYEV_SCORE_WEIGHT
+                    ? weights_score_launch(geo, h->weights, d->unit_begin + u0, cnt, h->n, h->stage_score, h->stream)
+                    : score_launch(geo, h->st, d->unit_begin + u0, cnt, h->n, h->t, h->score_mode, h->stage_score, h->stream);
             if (e == cudaSuccess)
                 e = cudaMemcpyAsync(d->score + (size_t)u0 * cap, h->stage_score, (size_t)cnt * cap * sizeof(double), cudaMemcpyDeviceToHost, h->stream);
             if (e == cudaSuccess) e = cudaStreamSynchronize(h->stream);
@@ -1540,6 +1872,16 @@ int lazyev_load_state(lazyev_t* h, const lazyev_dump_t* d, int prefill) {
         e = cudaMemcpy2DAsync(h->st.tsm, (size_t)h->capacity * 8, pairs.data(), (size_t)d->n * 8, (size_t)d->n * 8, h->units,
                               cudaMemcpyHostToDevice, h->stream);
     if (e == cudaSuccess && d->pbar) e = cudaMemcpy2DAsync(h->st.pbar, (size_t)h->capacity * 4, d->pbar, scap * 4, width, h->units, cudaMemcpyHostToDevice, h->stream);
+    std::vector<float> weights;
+    if (h->weights && h->score_mode == LAZYEV_SCORE_WEIGHT && d->score) {
+        weights.resize((size_t)h->units * d->n);
+        for (int u = 0; u < h->units; ++u)
+            for (int i = 0; i < d->n; ++i) weights[(size_t)u * d->n + i] = (float)d->score[(size_t)u * scap + i];
+        if (e == cudaSuccess)
+            e = cudaMemcpy2DAsync(h->weights, (size_t)h->capacity * 4, weights.data(), width, width, h->units, cudaMemcpyHostToDevice, h->stream);
+    } else if (e == cudaSuccess) {
+        e = clear_weights(h, 0, d->n);
+    }
     if (e != cudaSuccess) return cuda_fail(h, e, "state upload");
     // K / V rows: swizzled into pages on the host, one page per copy
     const int np = (d->n + kPageTokens - 1) / kPageTokens;
@@ -1569,6 +1911,7 @@ int lazyev_load_state(lazyev_t* h, const lazyev_dump_t* d, int prefill) {
     h->prefill = prefill;
     h->n = d->n;
     h->t = d->t;
+    h->indexed = 0;
     return LAZYEV_OK;
 }
 

@@ -5,6 +5,8 @@
 
 namespace lzk {
 
+constexpr int kTypeBF16 = 0, kTypeF16 = 1, kTypeF32 = 2;      // LAZYEV_BF16 ...
+
 // ---- attention over a shared prefix ------------------------------------------------------------------
 // How the prefix kernel's work is laid out.
 struct PrefixPlan {
@@ -59,6 +61,90 @@ cudaError_t prefix_clear_launch(const PrefixPlan& plan, float2* ml, cudaStream_t
 cudaError_t prefix_launch(const PrefixPlan& plan, const PrefixArgs& a, cudaStream_t stream);
 // Zeroes the slots behind the last token in every unit's last page.
 cudaError_t clear_tail_launch(const Geometry& geo, uint8_t* pool, StateView st, int n, cudaStream_t stream);
+
+// ---- attention of a chunk of tokens ------------------------------------------------------------------
+// How the chunk kernel's work is laid out: an item is a unit with two of its row tiles (the odd last one alone), a step one key
+// tile of an item.
+struct ChunkPlan {
+    int layers, batch, kv_heads, group;
+    int tokens, context;                // of the chunk; own tokens before it
+    int tile_tokens, tiles, pairs;      // tokens per row tile, row tiles per unit, items per unit
+    int prefix_n, prefix_tiles, prefix_share;   // of an attached prefix: tokens, key tiles, sequences per prefix sequence
+    int unit_steps;                     // steps of a unit's items together
+    int blocks, per, extra;             // contiguous parts of the walk, as in PrefixPlan
+};
+constexpr int kChunkMaxBlocks = 256;
+constexpr int kChunkCounters = kChunkMaxBlocks * 8;    // per block, stream and quarter of a row tile: who has written a shared item's sums
+
+__host__ __device__ __forceinline__ int chunk_key_tiles(const ChunkPlan& p, int pair) {
+    const int last = 2 * p.tile_tokens * (pair + 1);   // (a pair's tokens never see further than the chunk's end)
+    return p.prefix_tiles + (p.context + (last < p.tokens ? last : p.tokens) + 127) / 128;
+}
+
+struct RowView {           // head rows of 128 contiguous elements; strides in elements
+    const void* data;      // null: no rows of this kind
+    long long stride_layer, stride_batch, stride_token, stride_head;
+    int dtype;
+};
+
+struct ChunkArgs {
+    const PrefixPool* pool;             // the own pages as the kernel addresses them, and the prefix's
+    const PrefixPool* prefix_pool;
+    const uint8_t* pages;
+    const uint8_t* prefix_pages;
+    const int32_t* page_table;
+    const int32_t* prefix_table;
+    int pages_per_unit, total_pages, prefix_pages_per_unit, prefix_total_pages;
+    RowView q, out;                     // q bf16
+    const PrefixPool* q_map;            // of chunk_query_map()
+    float* o;                           // sums of items that several blocks share (chunk_workspace_bytes)
+    float2* ml;
+    int32_t* counters;                  // [kChunkCounters], zero
+    float* norms;                       // [units][tiles][2][128]: a row's reference and 1 / its sum of exp2(x - reference), or null
+    int32_t* status;
+    unsigned long long wait_limit_ns;
+    int stop_after_tiles;
+};
+// blocks = 0: more steps than an int counts.
+ChunkPlan chunk_plan(int layers, int batch, int kv_heads, int group, int n, int tokens, int prefix_n, int prefix_share, int num_sms);
+size_t chunk_sums_bytes(int num_sms);                  // o, then ml
+size_t chunk_ml_offset(int num_sms);
+cudaError_t chunk_prepare();
+// The queries as the kernels address them; false: strides that a tensor map cannot have.
+bool chunk_query_map(const ChunkPlan& plan, const RowView& q, PrefixPool* out);
+cudaError_t chunk_launch(const ChunkPlan& plan, const ChunkArgs& a, cudaStream_t stream);
+
+// ---- the weights that tokens receive -------------------------------------------------------------------
+// An item is a unit with a pair of 128-key tiles, a step one row tile of the chunk that sees it.
+struct WeighPlan {
+    int pairs, unit_steps;
+    int blocks, per, extra;
+};
+// First row tile with a token that sees the first key of pair `pair`.
+__host__ __device__ __forceinline__ int weigh_first_tile(const ChunkPlan& p, int pair) {
+    const int behind = 256 * pair - p.context;             // tokens of the chunk before that key
+    return behind > 0 ? behind / p.tile_tokens : 0;
+}
+struct WeighArgs {
+    const PrefixPool* pool;
+    const PrefixPool* q_map;
+    const int32_t* page_table;
+    int pages_per_unit, total_pages, capacity;
+    const float* norms;                 // of the chunk launch before
+    float* weights;                     // [units][capacity]
+    int add;                            // 0: they become this chunk's
+    float* sums;
+    int32_t* counters;                  // [kChunkCounters], zero
+    int32_t* status;
+    unsigned long long wait_limit_ns;
+    int stop_after_tiles;
+};
+WeighPlan weigh_plan(const ChunkPlan& chunk, int num_sms);
+size_t weigh_sums_bytes(int num_sms);
+cudaError_t weigh_prepare();
+cudaError_t weigh_launch(const WeighPlan& plan, const ChunkPlan& chunk, const WeighArgs& a, cudaStream_t stream);
+// A decode step's probabilities onto the weights of its n tokens; the newest one's begin.
+cudaError_t step_weights_launch(const Geometry& geo, float* weights, const float* pbar, int n, cudaStream_t stream);
 
 // ---- decode ------------------------------------------------------------------
 struct DecodeConfig {
@@ -118,14 +204,7 @@ cudaError_t append_launch(const Geometry& geo, uint8_t* pool, StateView st, cons
                           int slot, int t, int position, cudaStream_t stream);
 
 // ---- head rows: norm, rotation, paged append -------------------------------------------------------
-constexpr int kTypeBF16 = 0, kTypeF16 = 1, kTypeF32 = 2;      // LAZYEV_BF16 ...
 constexpr int kMaxPairs = kHeadDim / 2;
-
-struct RowView {           // head rows of 128 contiguous elements; strides in elements
-    const void* data;      // null: no rows of this kind
-    long long stride_layer, stride_batch, stride_token, stride_head;
-    int dtype;
-};
 
 struct RowsArgs {
     RowView q, k, v, q_out, k_out;      // k_out without a pool, v with one; q, k, v of one type, q_out and k_out too
@@ -191,6 +270,41 @@ cudaError_t compact_launch(const Geometry& geo, uint8_t* pool, StateView st, con
 // Eq. (2) for every slot < n of units [unit_begin, unit_begin + unit_count) into out[unit][capacity].
 cudaError_t score_launch(const Geometry& geo, StateView st, int unit_begin, int unit_count, int n, int t,
                          int score_mode, double* out, cudaStream_t stream);
+
+// ---- selection by weight, and into another cache -----------------------------------------------------
+cudaError_t keep_prepare();
+// Like select_launch() with the weights as scores, for any number of candidates.
+cudaError_t weigh_select_launch(const Geometry& geo, StateView st, const float* weights, const EvictArgs& a, cudaStream_t stream);
+cudaError_t compact_weights_launch(const Geometry& geo, float* weights, const EvictArgs& a, cudaStream_t stream);
+cudaError_t weights_score_launch(const Geometry& geo, const float* weights, int unit_begin, int unit_count, int n, double* out, cudaStream_t stream);
+
+struct KeepArgs {
+    Geometry from_geo, to_geo;
+    StateView from, to;
+    const uint8_t* from_pool;
+    uint8_t* to_pool;
+    const float* from_weights;          // null: zeros
+    float* to_weights;                  // null: none kept
+    const int32_t* src;                 // [units][keep]; null: slot j moves to slot j
+    int keep, n;
+};
+cudaError_t keep_launch(const KeepArgs& a, cudaStream_t stream);
+
+// ---- selected blocks -------------------------------------------------------------------------------------
+struct BlocksArgs {
+    Geometry geo;
+    const uint8_t* pool;
+    const int32_t* page_table;
+    void* bounds;                       // [units][pages_per_unit][2 (high, low)][128] bf16
+    unsigned long long* keys;           // [units][pages_per_unit]
+    const void* q;
+    int32_t* table;                     // [units][pages_per_unit]: the selected pages, in order
+    int32_t* selected;                  // [units][asked] block numbers, -1 behind the last; or null
+    int32_t* status;
+};
+cudaError_t bounds_launch(const BlocksArgs& a, int first, int count, int num_sms, cudaStream_t stream);
+// Of the first `count` blocks the `picked` best, and the one behind them.
+cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, cudaStream_t stream);
 
 // hist[b] (b < bins - 1) = cached tokens of the unit range with MRI = b; hist[bins - 1] = the rest.
 cudaError_t mri_histogram_launch(const Geometry& geo, StateView st, int unit_begin, int unit_count, int n, int bins,

@@ -97,12 +97,6 @@ __device__ __forceinline__ Piece piece_at(const PrefixPlan& pl, int x, int end) 
     return pc;
 }
 
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
-                 "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-                 : "memory");
-}
-
 // 64 columns of the accumulator times a factor per row.
 __device__ __noinline__ void rescale(uint32_t cols, float f) {
 #pragma unroll 1
@@ -117,30 +111,6 @@ __device__ __noinline__ void rescale(uint32_t cols, float f) {
     }
     tmem_wait_st();
 }
-
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
-}
-
-// A unit's page numbers, 32 at a time in the lanes of a warp.
-struct PageList {
-    const int32_t* table;
-    int last, first;                               // last page of the unit; first page of those in the lanes
-    int32_t entry;
-    __device__ __forceinline__ void open(const int32_t* t, int last_page, int page) {
-        table = t;
-        last = last_page;
-        first = page;
-    }
-    __device__ __forceinline__ void fetch(int page) {
-        first = page;
-        entry = table[min(page + (int)(threadIdx.x & 31), last)];
-    }
-    __device__ __forceinline__ int32_t at(int page) {      // pages are asked for in ascending order
-        if (page >= first + 32) fetch(page);
-        return __shfl_sync(0xffffffffu, entry, page - first);
-    }
-};
 
 __global__ void __launch_bounds__(kThreads, 1)
 prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ PrefixParams p) {

@@ -33,6 +33,14 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* m
         : "memory");
 }
 
+__device__ __forceinline__ void tma_load_5d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, int w, int v, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+            smem_u32(smem_dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(smem_u32(bar))
+        : "memory");
+}
+
 // Tile store shared -> global through a tensor map (rows outside the tensor are dropped).
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, int x, int y, int z, int w, const void* smem_src) {
     asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(
@@ -76,6 +84,12 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
         "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
         : "memory");
+}
+
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
+                 "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
 }
 
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
@@ -207,6 +221,30 @@ struct Ring {
     uint32_t count = 0;
     __device__ __forceinline__ uint32_t stage(uint32_t n) const { return count % n; }
     __device__ __forceinline__ uint32_t parity(uint32_t n) const { return (count / n) & 1u; }
+};
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+
+// A unit's page numbers, 32 at a time in the lanes of a warp.
+struct PageList {
+    const int32_t* table;
+    int last, first;                               // last page of the unit; first page of those in the lanes
+    int32_t entry;
+    __device__ __forceinline__ void open(const int32_t* t, int last_page, int page) {
+        table = t;
+        last = last_page;
+        first = page;
+    }
+    __device__ __forceinline__ void fetch(int page) {
+        first = page;
+        entry = table[min(page + (int)(threadIdx.x & 31), last)];
+    }
+    __device__ __forceinline__ int32_t at(int page) {      // pages are asked for in ascending order
+        if (page >= first + 32) fetch(page);
+        return __shfl_sync(0xffffffffu, entry, page - first);
+    }
 };
 
 // ---- tensor maps (host) -------------------------------------------------------------------------

@@ -1,0 +1,460 @@
+// The weight that every cached token receives from a chunk of query rows, and the running sum of a decode step's.
+//
+// For own token j of a unit, over the T tokens of the chunk and the G heads of its KV head:
+//   weight[j] (+)= 1 / G sum over rows r that see j of exp2(x_r[j] - m_r) / l_r
+// with the logits x and the rows' references m and sums l as in chunk.cu, which leaves the last two in memory.  A row's sum is
+// known only after all its keys, hence a second pass over the logits, but no second product: keys are the accumulator rows here
+// (S = K Q^T), so a key's sum over the query rows stays in two threads' registers, in fp32 throughout, and is written once.
+//
+// An item is a pair of 128-key tiles of a unit, a stream each, with the row tiles of the chunk that see it; the walk over (item, row
+// tile) is cut into equal contiguous parts, one per persistent block, as in chunk.cu; sums of an item that several blocks share go
+// through memory and the last of them to arrive adds them up in order.  Three key tiles and the row tiles of three steps are in
+// shared memory, and each stream has two logit tiles in tensor memory, so that the tensor core runs ahead of the exponentials.
+//
+// Bound by the exponentials, one per row and key (the tensor core needs half their time); few rows: HBM, the keys once.
+//
+// Warp roles: warps 0-15 exponentials, warp 16 TMA producer, warp 17 MMA issuer.  All mbarrier waits are bounded.
+#include <string.h>
+
+#include "internal.h"
+#include "tensor.cuh"
+
+namespace lzk {
+
+namespace {
+
+constexpr int kTile = 128;                         // keys of a key tile, rows of a row tile
+constexpr int kBoxBytes = kTile * 128;             // half an operand: 128 rows x 64 bf16
+constexpr int kOperandBytes = 2 * kBoxBytes;
+constexpr int kRing = 3;                           // row tiles in flight
+constexpr int kStreamWarps = 8;                    // two warps per 32 keys, half of the rows each
+constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 1);
+
+constexpr int kKeys = 3;                           // key tiles in flight
+constexpr int kOffK = 0;
+constexpr int kOffRing = kOffK + kKeys * kOperandBytes;
+constexpr int kOffNorms = kOffRing + kRing * kOperandBytes;     // [kRing][2][128]
+constexpr int kNormBytes = 2 * kTile * 4;
+constexpr int kSmem = kOffNorms + kRing * kNormBytes;
+constexpr uint32_t kTmemCols = 512;                // [stream][2 buffers][128]
+
+struct Bars {
+    uint64_t k_full[kKeys], k_empty[kKeys];
+    uint64_t full[kRing], empty[kRing];
+    uint64_t s_full[2][2], s_empty[2][2];          // [stream][buffer]
+    uint64_t drain;
+};
+
+struct WeighParams {
+    WeighPlan plan;
+    ChunkPlan chunk;
+    const int32_t* page_table;
+    const float* norms;
+    float* weights;
+    float* sums;                                   // [2 blocks][2 streams][128]
+    int32_t* counters;
+    int32_t* status;
+    int pages_per_unit, total_pages, capacity, add;
+    float scale_log2, inv_group;
+    unsigned long long wait_limit_ns;
+    int stop_after_tiles;
+};
+
+__device__ __forceinline__ int part_begin(const WeighPlan& p, int block) { return block * p.per + min(block, p.extra); }
+__device__ __forceinline__ int block_of(const WeighPlan& p, int x) {
+    const int longer = p.extra * (p.per + 1);
+    return x < longer ? x / (p.per + 1) : p.extra + (x - longer) / p.per;
+}
+
+// One block's part of an item: row tiles [q0, q1) of first .. tiles.
+struct Piece {
+    int unit, pair, start;                         // the item, and the step it starts at
+    int first, q0, q1, tiles;
+};
+
+struct Walk {
+    int x, end, unit, pair, start;
+    __device__ __forceinline__ int steps(const WeighParams& p) const { return p.chunk.tiles - weigh_first_tile(p.chunk, pair); }
+    __device__ __forceinline__ void begin(const WeighParams& p, int block) {
+        const WeighPlan& pl = p.plan;
+        x = part_begin(pl, block);
+        end = part_begin(pl, block + 1);
+        unit = x / pl.unit_steps;
+        start = unit * pl.unit_steps;
+        // items before the chunk's first token all take every row tile
+        pair = min((x - start) / p.chunk.tiles, min(p.chunk.context / (2 * kTile), pl.pairs - 1));
+        start += pair * p.chunk.tiles;
+        for (int n = steps(p); x - start >= n; n = steps(p)) {
+            start += n;
+            ++pair;
+        }
+    }
+    __device__ __forceinline__ bool more() const { return x < end; }
+    __device__ __forceinline__ Piece next(const WeighParams& p) {
+        Piece pc;
+        pc.unit = unit;
+        pc.pair = pair;
+        pc.start = start;
+        pc.tiles = p.chunk.tiles;
+        pc.first = weigh_first_tile(p.chunk, pair);
+        pc.q0 = pc.first + (x - start);
+        pc.q1 = min(pc.tiles, pc.q0 + (end - x));
+        x += pc.q1 - pc.q0;
+        if (pc.q1 == pc.tiles) {
+            start += pc.tiles - pc.first;
+            if (++pair == p.plan.pairs) {
+                pair = 0;
+                ++unit;
+            }
+        }
+        return pc;
+    }
+};
+
+__global__ void __launch_bounds__(kThreads, 1)
+weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ WeighParams p) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ Bars bars;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word, last_flag[2][4];
+    __shared__ float halves[2][kTile];
+    volatile int* abort_flag = &abort_word;
+    const ChunkPlan& ch = p.chunk;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    Walk walk;
+    walk.begin(p, blockIdx.x);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kKeys; ++i) {
+            mbar_init(&bars.k_full[i], 1);
+            mbar_init(&bars.k_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(&bars.s_full[i][b], 1);
+                mbar_init(&bars.s_empty[i][b], kStreamWarps);
+            }
+        }
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&bars.full[i], 1);
+            mbar_init(&bars.empty[i], 1 + 2 * kStreamWarps);       // the products, and everyone who reads the norms
+        }
+        mbar_init(&bars.drain, 1);
+        abort_word = 0;
+        fence_barrier_init();
+    }
+    if (warp == kProducer && lane == 0) {
+        prefetch_map(&map_q);
+        prefetch_map(&map_kv);
+    }
+    // rows of a row tile that no query row ever fills: zeros
+    for (int i = threadIdx.x; i < kRing * kOperandBytes / 16; i += kThreads)
+        reinterpret_cast<uint4*>(smem + kOffRing)[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async();
+    if (warp == 0) {
+        tmem_alloc(&tmem_slot, kTmemCols);
+        tmem_relinquish_alloc_permit();
+    }
+    tmem_fence_before_sync();
+    __syncthreads();
+    tmem_fence_after_sync();
+    const uint32_t tmem_base = tmem_slot;
+    const unsigned long long limit = p.wait_limit_ns;
+
+    if (warp == kProducer) {
+        // ------------------------------------------------------------------ TMA producer
+        Ring rr, kr;
+        bool ok = true;
+        int k_tiles = 0;
+        const uint32_t q_bytes = (uint32_t)(ch.tile_tokens * ch.group) * 256u;
+        auto wait_on = [&](uint64_t* bar, uint32_t parity) { ok = __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag, p.status, limit)); };
+        while (walk.more() && ok) {
+            const Piece pc = walk.next(p);
+            const int head = pc.unit % ch.kv_heads, ls = pc.unit / ch.kv_heads;
+            // diagnostics: no copy beyond the first stop_after_tiles K tiles
+            if (p.stop_after_tiles >= 0 && k_tiles + 2 > p.stop_after_tiles) break;
+            k_tiles += 2;
+            const int last_page = (ch.context + ch.tokens - 1) / kPageTokens;
+            int32_t page = p.page_table[(long long)pc.unit * p.pages_per_unit + min(4 * pc.pair + (lane & 3), last_page)];
+            if (page < 0 || page >= p.total_pages) {
+                atomicOr(p.status, kStatusBadIndex);
+                page = 0;
+            }
+            for (int s = 0; s < 2 && ok; ++s) {            // a stream's tile: two pages, both halves of the rows
+                const uint32_t ks = kr.stage(kKeys);
+                const int32_t p0 = __shfl_sync(0xffffffffu, page, 2 * s), p1 = __shfl_sync(0xffffffffu, page, 2 * s + 1);
+                wait_on(&bars.k_empty[ks], kr.parity(kKeys) ^ 1u);
+                if (!ok) break;
+                uint8_t* dst = smem + kOffK + ks * kOperandBytes;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bars.k_full[ks], kOperandBytes);
+                    tma_load_3d(dst, &map_kv, 0, 0, p0, &bars.k_full[ks]);
+                    tma_load_3d(dst + kBoxBytes / 2, &map_kv, 0, 0, p1, &bars.k_full[ks]);
+                    tma_load_3d(dst + kBoxBytes, &map_kv, 64, 0, p0, &bars.k_full[ks]);
+                    tma_load_3d(dst + kBoxBytes + kBoxBytes / 2, &map_kv, 64, 0, p1, &bars.k_full[ks]);
+                }
+                __syncwarp();
+                ++kr.count;
+            }
+            for (int t = pc.q0; t < pc.q1 && ok; ++t) {
+                const uint32_t st = rr.stage(kRing);
+                wait_on(&bars.empty[st], rr.parity(kRing) ^ 1u);
+                if (!ok) break;
+                if (elect_one()) {
+                    uint8_t* dst = smem + kOffRing + st * kOperandBytes;
+                    mbar_arrive_expect_tx(&bars.full[st], q_bytes + kNormBytes);
+                    tma_load_5d(dst, &map_q, 0, head * ch.group, t * ch.tile_tokens, ls % ch.batch, ls / ch.batch, &bars.full[st]);
+                    tma_load_5d(dst + kBoxBytes, &map_q, 64, head * ch.group, t * ch.tile_tokens, ls % ch.batch, ls / ch.batch, &bars.full[st]);
+                    bulk_load(smem + kOffNorms + st * kNormBytes, p.norms + ((long long)pc.unit * ch.tiles + t) * 2 * kTile, kNormBytes, &bars.full[st]);
+                }
+                __syncwarp();
+                ++rr.count;
+            }
+        }
+        // the copies already issued land before the block exits, whoever gives up and when
+        auto drain = [&](uint64_t* full, const Ring& r, uint32_t n) {
+            const uint32_t last = r.count < n ? r.count : n;
+            for (uint32_t k = r.count - last; k < r.count; ++k)
+                wait_bar(&full[k % n], (k / n) & 1u, abort_flag, p.status, limit, false);
+        };
+        drain(bars.full, rr, kRing);
+        drain(bars.k_full, kr, kKeys);
+    } else if (warp == kIssuer) {
+        // ------------------------------------------------------------------ MMA issuer
+        bool ok = true;
+        auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+            if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, abort_flag, p.status, limit));
+        };
+        Ring rr, kr, sr;
+        const uint64_t k_desc = smem_desc(smem_u32(smem + kOffK), 16, 1024), q_desc = smem_desc(smem_u32(smem + kOffRing), 16, 1024);
+        constexpr uint32_t kStep = kOperandBytes >> 4;
+        while (walk.more() && ok) {
+            const Piece pc = walk.next(p);
+            uint32_t ks[2];
+            for (int s = 0; s < 2; ++s, ++kr.count) {
+                ks[s] = kr.stage(kKeys);
+                wait_on(&bars.k_full[ks[s]], kr.parity(kKeys));
+            }
+            for (int t = pc.q0; t < pc.q1 && ok; ++t) {
+                const uint32_t st = rr.stage(kRing), buf = sr.stage(2);
+                wait_on(&bars.full[st], rr.parity(kRing));
+                for (int s = 0; s < 2; ++s) {
+                    wait_on(&bars.s_empty[s][buf], sr.parity(2) ^ 1u);
+                    tmem_fence_after_sync();
+                    if (ok && elect_one()) {
+                        const uint64_t a = k_desc + ks[s] * kStep, b = q_desc + st * kStep;
+#pragma unroll
+                        for (int s8 = 0; s8 < 8; ++s8) {
+                            const uint32_t off = ((s8 >> 2) * kBoxBytes + (s8 & 3) * 32) >> 4;
+                            umma_bf16(tmem_base + (s * 2 + buf) * 128, a + off, b + off, instr_desc(false), s8 > 0);
+                        }
+                        umma_commit(&bars.s_full[s][buf]);
+                        if (s == 1) umma_commit(&bars.empty[st]);
+                        if (t + 1 == pc.q1) umma_commit(&bars.k_empty[ks[s]]);
+                    }
+                    __syncwarp();
+                }
+                ++rr.count;
+                ++sr.count;
+            }
+        }
+        // every MMA issued is complete before tensor memory goes back
+        if (elect_one()) umma_commit(&bars.drain);
+        __syncwarp();
+        wait_bar(&bars.drain, 0, abort_flag, p.status, limit, false);
+    } else {
+        // ------------------------------------------------------------------ exponentials
+        // Accumulator row = TMEM lane = key; the warps w and w + 4 of a stream share 32 keys and take 64 of the 128 rows each.
+        const int s = warp / kStreamWarps, hf = (warp >> 2) & 1, quarter = warp & 3, row = 32 * quarter + lane;
+        const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16);
+        const int pair_bar = 1 + s * 4 + quarter;
+        bool dead = false;
+        auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+            const bool gave_up = dead || !wait_bar(bar, parity, abort_flag, p.status, limit);
+            dead = __any_sync(0xffffffffu, gave_up);
+        };
+        Ring rr, sr;
+        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
+        const int n = ch.context + ch.tokens;
+        while (walk.more()) {
+            const Piece pc = walk.next(p);
+            const int key0 = (2 * pc.pair + s) * kTile + 32 * quarter;         // of this warp
+            uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
+            float alone = 0.f;                                                 // (rows taken one by one)
+            for (int t = pc.q0; t < pc.q1; ++t) {
+                const uint32_t st = rr.stage(kRing), buf = sr.stage(2);
+                wait_on(&bars.full[st], rr.parity(kRing));                      // (the norms)
+                wait_on(&bars.s_full[s][buf], sr.parity(2));
+                tmem_fence_after_sync();
+                const float* norm = reinterpret_cast<const float*>(smem + kOffNorms + st * kNormBytes) + 64 * hf;
+                const uint32_t cols = lane_base + (s * 2 + buf) * 128 + 64 * hf;
+                const int tok0 = t * ch.tile_tokens, rows = min(ch.tile_tokens, ch.tokens - tok0) * ch.group;
+                // rows [from, rows) see this thread's key; [0, rows) all keys of the warp when the last one lies before the tile
+                const bool all = key0 + 31 <= ch.context + tok0;
+                const int from = (key0 + lane - ch.context - tok0) * ch.group;
+                const bool none = key0 >= n || (key0 - ch.context - tok0) * ch.group >= rows;
+#pragma unroll 1
+                for (int c = 0; c < 64; c += 32) {
+                    const int col = 64 * hf + c;
+                    if (none || col >= rows) break;
+                    float v[32];
+                    tmem_ld32(cols + c, v);
+                    tmem_wait_ld();
+                    // (sums of 32 rows first: short chains of additions)
+                    if (all && col + 32 <= rows) {
+                        uint64_t c0 = pack2(0.f, 0.f), c1 = c0;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 m = *reinterpret_cast<const float4*>(norm + c + i), f = *reinterpret_cast<const float4*>(norm + kTile + c + i);
+                            float e0, e1, e2, e3;
+                            unpack2(fma2(pack2(v[i], v[i + 1]), scale2, pack2(-m.x, -m.y)), e0, e1);
+                            unpack2(fma2(pack2(v[i + 2], v[i + 3]), scale2, pack2(-m.z, -m.w)), e2, e3);
+                            c0 = fma2(pack2(fast_exp2(e0), fast_exp2(e1)), pack2(f.x, f.y), c0);
+                            c1 = fma2(pack2(fast_exp2(e2), fast_exp2(e3)), pack2(f.z, f.w), c1);
+                        }
+                        sum0 = add2(sum0, c0);
+                        sum1 = add2(sum1, c1);
+                    } else {
+                        float some = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float w = fast_exp2(fmaf(v[i], p.scale_log2, -norm[c + i])) * norm[kTile + c + i];
+                            some += col + i >= from && col + i < rows ? w : 0.f;
+                        }
+                        alone += some;
+                    }
+                }
+                tmem_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&bars.s_empty[s][buf]);
+                    mbar_arrive(&bars.empty[st]);
+                }
+                ++rr.count;
+                ++sr.count;
+            }
+            float a0, a1, mine;
+            unpack2(add2(sum0, sum1), a0, a1);
+            mine = a0 + a1 + alone;
+            if (hf) halves[s][row] = mine;
+            named_barrier_sync(pair_bar, 64);
+            const bool whole = pc.q1 - pc.q0 == pc.tiles - pc.first;
+            const int key = key0 + lane;
+            auto put = [&](float sum) {
+                const long long at = (long long)pc.unit * p.capacity + key;
+                if (key < n && in_bounds(key < p.capacity, p.status)) p.weights[at] = (p.add ? p.weights[at] : 0.f) + sum * p.inv_group;
+            };
+            if (!hf) mine += halves[s][row];
+            if (whole) {
+                if (!hf) put(mine);
+            } else if (!hf) {
+                // the last block of the item to come here adds the sums of all, in order
+                auto slot_of = [&](int block, int first_step) {
+                    return ((2 * block + (first_step == part_begin(p.plan, block) ? 0 : 1)) * 2 + s) * kTile + row;
+                };
+                const int first_block = block_of(p.plan, pc.start);
+                const int blocks = block_of(p.plan, pc.start + pc.tiles - pc.first - 1) - first_block + 1;
+                p.sums[slot_of(blockIdx.x, pc.start + pc.q0 - pc.first)] = mine;
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) {
+                    int* counter = p.counters + (first_block * 2 + s) * 4 + quarter;
+                    const bool last = atomicAdd(counter, 1) == blocks - 1;
+                    if (last) *counter = 0;                    // (for the next launch)
+                    last_flag[s][quarter] = last;
+                }
+                __syncwarp();
+                if (last_flag[s][quarter]) {
+                    __threadfence();
+                    float sum = 0.f;
+                    for (int b = 0; b < blocks; ++b) {
+                        const int block = first_block + b;
+                        sum += __ldcg(&p.sums[slot_of(block, b == 0 ? pc.start : part_begin(p.plan, block))]);
+                    }
+                    put(sum);
+                }
+                __syncwarp();
+            }
+            named_barrier_sync(pair_bar, 64);              // (halves may be written again)
+        }
+    }
+
+    tmem_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) {
+        tmem_fence_after_sync();
+        tmem_dealloc(tmem_base, kTmemCols);
+    }
+}
+
+// weights[u][i] += pbar[u][i] for i < n - 1, and the newest token's begins with its own: one thread per four slots.
+__global__ void step_weights_kernel(float* weights, const float* pbar, int units, int capacity, int n) {
+    const long long quads = (long long)units * (capacity / 4);
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < quads; i += (long long)gridDim.x * blockDim.x) {
+        const int slot = (int)(i % (capacity / 4)) * 4;
+        if (slot >= n) continue;
+        float4 w = reinterpret_cast<const float4*>(weights)[i];
+        const float4 add = reinterpret_cast<const float4*>(pbar)[i];
+        w.x = (slot < n - 1 ? w.x : 0.f) + add.x;
+        w.y = (slot + 1 < n - 1 ? w.y : 0.f) + add.y;
+        w.z = (slot + 2 < n - 1 ? w.z : 0.f) + add.z;
+        w.w = (slot + 3 < n - 1 ? w.w : 0.f) + add.w;
+        reinterpret_cast<float4*>(weights)[i] = w;         // (slots behind n: whatever; they begin anew when a token comes)
+    }
+}
+
+}  // namespace
+
+WeighPlan weigh_plan(const ChunkPlan& ch, int num_sms) {
+    WeighPlan pl;
+    pl.pairs = (ch.context + ch.tokens + 2 * kTile - 1) / (2 * kTile);
+    const int before = ch.context / (2 * kTile) < pl.pairs ? ch.context / (2 * kTile) : pl.pairs;
+    long long steps = (long long)before * ch.tiles;
+    for (int j = before; j < pl.pairs; ++j) steps += ch.tiles - weigh_first_tile(ch, j);
+    const long long work = (long long)ch.layers * ch.batch * ch.kv_heads * steps;
+    pl.unit_steps = steps > 0x40000000 ? 0 : (int)steps;
+    if (num_sms > kChunkMaxBlocks) num_sms = kChunkMaxBlocks;
+    pl.blocks = work > 0x40000000 ? 0 : (int)(work < num_sms ? work : num_sms);
+    pl.per = pl.extra = 0;
+    if (pl.blocks == 0) return pl;
+    pl.per = (int)(work / pl.blocks);
+    pl.extra = (int)(work % pl.blocks);
+    return pl;
+}
+
+size_t weigh_sums_bytes(int num_sms) { return (size_t)(num_sms < kChunkMaxBlocks ? num_sms : kChunkMaxBlocks) * 2 * 2 * kTile * sizeof(float); }
+
+cudaError_t weigh_prepare() { return cudaFuncSetAttribute(weigh_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); }
+
+cudaError_t weigh_launch(const WeighPlan& plan, const ChunkPlan& chunk, const WeighArgs& a, cudaStream_t stream) {
+    CUtensorMap mq, mkv;
+    memcpy(&mq, a.q_map, sizeof(mq));
+    memcpy(&mkv, a.pool, sizeof(mkv));
+    WeighParams p;
+    p.plan = plan;
+    p.chunk = chunk;
+    p.page_table = a.page_table;
+    p.norms = a.norms;
+    p.weights = a.weights;
+    p.sums = a.sums;
+    p.counters = a.counters;
+    p.status = a.status;
+    p.pages_per_unit = a.pages_per_unit;
+    p.total_pages = a.total_pages;
+    p.capacity = a.capacity;
+    p.add = a.add;
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)kHeadDim);
+    p.inv_group = 1.f / (float)chunk.group;
+    p.wait_limit_ns = a.wait_limit_ns;
+    p.stop_after_tiles = a.stop_after_tiles;
+    weigh_kernel<<<plan.blocks, kThreads, kSmem, stream>>>(mq, mkv, p);
+    return cudaGetLastError();
+}
+
+cudaError_t step_weights_launch(const Geometry& geo, float* weights, const float* pbar, int n, cudaStream_t stream) {
+    const long long quads = (long long)geo.units * (geo.capacity / 4), blocks = (quads + 255) / 256;
+    step_weights_kernel<<<(unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, stream>>>(weights, pbar, geo.units, geo.capacity, n);
+    return cudaGetLastError();
+}
+
+}  // namespace lzk
