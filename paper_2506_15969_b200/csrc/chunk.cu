@@ -39,6 +39,7 @@ constexpr int kOperandBytes = 2 * kBoxBytes;       // a 128 x 128 bf16 operand (
 constexpr int kRing = 5;                           // K and V tiles in flight, in the order they are used
 constexpr int kStreamWarps = 8;                    // two warps per 32 accumulator rows, half of the columns each
 constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 2);      // an issuer per stream
+constexpr int kLeastSteps = 6;                     // of a block's part
 constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the reference by
 
 constexpr int kOffQ = 0;                           // two row tiles
@@ -94,13 +95,22 @@ struct Piece {
 
 struct Walk {
     int x, end, unit, pair, start;
+    __device__ __forceinline__ void item_done(const ChunkPlan& pl) {
+        start += chunk_item_steps(pl, pair);
+        x = start;
+        if (++pair == pl.pairs) {
+            pair = 0;
+            ++unit;
+        }
+    }
     __device__ __forceinline__ void begin(const ChunkPlan& pl, int block) {
         x = part_begin(pl, block);
         end = part_begin(pl, block + 1);
         unit = x / pl.unit_steps;
         start = unit * pl.unit_steps;
         pair = 0;
-        for (int kt = chunk_key_tiles(pl, 0); x - start >= kt; kt = chunk_key_tiles(pl, ++pair)) start += kt;
+        for (int n = chunk_item_steps(pl, 0); x - start >= n; n = chunk_item_steps(pl, ++pair)) start += n;
+        if (x - start >= chunk_key_tiles(pl, pair)) item_done(pl);     // (behind the item's key tiles)
     }
     __device__ __forceinline__ bool more() const { return x < end; }
     __device__ __forceinline__ Piece next(const ChunkPlan& pl) {
@@ -113,28 +123,20 @@ struct Walk {
         pc.k1 = min(pc.kt, pc.k0 + (end - x));
         pc.both = 2 * pair + 1 < pl.tiles;
         x += pc.tiles();
-        if (pc.k1 == pc.kt) {
-            start += pc.kt;
-            if (++pair == pl.pairs) {
-                pair = 0;
-                ++unit;
-            }
-        }
+        if (pc.k1 == pc.kt) item_done(pl);
         return pc;
     }
 };
 
-// 64 columns of the accumulator times a factor per row.
-__device__ __noinline__ void rescale(uint32_t cols, float f) {
+// 64 columns of the accumulator times a factor per row.  (Few registers at a time, and no call, for which the caller would keep
+// values out of the way in every turn.)
+__device__ __forceinline__ void rescale(uint32_t cols, float f) {
 #pragma unroll 1
-    for (int c = 0; c < 64; c += 16) {
-        float o[16];
-        tmem_ld16(cols + c, o);
+    for (int c = 0; c < 64; c += 4) {
+        float o[4];
+        tmem_ld4(cols + c, o[0], o[1], o[2], o[3]);
         tmem_wait_ld();
-        uint32_t w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * f);
-        tmem_st16(cols + c, w);
+        tmem_st4(cols + c, o[0] * f, o[1] * f, o[2] * f, o[3] * f);
     }
     tmem_wait_st();
 }
@@ -237,31 +239,250 @@ __device__ __forceinline__ void store4(const RowView& out, long long at, int col
         *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(const_cast<void*>(out.data)) + at + col) =
             make_uint2(pack_pair(v.x, v.y, out.dtype), pack_pair(v.z, v.w, out.dtype));
 }
-// Sixteen, from a multiple of 16 on.
-__device__ __forceinline__ void store16(const RowView& out, long long at, int col, const float (&v)[16]) {
-    if (out.dtype == kTypeF32) {
-        float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(const_cast<void*>(out.data)) + at + col);
+// x[c] of lane q is 16-byte chunk c of the q-th row of its quad of lanes; afterwards x[j] of lane q is chunk q of row j.
+__device__ __forceinline__ void turn_quads(uint32_t (&x)[4][4], int lane) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-    } else {
-        uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(const_cast<void*>(out.data)) + at + col);
+    for (int bit = 1; bit < 4; bit <<= 1) {
+        const bool up = lane & bit;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            dst[i] = make_uint4(pack_pair(v[8 * i], v[8 * i + 1], out.dtype), pack_pair(v[8 * i + 2], v[8 * i + 3], out.dtype),
-                                pack_pair(v[8 * i + 4], v[8 * i + 5], out.dtype), pack_pair(v[8 * i + 6], v[8 * i + 7], out.dtype));
+        for (int c = 0; c < 4; ++c) {
+            if (c & bit) continue;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? x[c][w] : x[c | bit][w], bit);
+                (up ? x[c][w] : x[c | bit][w]) = got;
+            }
+        }
     }
 }
 
+__device__ __forceinline__ void sts(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+__device__ __forceinline__ float lds(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+
+// The last of the own keys [from, to) with a value that is not finite, or -1: a whole warp.
+__device__ __noinline__ int last_bad_value(const ChunkParams& p, int unit, int from, int to) {
+    const int lane = threadIdx.x & 31;
+    for (int j = to - 1; j >= from; --j) {
+        int32_t pp = p.page_table[(long long)unit * p.pages_per_unit + j / kPageTokens];
+        if (pp < 0 || pp >= p.total_pages) pp = 0;
+        const uint2 v = *reinterpret_cast<const uint2*>(p.pages + (size_t)pp * kPageBytes + kPageHalfBytes + (j % kPageTokens) * kRowBytes + lane * 8);
+        const bool odd = !finite(bf16_lo_as_float(v.x)) || !finite(bf16_hi_as_float(v.x)) || !finite(bf16_lo_as_float(v.y)) || !finite(bf16_hi_as_float(v.y));
+        if (__any_sync(0xffffffffu, odd)) return j;
+    }
+    return -1;
+}
+
+// Rows (lanes of `again`) that a value reached which they do not see, or see: the first kind again, over their own keys.
+__device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair, int tile, unsigned again, float m, float l, int col0, int cols) {
+    const ChunkPlan& pl = p.plan;
+    const int lane = threadIdx.x & 31, row = 32 * ((threadIdx.x >> 5) & 3) + lane;
+    const int r_tok = row / pl.group, r_head = row - r_tok * pl.group, tok = tile * pl.tile_tokens + r_tok;
+    const UnitAt at = unit_at(pl, unit);
+    const int to = pl.context + min(pl.tokens, 2 * pl.tile_tokens * (pair + 1));       // (behind them there are zeros)
+    const int bad = last_bad_value(p, unit, pl.context + tile * pl.tile_tokens + 1, to);
+    again &= __ballot_sync(0xffffffffu, bad > pl.context + tok);
+    while (again) {
+        const int i = __ffs(again) - 1;
+        again &= again - 1;
+        const int tok_i = __shfl_sync(0xffffffffu, tok, i), head_i = __shfl_sync(0xffffffffu, r_head, i);
+        const float m_i = __shfl_sync(0xffffffffu, m, i), l_i = __shfl_sync(0xffffffffu, l, i);
+        const float4 o = redo_row(p, unit, tok_i, head_i, m_i, l_i);
+        if (4 * lane >= col0 && 4 * lane < col0 + cols)
+            store4(p.out, row_offset(p.out, at, tok_i, at.head * pl.group + head_i), 4 * lane, o);
+    }
+}
+
+// What finish_piece() is told: by value, so that nothing of it is fetched from the parameters there.
+struct Finish {
+    uint8_t* out;                                  // of this thread's row; null: no such row
+    float4* o;                                     // shared sums, slot 0
+    float2* ml;
+    int* counter;                                  // of this tile's quarter
+    float* norm;                                   // of this thread's row, or null
+    int dtype;
+    int blocks, first_block, slot0;                // that share the item (1: whole), and the first one's slot
+    int own_slot;
+    int unit, pair;
+    bool both, two;                                // two row tiles, a stream each; else one, and do both streams have a key tile of it?
+};
+
+// A piece's sums, for the warps of rows that exist: the output of an item that is the block's own, else its share in memory, and from
+// the last block of the item to come here the output of all.  (Not inlined: the loop over the keys needs the registers.)
+__device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, uint32_t tmem_base, const Finish f, float m, float l) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int s = warp / kStreamWarps, hf = (warp >> 2) & 1, quarter = warp & 3, row = 32 * quarter + lane;
+    const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16);
+    float* mine = reinterpret_cast<float*>(smem + kOffExchange) + (s * kTile + row) * 2 + hf;
+    const float* other = reinterpret_cast<const float*>(smem + kOffExchange) + (s * kTile + row) * 2 + (hf ^ 1);
+    const int pair_bar = 1 + s * 4 + quarter, quad_bar = 9 + quarter;
+    const bool whole = f.blocks == 1, speaks = hf == 0 && (f.both || s == 0);      // one thread per row
+    const int half = f.both ? s : 0, bar = f.both ? pair_bar : quad_bar, threads = f.both ? 64 : 128;
+    *mine = l;
+    named_barrier_sync(pair_bar, 64);
+    l += *other;
+    named_barrier_sync(pair_bar, 64);
+    // the columns of this thread's row that are its own from here on: 64, or, of a single row tile, 32
+    int col0 = 64 * hf, cols = 64;
+    float f0 = 1.f, f1 = 0.f;                              // factors of the two streams' accumulators
+    if (!f.both) {
+        // (Each stream's warps have waited for their own accumulator; the barrier passes that on.)
+        *mine = hf ? l : m;
+        tmem_fence_before_sync();
+        named_barrier_sync(quad_bar, 128);
+        tmem_fence_after_sync();
+        const float2* ml = reinterpret_cast<const float2*>(smem + kOffExchange) + row;
+        const float2 a0 = ml[0], a1 = ml[kTile];
+        m = fmaxf(a0.x, a1.x);
+        f0 = a0.x > -INFINITY ? fast_exp2(a0.x - m) : 1.f;
+        f1 = a1.x > -INFINITY ? fast_exp2(a1.x - m) : 1.f;
+        l = a0.y * f0 + a1.y * f1;                         // (a stream without a tile has m = -inf, l = 0)
+        col0 = 64 * s + 32 * hf;
+        cols = 32;
+    }
+    auto own_sums = [&](int c, float (&o)[16]) {           // columns c .. c + 15 of the accumulator
+        if (f.both) {
+            tmem_ld16(lane_base + kColO + s * 128 + c, o);
+            tmem_wait_ld();
+        } else {
+            float o1[16];
+            tmem_ld16(lane_base + kColO + c, o);
+            tmem_ld16(lane_base + kColO + 128 + c, o1);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = o[i] * f0 + (f.two ? o1[i] * f1 : 0.f);
+        }
+    };
+    // Sums in memory, 16 bytes of a row at a time, the rows of a tile side by side: a block has at most two pieces of shared
+    // items, one at either end of its part.
+    auto tile_of = [&](int slot) { return (slot * 2 + half) * kTile; };
+    auto slot_of = [&](int b) { return b == 0 ? f.slot0 : 2 * (f.first_block + b); };
+    bool emits = whole;
+    if (!whole) {
+        if (f.out && speaks) f.ml[tile_of(f.own_slot) + row] = make_float2(m, l);
+        float4* dst = f.o + (long long)tile_of(f.own_slot) * (kHeadDim / 4) + row;
+#pragma unroll 1
+        for (int c = col0; c < col0 + cols; c += 16) {
+            float o[16];
+            own_sums(c, o);
+            if (!f.out) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[(c / 4 + i) * kTile] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        }
+        // the last block of the item to come here joins the sums of all
+        volatile int* last_flag = reinterpret_cast<volatile int*>(smem + kOffMisc + 512 + 8) + half * 4 + quarter;
+        __threadfence();
+        named_barrier_sync(bar, threads);
+        if (speaks && lane == 0) {
+            const bool last = atomicAdd(f.counter, 1) == f.blocks - 1;
+            if (last) *f.counter = 0;                      // (for the next launch)
+            *last_flag = last;
+        }
+        named_barrier_sync(bar, threads);
+        emits = *last_flag != 0;
+        if (emits) {
+            __threadfence();
+            m = -INFINITY;
+            l = 0.f;
+            if (f.out) {
+#pragma unroll 4
+                for (int b = 0; b < f.blocks; ++b) m = fmaxf(m, __ldcg(&f.ml[tile_of(slot_of(b)) + row]).x);
+#pragma unroll 4
+                for (int b = 0; b < f.blocks; ++b) {
+                    const float2 ml = __ldcg(&f.ml[tile_of(slot_of(b)) + row]);
+                    l = fmaf(ml.y, ml.x > -INFINITY ? fast_exp2(ml.x - m) : 1.f, l);
+                }
+            }
+        }
+    }
+    if (emits) {
+        // quads of lanes hand each other's rows round, so that a row's 64 bytes are stored by neighbours
+        uint8_t* out_of[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out_of[j] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(f.out), (lane & ~3) + j));
+        bool sound = true;
+        const float inv = 1.f / l;
+        const bool wide = f.dtype == kTypeF32;
+        const int step = wide ? 16 : 32;                   // columns of a row in 64 bytes
+#pragma unroll 1
+        for (int c = col0; c < col0 + cols; c += step) {
+            uint32_t x[4][4];
+#pragma unroll 1
+            for (int part = 0; part < step; part += 16) {
+                float o[16];
+                if (whole) {
+                    own_sums(c + part, o);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll 2
+                    for (int b = 0; b < f.blocks && f.out; ++b) {
+                        const int from = tile_of(slot_of(b));
+                        const float top = __ldcg(&f.ml[from + row].x);
+                        const float4* src = f.o + (long long)from * (kHeadDim / 4) + row;
+                        float4 v4[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v4[i] = __ldcg(&src[((c + part) / 4 + i) * kTile]);
+                        // (no logit above -inf: sums of zero, or not a number, that count as they are)
+                        const float w = top > -INFINITY ? fast_exp2(top - m) : 1.f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            o[4 * i] = fmaf(v4[i].x, w, o[4 * i]);
+                            o[4 * i + 1] = fmaf(v4[i].y, w, o[4 * i + 1]);
+                            o[4 * i + 2] = fmaf(v4[i].z, w, o[4 * i + 2]);
+                            o[4 * i + 3] = fmaf(v4[i].w, w, o[4 * i + 3]);
+                        }
+                    }
+                }
+                float odd = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    o[i] *= inv;
+                    odd = fmaf(o[i], 0.f, odd);            // (not a number as soon as one of them is not finite)
+                }
+                sound = sound && odd == 0.f;
+                if (wide) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i >> 2][i & 3] = __float_as_uint(o[i]);
+                } else if (part == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i >> 2][i & 3] = pack_pair(o[2 * i], o[2 * i + 1], f.dtype);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[2 + (i >> 2)][i & 3] = pack_pair(o[2 * i], o[2 * i + 1], f.dtype);
+                }
+            }
+            turn_quads(x, lane);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (out_of[j])
+                    *reinterpret_cast<uint4*>(out_of[j] + c * (wide ? 4 : 2) + 16 * (lane & 3)) = make_uint4(x[j][0], x[j][1], x[j][2], x[j][3]);
+        }
+        if (f.norm && speaks) {
+            f.norm[0] = m;
+            f.norm[kTile] = inv;
+        }
+        const unsigned again = __ballot_sync(0xffffffffu, f.out && !sound && finite(l) && finite(m));
+        if (again) redo_rows(*p, f.unit, f.pair, 2 * f.pair + half, again, m, l, col0, cols);
+    }
+    if (!f.both) {
+        tmem_fence_before_sync();
+        named_barrier_sync(quad_bar, 128);                 // all are done with both accumulators and the exchange
+    }
+}
 
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_prefix,
              const __grid_constant__ ChunkParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];
     Bars* bars = reinterpret_cast<Bars*>(smem + kOffMisc);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffMisc + 512);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffMisc + 512);      // then the abort flag, and [2 streams][4 quarters] of finish_piece()
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    volatile int* last_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);      // [2 streams][4 quarters of a row tile]
     const ChunkPlan& pl = p.plan;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Walk walk;
@@ -284,14 +505,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == kProducer && lane == 0) {
-        prefetch_map(&map_q);
-        prefetch_map(&map_kv);
+    // the producer's first page numbers, asked for before everything else
+    KeyPages first_pages;
+    if (warp == kProducer) {
+        if (lane == 0) {
+            prefetch_map(&map_q);
+            prefetch_map(&map_kv);
+        }
+        if (walk.more()) first_pages.open(p, walk.unit, unit_at(pl, walk.unit), walk.x - walk.start);
     }
-    // rows of a row tile that no query row ever fills (128 is no multiple of G): zeros, like all of Q before the first tile
-    for (int i = threadIdx.x; i < 2 * kOperandBytes / 16; i += kThreads)
-        reinterpret_cast<uint4*>(smem + kOffQ)[i] = make_uint4(0u, 0u, 0u, 0u);
-    fence_proxy_async();
+    // (rows of a row tile that no query row fills hold whatever they hold: an accumulator row depends on its own row only)
     if (warp == 0) {
         tmem_alloc(tmem_slot, kTmemCols);
         tmem_relinquish_alloc_permit();
@@ -313,8 +536,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         while (walk.more() && ok) {
             const Piece pc = walk.next(pl);
             const UnitAt at = unit_at(pl, pc.unit);
-            KeyPages k_pages, v_pages;
-            k_pages.open(p, pc.unit, at, pc.k0);
+            KeyPages k_pages = first_pages, v_pages;
+            if (rr.count > 0) k_pages.open(p, pc.unit, at, pc.k0);
             v_pages = k_pages;
             // a K (half = 0) or V (half = 1) tile: 64 rows x 64 elements per box, two pages, both halves of the rows
             auto load_tile = [&](KeyPages& list, int kt, int half) {
@@ -341,10 +564,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 __syncwarp();
                 ++rr.count;
             };
-            for (int s = 0; s < (pc.both ? 2 : 1) && ok; ++s) {
+            const int ahead = pc.both ? 1 : 2, nt = pc.tiles();
+            auto load_k = [&](int j) {
+                // diagnostics: no copy beyond the first stop_after_tiles K tiles
+                if (p.stop_after_tiles >= 0 && k_tiles >= p.stop_after_tiles) ok = false;
+                ++k_tiles;
+                if (ok) load_tile(k_pages, pc.k0 + j, 0);
+            };
+            auto load_q = [&](int s) {
                 const uint32_t qs = qr.stage(2);
                 wait_on(&bars->q_empty[qs], qr.parity(2) ^ 1u);
-                if (!ok) break;
+                if (!ok) return;
                 uint8_t* dst = smem + kOffQ + qs * kOperandBytes;
                 const int tok = (2 * pc.pair + s) * pl.tile_tokens;
                 if (elect_one()) {
@@ -354,15 +584,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 }
                 __syncwarp();
                 ++qr.count;
-            }
-            const int ahead = pc.both ? 1 : 2, nt = pc.tiles();
-            auto load_k = [&](int j) {
-                // diagnostics: no copy beyond the first stop_after_tiles K tiles
-                if (p.stop_after_tiles >= 0 && k_tiles >= p.stop_after_tiles) ok = false;
-                ++k_tiles;
-                if (ok) load_tile(k_pages, pc.k0 + j, 0);
             };
-            for (int j = 0; j < min(ahead, nt) && ok; ++j) load_k(j);
+            // The first keys come before the queries, whose slots are free only when the last logits of the piece before are done; at
+            // the start the queries need no page number.
+            const bool early = rr.count == 0;
+            for (int i = 0; i < 2; ++i) {
+                if ((i == 0) == early)
+                    for (int s = 0; s < (pc.both ? 2 : 1) && ok; ++s) load_q(s);
+                else
+                    for (int j = 0; j < min(ahead, nt) && ok; ++j) load_k(j);
+            }
             for (int j = 0; j < nt && ok; ++j) {
                 load_tile(v_pages, pc.k0 + j, 1);
                 if (ok && j + ahead < nt) load_k(j + ahead);
@@ -496,11 +727,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         // Accumulator row = TMEM lane; the warps w and w + 4 of a stream share 32 rows and take 64 of the 128 columns each (a
         // row's chain of exponentials is what a stream's turn is made of: two threads halve it).
         const int s = warp / kStreamWarps, hf = (warp >> 2) & 1, quarter = warp & 3, row = 32 * quarter + lane;
-        const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16);
-        const uint32_t s_cols = lane_base + kColS + s * 128 + hf * 64, o_cols = lane_base + kColO + s * 128 + hf * 64;
-        float* mine = reinterpret_cast<float*>(smem + kOffExchange) + (s * kTile + row) * 2 + hf;
-        const float* other = reinterpret_cast<const float*>(smem + kOffExchange) + (s * kTile + row) * 2 + (hf ^ 1);
-        const int pair_bar = 1 + s * 4 + quarter, quad_bar = 9 + quarter;      // of the two warps of a row; of the four of both streams
+        const uint32_t s_cols = tmem_base + ((uint32_t)(32 * quarter) << 16) + kColS + s * 128 + hf * 64;     // (O is kColO - kColS further)
+        const uint32_t mine = smem_u32(smem + kOffExchange) + ((s * kTile + row) * 2 + hf) * 4;                 // (the other thread's: ^ 4)
+        const int pair_bar = 1 + s * 4 + quarter;                      // of the two warps of a row (9 + quarter: of the four of both streams)
         uint32_t s_uses = 0, o_uses = 0;
         // A warp whose wait gives up goes on through the same loops, so that its partner's barriers get all their threads, but waits
         // for nothing any more; what it computes means nothing.
@@ -509,90 +738,101 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             const bool gave_up = dead || !wait_bar(bar, parity, abort_flag, p.status, limit);
             dead = __any_sync(0xffffffffu, gave_up);
         };
-        const int r_tok = row / pl.group, r_head = row - r_tok * pl.group;     // token and head of this row inside its tile
+        const int r_tok = row / pl.group;                              // token of this row inside its tile
         while (walk.more()) {
             const Piece pc = walk.next(pl);
             const int nt = pc.stream_tiles(s);
-            const int tile = 2 * pc.pair + (pc.both ? s : 0), tok0 = tile * pl.tile_tokens;
-            const int tok = tok0 + r_tok;
-            const bool valid = r_tok < pl.tile_tokens && tok < pl.tokens;
-            const bool warp_on = __any_sync(0xffffffffu, valid);       // (the same in both warps of the rows)
-            // own keys that this row sees, and that every row of the tile sees
-            const int sees = pl.context + (valid ? tok + 1 : pl.tokens), all_see = pl.context + tok0 + 1;
             float m = -INFINITY, l = 0.f;
-            for (int t = 0; t < nt; ++t) {
-                wait_on(&bars->s_full[s], s_uses & 1u);
-                ++s_uses;
-                tmem_fence_after_sync();
-                if (warp_on) {
-                    float v[2][32];
-                    tmem_ld32(s_cols, v[0]);
-                    tmem_ld32(s_cols + 32, v[1]);
-                    tmem_wait_ld();
-                    const int kt = pc.key_tile(s, t);
-                    const bool own = kt >= pl.prefix_tiles;
-                    const int key0 = (own ? kt - pl.prefix_tiles : kt) * kTile + hf * 64;
-                    if (key0 + 64 > (own ? all_see : pl.prefix_n)) {
-                        const int to = (own ? sees : pl.prefix_n) - key0;
+            bool warp_on;
+            {
+                const int tok0 = (2 * pc.pair + (pc.both ? s : 0)) * pl.tile_tokens, tok = tok0 + r_tok;
+                const bool valid = r_tok < pl.tile_tokens && tok < pl.tokens;
+                warp_on = __any_sync(0xffffffffu, valid);              // (the same in both warps of the rows)
+                const float margin = valid ? kRaiseMargin : INFINITY;  // (a row that does not exist raises nothing)
+                // keys before the first one of a tile's half, and own keys that this row sees, and that every row of the tile sees; of
+                // the prefix's tiles all rows see the same
+                int key0 = pc.key_tile(s, 0) * kTile + hf * 64 - pl.prefix_tiles * kTile;
+                const int sees = pl.context + (valid ? tok + 1 : pl.tokens), all_see = pl.context + tok0 + 1;
+                for (int t = 0; t < nt; ++t, key0 += pc.both ? kTile : 2 * kTile) {
+                    wait_on(&bars->s_full[s], s_uses & 1u);
+                    ++s_uses;
+                    tmem_fence_after_sync();
+                    if (warp_on) {
+                        const int all_to = key0 < 0 ? pl.prefix_n - pl.prefix_tiles * kTile - key0 : all_see - key0;
+                        const int to = key0 < 0 ? all_to : sees - key0;        // this row sees the first `to` of the 64 keys
+                        auto load = [&](int c, float (&v)[32]) {               // 32 logits, masked
+                            tmem_ld32(s_cols + c, v);
+                            tmem_wait_ld();
+                            if (all_to < c + 32) {
 #pragma unroll
-                        for (int c = 0; c < 2; ++c)
+                                for (int i = 0; i < 32; ++i) v[i] = c + i < to ? v[i] : -INFINITY;
+                            }
+                        };
+                        auto top_of = [](const float (&v)[32]) {
+                            float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[c][i] = 32 * c + i < to ? v[c][i] : -INFINITY;
-                    }
-                    float mx[4] = {v[0][0], v[0][1], v[1][0], v[1][1]};
-#pragma unroll
-                    for (int i = 2; i < 32; i += 2) {
-                        mx[(i >> 1) & 1] = fmax3(mx[(i >> 1) & 1], v[0][i], v[0][i + 1]);
-                        mx[2 + ((i >> 1) & 1)] = fmax3(mx[2 + ((i >> 1) & 1)], v[1][i], v[1][i + 1]);
-                    }
-                    // the row's maximum over both halves; both threads of the row take the same decisions from here on
-                    *mine = fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
-                    named_barrier_sync(pair_bar, 64);
-                    const float top = fmaxf(*mine, *other) * p.scale_log2;
-                    if (__any_sync(0xffffffffu, top > m + kRaiseMargin && valid)) {
-                        const float to = fmaxf(m, top);
-                        const float f = m == to ? 1.f : fast_exp2(m - to);
-                        if (t > 0) rescale(o_cols, f);
-                        l *= f;
-                        m = to;
-                    }
-                    const float ref = m == -INFINITY ? 0.f : m;      // every logit -inf: all weights are zero
-                    const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), minus2 = pack2(-ref, -ref);
-                    uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {                      // 16 columns at a time
-                        if (c == 2) {                                  // the first half of P is there: its product may begin
-                            tmem_wait_st();
-                            tmem_fence_before_sync();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&bars->p_full[s][0]);
+                            for (int i = 4; i < 32; i += 4) {
+                                mx[0] = fmax3(mx[0], v[i], v[i + 1]);
+                                mx[1] = fmax3(mx[1], v[i + 2], v[i + 3]);
+                            }
+                            return fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
+                        };
+                        // The second half of the logits is read twice, for the maximum and for the weights: 64 of them at once do not
+                        // leave the registers that the rest of the loop needs.
+                        float v[32];
+                        load(32, v);
+                        float top = top_of(v);
+                        load(0, v);
+                        top = fmaxf(top, top_of(v));
+                        // the row's maximum over both halves; both threads of the row take the same decisions from here on
+                        sts(mine, top);
+                        named_barrier_sync(pair_bar, 64);
+                        top = fmaxf(top, lds(mine ^ 4u)) * p.scale_log2;
+                        if (__any_sync(0xffffffffu, top > m + margin)) {
+                            const float next = fmaxf(m, top);
+                            const float f = m == next ? 1.f : fast_exp2(m - next);
+                            if (t > 0) rescale(s_cols + kColO - kColS, f);
+                            l *= f;
+                            m = next;
                         }
-                        uint32_t w16[8];
+                        const float ref = m == -INFINITY ? 0.f : m;      // every logit -inf: all weights are zero
+                        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), minus2 = pack2(-ref, -ref);
+                        uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float x0 = v[c >> 1][16 * (c & 1) + 2 * i], x1 = v[c >> 1][16 * (c & 1) + 2 * i + 1];
-                            float e0, e1;
-                            unpack2(fma2(pack2(x0, x1), scale2, minus2), e0, e1);
-                            e0 = fast_exp2(e0);
-                            e1 = fast_exp2(e1);
-                            w16[i] = pack_bf16(e0, e1);
-                            if (i & 1)
-                                sum1 = add2(sum1, pack2(e0, e1));
-                            else
-                                sum0 = add2(sum0, pack2(e0, e1));
+                        for (int c = 0; c < 4; ++c) {                      // 16 columns at a time
+                            if (c == 2) {                                  // the first half of P is there: its product may begin
+                                tmem_wait_st();
+                                tmem_fence_before_sync();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(&bars->p_full[s][0]);
+                                load(32, v);
+                            }
+                            uint32_t w16[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                float e0, e1;
+                                unpack2(fma2(pack2(v[16 * (c & 1) + 2 * i], v[16 * (c & 1) + 2 * i + 1]), scale2, minus2), e0, e1);
+                                e0 = fast_exp2(e0);
+                                e1 = fast_exp2(e1);
+                                w16[i] = pack_bf16(e0, e1);
+                                if (i & 1)
+                                    sum1 = add2(sum1, pack2(e0, e1));
+                                else
+                                    sum0 = add2(sum0, pack2(e0, e1));
+                            }
+                            tmem_st8(s_cols + 8 * c, w16);                 // two keys per column
                         }
-                        tmem_st8(s_cols + 8 * c, w16);                 // two keys per column
+                        float a0, a1;
+                        unpack2(add2(sum0, sum1), a0, a1);
+                        l += a0 + a1;
+                        tmem_wait_st();
+                    } else if (lane == 0) {
+                        mbar_arrive(&bars->p_full[s][0]);
                     }
-                    float a0, a1;
-                    unpack2(add2(sum0, sum1), a0, a1);
-                    l += a0 + a1;
-                    tmem_wait_st();
-                } else if (lane == 0) {
-                    mbar_arrive(&bars->p_full[s][0]);
+                    tmem_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars->p_full[s][1]);
                 }
-                tmem_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars->p_full[s][1]);
             }
             // ---- the piece's sums
             if (nt > 0) {
@@ -600,146 +840,33 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                 ++o_uses;
             }
             tmem_fence_after_sync();
-            const bool speaks = hf == 0 && (pc.both || s == 0);        // one thread per row
-            auto put_norm = [&](int row_i, float reference, float inv) {
-                float* norm = p.norms + ((long long)pc.unit * pl.tiles + tile) * 2 * kTile + row_i;
-                norm[0] = reference;
-                norm[kTile] = inv;
-            };
             if (warp_on) {
                 const UnitAt at = unit_at(pl, pc.unit);
-                const bool whole = pc.tiles() == pc.kt;
-                const long long out_at = valid ? row_offset(p.out, at, tok, at.head * pl.group + r_head) : 0;
-                // where shared sums of this item go: a block has at most two such pieces, one at either end of its part
-                auto slot_of = [&](int block, int first_step) { return 2 * block + (first_step == part_begin(pl, block) ? 0 : 1); };
-                const int half = pc.both ? s : 0;
-                const long long sums_at = ((long long)(2 * blockIdx.x + (pc.start + pc.k0 == part_begin(pl, blockIdx.x) ? 0 : 1)) * 2 + half) * kTile + row;
-                *mine = l;
-                named_barrier_sync(pair_bar, 64);
-                l += *other;
-                named_barrier_sync(pair_bar, 64);
-                // 16 columns of sums, final or to be joined
-                bool sound = true;
-                auto put = [&](int col, float (&o)[16], float inv) {
-                    if (!valid) return;
-                    if (whole) {
-                        float odd = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            o[i] *= inv;
-                            odd = fmaf(o[i], 0.f, odd);                // (not a number as soon as one of them is not finite)
-                        }
-                        sound = sound && odd == 0.f;
-                        store16(p.out, out_at, col, o);
-                    } else {
-                        float4* dst = reinterpret_cast<float4*>(p.o + sums_at * kHeadDim + col);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                    }
-                };
-                int col0 = 64 * hf, cols = 64;                         // of this thread's row
-                if (pc.both) {
-                    const float inv = 1.f / l;
-#pragma unroll 1
-                    for (int c = 0; c < 64; c += 16) {
-                        float o[16];
-                        tmem_ld16(o_cols + c, o);
-                        tmem_wait_ld();
-                        put(col0 + c, o, inv);
-                    }
-                } else {
-                    // The two streams' sums into one: four threads per row, 32 columns each.  (Each stream's warps have waited for
-                    // their own accumulator; the barrier passes that on.)
-                    *mine = hf ? l : m;
-                    tmem_fence_before_sync();
-                    named_barrier_sync(quad_bar, 128);
-                    tmem_fence_after_sync();
-                    const float2* ml = reinterpret_cast<const float2*>(smem + kOffExchange) + row;
-                    const float2 a0 = ml[0], a1 = ml[kTile];
-                    m = fmaxf(a0.x, a1.x);
-                    const float f0 = a0.x > -INFINITY ? fast_exp2(a0.x - m) : 1.f, f1 = a1.x > -INFINITY ? fast_exp2(a1.x - m) : 1.f;
-                    l = a0.y * f0 + a1.y * f1;                         // (a stream without a tile has m = -inf, l = 0)
-                    const float inv = 1.f / l;
-                    col0 = 64 * s + 32 * hf;
-                    cols = 32;
-#pragma unroll 1
-                    for (int c = 0; c < 32; c += 16) {
-                        float o0[16], o1[16];
-                        tmem_ld16(lane_base + kColO + col0 + c, o0);
-                        tmem_ld16(lane_base + kColO + 128 + col0 + c, o1);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o0[i] = o0[i] * f0 + (pc.tiles() > 1 ? o1[i] * f1 : 0.f);
-                        put(col0 + c, o0, inv);
-                    }
-                    tmem_fence_before_sync();
-                    named_barrier_sync(quad_bar, 128);                 // all are done with both accumulators and the exchange
+                const int tile = 2 * pc.pair + (pc.both ? s : 0), tok = tile * pl.tile_tokens + r_tok, half = pc.both ? s : 0;
+                const bool valid = r_tok < pl.tile_tokens && tok < pl.tokens;
+                Finish f;
+                f.dtype = p.out.dtype;
+                f.out = valid ? reinterpret_cast<uint8_t*>(const_cast<void*>(p.out.data)) +
+                                    row_offset(p.out, at, tok, at.head * pl.group + row - r_tok * pl.group) * (f.dtype == kTypeF32 ? 4 : 2)
+                              : nullptr;
+                f.norm = valid && p.norms ? p.norms + ((long long)pc.unit * pl.tiles + tile) * 2 * kTile + row : nullptr;
+                f.o = reinterpret_cast<float4*>(p.o);
+                f.ml = p.ml;
+                f.unit = pc.unit;
+                f.pair = pc.pair;
+                f.both = pc.both;
+                f.two = pc.tiles() > 1;
+                f.blocks = 1;
+                f.first_block = f.slot0 = f.own_slot = 0;
+                f.counter = nullptr;
+                if (pc.tiles() != pc.kt) {
+                    f.first_block = block_of(pl, pc.start);
+                    f.blocks = block_of(pl, pc.start + pc.kt - 1) - f.first_block + 1;
+                    f.slot0 = 2 * f.first_block + (pc.start == part_begin(pl, f.first_block) ? 0 : 1);
+                    f.own_slot = 2 * (int)blockIdx.x + (pc.start + pc.k0 == part_begin(pl, blockIdx.x) ? 0 : 1);
+                    f.counter = p.counters + (f.first_block * 2 + half) * 4 + quarter;
                 }
-                if (whole) {
-                    if (p.norms && speaks && valid) put_norm(row, m, 1.f / l);
-                    // rows that a value reached which they do not see (or that see one that is not finite)
-                    unsigned again = __ballot_sync(0xffffffffu, valid && !sound && finite(l) && finite(m));
-                    while (again) {
-                        const int i = __ffs(again) - 1;
-                        again &= again - 1;
-                        const int tok_i = __shfl_sync(0xffffffffu, tok, i), head_i = __shfl_sync(0xffffffffu, r_head, i);
-                        const float m_i = __shfl_sync(0xffffffffu, m, i), l_i = __shfl_sync(0xffffffffu, l, i);
-                        const float4 o = redo_row(p, pc.unit, tok_i, head_i, m_i, l_i);
-                        if (4 * lane >= col0 && 4 * lane < col0 + cols)
-                            store4(p.out, row_offset(p.out, at, tok_i, at.head * pl.group + head_i), 4 * lane, o);
-                    }
-                } else {
-                    if (valid && speaks) p.ml[sums_at] = make_float2(m, l);
-                    // the last block of the item to come here joins the sums of all
-                    const int first_block = block_of(pl, pc.start), blocks = block_of(pl, pc.start + pc.kt - 1) - first_block + 1;
-                    const int bar = pc.both ? pair_bar : quad_bar, threads = pc.both ? 64 : 128;
-                    __threadfence();
-                    named_barrier_sync(bar, threads);
-                    if (speaks && lane == 0) {
-                        int* counter = p.counters + (first_block * 2 + half) * 4 + quarter;
-                        const bool last = atomicAdd(counter, 1) == blocks - 1;
-                        if (last) *counter = 0;                        // (for the next launch)
-                        last_flag[half * 4 + quarter] = last;
-                    }
-                    named_barrier_sync(bar, threads);
-                    if (last_flag[half * 4 + quarter]) {
-                        __threadfence();
-                        const int warps = threads / 32, nth = pc.both ? hf : 2 * s + hf;
-                        for (int i = nth; i < 32; i += warps) {        // a row per warp, four columns per lane
-                            const int row_i = 32 * quarter + i, tok_r = row_i / pl.group, tok_i = tok0 + tok_r;
-                            if (tok_r >= pl.tile_tokens || tok_i >= pl.tokens) break;
-                            auto sums_of = [&](int b) {
-                                const int block = first_block + b;
-                                return ((long long)slot_of(block, b == 0 ? pc.start : part_begin(pl, block)) * 2 + half) * kTile + row_i;
-                            };
-                            float top = -INFINITY;
-                            for (int b = lane; b < blocks; b += 32) top = fmaxf(top, __ldcg(&p.ml[sums_of(b)]).x);
-#pragma unroll
-                            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                            float sum = 0.f;
-                            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                            for (int b = 0; b < blocks; ++b) {
-                                const float2 ml = __ldcg(&p.ml[sums_of(b)]);
-                                const float4 part = __ldcg(reinterpret_cast<const float4*>(p.o + sums_of(b) * kHeadDim) + lane);
-                                // (no logit above -inf: sums of zero, or not a number, that count as they are)
-                                const float f = ml.x > -INFINITY ? fast_exp2(ml.x - top) : 1.f;
-                                sum = fmaf(ml.y, f, sum);
-                                o.x = fmaf(part.x, f, o.x);
-                                o.y = fmaf(part.y, f, o.y);
-                                o.z = fmaf(part.z, f, o.z);
-                                o.w = fmaf(part.w, f, o.w);
-                            }
-                            const float inv = 1.f / sum;
-                            o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-                            const int head_i = row_i - tok_r * pl.group;
-                            const bool good = finite(o.x) && finite(o.y) && finite(o.z) && finite(o.w);
-                            if (!__all_sync(0xffffffffu, good) && finite(sum) && finite(top)) o = redo_row(p, pc.unit, tok_i, head_i, top, sum);
-                            store4(p.out, row_offset(p.out, at, tok_i, at.head * pl.group + head_i), 4 * lane, o);
-                            if (p.norms && lane == 0) put_norm(row_i, top, inv);
-                        }
-                    }
-                }
+                finish_piece(&p, smem, tmem_base, f, m, l);
             }
             tmem_fence_before_sync();
         }
@@ -770,11 +897,12 @@ ChunkPlan chunk_plan(int layers, int batch, int kv_heads, int group, int n, int 
     pl.prefix_tiles = (prefix_n + kTile - 1) / kTile;
     pl.prefix_share = prefix_share;
     long long steps = 0;
-    for (int j = 0; j < pl.pairs; ++j) steps += chunk_key_tiles(pl, j);
+    for (int j = 0; j < pl.pairs; ++j) steps += chunk_item_steps(pl, j);
     const long long work = (long long)layers * batch * kv_heads * steps;
     pl.unit_steps = steps > 0x40000000 ? 0 : (int)steps;
     if (num_sms > kChunkMaxBlocks) num_sms = kChunkMaxBlocks;
-    pl.blocks = work > 0x40000000 ? 0 : (int)(work < num_sms ? work : num_sms);
+    const long long useful = (work + kLeastSteps - 1) / kLeastSteps;
+    pl.blocks = work > 0x40000000 ? 0 : (int)(useful < num_sms ? useful : num_sms);
     pl.per = pl.extra = 0;
     if (pl.blocks == 0) return pl;
     pl.per = (int)(work / pl.blocks);

@@ -147,10 +147,7 @@ weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         prefetch_map(&map_q);
         prefetch_map(&map_kv);
     }
-    // rows of a row tile that no query row ever fills: zeros
-    for (int i = threadIdx.x; i < kRing * kOperandBytes / 16; i += kThreads)
-        reinterpret_cast<uint4*>(smem + kOffRing)[i] = make_uint4(0u, 0u, 0u, 0u);
-    fence_proxy_async();
+    // (rows of a row tile that no query row fills hold whatever they hold: their columns are left out)
     if (warp == 0) {
         tmem_alloc(&tmem_slot, kTmemCols);
         tmem_relinquish_alloc_permit();
