@@ -21,7 +21,7 @@
 // row whose logits are finite and whose output is not -- a value inside the chunk, seen by later rows of the same
 // item only, or one that the row sees itself -- is computed again over its own keys alone.
 //
-// Warp roles: warps 0-15 softmax and output, warp 16 TMA producer, warps 17 and 18 MMA issuers, one per stream.  All mbarrier waits are bounded.
+// Warp roles: warps 0-7 softmax and output, warp 8 TMA producer, warps 9 and 10 MMA issuers, one per stream.  All mbarrier waits are bounded.
 #include <string.h>
 
 #include <cuda_fp16.h>
@@ -37,15 +37,16 @@ constexpr int kTile = 128;                         // rows of a row tile, keys o
 constexpr int kBoxBytes = kTile * 128;             // half an operand: 128 rows x 64 bf16
 constexpr int kOperandBytes = 2 * kBoxBytes;       // a 128 x 128 bf16 operand (32 KiB)
 constexpr int kRing = 5;                           // K and V tiles in flight, in the order they are used
-constexpr int kStreamWarps = 8;                    // two warps per 32 accumulator rows, half of the columns each
-constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 2);      // an issuer per stream
+constexpr int kStreamWarps = 4;                    // a thread per accumulator row
+constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 3);      // an issuer per stream; a whole number of warpgroups
 constexpr int kLeastSteps = 6;                     // of a block's part
 constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the reference by
 
 constexpr int kOffQ = 0;                           // two row tiles
 constexpr int kOffRing = kOffQ + 2 * kOperandBytes;
 constexpr int kOffMisc = kOffRing + kRing * kOperandBytes;
-constexpr int kOffExchange = kOffMisc + 1024;      // [2 streams][128 rows][2]: what the two threads of a row tell each other
+constexpr int kOffExchange = kOffMisc + 1024;      // [2 streams][128 rows] (m, l): what the streams' threads of a row tell each other
+constexpr int kOffAside = kOffMisc + 576, kAsideInts = 12;      // per softmax warp
 constexpr int kSmem = kOffExchange + 2048;
 
 constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;     // per stream: 128 columns of S / P, 128 of O
@@ -128,15 +129,16 @@ struct Walk {
     }
 };
 
-// 64 columns of the accumulator times a factor per row.  (Few registers at a time, and no call, for which the caller would keep
-// values out of the way in every turn.)
+// The accumulator's 128 columns times a factor per row.  (Few registers at a time: the caller's are full of logits.)
 __device__ __forceinline__ void rescale(uint32_t cols, float f) {
 #pragma unroll 1
-    for (int c = 0; c < 64; c += 4) {
-        float o[4];
+    for (int c = 0; c < kHeadDim; c += 8) {
+        float o[8];
         tmem_ld4(cols + c, o[0], o[1], o[2], o[3]);
+        tmem_ld4(cols + c + 4, o[4], o[5], o[6], o[7]);
         tmem_wait_ld();
         tmem_st4(cols + c, o[0] * f, o[1] * f, o[2] * f, o[3] * f);
+        tmem_st4(cols + c + 4, o[4] * f, o[5] * f, o[6] * f, o[7] * f);
     }
     tmem_wait_st();
 }
@@ -256,13 +258,6 @@ __device__ __forceinline__ void turn_quads(uint32_t (&x)[4][4], int lane) {
     }
 }
 
-__device__ __forceinline__ void sts(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
-__device__ __forceinline__ float lds(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
 // The last of the own keys [from, to) with a value that is not finite, or -1: a whole warp.
@@ -316,46 +311,40 @@ struct Finish {
 // the last block of the item to come here the output of all.  (Not inlined: the loop over the keys needs the registers.)
 __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, uint32_t tmem_base, const Finish f, float m, float l) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int s = warp / kStreamWarps, hf = (warp >> 2) & 1, quarter = warp & 3, row = 32 * quarter + lane;
+    const int s = warp / kStreamWarps, quarter = warp & 3, row = 32 * quarter + lane;
     const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16);
-    float* mine = reinterpret_cast<float*>(smem + kOffExchange) + (s * kTile + row) * 2 + hf;
-    const float* other = reinterpret_cast<const float*>(smem + kOffExchange) + (s * kTile + row) * 2 + (hf ^ 1);
-    const int pair_bar = 1 + s * 4 + quarter, quad_bar = 9 + quarter;
-    const bool whole = f.blocks == 1, speaks = hf == 0 && (f.both || s == 0);      // one thread per row
-    const int half = f.both ? s : 0, bar = f.both ? pair_bar : quad_bar, threads = f.both ? 64 : 128;
-    *mine = l;
-    named_barrier_sync(pair_bar, 64);
-    l += *other;
-    named_barrier_sync(pair_bar, 64);
-    // the columns of this thread's row that are its own from here on: 64, or, of a single row tile, 32
-    int col0 = 64 * hf, cols = 64;
+    const int both_bar = 1 + quarter;                      // of the two streams' warps of 32 rows
+    const bool whole = f.blocks == 1, speaks = f.both || s == 0;       // one thread per row
+    const int half = f.both ? s : 0;
+    // the columns of this thread's row that are its own from here on: all, or, of a single row tile, half of them
+    int col0 = 0, cols = kHeadDim;
     float f0 = 1.f, f1 = 0.f;                              // factors of the two streams' accumulators
     if (!f.both) {
         // (Each stream's warps have waited for their own accumulator; the barrier passes that on.)
-        *mine = hf ? l : m;
+        float2* ml = reinterpret_cast<float2*>(smem + kOffExchange) + row;
+        ml[s * kTile] = make_float2(m, l);
         tmem_fence_before_sync();
-        named_barrier_sync(quad_bar, 128);
+        named_barrier_sync(both_bar, 64);
         tmem_fence_after_sync();
-        const float2* ml = reinterpret_cast<const float2*>(smem + kOffExchange) + row;
         const float2 a0 = ml[0], a1 = ml[kTile];
         m = fmaxf(a0.x, a1.x);
         f0 = a0.x > -INFINITY ? fast_exp2(a0.x - m) : 1.f;
         f1 = a1.x > -INFINITY ? fast_exp2(a1.x - m) : 1.f;
         l = a0.y * f0 + a1.y * f1;                         // (a stream without a tile has m = -inf, l = 0)
-        col0 = 64 * s + 32 * hf;
-        cols = 32;
+        col0 = 64 * s;
+        cols = 64;
     }
-    auto own_sums = [&](int c, float (&o)[16]) {           // columns c .. c + 15 of the accumulator
+    auto own_sums = [&](int c, float (&o)[32]) {           // columns c .. c + 31 of the accumulator
         if (f.both) {
-            tmem_ld16(lane_base + kColO + s * 128 + c, o);
+            tmem_ld32(lane_base + kColO + s * 128 + c, o);
             tmem_wait_ld();
         } else {
-            float o1[16];
-            tmem_ld16(lane_base + kColO + c, o);
-            tmem_ld16(lane_base + kColO + 128 + c, o1);
+            float o1[32];
+            tmem_ld32(lane_base + kColO + c, o);
+            tmem_ld32(lane_base + kColO + 128 + c, o1);
             tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = o[i] * f0 + (f.two ? o1[i] * f1 : 0.f);
+            for (int i = 0; i < 32; ++i) o[i] = o[i] * f0 + (f.two ? o1[i] * f1 : 0.f);
         }
     };
     // Sums in memory, 16 bytes of a row at a time, the rows of a tile side by side: a block has at most two pieces of shared
@@ -367,23 +356,29 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
         if (f.out && speaks) f.ml[tile_of(f.own_slot) + row] = make_float2(m, l);
         float4* dst = f.o + (long long)tile_of(f.own_slot) * (kHeadDim / 4) + row;
 #pragma unroll 1
-        for (int c = col0; c < col0 + cols; c += 16) {
-            float o[16];
+        for (int c = col0; c < col0 + cols; c += 32) {
+            float o[32];
             own_sums(c, o);
             if (!f.out) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dst[(c / 4 + i) * kTile] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            for (int i = 0; i < 8; ++i) dst[(c / 4 + i) * kTile] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         }
         // the last block of the item to come here joins the sums of all
         volatile int* last_flag = reinterpret_cast<volatile int*>(smem + kOffMisc + 512 + 8) + half * 4 + quarter;
+        auto all_here = [&] {
+            if (f.both)
+                __syncwarp();
+            else
+                named_barrier_sync(both_bar, 64);
+        };
         __threadfence();
-        named_barrier_sync(bar, threads);
+        all_here();
         if (speaks && lane == 0) {
             const bool last = atomicAdd(f.counter, 1) == f.blocks - 1;
             if (last) *f.counter = 0;                      // (for the next launch)
             *last_flag = last;
         }
-        named_barrier_sync(bar, threads);
+        all_here();
         emits = *last_flag != 0;
         if (emits) {
             __threadfence();
@@ -405,64 +400,73 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
         uint8_t* out_of[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) out_of[j] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(f.out), (lane & ~3) + j));
-        bool sound = true;
         const float inv = 1.f / l;
+        const uint64_t inv2 = pack2(inv, inv), zero2 = pack2(0.f, 0.f);
+        uint64_t odd = zero2;                              // (not a number as soon as an output is not finite)
         const bool wide = f.dtype == kTypeF32;
-        const int step = wide ? 16 : 32;                   // columns of a row in 64 bytes
-#pragma unroll 1
-        for (int c = col0; c < col0 + cols; c += step) {
-            uint32_t x[4][4];
-#pragma unroll 1
-            for (int part = 0; part < step; part += 16) {
-                float o[16];
-                if (whole) {
-                    own_sums(c + part, o);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] = 0.f;
-#pragma unroll 2
-                    for (int b = 0; b < f.blocks && f.out; ++b) {
-                        const int from = tile_of(slot_of(b));
-                        const float top = __ldcg(&f.ml[from + row].x);
-                        const float4* src = f.o + (long long)from * (kHeadDim / 4) + row;
-                        float4 v4[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v4[i] = __ldcg(&src[((c + part) / 4 + i) * kTile]);
-                        // (no logit above -inf: sums of zero, or not a number, that count as they are)
-                        const float w = top > -INFINITY ? fast_exp2(top - m) : 1.f;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            o[4 * i] = fmaf(v4[i].x, w, o[4 * i]);
-                            o[4 * i + 1] = fmaf(v4[i].y, w, o[4 * i + 1]);
-                            o[4 * i + 2] = fmaf(v4[i].z, w, o[4 * i + 2]);
-                            o[4 * i + 3] = fmaf(v4[i].w, w, o[4 * i + 3]);
-                        }
-                    }
-                }
-                float odd = 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    o[i] *= inv;
-                    odd = fmaf(o[i], 0.f, odd);            // (not a number as soon as one of them is not finite)
-                }
-                sound = sound && odd == 0.f;
-                if (wide) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i >> 2][i & 3] = __float_as_uint(o[i]);
-                } else if (part == 0) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i >> 2][i & 3] = pack_pair(o[2 * i], o[2 * i + 1], f.dtype);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[2 + (i >> 2)][i & 3] = pack_pair(o[2 * i], o[2 * i + 1], f.dtype);
-                }
-            }
+        auto put_quads = [&](uint32_t (&x)[4][4], int byte) {
             turn_quads(x, lane);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (out_of[j])
-                    *reinterpret_cast<uint4*>(out_of[j] + c * (wide ? 4 : 2) + 16 * (lane & 3)) = make_uint4(x[j][0], x[j][1], x[j][2], x[j][3]);
+                if (out_of[j]) *reinterpret_cast<uint4*>(out_of[j] + byte + 16 * (lane & 3)) = make_uint4(x[j][0], x[j][1], x[j][2], x[j][3]);
+        };
+#pragma unroll 1
+        for (int c = col0; c < col0 + cols; c += 32) {
+            float o[32];
+            if (whole) {
+                own_sums(c, o);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0.f;
+#pragma unroll 2
+                for (int b = 0; b < f.blocks && f.out; ++b) {      // (512 bytes of a row in flight)
+                    const int from = tile_of(slot_of(b));
+                    const float top = __ldcg(&f.ml[from + row].x);
+                    const float4* src = f.o + (long long)from * (kHeadDim / 4) + row;
+                    float4 v4[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v4[i] = __ldcg(&src[(c / 4 + i) * kTile]);
+                    // (no logit above -inf: sums of zero, or not a number, that count as they are)
+                    const float w = top > -INFINITY ? fast_exp2(top - m) : 1.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        o[4 * i] = fmaf(v4[i].x, w, o[4 * i]);
+                        o[4 * i + 1] = fmaf(v4[i].y, w, o[4 * i + 1]);
+                        o[4 * i + 2] = fmaf(v4[i].z, w, o[4 * i + 2]);
+                        o[4 * i + 3] = fmaf(v4[i].w, w, o[4 * i + 3]);
+                    }
+                }
+            }
+            uint32_t x[4][4];
+            if (wide) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint64_t v = mul2(pack2(o[16 * h + 2 * i], o[16 * h + 2 * i + 1]), inv2);
+                        odd = fma2(v, zero2, odd);
+                        float v0, v1;
+                        unpack2(v, v0, v1);
+                        x[i >> 1][2 * (i & 1)] = __float_as_uint(v0);
+                        x[i >> 1][2 * (i & 1) + 1] = __float_as_uint(v1);
+                    }
+                    put_quads(x, 4 * (c + 16 * h));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint64_t v = mul2(pack2(o[2 * i], o[2 * i + 1]), inv2);
+                    odd = fma2(v, zero2, odd);
+                    float v0, v1;
+                    unpack2(v, v0, v1);
+                    x[i >> 2][i & 3] = pack_pair(v0, v1, f.dtype);
+                }
+                put_quads(x, 2 * c);
+            }
         }
+        float odd0, odd1;
+        unpack2(odd, odd0, odd1);
+        const bool sound = odd0 + odd1 == 0.f;
         if (f.norm && speaks) {
             f.norm[0] = m;
             f.norm[kTile] = inv;
@@ -472,7 +476,7 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
     }
     if (!f.both) {
         tmem_fence_before_sync();
-        named_barrier_sync(quad_bar, 128);                 // all are done with both accumulators and the exchange
+        named_barrier_sync(both_bar, 64);                  // both are done with both accumulators and the exchange
     }
 }
 
@@ -607,7 +611,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         };
         drain(bars->full, rr, kRing);
         drain(bars->q_full, qr, 2);
-    } else if (warp >= kIssuer) {
+    } else if (warp >= kIssuer && warp < kIssuer + 2) {
         // ------------------------------------------------------------------ MMA issuers, one warp per stream
         // Who issues when, the turns between the two warps and the uses of the ring that each looks at: as in prefix.cu.
         const int s = warp - kIssuer;
@@ -631,13 +635,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         const uint64_t q_desc = smem_desc(smem_u32(smem + kOffQ), 16, 1024), k_desc = smem_desc(smem_u32(smem + kOffRing), 16, 1024);
         const uint64_t v_desc = smem_desc(smem_u32(smem + kOffRing), kBoxBytes, 1024);
         constexpr uint32_t kStep = kOperandBytes >> 4;              // from operand to operand, in a descriptor's units
-        // O += P V for the keys of P's half `part`: the first or the second 32 of every 64
+        // O += P V for the first or the second 64 keys
         auto issue_o = [&](uint32_t st, int part, bool first) {
             const uint64_t b = v_desc + st * kStep;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {           // 16 keys per instruction
-                const int s8 = (i >> 1) * 4 + part * 2 + (i & 1);
-                umma_bf16_ts(o_col, s_col + (s8 >> 2) * 64 + (s8 & 3) * 8, b + s8 * (2048 >> 4), instr_desc(true), !first || i > 0);
+                const int s8 = 4 * part + i;
+                umma_bf16_ts(o_col, s_col + s8 * 8, b + s8 * (2048 >> 4), instr_desc(true), !first || i > 0);
             }
         };
         while (walk.more()) {
@@ -722,14 +726,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         if (elect_one()) umma_commit(&bars->drain[s]);
         __syncwarp();
         wait_bar(&bars->drain[s], 0, abort_flag, p.status, limit, false);
-    } else {
+    } else if (warp < kProducer) {
         // ------------------------------------------------------------------ softmax and output
-        // Accumulator row = TMEM lane; the warps w and w + 4 of a stream share 32 rows and take 64 of the 128 columns each (a
-        // row's chain of exponentials is what a stream's turn is made of: two threads halve it).
-        const int s = warp / kStreamWarps, hf = (warp >> 2) & 1, quarter = warp & 3, row = 32 * quarter + lane;
-        const uint32_t s_cols = tmem_base + ((uint32_t)(32 * quarter) << 16) + kColS + s * 128 + hf * 64;     // (O is kColO - kColS further)
-        const uint32_t mine = smem_u32(smem + kOffExchange) + ((s * kTile + row) * 2 + hf) * 4;                 // (the other thread's: ^ 4)
-        const int pair_bar = 1 + s * 4 + quarter;                      // of the two warps of a row (9 + quarter: of the four of both streams)
+        // Accumulator row = TMEM lane = thread: a row's logits are all in one thread's registers, so nothing is exchanged between the
+        // maximum and the weights (two threads per row halve the exponentials' chain, but not their time on the special function
+        // units, and wait for each other: the long document took 2180 us so).
+        const int s = warp / kStreamWarps, quarter = warp & 3, row = 32 * quarter + lane;
+        const uint32_t s_cols = tmem_base + ((uint32_t)(32 * quarter) << 16) + kColS + s * 128;                // (O is kColO - kColS further)
         uint32_t s_uses = 0, o_uses = 0;
         // A warp whose wait gives up goes on through the same loops, so that its partner's barriers get all their threads, but waits
         // for nothing any more; what it computes means nothing.
@@ -739,55 +742,58 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             dead = __any_sync(0xffffffffu, gave_up);
         };
         const int r_tok = row / pl.group;                              // token of this row inside its tile
-        while (walk.more()) {
-            const Piece pc = walk.next(pl);
-            const int nt = pc.stream_tiles(s);
+        // Where the walk is waits in shared memory: the loop over the keys needs the registers.
+        volatile int* aside = reinterpret_cast<volatile int*>(smem + kOffAside) + warp * kAsideInts;
+        auto put_aside = [&](const Walk& w) {
+            aside[0] = w.x, aside[1] = w.end, aside[2] = w.unit, aside[3] = w.pair, aside[4] = w.start;    // (all lanes the same)
+            __syncwarp();
+        };
+        put_aside(walk);
+        while (aside[0] < aside[1]) {
             float m = -INFINITY, l = 0.f;
             bool warp_on;
+            int nt;
             {
+                Walk here{aside[0], aside[1], aside[2], aside[3], aside[4]};
+                const Piece pc = here.next(pl);
+                __syncwarp();
+                aside[5] = pc.unit, aside[6] = pc.pair, aside[7] = pc.start, aside[8] = pc.kt, aside[9] = pc.k0, aside[10] = pc.k1;
+                put_aside(here);
+                nt = pc.stream_tiles(s);
                 const int tok0 = (2 * pc.pair + (pc.both ? s : 0)) * pl.tile_tokens, tok = tok0 + r_tok;
                 const bool valid = r_tok < pl.tile_tokens && tok < pl.tokens;
-                warp_on = __any_sync(0xffffffffu, valid);              // (the same in both warps of the rows)
+                warp_on = __any_sync(0xffffffffu, valid);
                 const float margin = valid ? kRaiseMargin : INFINITY;  // (a row that does not exist raises nothing)
-                // keys before the first one of a tile's half, and own keys that this row sees, and that every row of the tile sees; of
+                // keys before the first one of a tile, and own keys that this row sees, and that every row of the tile sees; of
                 // the prefix's tiles all rows see the same
-                int key0 = pc.key_tile(s, 0) * kTile + hf * 64 - pl.prefix_tiles * kTile;
-                const int sees = pl.context + (valid ? tok + 1 : pl.tokens), all_see = pl.context + tok0 + 1;
-                for (int t = 0; t < nt; ++t, key0 += pc.both ? kTile : 2 * kTile) {
+                int key0 = pc.key_tile(s, 0) * kTile - pl.prefix_tiles * kTile;
+                const int sees = pl.context + (valid ? tok + 1 : pl.tokens), all_see = pl.context + tok0 + 1, step = pc.both ? kTile : 2 * kTile;
+#pragma unroll 1
+                for (int t = 0; t < nt; ++t, key0 += step) {
                     wait_on(&bars->s_full[s], s_uses & 1u);
                     ++s_uses;
                     tmem_fence_after_sync();
                     if (warp_on) {
+                        float v[4][32];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_ld32(s_cols + 32 * c, v[c]);
+                        tmem_wait_ld();
                         const int all_to = key0 < 0 ? pl.prefix_n - pl.prefix_tiles * kTile - key0 : all_see - key0;
-                        const int to = key0 < 0 ? all_to : sees - key0;        // this row sees the first `to` of the 64 keys
-                        auto load = [&](int c, float (&v)[32]) {               // 32 logits, masked
-                            tmem_ld32(s_cols + c, v);
-                            tmem_wait_ld();
-                            if (all_to < c + 32) {
+                        if (all_to < kTile) {                          // this row sees the first `to` of the keys
+                            const int to = key0 < 0 ? all_to : sees - key0;
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) v[i] = c + i < to ? v[i] : -INFINITY;
-                            }
-                        };
-                        auto top_of = [](const float (&v)[32]) {
-                            float mx[4] = {v[0], v[1], v[2], v[3]};
+                            for (int c = 0; c < 4; ++c)
 #pragma unroll
-                            for (int i = 4; i < 32; i += 4) {
-                                mx[0] = fmax3(mx[0], v[i], v[i + 1]);
-                                mx[1] = fmax3(mx[1], v[i + 2], v[i + 3]);
-                            }
-                            return fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
-                        };
-                        // The second half of the logits is read twice, for the maximum and for the weights: 64 of them at once do not
-                        // leave the registers that the rest of the loop needs.
-                        float v[32];
-                        load(32, v);
-                        float top = top_of(v);
-                        load(0, v);
-                        top = fmaxf(top, top_of(v));
-                        // the row's maximum over both halves; both threads of the row take the same decisions from here on
-                        sts(mine, top);
-                        named_barrier_sync(pair_bar, 64);
-                        top = fmaxf(top, lds(mine ^ 4u)) * p.scale_log2;
+                                for (int i = 0; i < 32; ++i) v[c][i] = 32 * c + i < to ? v[c][i] : -INFINITY;
+                        }
+                        float mx[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            mx[c] = fmaxf(v[c][0], v[c][1]);
+#pragma unroll
+                            for (int i = 2; i < 32; i += 2) mx[c] = fmax3(mx[c], v[c][i], v[c][i + 1]);
+                        }
+                        const float top = fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * p.scale_log2;
                         if (__any_sync(0xffffffffu, top > m + margin)) {
                             const float next = fmaxf(m, top);
                             const float f = m == next ? 1.f : fast_exp2(m - next);
@@ -799,19 +805,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                         const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), minus2 = pack2(-ref, -ref);
                         uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {                      // 16 columns at a time
-                            if (c == 2) {                                  // the first half of P is there: its product may begin
+                        for (int c = 0; c < 8; ++c) {                      // 16 columns at a time
+                            if (c == 4) {                                  // the first half of P is there: its product may begin
                                 tmem_wait_st();
                                 tmem_fence_before_sync();
                                 __syncwarp();
                                 if (lane == 0) mbar_arrive(&bars->p_full[s][0]);
-                                load(32, v);
                             }
                             uint32_t w16[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 float e0, e1;
-                                unpack2(fma2(pack2(v[16 * (c & 1) + 2 * i], v[16 * (c & 1) + 2 * i + 1]), scale2, minus2), e0, e1);
+                                unpack2(fma2(pack2(v[c >> 1][16 * (c & 1) + 2 * i], v[c >> 1][16 * (c & 1) + 2 * i + 1]), scale2, minus2), e0, e1);
                                 e0 = fast_exp2(e0);
                                 e1 = fast_exp2(e1);
                                 w16[i] = pack_bf16(e0, e1);
@@ -841,6 +846,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             }
             tmem_fence_after_sync();
             if (warp_on) {
+                const Piece pc{aside[5], aside[6], aside[7], aside[8], aside[9], aside[10], 2 * aside[6] + 1 < pl.tiles};
                 const UnitAt at = unit_at(pl, pc.unit);
                 const int tile = 2 * pc.pair + (pc.both ? s : 0), tok = tile * pl.tile_tokens + r_tok, half = pc.both ? s : 0;
                 const bool valid = r_tok < pl.tile_tokens && tok < pl.tokens;
