@@ -882,6 +882,7 @@ int lazyev_bind(lazyev_t* h, void* kv_pool, void* state, void* scratch, void* cu
     if ((e = chunk_prepare()) != cudaSuccess) return cuda_fail(h, e, "chunk kernel set-up");
     if ((e = weigh_prepare()) != cudaSuccess) return cuda_fail(h, e, "weight kernel set-up");
     if ((e = keep_prepare()) != cudaSuccess) return cuda_fail(h, e, "select kernel set-up");
+    if ((e = blocks_prepare()) != cudaSuccess) return cuda_fail(h, e, "block selection set-up");
 
     const Sizes s = sizes_of(h);
     h->stream = (cudaStream_t)cuda_stream;
@@ -1537,14 +1538,15 @@ int lazyev_attend_chunk(lazyev_t* h, const lazyev_rows_t* q, int n_tokens, const
 namespace {
 
 struct BlockSpace {
-    size_t keys, table, pbar, bytes;       // offsets (the bounds come first)
+    size_t rough, exact, table, pbar, bytes;       // offsets (the bounds come first)
 };
 
 BlockSpace block_space(const lazyev_t* h) {
     const size_t pages = (size_t)h->units * h->pages_per_unit;
     BlockSpace s;
-    s.keys = align_up(pages * 2 * kRowBytes, 256);
-    s.table = s.keys + align_up(pages * sizeof(unsigned long long), 256);
+    s.rough = align_up(pages * 2 * kRowBytes, 256);
+    s.exact = s.rough + align_up(pages * 2 * sizeof(uint32_t), 256);
+    s.table = s.exact + align_up(pages * sizeof(unsigned long long), 256);
     s.pbar = s.table + align_up(pages * sizeof(int32_t), 256);
     s.bytes = s.pbar + align_up((size_t)h->units * h->capacity * sizeof(float), 256);
     return s;
@@ -1557,7 +1559,8 @@ BlocksArgs blocks_args(const lazyev_t* h) {
     a.pool = h->pool;
     a.page_table = h->st.page_table;
     a.bounds = h->block_space;
-    a.keys = (unsigned long long*)(h->block_space + s.keys);
+    a.rough = (uint32_t*)(h->block_space + s.rough);
+    a.exact = (unsigned long long*)(h->block_space + s.exact);
     a.table = (int32_t*)(h->block_space + s.table);
     a.status = h->st.status;
     return a;
@@ -1618,9 +1621,10 @@ int lazyev_attend_sparse(lazyev_t* h, const void* q, int blocks, void* out, int3
     BlocksArgs a = blocks_args(h);
     a.q = q;
     a.selected = selected;
-    const cudaError_t e = pick_launch(a, last, picked, blocks, h->stream);
+    int launches = 0;
+    const cudaError_t e = pick_launch(a, last, picked, blocks, h->num_sms, &launches, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "block selection launch");
-    h->launches += picked > 0 && picked < last ? 2 : 1;
+    h->launches += launches;
     StateView view = h->st;
     view.page_table = a.table;
     view.pbar = (float*)(h->block_space + block_space(h).pbar);

@@ -5,14 +5,16 @@
 // and a unit's G query heads give it the score
 //   s_b = sum_g sum_d max(q_g[d] high_b[d], q_g[d] low_b[d]) = sum_d (P[d] high_b[d] + N[d] low_b[d]),
 //   P[d] = sum_g max(q_g[d], 0),  N[d] = sum_g min(q_g[d], 0):
-// no key between the bounds has larger logits summed over the heads.  The products are exact, and the sums are taken in fp64, where
-// orders of magnitude and of summation do not move a score past its neighbour: which blocks are read does not depend on rounding.
+// no key between the bounds has larger logits summed over the heads.  Which blocks are read does not depend on fp32 rounding: blocks near
+// the cut are compared by scores in fp64, where the products are exact (all of them in fp64 is four times slower than their bytes:
+// 128 units of 2047 blocks, 77 us instead of 20, most of it conversions).
 // The newest block (the only one that may be partly filled) and the blocks - 1 best others, of equals the older, become a
 // page table of their own, in order, which the decode kernel reads like any other: K and V of blocks * 64 tokens instead of n.
 //
 //   bounds_kernel -- the bounds, once per block (keys behind the newest block do not change any more)
-//   score_kernel  -- 512 bytes per block and 256 fp64 fmas: a warp per block, lanes 0-15 the high row, 16-31 the low one
-//   pick_kernel   -- one block of threads per unit: radix select over the scores, page table, list
+//   pick_kernel   -- one block of threads per unit: scores, radix select over them, page table, list.  512 bytes per block, a
+//                    warp per block, lanes 0-15 the high row, 16-31 the low one
+//   score_kernel  -- the scores by many blocks of threads, for long caches of few units
 #include "internal.h"
 #include "select.cuh"
 
@@ -58,19 +60,26 @@ __global__ void __launch_bounds__(256) bounds_kernel(BlocksArgs a, int first, in
     }
 }
 
-// Larger scores have larger keys; what is no number comes first of all.  (The select starts at 1: 0 is no score's.)
-__device__ __forceinline__ unsigned long long score_key(double s) {
+// Larger scores have larger keys; what is no number comes first of all.
+__device__ __forceinline__ unsigned long long exact_key(double s) {
     if (s != s) return ~0ull;
     const long long b = __double_as_longlong(s == 0.0 ? 0.0 : s);
     return b < 0 ? ~(unsigned long long)b : (unsigned long long)b | 0x8000000000000000ull;
 }
+__device__ __forceinline__ uint32_t rough_key(float s) {
+    if (s != s) return ~0u;
+    const uint32_t b = __float_as_uint(s == 0.f ? 0.f : s);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float rough_score(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-constexpr int kScoreThreads = 256, kBlocksPerWarp = 8;
-
-__global__ void __launch_bounds__(kScoreThreads) score_kernel(BlocksArgs a, int count) {
-    const int u = blockIdx.y, lane = threadIdx.x & 31, c = lane & 15, G = a.geo.group;
-    // this lane's eight dimensions of P (lanes 0-15) or N
-    double part[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+// A lane's part of P (lanes 0-15) or N for its eight dimensions.
+struct Sides {
+    double part[8];
+};
+__device__ __forceinline__ Sides sides_of(const BlocksArgs& a, int u) {
+    const int lane = threadIdx.x & 31, c = lane & 15, G = a.geo.group;
+    Sides s = {{0, 0, 0, 0, 0, 0, 0, 0}};
     const uint4* q = reinterpret_cast<const uint4*>(a.q) + (size_t)u * G * kChunksPerRow + c;
     for (int g = 0; g < G; ++g) {
         const uint4 x = q[g * kChunksPerRow];
@@ -79,75 +88,261 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(BlocksArgs a, int 
         for (int i = 0; i < 4; ++i) {
             const float e0 = bf16_lo_as_float(w[i]), e1 = bf16_hi_as_float(w[i]);
             // (what is no number goes into both sums)
-            part[2 * i] += e0 != e0 || (lane < 16 ? e0 > 0.f : e0 < 0.f) ? (double)e0 : 0.0;
-            part[2 * i + 1] += e1 != e1 || (lane < 16 ? e1 > 0.f : e1 < 0.f) ? (double)e1 : 0.0;
+            s.part[2 * i] += e0 != e0 || (lane < 16 ? e0 > 0.f : e0 < 0.f) ? (double)e0 : 0.0;
+            s.part[2 * i + 1] += e1 != e1 || (lane < 16 ? e1 > 0.f : e1 < 0.f) ? (double)e1 : 0.0;
         }
     }
-    const int warp = (blockIdx.x * kScoreThreads + threadIdx.x) >> 5, b0 = warp * kBlocksPerWarp;
-    const uint4* rows = reinterpret_cast<const uint4*>(a.bounds) + (size_t)u * a.geo.pages_per_unit * 2 * kChunksPerRow + lane;
-    uint4 x[kBlocksPerWarp];
+    return s;
+}
+
+__device__ __forceinline__ const uint4* bound_rows(const BlocksArgs& a, int u) {
+    return reinterpret_cast<const uint4*>(a.bounds) + (size_t)u * a.geo.pages_per_unit * 2 * kChunksPerRow;
+}
+
+// The score of one block in fp64, in every lane.
+__device__ __forceinline__ double exact_score(const uint4* rows, const Sides& s, int b) {
+    const uint4 x = __ldg(rows + (size_t)b * 2 * kChunksPerRow + (threadIdx.x & 31));
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    double v = 0.0;
 #pragma unroll
-    for (int i = 0; i < kBlocksPerWarp; ++i)
-        x[i] = b0 + i < count ? rows[(size_t)(b0 + i) * 2 * kChunksPerRow] : make_uint4(0u, 0u, 0u, 0u);
+    for (int j = 0; j < 4; ++j) {
+        v = fma(s.part[2 * j], (double)bf16_lo_as_float(w[j]), v);
+        v = fma(s.part[2 * j + 1], (double)bf16_hi_as_float(w[j]), v);
+    }
 #pragma unroll
-    for (int i = 0; i < kBlocksPerWarp; ++i) {
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+constexpr int kBatch = 8;                  // blocks of a warp in flight
+// An fp32 score is off by less than this of the sum of its terms' magnitudes: P rounded, eight products and five sums, 14 roundings
+// of 2^-24, with room.
+constexpr float kRoughError = 1.f / (1 << 19);
+
+// Rough scores of blocks b0 .. b0 + 7: lane 4 i + j, any j, gets that of block b0 + i.  The eight sums over the lanes are folded into
+// each other: half of them go to the other half of the lanes at every step, nine exchanges instead of forty.  `size` grows to the
+// largest sum of magnitudes that this lane's dimensions had.
+__device__ __forceinline__ float rough_batch(const uint4* rows, const float (&side)[8], int b0, int count, float& size) {
+    const int lane = threadIdx.x & 31;
+    uint4 x[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+        x[i] = b0 + i < count ? __ldg(rows + (size_t)(b0 + i) * 2 * kChunksPerRow + lane) : make_uint4(0u, 0u, 0u, 0u);
+    float v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
         const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        double s = 0.0;
+        float sum = 0.f, all = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            s = fma(part[2 * j], (double)bf16_lo_as_float(w[j]), s);
-            s = fma(part[2 * j + 1], (double)bf16_hi_as_float(w[j]), s);
+            const float lo = bf16_lo_as_float(w[j]), hi = bf16_hi_as_float(w[j]);
+            sum = fmaf(side[2 * j], lo, sum);
+            sum = fmaf(side[2 * j + 1], hi, sum);
+            all = fmaf(fabsf(side[2 * j]), fabsf(lo), all);
+            all = fmaf(fabsf(side[2 * j + 1]), fabsf(hi), all);
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0 && b0 + i < count) a.keys[(size_t)u * a.geo.pages_per_unit + b0 + i] = score_key(s);
+        v[i] = sum;
+        size = all > size || all != all ? all : size;
     }
+#pragma unroll
+    for (int half = 4, bit = 16; half > 0; half >>= 1, bit >>= 1) {
+        const bool up = lane & bit;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+            const float give = up ? v[i] : v[i + half], own = up ? v[i + half] : v[i];
+            v[i] = own + __shfl_xor_sync(0xffffffffu, give, bit);
+        }
+    }
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+    return v[0];
+}
+
+// Scores the blocks that a warp takes (from b0 on, `step` apart) into `put`; returns the largest sum of magnitudes, or more.
+template <typename Put>
+__device__ __forceinline__ float rough_scores(const BlocksArgs& a, int u, int count, int b0, int step, const Put& put) {
+    const int lane = threadIdx.x & 31;
+    const Sides s = sides_of(a, u);
+    float side[8], size = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) side[i] = (float)s.part[i];
+    const uint4* rows = bound_rows(a, u);
+    for (; b0 < count; b0 += step) {
+        const float score = rough_batch(rows, side, b0, count, size);
+        const int b = b0 + (lane >> 2);
+        if ((lane & 3) == 0 && b < count) put(b, rough_key(score));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) size += __shfl_xor_sync(0xffffffffu, size, o);
+    return size;
 }
 
 constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
+constexpr int kCachedKeys = 16384;         // of a unit in shared memory; of longer caches they stay in L2
+// Up to here a unit's own block of threads scores them; behind it, where units are too few to fill the GPU, a launch over many.
+constexpr int kScoreAlone = 256;
+constexpr int kScoreWarps = 8;
 
-// Candidates are blocks 0 .. count - 1, `picked` of them (may be 0, or all) are taken; then the newest block.
-__global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int count, int picked, int asked) {
-    __shared__ TopShared<unsigned long long> sh;
+// a.rough: per unit pages_per_unit rough keys, and behind them one sum of magnitudes per warp of this launch.
+__global__ void __launch_bounds__(32 * kScoreWarps) score_kernel(BlocksArgs a, int count) {
+    const int u = blockIdx.y, warp = blockIdx.x * kScoreWarps + (threadIdx.x >> 5);
+    uint32_t* keys = a.rough + (size_t)u * 2 * a.geo.pages_per_unit;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const float size = rough_scores(a, u, count, warp * kBatch, gridDim.x * kScoreWarps * kBatch, [&](int b, uint32_t key) { keys[b] = key; });
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<float*>(keys)[a.geo.pages_per_unit + warp] = size;
+}
+
+// Candidates are blocks 0 .. count - 1, `picked` of them (may be 0, or all) are taken; then the newest block.  The cut comes from
+// rough scores in fp32: with E the most that one is off, a block more than 2 E above the rough cut is above the exact one and a
+// block more than 2 E below it below, and only those between are scored in fp64 -- a handful, or, where scores are no numbers or
+// alike, up to all.  score_warps = 0: the scores are made here.
+__global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int count, int picked, int asked, int score_warps) {
+    extern __shared__ uint32_t cached[];
+    __shared__ TopShared<unsigned long long> wide;
+    TopShared<uint32_t>& sh = *reinterpret_cast<TopShared<uint32_t>*>(&wide);      // (one select after the other)
+    __shared__ uint32_t least[kPickWarps], most[kPickWarps];
+    __shared__ float sizes[kPickWarps];
+    __shared__ int between[kSurvivors];
+    __shared__ unsigned long long exact[kSurvivors];
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned long long* keys = a.keys + (size_t)u * a.geo.pages_per_unit;
+    uint32_t* stored = a.rough + (size_t)u * 2 * a.geo.pages_per_unit;
     const int32_t* table = a.page_table + (size_t)u * a.geo.pages_per_unit;
     int32_t* to = a.table + (size_t)u * a.geo.pages_per_unit;
     int32_t* list = a.selected ? a.selected + (size_t)u * asked : nullptr;
+    uint32_t* keys = count <= kCachedKeys ? cached : stored;
+    const bool chosen = picked > 0 && picked < count;
     auto put = [&](int j, int block) {
         to[j] = table[block];
         if (list) list[j] = block;
     };
+    float size = 0.f;
+    if (chosen && score_warps == 0) {
+        size = rough_scores(a, u, count, warp * kBatch, kPickWarps * kBatch, [&](int b, uint32_t key) { keys[b] = key; });
+    } else {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (chosen) {
+            if (keys == cached)
+                for (int i = tid; i < count; i += kPickThreads) cached[i] = __ldcg(stored + i);
+            for (int i = tid; i < score_warps; i += kPickThreads) {
+                const float s = __ldcg(reinterpret_cast<const float*>(stored) + a.geo.pages_per_unit + i);
+                size = s > size || s != s ? s : size;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const float s = __shfl_xor_sync(0xffffffffu, size, o);
+                size = s > size || s != s ? s : size;
+            }
+        }
+    }
     if (picked == count) {                                  // all of them
         for (int b = tid; b < count; b += kPickThreads) put(b, b);
-    } else if (picked > 0) {
-        const Cut<unsigned long long> cut = top_cut<kPickThreads, unsigned long long>(count, picked, sh, [&](int i) { return keys[i]; });
+    } else if (chosen) {
+        if (lane == 0) sizes[warp] = size;
+        __syncthreads();
+        // Scores of a unit are mostly of one magnitude: counted from the least one, the leading digits of their keys differ.
+        uint32_t lo = ~0u, hi = 0u;
+        for (int i = tid; i < count; i += kPickThreads) {
+            lo = min(lo, keys[i]);
+            hi = max(hi, keys[i]);
+        }
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        if (lane == 0) {
+            least[warp] = lo;
+            most[warp] = hi;
+        }
+        __syncthreads();
+        for (int w = 0; w < kPickWarps; ++w) {
+            lo = min(lo, least[w]);
+            hi = max(hi, most[w]);
+            size = sizes[w] > size || sizes[w] != sizes[w] ? sizes[w] : size;
+        }
+        const Cut<uint32_t> cut = top_cut<kPickThreads, uint32_t>(count, picked, 32 - __clz(hi - lo), sh, [&](int i) { return keys[i] - lo; });
+        // (the cut may lie between two keys: the k-th is the least one above it)
+        uint32_t kth = cut.kth + lo;
+        if (cut.ties == 0) {
+            uint32_t next = ~0u;
+            for (int i = tid; i < count; i += kPickThreads)
+                if (keys[i] > kth) next = min(next, keys[i]);
+            next = __reduce_min_sync(0xffffffffu, next);
+            __syncthreads();
+            if (lane == 0) least[warp] = next;
+            __syncthreads();
+            for (int w = 0; w < kPickWarps; ++w) next = min(next, least[w]);
+            kth = next;
+        }
+        const float t = rough_score(kth), reach = 2.f * kRoughError * size;
+        // 1: above whatever the exact scores are, 0: below, 2: between (all of them where something is no number or infinite)
+        const bool sane = fabsf(t) < INFINITY && reach < INFINITY;
+        auto side_of = [&](uint32_t key) {
+            if (!sane || key == ~0u) return 2;
+            const float s = rough_score(key);
+            return s > t + reach ? 1 : s < t - reach ? 0 : 2;
+        };
+        int sure = 0, open = 0;
+        for (int i = tid; i < count; i += kPickThreads) {
+            const int side = side_of(keys[i]);
+            sure += side == 1;
+            open += side == 2;
+        }
+        int all_sure, all_open;
+        block_rank<kPickThreads>(sure, sh.warp_sums, &all_sure);
+        const int open_before = block_rank<kPickThreads>(open, sh.warp_sums, &all_open);
+        const int need = picked - all_sure;
+        // afterwards a key is ~0 for a block that is taken and 0 for one that is not
+        if (all_open == need) {
+            for (int i = tid; i < count; i += kPickThreads) keys[i] = side_of(keys[i]) != 0 ? ~0u : 0u;
+        } else if (all_open <= kSurvivors) {
+            int at = open_before;
+            for (int i = tid; i < count; i += kPickThreads) {
+                const int side = side_of(keys[i]);
+                if (side == 2 && at < kSurvivors) between[at++] = i;
+                keys[i] = side == 1 ? ~0u : 0u;
+            }
+            __syncthreads();
+            const Sides s = sides_of(a, u);
+            for (int i = warp; i < all_open; i += kPickWarps) {
+                const unsigned long long key = exact_key(exact_score(bound_rows(a, u), s, between[i]));
+                if (lane == 0) exact[i] = key;
+            }
+            __syncthreads();
+            if (tid < all_open) {                           // of equals the older
+                int before = 0;
+                for (int j = 0; j < all_open; ++j) before += exact[j] > exact[tid] || (exact[j] == exact[tid] && between[j] < between[tid]);
+                if (before < need) keys[between[tid]] = ~0u;
+            }
+        } else {
+            // many: all their exact keys, and a select over those (0 is no exact key)
+            const Sides s = sides_of(a, u);
+            unsigned long long* exacts = a.exact + (size_t)u * a.geo.pages_per_unit;
+            for (int i = warp; i < count; i += kPickWarps) {
+                const unsigned long long key = side_of(keys[i]) == 2 ? exact_key(exact_score(bound_rows(a, u), s, i)) : 0ull;
+                if (lane == 0) exacts[i] = key;
+            }
+            __syncthreads();
+            const Cut<unsigned long long> last = top_cut<kPickThreads, unsigned long long>(count, need, 64, wide, [&](int i) { return exacts[i]; });
+            const int per = (count + kPickThreads - 1) / kPickThreads, from = min(count, tid * per), till = min(count, from + per);
+            int ties = 0;
+            for (int i = from; i < till; ++i) ties += exacts[i] == last.kth;
+            int total, tie = block_rank<kPickThreads>(ties, sh.warp_sums, &total);
+            for (int i = from; i < till; ++i) {             // of equals the older
+                const bool take = side_of(keys[i]) == 1 || exacts[i] > last.kth || (exacts[i] == last.kth && tie < last.ties);
+                tie += exacts[i] == last.kth;
+                keys[i] = take ? ~0u : 0u;
+            }
+        }
+        __syncthreads();
         const int seg = ((count + kPickWarps - 1) / kPickWarps + 31) / 32 * 32;
         const int seg_b = min(count, warp * seg), seg_e = min(count, seg_b + seg);
-        const unsigned lt = (1u << lane) - 1u;
-        int above = 0, ties = 0;
+        int kept = 0, all;
+        for (int i0 = seg_b; i0 < seg_e; i0 += 32) kept += __popc(__ballot_sync(0xffffffffu, i0 + lane < seg_e && keys[min(i0 + lane, count - 1)] != 0u));
+        int dst = __shfl_sync(0xffffffffu, block_rank<kPickThreads>(lane == 0 ? kept : 0, sh.warp_sums, &all), 0);
         for (int i0 = seg_b; i0 < seg_e; i0 += 32) {
-            const bool in = i0 + lane < seg_e;
-            const unsigned long long x = in ? keys[i0 + lane] : 0ull;
-            above += __popc(__ballot_sync(0xffffffffu, in && x > cut.kth));
-            ties += __popc(__ballot_sync(0xffffffffu, in && x == cut.kth));
-        }
-        int all;
-        const int ties_before = __shfl_sync(0xffffffffu, block_rank<kPickThreads>(lane == 0 ? ties : 0, sh.warp_sums, &all), 0);
-        const int kept = above + max(0, min(ties, cut.ties - ties_before));
-        const int before = __shfl_sync(0xffffffffu, block_rank<kPickThreads>(lane == 0 ? kept : 0, sh.warp_sums, &all), 0);
-        int dst = before, tie = ties_before;
-        for (int i0 = seg_b; i0 < seg_e; i0 += 32) {
-            const bool in = i0 + lane < seg_e;
-            const unsigned long long x = in ? keys[i0 + lane] : 0ull;
-            const bool equal = in && x == cut.kth;
-            const unsigned tie_mask = __ballot_sync(0xffffffffu, equal);
-            const bool keep = in && (x > cut.kth || (equal && tie + __popc(tie_mask & lt) < cut.ties));
+            const bool keep = i0 + lane < seg_e && keys[min(i0 + lane, count - 1)] != 0u;
             const unsigned keep_mask = __ballot_sync(0xffffffffu, keep);
-            const int j = dst + __popc(keep_mask & lt);
+            const int j = dst + __popc(keep_mask & ((1u << lane) - 1u));
             if (keep && j < picked) put(j, i0 + lane);
             dst += __popc(keep_mask);
-            tie += __popc(tie_mask);
         }
         if (tid == 0 && all != picked) atomicOr(a.status, kStatusBadIndex);
     }
@@ -165,22 +360,35 @@ cudaError_t bounds_launch(const BlocksArgs& a, int first, int count, int num_sms
     return cudaGetLastError();
 }
 
-cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, cudaStream_t stream) {
-    if (picked > 0 && picked < count) {
-        const int per = kScoreThreads / 32 * kBlocksPerWarp;
-        for (int u0 = 0; u0 < a.geo.units; u0 += 65535) {  // (a grid's second dimension ends at 65535)
-            BlocksArgs part = a;
-            part.q = reinterpret_cast<const uint4*>(a.q) + (size_t)u0 * a.geo.group * kChunksPerRow;
-            part.bounds = reinterpret_cast<uint8_t*>(a.bounds) + (size_t)u0 * a.geo.pages_per_unit * 2 * kRowBytes;
-            part.keys += (size_t)u0 * a.geo.pages_per_unit;
-            const int some = a.geo.units - u0 < 65535 ? a.geo.units - u0 : 65535;
-            score_kernel<<<dim3((count + per - 1) / per, some), kScoreThreads, 0, stream>>>(part, count);
-        }
+cudaError_t blocks_prepare() {
+    return cudaFuncSetAttribute(pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kCachedKeys * (int)sizeof(uint32_t));
+}
+
+cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, int num_sms, int* launches, cudaStream_t stream) {
+    *launches = 1;
+    const bool chosen = picked > 0 && picked < count;
+    int score_warps = 0;
+    if (chosen && count > kScoreAlone && a.geo.units < num_sms / 2) {
+        // (far from the limit of a grid's second dimension; the warps' sums fit behind the keys)
+        const int per = kScoreWarps * kBatch, most = (4 * num_sms + a.geo.units - 1) / a.geo.units, parts = (count + per - 1) / per;
+        const dim3 grid(parts < most ? parts : most, a.geo.units);
+        score_warps = (int)grid.x * kScoreWarps;
+        score_kernel<<<grid, 32 * kScoreWarps, 0, stream>>>(a, count);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
+        *launches = 2;
     }
-    pick_kernel<<<a.geo.units, kPickThreads, 0, stream>>>(a, count, picked, asked);
-    return cudaGetLastError();
+    cudaLaunchAttribute beside = {};
+    beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    beside.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(a.geo.units);
+    c.blockDim = dim3(kPickThreads);
+    c.dynamicSmemBytes = chosen && count <= kCachedKeys ? (size_t)count * sizeof(uint32_t) : 0;
+    c.stream = stream;
+    c.attrs = &beside;
+    c.numAttrs = score_warps > 0 ? 1 : 0;      // begins beside the end of the scores
+    return cudaLaunchKernelEx(&c, pick_kernel, a, count, picked, asked, score_warps);
 }
 
 }  // namespace lzk

@@ -468,7 +468,7 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
         unpack2(odd, odd0, odd1);
         const bool sound = odd0 + odd1 == 0.f;
         if (f.norm && speaks) {
-            f.norm[0] = m;
+            f.norm[0] = -m;
             f.norm[kTile] = inv;
         }
         const unsigned again = __ballot_sync(0xffffffffu, f.out && !sound && finite(l) && finite(m));

@@ -103,7 +103,7 @@ struct ChunkArgs {
     float* o;                           // sums of items that several blocks share (chunk_workspace_bytes)
     float2* ml;
     int32_t* counters;                  // [kChunkCounters], zero
-    float* norms;                       // [units][tiles][2][128]: a row's reference and 1 / its sum of exp2(x - reference), or null
+    float* norms;                       // [units][tiles][2][128]: minus a row's reference, and 1 / its sum of exp2(x - reference); or null
     int32_t* status;
     unsigned long long wait_limit_ns;
     int stop_after_tiles;
@@ -299,15 +299,17 @@ struct BlocksArgs {
     const uint8_t* pool;
     const int32_t* page_table;
     void* bounds;                       // [units][pages_per_unit][2 (high, low)][128] bf16
-    unsigned long long* keys;           // [units][pages_per_unit]
+    uint32_t* rough;                    // [units][2][pages_per_unit]
+    unsigned long long* exact;          // [units][pages_per_unit]
     const void* q;
     int32_t* table;                     // [units][pages_per_unit]: the selected pages, in order
     int32_t* selected;                  // [units][asked] block numbers, -1 behind the last; or null
     int32_t* status;
 };
 cudaError_t bounds_launch(const BlocksArgs& a, int first, int count, int num_sms, cudaStream_t stream);
+cudaError_t blocks_prepare();
 // Of the first `count` blocks the `picked` best, and the one behind them.
-cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, cudaStream_t stream);
+cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, int num_sms, int* launches, cudaStream_t stream);
 
 // hist[b] (b < bins - 1) = cached tokens of the unit range with MRI = b; hist[bins - 1] = the rest.
 cudaError_t mri_histogram_launch(const Geometry& geo, StateView st, int unit_begin, int unit_count, int n, int bins,

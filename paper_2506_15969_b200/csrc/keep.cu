@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(kThreads) weigh_select_kernel(Geometry geo, St
         __syncthreads();
     }
     auto key = [&](int i) -> uint32_t { return kCached ? cached[i] : weight_key(__ldg(w + i)); };
-    const Cut<uint32_t> cut = top_cut<kThreads, uint32_t>(count, k, sh, key);
+    const Cut<uint32_t> cut = top_cut<kThreads, uint32_t>(count, k, 32, sh, key);
 
     // Each warp owns a contiguous segment and walks it 32 at a time: ranks in slot order come from ballots.
     const int seg = ((count + kWarps - 1) / kWarps + 31) / 32 * 32;

@@ -47,16 +47,16 @@ __device__ __forceinline__ int block_rank(int v, int* warp_sums, int* total) {
     return before + incl - v;
 }
 
-// The cut of the k largest (1 <= k <= count) of key(0) .. key(count - 1).  One pass over the keys per digit, until the
-// k-th key's bin is wanted whole or holds few keys, which are ranked directly.
+// The cut of the k largest (1 <= k <= count) of key(0) .. key(count - 1), all below 2^width.  One pass over the keys per digit, until
+// the k-th key's bin is wanted whole or holds few keys, which are ranked directly.
 template <int kThreads, typename Key, typename Load>
-__device__ Cut<Key> top_cut(int count, int k, TopShared<Key>& sh, const Load& key) {
+__device__ Cut<Key> top_cut(int count, int k, int width, TopShared<Key>& sh, const Load& key) {
     static_assert(kBins % kThreads == 0, "");
-    constexpr int kPer = kBins / kThreads, kWidth = 8 * sizeof(Key);
+    constexpr int kPer = kBins / kThreads;
     const int tid = threadIdx.x;
     Key prefix = 0, mask = 0;
     int rem = k;
-    for (int left = kWidth; left > 0;) {
+    for (int left = width; left > 0;) {
         const int bits = left < kDigitBits ? left : kDigitBits, shift = left - bits;
         for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
         __syncthreads();
@@ -129,7 +129,7 @@ __device__ Cut<Key> top_cut(int count, int k, TopShared<Key>& sh, const Load& ke
         }
         __syncthreads();
     }
-    return Cut<Key>{prefix, rem};
+    return Cut<Key>{prefix, rem};       // (of no width at all: every key is zero, and k of them stay)
 }
 
 }  // namespace lzk

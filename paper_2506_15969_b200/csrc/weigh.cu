@@ -4,14 +4,16 @@
 //   weight[j] (+)= 1 / G sum over rows r that see j of exp2(x_r[j] - m_r) / l_r
 // with the logits x and the rows' references m and sums l as in chunk.cu, which leaves the last two in memory.  A row's sum is
 // known only after all its keys, hence a second pass over the logits, but no second product: keys are the accumulator rows here
-// (S = K Q^T), so a key's sum over the query rows stays in two threads' registers, in fp32 throughout, and is written once.
+// (S = K Q^T), so a key's sum over the query rows stays in four threads' registers, in fp32 throughout, and is written once.
 //
-// An item is a pair of 128-key tiles of a unit, a stream each, with the row tiles of the chunk that see it; the walk over (item, row
+// An item is a pair of 128-key tiles of a unit with the row tiles of the chunk that see it; the walk over (item, row
 // tile) is cut into equal contiguous parts, one per persistent block, as in chunk.cu; sums of an item that several blocks share go
 // through memory and the last of them to arrive adds them up in order.  Three key tiles and the row tiles of three steps are in
-// shared memory, and each stream has two logit tiles in tensor memory, so that the tensor core runs ahead of the exponentials.
+// shared memory, and two pairs of logit tiles in tensor memory, so that the tensor core runs ahead of the exponentials.
 //
-// Bound by the exponentials, one per row and key (the tensor core needs half their time); few rows: HBM, the keys once.
+// Bound by the exponentials, one per row and key (the tensor core needs half their time): 16 units, 4096 rows of 4096 tokens each, 160 us,
+// special function units 72 % busy under a profiler (a quarter of them as polynomials of degree 5 on the fma pipe changed nothing); few
+// rows: HBM, the keys once.
 //
 // Warp roles: warps 0-15 exponentials, warp 16 TMA producer, warp 17 MMA issuer.  All mbarrier waits are bounded.
 #include <string.h>
@@ -27,21 +29,22 @@ constexpr int kTile = 128;                         // keys of a key tile, rows o
 constexpr int kBoxBytes = kTile * 128;             // half an operand: 128 rows x 64 bf16
 constexpr int kOperandBytes = 2 * kBoxBytes;
 constexpr int kRing = 3;                           // row tiles in flight
-constexpr int kStreamWarps = 8;                    // two warps per 32 keys, half of the rows each
-constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 1);
+constexpr int kExpWarps = 16;                      // four warps per 32 keys of both tiles, a quarter of the rows each
+constexpr int kProducer = kExpWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 1);
 
 constexpr int kKeys = 3;                           // key tiles in flight
 constexpr int kOffK = 0;
 constexpr int kOffRing = kOffK + kKeys * kOperandBytes;
 constexpr int kOffNorms = kOffRing + kRing * kOperandBytes;     // [kRing][2][128]
 constexpr int kNormBytes = 2 * kTile * 4;
-constexpr int kSmem = kOffNorms + kRing * kNormBytes;
-constexpr uint32_t kTmemCols = 512;                // [stream][2 buffers][128]
+constexpr int kOffParts = kOffNorms + kRing * kNormBytes;       // [3 quarters of the rows][2 key tiles][128]
+constexpr int kSmem = kOffParts + 3 * 2 * kTile * 4;
+constexpr uint32_t kTmemCols = 512;                // [2 buffers][2 key tiles][128]
 
 struct Bars {
     uint64_t k_full[kKeys], k_empty[kKeys];
     uint64_t full[kRing], empty[kRing];
-    uint64_t s_full[2][2], s_empty[2][2];          // [stream][buffer]
+    uint64_t s_full[2], s_empty[2];                // [buffer]
     uint64_t drain;
 };
 
@@ -49,9 +52,9 @@ struct WeighParams {
     WeighPlan plan;
     ChunkPlan chunk;
     const int32_t* page_table;
-    const float* norms;
+    const float* norms;                            // minus the reference, then 1 / l
     float* weights;
-    float* sums;                                   // [2 blocks][2 streams][128]
+    float* sums;                                   // [2 blocks][2 key tiles][128]
     int32_t* counters;
     int32_t* status;
     int pages_per_unit, total_pages, capacity, add;
@@ -111,13 +114,18 @@ struct Walk {
     }
 };
 
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
+    float x0, x1;
+    unpack2(x, x0, x1);
+    return pack2(fast_exp2(x0), fast_exp2(x1));
+}
+
 __global__ void __launch_bounds__(kThreads, 1)
 weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ WeighParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ Bars bars;
     __shared__ uint32_t tmem_slot;
-    __shared__ int abort_word, last_flag[2][4];
-    __shared__ float halves[2][kTile];
+    __shared__ int abort_word, last_flag[4];
     volatile int* abort_flag = &abort_word;
     const ChunkPlan& ch = p.chunk;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -130,14 +138,12 @@ weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             mbar_init(&bars.k_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            for (int b = 0; b < 2; ++b) {
-                mbar_init(&bars.s_full[i][b], 1);
-                mbar_init(&bars.s_empty[i][b], kStreamWarps);
-            }
+            mbar_init(&bars.s_full[i], 1);
+            mbar_init(&bars.s_empty[i], kExpWarps);
         }
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&bars.full[i], 1);
-            mbar_init(&bars.empty[i], 1 + 2 * kStreamWarps);       // the products, and everyone who reads the norms
+            mbar_init(&bars.empty[i], 1 + kExpWarps);       // the products, and everyone who reads the norms
         }
         mbar_init(&bars.drain, 1);
         abort_word = 0;
@@ -235,22 +241,22 @@ weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             for (int t = pc.q0; t < pc.q1 && ok; ++t) {
                 const uint32_t st = rr.stage(kRing), buf = sr.stage(2);
                 wait_on(&bars.full[st], rr.parity(kRing));
-                for (int s = 0; s < 2; ++s) {
-                    wait_on(&bars.s_empty[s][buf], sr.parity(2) ^ 1u);
-                    tmem_fence_after_sync();
-                    if (ok && elect_one()) {
+                wait_on(&bars.s_empty[buf], sr.parity(2) ^ 1u);
+                tmem_fence_after_sync();
+                if (ok && elect_one()) {
+                    for (int s = 0; s < 2; ++s) {
                         const uint64_t a = k_desc + ks[s] * kStep, b = q_desc + st * kStep;
 #pragma unroll
                         for (int s8 = 0; s8 < 8; ++s8) {
                             const uint32_t off = ((s8 >> 2) * kBoxBytes + (s8 & 3) * 32) >> 4;
-                            umma_bf16(tmem_base + (s * 2 + buf) * 128, a + off, b + off, instr_desc(false), s8 > 0);
+                            umma_bf16(tmem_base + (buf * 2 + s) * 128, a + off, b + off, instr_desc(false), s8 > 0);
                         }
-                        umma_commit(&bars.s_full[s][buf]);
-                        if (s == 1) umma_commit(&bars.empty[st]);
                         if (t + 1 == pc.q1) umma_commit(&bars.k_empty[ks[s]]);
                     }
-                    __syncwarp();
+                    umma_commit(&bars.s_full[buf]);
+                    umma_commit(&bars.empty[st]);
                 }
+                __syncwarp();
                 ++rr.count;
                 ++sr.count;
             }
@@ -261,10 +267,11 @@ weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         wait_bar(&bars.drain, 0, abort_flag, p.status, limit, false);
     } else {
         // ------------------------------------------------------------------ exponentials
-        // Accumulator row = TMEM lane = key; the warps w and w + 4 of a stream share 32 keys and take 64 of the 128 rows each.
-        const int s = warp / kStreamWarps, hf = (warp >> 2) & 1, quarter = warp & 3, row = 32 * quarter + lane;
-        const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16);
-        const int pair_bar = 1 + s * 4 + quarter;
+        // Accumulator row = TMEM lane = key; a thread takes key `row` of both tiles and 32 of the 128 rows of the chunk, so that what it
+        // fetches of the rows serves two exponentials.
+        const int cq = warp >> 2, quarter = warp & 3, row = 32 * quarter + lane;
+        const uint32_t lane_base = tmem_base + ((uint32_t)(32 * quarter) << 16) + 32 * cq;
+        const int quad_bar = 1 + quarter;
         bool dead = false;
         auto wait_on = [&](uint64_t* bar, uint32_t parity) {
             const bool gave_up = dead || !wait_bar(bar, parity, abort_flag, p.status, limit);
@@ -273,106 +280,122 @@ weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         Ring rr, sr;
         const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
         const int n = ch.context + ch.tokens;
+        float* parts = reinterpret_cast<float*>(smem + kOffParts) + row;       // [cq - 1][tile][128]
         while (walk.more()) {
             const Piece pc = walk.next(p);
-            const int key0 = (2 * pc.pair + s) * kTile + 32 * quarter;         // of this warp
-            uint64_t sum0 = pack2(0.f, 0.f), sum1 = sum0;
-            float alone = 0.f;                                                 // (rows taken one by one)
+            const int key0 = 2 * pc.pair * kTile + 32 * quarter;               // of this warp, in the first tile; kTile further in the second
+            float sum[2] = {0.f, 0.f};
             for (int t = pc.q0; t < pc.q1; ++t) {
                 const uint32_t st = rr.stage(kRing), buf = sr.stage(2);
                 wait_on(&bars.full[st], rr.parity(kRing));                      // (the norms)
-                wait_on(&bars.s_full[s][buf], sr.parity(2));
+                wait_on(&bars.s_full[buf], sr.parity(2));
                 tmem_fence_after_sync();
-                const float* norm = reinterpret_cast<const float*>(smem + kOffNorms + st * kNormBytes) + 64 * hf;
-                const uint32_t cols = lane_base + (s * 2 + buf) * 128 + 64 * hf;
-                const int tok0 = t * ch.tile_tokens, rows = min(ch.tile_tokens, ch.tokens - tok0) * ch.group;
-                // rows [from, rows) see this thread's key; [0, rows) all keys of the warp when the last one lies before the tile
-                const bool all = key0 + 31 <= ch.context + tok0;
-                const int from = (key0 + lane - ch.context - tok0) * ch.group;
-                const bool none = key0 >= n || (key0 - ch.context - tok0) * ch.group >= rows;
-#pragma unroll 1
-                for (int c = 0; c < 64; c += 32) {
-                    const int col = 64 * hf + c;
-                    if (none || col >= rows) break;
-                    float v[32];
-                    tmem_ld32(cols + c, v);
+                const float* norm = reinterpret_cast<const float*>(smem + kOffNorms + st * kNormBytes) + 32 * cq;
+                const int tok0 = t * ch.tile_tokens, rows = min(ch.tile_tokens, ch.tokens - tok0) * ch.group - 32 * cq;
+                // Columns [0, rows) are rows of the chunk.  All of them see all keys of the warp in a tile that ends before them; none sees
+                // keys behind the last token.
+                if (rows > 0) {
+                    float v[2][32];
+                    tmem_ld32(lane_base + buf * 256, v[0]);
+                    tmem_ld32(lane_base + buf * 256 + 128, v[1]);
                     tmem_wait_ld();
-                    // (sums of 32 rows first: short chains of additions)
-                    if (all && col + 32 <= rows) {
-                        uint64_t c0 = pack2(0.f, 0.f), c1 = c0;
+                    if (key0 + kTile + 31 <= ch.context + tok0 && rows >= 32) {
+                        uint64_t c0[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)}, c1[2] = {c0[0], c0[0]};       // (sums of 32 rows first: short chains)
 #pragma unroll
                         for (int i = 0; i < 32; i += 4) {
-                            const float4 m = *reinterpret_cast<const float4*>(norm + c + i), f = *reinterpret_cast<const float4*>(norm + kTile + c + i);
-                            float e0, e1, e2, e3;
-                            unpack2(fma2(pack2(v[i], v[i + 1]), scale2, pack2(-m.x, -m.y)), e0, e1);
-                            unpack2(fma2(pack2(v[i + 2], v[i + 3]), scale2, pack2(-m.z, -m.w)), e2, e3);
-                            c0 = fma2(pack2(fast_exp2(e0), fast_exp2(e1)), pack2(f.x, f.y), c0);
-                            c1 = fma2(pack2(fast_exp2(e2), fast_exp2(e3)), pack2(f.z, f.w), c1);
-                        }
-                        sum0 = add2(sum0, c0);
-                        sum1 = add2(sum1, c1);
-                    } else {
-                        float some = 0.f;
+                            const float4 m = *reinterpret_cast<const float4*>(norm + i), f = *reinterpret_cast<const float4*>(norm + kTile + i);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float w = fast_exp2(fmaf(v[i], p.scale_log2, -norm[c + i])) * norm[kTile + c + i];
-                            some += col + i >= from && col + i < rows ? w : 0.f;
+                            for (int s = 0; s < 2; ++s) {
+                                const uint64_t x0 = fma2(pack2(v[s][i], v[s][i + 1]), scale2, pack2(m.x, m.y));
+                                const uint64_t x1 = fma2(pack2(v[s][i + 2], v[s][i + 3]), scale2, pack2(m.z, m.w));
+                                c0[s] = fma2(exp2_pair(x0), pack2(f.x, f.y), c0[s]);
+                                c1[s] = fma2(exp2_pair(x1), pack2(f.z, f.w), c1[s]);
+                            }
                         }
-                        alone += some;
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            float a0, a1;
+                            unpack2(add2(c0[s], c1[s]), a0, a1);
+                            sum[s] += a0 + a1;
+                        }
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            const int key = key0 + s * kTile;
+                            const int from = (key + lane - ch.context - tok0) * ch.group - 32 * cq;     // rows [from, rows) see this thread's key
+                            if (key >= n || (key - ch.context - tok0) * ch.group - 32 * cq >= rows) continue;
+                            float some = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const float w = fast_exp2(fmaf(v[s][i], p.scale_log2, norm[i])) * norm[kTile + i];
+                                some += i >= from && i < rows ? w : 0.f;
+                            }
+                            sum[s] += some;
+                        }
                     }
                 }
                 tmem_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(&bars.s_empty[s][buf]);
+                    mbar_arrive(&bars.s_empty[buf]);
                     mbar_arrive(&bars.empty[st]);
                 }
                 ++rr.count;
                 ++sr.count;
             }
-            float a0, a1, mine;
-            unpack2(add2(sum0, sum1), a0, a1);
-            mine = a0 + a1 + alone;
-            if (hf) halves[s][row] = mine;
-            named_barrier_sync(pair_bar, 64);
-            const bool whole = pc.q1 - pc.q0 == pc.tiles - pc.first;
-            const int key = key0 + lane;
-            auto put = [&](float sum) {
-                const long long at = (long long)pc.unit * p.capacity + key;
-                if (key < n && in_bounds(key < p.capacity, p.status)) p.weights[at] = (p.add ? p.weights[at] : 0.f) + sum * p.inv_group;
-            };
-            if (!hf) mine += halves[s][row];
-            if (whole) {
-                if (!hf) put(mine);
-            } else if (!hf) {
-                // the last block of the item to come here adds the sums of all, in order
-                auto slot_of = [&](int block, int first_step) {
-                    return ((2 * block + (first_step == part_begin(p.plan, block) ? 0 : 1)) * 2 + s) * kTile + row;
-                };
-                const int first_block = block_of(p.plan, pc.start);
-                const int blocks = block_of(p.plan, pc.start + pc.tiles - pc.first - 1) - first_block + 1;
-                p.sums[slot_of(blockIdx.x, pc.start + pc.q0 - pc.first)] = mine;
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) {
-                    int* counter = p.counters + (first_block * 2 + s) * 4 + quarter;
-                    const bool last = atomicAdd(counter, 1) == blocks - 1;
-                    if (last) *counter = 0;                    // (for the next launch)
-                    last_flag[s][quarter] = last;
-                }
-                __syncwarp();
-                if (last_flag[s][quarter]) {
-                    __threadfence();
-                    float sum = 0.f;
-                    for (int b = 0; b < blocks; ++b) {
-                        const int block = first_block + b;
-                        sum += __ldcg(&p.sums[slot_of(block, b == 0 ? pc.start : part_begin(p.plan, block))]);
-                    }
-                    put(sum);
-                }
-                __syncwarp();
+            // the four warps of 32 keys: one adds up
+            if (cq > 0) {
+                parts[(cq - 1) * 2 * kTile] = sum[0];
+                parts[(cq - 1) * 2 * kTile + kTile] = sum[1];
             }
-            named_barrier_sync(pair_bar, 64);              // (halves may be written again)
+            named_barrier_sync(quad_bar, 128);
+            if (cq == 0) {
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    sum[0] += parts[q * 2 * kTile];
+                    sum[1] += parts[q * 2 * kTile + kTile];
+                }
+                const bool whole = pc.q1 - pc.q0 == pc.tiles - pc.first;
+                auto put = [&](int s, float total) {
+                    const int key = key0 + s * kTile + lane;
+                    const long long at = (long long)pc.unit * p.capacity + key;
+                    if (key < n && in_bounds(key < p.capacity, p.status)) p.weights[at] = (p.add ? p.weights[at] : 0.f) + total * p.inv_group;
+                };
+                if (whole) {
+                    put(0, sum[0]);
+                    put(1, sum[1]);
+                } else {
+                    // the last block of the item to come here adds the sums of all, in order
+                    auto slot_of = [&](int block, int first_step) { return (2 * block + (first_step == part_begin(p.plan, block) ? 0 : 1)) * 2 * kTile + row; };
+                    const int first_block = block_of(p.plan, pc.start);
+                    const int blocks = block_of(p.plan, pc.start + pc.tiles - pc.first - 1) - first_block + 1;
+                    float* own = p.sums + slot_of(blockIdx.x, pc.start + pc.q0 - pc.first);
+                    own[0] = sum[0];
+                    own[kTile] = sum[1];
+                    __threadfence();
+                    __syncwarp();
+                    if (lane == 0) {
+                        int* counter = p.counters + first_block * 4 + quarter;
+                        const bool last = atomicAdd(counter, 1) == blocks - 1;
+                        if (last) *counter = 0;                    // (for the next launch)
+                        last_flag[quarter] = last;
+                    }
+                    __syncwarp();
+                    if (last_flag[quarter]) {
+                        __threadfence();
+                        float total[2] = {0.f, 0.f};
+                        for (int b = 0; b < blocks; ++b) {
+                            const float* from = p.sums + slot_of(first_block + b, b == 0 ? pc.start : part_begin(p.plan, first_block + b));
+                            total[0] += __ldcg(from);
+                            total[1] += __ldcg(from + kTile);
+                        }
+                        put(0, total[0]);
+                        put(1, total[1]);
+                    }
+                    __syncwarp();
+                }
+            }
+            named_barrier_sync(quad_bar, 128);             // (the parts may be written again)
         }
     }
 

@@ -522,6 +522,41 @@ def test_sparse_ties_go_to_the_older_block_and_all_blocks_are_attend():
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("n", [64 * 200 + 3, 64 * 700 + 3])       # scored by a unit's own block of threads, by many
+@pytest.mark.parametrize("kind", ["no queries", "close", "many close", "far apart", "infinite", "negative"])
+def test_sparse_scores_near_the_cut(n, kind):
+    """Blocks whose scores are equal, closer than float32 tells apart, or of very different size: the choice is that of 64 bits."""
+    g = gen(23)
+    L, B, Hq, Hkv, blocks = 1, 2, 8, 2, 70
+    last = (n - 1) // 64
+    k = randn(g, L, B, Hkv, n, D)
+    q = randn(g, L, B, Hq, D)
+    if kind == "no queries":
+        q.zero_()
+    elif kind in ("close", "many close"):
+        # large equal parts and differences of 2^-30 of them in one dimension
+        k[:] = 0
+        k[..., 0] = 256.0
+        q[:] = 0
+        q[..., 0], q[..., 1] = 256.0, 2.0 ** -7
+        some = last if kind == "many close" else 100
+        step = torch.randint(1, 200, (L, B, Hkv, some), generator=g, device="cuda").to(torch.bfloat16) * 2.0 ** -9
+        k[:, :, :, :some * 64, 1] = step.repeat_interleave(64, -1)
+        k[:, :, :, some * 64:, 0] = 128.0
+    elif kind == "far apart":
+        k *= torch.exp(6 * torch.randn(L, B, Hkv, n // 64 + 1, generator=g, device="cuda")).repeat_interleave(64, -1)[..., :n, None].to(torch.bfloat16)
+    elif kind == "infinite":
+        k[:, :, :, 64 * 5 + 3, 7] = float("inf")
+        k[:, :, :, 64 * 9 + 3, 7] = float("-inf")
+    else:
+        k, q = -k.abs() - 1, q.abs()
+    e, k, v = loaded(g, L, B, Hq, Hkv, n, k=k.contiguous())
+    sel = torch.full((L * B * Hkv, blocks), 99, dtype=torch.int32, device="cuda")
+    e.attend_sparse(q, torch.empty_like(q), blocks, sel)
+    e.synchronize()
+    assert np.array_equal(sel.cpu().numpy(), sparse_ref(q, k, v, blocks)[2])
+
+
 def test_sparse_follows_the_cache():
     """Bounds of blocks that fill while decoding, after an eviction, after a reset, after a fork; pages that a caller has written."""
     g = gen(15)
