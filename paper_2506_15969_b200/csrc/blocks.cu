@@ -114,20 +114,21 @@ __device__ __forceinline__ double exact_score(const uint4* rows, const Sides& s,
     return v;
 }
 
-constexpr int kBatch = 8;                  // blocks of a warp in flight
+constexpr int kBatch = 8;                  // blocks that a warp sums at once; as many are under way
 // An fp32 score is off by less than this of the sum of its terms' magnitudes: P rounded, eight products and five sums, 14 roundings
 // of 2^-24, with room.
 constexpr float kRoughError = 1.f / (1 << 19);
 
-// Rough scores of blocks b0 .. b0 + 7: lane 4 i + j, any j, gets that of block b0 + i.  The eight sums over the lanes are folded into
+// Rough scores of kBatch blocks, that of the i-th in the i-th kBatch-th of the lanes.  The sums over the lanes are folded into
 // each other: half of them go to the other half of the lanes at every step, nine exchanges instead of forty.  `size` grows to the
 // largest sum of magnitudes that this lane's dimensions had.
-__device__ __forceinline__ float rough_batch(const uint4* rows, const float (&side)[8], int b0, int count, float& size) {
-    const int lane = threadIdx.x & 31;
-    uint4 x[kBatch];
+__device__ __forceinline__ void load_batch(const uint4* rows, int b0, int count, uint4 (&x)[kBatch]) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i)
-        x[i] = b0 + i < count ? __ldg(rows + (size_t)(b0 + i) * 2 * kChunksPerRow + lane) : make_uint4(0u, 0u, 0u, 0u);
+        x[i] = b0 + i < count ? __ldg(rows + (size_t)(b0 + i) * 2 * kChunksPerRow + (threadIdx.x & 31)) : make_uint4(0u, 0u, 0u, 0u);
+}
+__device__ __forceinline__ float rough_batch(const uint4 (&x)[kBatch], const float (&side)[8], float& size) {
+    const int lane = threadIdx.x & 31;
     float v[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
@@ -145,7 +146,7 @@ __device__ __forceinline__ float rough_batch(const uint4* rows, const float (&si
         size = all > size || all != all ? all : size;
     }
 #pragma unroll
-    for (int half = 4, bit = 16; half > 0; half >>= 1, bit >>= 1) {
+    for (int half = kBatch / 2, bit = 16; half > 0; half >>= 1, bit >>= 1) {
         const bool up = lane & bit;
 #pragma unroll
         for (int i = 0; i < half; ++i) {
@@ -153,8 +154,8 @@ __device__ __forceinline__ float rough_batch(const uint4* rows, const float (&si
             v[i] = own + __shfl_xor_sync(0xffffffffu, give, bit);
         }
     }
-    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
-    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+#pragma unroll
+    for (int bit = 16 / kBatch; bit > 0; bit >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], bit);
     return v[0];
 }
 
@@ -167,21 +168,29 @@ __device__ __forceinline__ float rough_scores(const BlocksArgs& a, int u, int co
 #pragma unroll
     for (int i = 0; i < 8; ++i) side[i] = (float)s.part[i];
     const uint4* rows = bound_rows(a, u);
-    for (; b0 < count; b0 += step) {
-        const float score = rough_batch(rows, side, b0, count, size);
-        const int b = b0 + (lane >> 2);
-        if ((lane & 3) == 0 && b < count) put(b, rough_key(score));
+    uint4 x[2][kBatch];
+    load_batch(rows, b0, count, x[0]);
+    auto batch = [&](int i) {                              // (the next one is under way while one is summed)
+        load_batch(rows, b0 + step, count, x[i ^ 1]);
+        const float score = rough_batch(x[i], side, size);
+        const int b = b0 + lane / (32 / kBatch);
+        if (lane % (32 / kBatch) == 0 && b < count) put(b, rough_key(score));
+        b0 += step;
+    };
+    while (b0 < count) {
+        batch(0);
+        if (b0 < count) batch(1);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) size += __shfl_xor_sync(0xffffffffu, size, o);
     return size;
 }
 
-constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
 constexpr int kCachedKeys = 16384;         // of a unit in shared memory; of longer caches they stay in L2
-// Up to here a unit's own block of threads scores them; behind it, where units are too few to fill the GPU, a launch over many.
-constexpr int kScoreAlone = 256;
 constexpr int kScoreWarps = 8;
+// Up to here, and where there are units for half of the SMs, a unit's own block of threads scores its blocks; else many score first.
+// (256 units of 1024 blocks, whole call: 50 us alone, 64 with a launch of its own; 2 units of 1024: 28.7 and 22.6; 128 of 255: 20.9, 22.5.)
+constexpr int kScoreAlone = 256;
 
 // a.rough: per unit pages_per_unit rough keys, and behind them one sum of magnitudes per warp of this launch.
 __global__ void __launch_bounds__(32 * kScoreWarps) score_kernel(BlocksArgs a, int count) {
@@ -196,12 +205,14 @@ __global__ void __launch_bounds__(32 * kScoreWarps) score_kernel(BlocksArgs a, i
 // rough scores in fp32: with E the most that one is off, a block more than 2 E above the rough cut is above the exact one and a
 // block more than 2 E below it below, and only those between are scored in fp64 -- a handful, or, where scores are no numbers or
 // alike, up to all.  score_warps = 0: the scores are made here.
-__global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int count, int picked, int asked, int score_warps) {
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads) pick_kernel(BlocksArgs a, int count, int picked, int asked, int score_warps) {
+    constexpr int kWarps = kThreads / 32;
     extern __shared__ uint32_t cached[];
     __shared__ TopShared<unsigned long long> wide;
     TopShared<uint32_t>& sh = *reinterpret_cast<TopShared<uint32_t>*>(&wide);      // (one select after the other)
-    __shared__ uint32_t least[kPickWarps], most[kPickWarps];
-    __shared__ float sizes[kPickWarps];
+    __shared__ uint32_t least[kWarps], most[kWarps];
+    __shared__ float sizes[kWarps];
     __shared__ int between[kSurvivors];
     __shared__ unsigned long long exact[kSurvivors];
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -217,13 +228,13 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int co
     };
     float size = 0.f;
     if (chosen && score_warps == 0) {
-        size = rough_scores(a, u, count, warp * kBatch, kPickWarps * kBatch, [&](int b, uint32_t key) { keys[b] = key; });
+        size = rough_scores(a, u, count, warp * kBatch, kWarps * kBatch, [&](int b, uint32_t key) { keys[b] = key; });
     } else {
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (chosen) {
             if (keys == cached)
-                for (int i = tid; i < count; i += kPickThreads) cached[i] = __ldcg(stored + i);
-            for (int i = tid; i < score_warps; i += kPickThreads) {
+                for (int i = tid; i < count; i += kThreads) cached[i] = __ldcg(stored + i);
+            for (int i = tid; i < score_warps; i += kThreads) {
                 const float s = __ldcg(reinterpret_cast<const float*>(stored) + a.geo.pages_per_unit + i);
                 size = s > size || s != s ? s : size;
             }
@@ -235,41 +246,54 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int co
         }
     }
     if (picked == count) {                                  // all of them
-        for (int b = tid; b < count; b += kPickThreads) put(b, b);
+        for (int b = tid; b < count; b += kThreads) put(b, b);
     } else if (chosen) {
         if (lane == 0) sizes[warp] = size;
         __syncthreads();
-        // Scores of a unit are mostly of one magnitude: counted from the least one, the leading digits of their keys differ.
-        uint32_t lo = ~0u, hi = 0u;
-        for (int i = tid; i < count; i += kPickThreads) {
-            lo = min(lo, keys[i]);
-            hi = max(hi, keys[i]);
-        }
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        if (lane == 0) {
-            least[warp] = lo;
-            most[warp] = hi;
-        }
-        __syncthreads();
-        for (int w = 0; w < kPickWarps; ++w) {
-            lo = min(lo, least[w]);
-            hi = max(hi, most[w]);
-            size = sizes[w] > size || sizes[w] != sizes[w] ? sizes[w] : size;
-        }
-        const Cut<uint32_t> cut = top_cut<kPickThreads, uint32_t>(count, picked, 32 - __clz(hi - lo), sh, [&](int i) { return keys[i] - lo; });
-        // (the cut may lie between two keys: the k-th is the least one above it)
-        uint32_t kth = cut.kth + lo;
-        if (cut.ties == 0) {
-            uint32_t next = ~0u;
-            for (int i = tid; i < count; i += kPickThreads)
-                if (keys[i] > kth) next = min(next, keys[i]);
-            next = __reduce_min_sync(0xffffffffu, next);
+        for (int w = 0; w < kWarps; ++w) size = sizes[w] > size || sizes[w] != sizes[w] ? sizes[w] : size;
+        uint32_t kth;
+        if (count <= kThreads) {                            // few: ranked one against the other
+            int above = 0, equal = 0;
+            const uint32_t mine = tid < count ? keys[tid] : 0u;
+            for (int j = 0; j < count; ++j) {
+                above += keys[j] > mine;
+                equal += keys[j] == mine;
+            }
+            if (tid < count && above < picked && picked <= above + equal) least[0] = mine;
             __syncthreads();
-            if (lane == 0) least[warp] = next;
+            kth = least[0];
+        } else {
+            // Scores of a unit are mostly of one magnitude: counted from the least one, the leading digits of their keys differ.
+            uint32_t lo = ~0u, hi = 0u;
+            for (int i = tid; i < count; i += kThreads) {
+                lo = min(lo, keys[i]);
+                hi = max(hi, keys[i]);
+            }
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            if (lane == 0) {
+                least[warp] = lo;
+                most[warp] = hi;
+            }
             __syncthreads();
-            for (int w = 0; w < kPickWarps; ++w) next = min(next, least[w]);
-            kth = next;
+            for (int w = 0; w < kWarps; ++w) {
+                lo = min(lo, least[w]);
+                hi = max(hi, most[w]);
+            }
+            const Cut<uint32_t> cut = top_cut<kThreads, uint32_t>(count, picked, 32 - __clz(hi - lo), sh, [&](int i) { return keys[i] - lo; });
+            // (the cut may lie between two keys: the k-th is the least one above it)
+            kth = cut.kth + lo;
+            if (cut.ties == 0) {
+                uint32_t next = ~0u;
+                for (int i = tid; i < count; i += kThreads)
+                    if (keys[i] > kth) next = min(next, keys[i]);
+                next = __reduce_min_sync(0xffffffffu, next);
+                __syncthreads();
+                if (lane == 0) least[warp] = next;
+                __syncthreads();
+                for (int w = 0; w < kWarps; ++w) next = min(next, least[w]);
+                kth = next;
+            }
         }
         const float t = rough_score(kth), reach = 2.f * kRoughError * size;
         // 1: above whatever the exact scores are, 0: below, 2: between (all of them where something is no number or infinite)
@@ -280,28 +304,28 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int co
             return s > t + reach ? 1 : s < t - reach ? 0 : 2;
         };
         int sure = 0, open = 0;
-        for (int i = tid; i < count; i += kPickThreads) {
+        for (int i = tid; i < count; i += kThreads) {
             const int side = side_of(keys[i]);
             sure += side == 1;
             open += side == 2;
         }
         int all_sure, all_open;
-        block_rank<kPickThreads>(sure, sh.warp_sums, &all_sure);
-        const int open_before = block_rank<kPickThreads>(open, sh.warp_sums, &all_open);
+        block_rank<kThreads>(sure, sh.warp_sums, &all_sure);
+        const int open_before = block_rank<kThreads>(open, sh.warp_sums, &all_open);
         const int need = picked - all_sure;
         // afterwards a key is ~0 for a block that is taken and 0 for one that is not
         if (all_open == need) {
-            for (int i = tid; i < count; i += kPickThreads) keys[i] = side_of(keys[i]) != 0 ? ~0u : 0u;
+            for (int i = tid; i < count; i += kThreads) keys[i] = side_of(keys[i]) != 0 ? ~0u : 0u;
         } else if (all_open <= kSurvivors) {
             int at = open_before;
-            for (int i = tid; i < count; i += kPickThreads) {
+            for (int i = tid; i < count; i += kThreads) {
                 const int side = side_of(keys[i]);
                 if (side == 2 && at < kSurvivors) between[at++] = i;
                 keys[i] = side == 1 ? ~0u : 0u;
             }
             __syncthreads();
             const Sides s = sides_of(a, u);
-            for (int i = warp; i < all_open; i += kPickWarps) {
+            for (int i = warp; i < all_open; i += kWarps) {
                 const unsigned long long key = exact_key(exact_score(bound_rows(a, u), s, between[i]));
                 if (lane == 0) exact[i] = key;
             }
@@ -315,16 +339,16 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int co
             // many: all their exact keys, and a select over those (0 is no exact key)
             const Sides s = sides_of(a, u);
             unsigned long long* exacts = a.exact + (size_t)u * a.geo.pages_per_unit;
-            for (int i = warp; i < count; i += kPickWarps) {
+            for (int i = warp; i < count; i += kWarps) {
                 const unsigned long long key = side_of(keys[i]) == 2 ? exact_key(exact_score(bound_rows(a, u), s, i)) : 0ull;
                 if (lane == 0) exacts[i] = key;
             }
             __syncthreads();
-            const Cut<unsigned long long> last = top_cut<kPickThreads, unsigned long long>(count, need, 64, wide, [&](int i) { return exacts[i]; });
-            const int per = (count + kPickThreads - 1) / kPickThreads, from = min(count, tid * per), till = min(count, from + per);
+            const Cut<unsigned long long> last = top_cut<kThreads, unsigned long long>(count, need, 64, wide, [&](int i) { return exacts[i]; });
+            const int per = (count + kThreads - 1) / kThreads, from = min(count, tid * per), till = min(count, from + per);
             int ties = 0;
             for (int i = from; i < till; ++i) ties += exacts[i] == last.kth;
-            int total, tie = block_rank<kPickThreads>(ties, sh.warp_sums, &total);
+            int total, tie = block_rank<kThreads>(ties, sh.warp_sums, &total);
             for (int i = from; i < till; ++i) {             // of equals the older
                 const bool take = side_of(keys[i]) == 1 || exacts[i] > last.kth || (exacts[i] == last.kth && tie < last.ties);
                 tie += exacts[i] == last.kth;
@@ -332,11 +356,11 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int co
             }
         }
         __syncthreads();
-        const int seg = ((count + kPickWarps - 1) / kPickWarps + 31) / 32 * 32;
+        const int seg = ((count + kWarps - 1) / kWarps + 31) / 32 * 32;
         const int seg_b = min(count, warp * seg), seg_e = min(count, seg_b + seg);
         int kept = 0, all;
         for (int i0 = seg_b; i0 < seg_e; i0 += 32) kept += __popc(__ballot_sync(0xffffffffu, i0 + lane < seg_e && keys[min(i0 + lane, count - 1)] != 0u));
-        int dst = __shfl_sync(0xffffffffu, block_rank<kPickThreads>(lane == 0 ? kept : 0, sh.warp_sums, &all), 0);
+        int dst = __shfl_sync(0xffffffffu, block_rank<kThreads>(lane == 0 ? kept : 0, sh.warp_sums, &all), 0);
         for (int i0 = seg_b; i0 < seg_e; i0 += 32) {
             const bool keep = i0 + lane < seg_e && keys[min(i0 + lane, count - 1)] != 0u;
             const unsigned keep_mask = __ballot_sync(0xffffffffu, keep);
@@ -348,7 +372,7 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BlocksArgs a, int co
     }
     if (tid == 0) put(picked, count);
     if (list)
-        for (int j = picked + 1 + tid; j < asked; j += kPickThreads) list[j] = -1;
+        for (int j = picked + 1 + tid; j < asked; j += kThreads) list[j] = -1;
 }
 
 }  // namespace
@@ -361,7 +385,7 @@ cudaError_t bounds_launch(const BlocksArgs& a, int first, int count, int num_sms
 }
 
 cudaError_t blocks_prepare() {
-    return cudaFuncSetAttribute(pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kCachedKeys * (int)sizeof(uint32_t));
+    return cudaFuncSetAttribute(pick_kernel<512>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCachedKeys * (int)sizeof(uint32_t));
 }
 
 cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, int num_sms, int* launches, cudaStream_t stream) {
@@ -369,7 +393,7 @@ cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, i
     const bool chosen = picked > 0 && picked < count;
     int score_warps = 0;
     if (chosen && count > kScoreAlone && a.geo.units < num_sms / 2) {
-        // (far from the limit of a grid's second dimension; the warps' sums fit behind the keys)
+        // Too few units to fill the GPU with a block of threads each: many score, then one each picks.  (Far from the limit of a grid's second dimension; the warps' sums fit behind the keys)
         const int per = kScoreWarps * kBatch, most = (4 * num_sms + a.geo.units - 1) / a.geo.units, parts = (count + per - 1) / per;
         const dim3 grid(parts < most ? parts : most, a.geo.units);
         score_warps = (int)grid.x * kScoreWarps;
@@ -383,12 +407,13 @@ cudaError_t pick_launch(const BlocksArgs& a, int count, int picked, int asked, i
     beside.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(a.geo.units);
-    c.blockDim = dim3(kPickThreads);
+    const int threads = count <= 128 ? 128 : count <= 256 ? 256 : 512;     // (a key each, where they are few)
+    c.blockDim = dim3(threads);
     c.dynamicSmemBytes = chosen && count <= kCachedKeys ? (size_t)count * sizeof(uint32_t) : 0;
     c.stream = stream;
     c.attrs = &beside;
     c.numAttrs = score_warps > 0 ? 1 : 0;      // begins beside the end of the scores
-    return cudaLaunchKernelEx(&c, pick_kernel, a, count, picked, asked, score_warps);
+    return cudaLaunchKernelEx(&c, threads == 128 ? pick_kernel<128> : threads == 256 ? pick_kernel<256> : pick_kernel<512>, a, count, picked, asked, score_warps);
 }
 
 }  // namespace lzk
