@@ -55,6 +55,7 @@ struct lazyev {
     int weights_on = 0;
     float* weights = nullptr;              // [units][capacity], behind the status word in the state region
     int32_t* counters = nullptr;           // scratch of the chunk kernels, zero between launches: [2][kChunkCounters]
+    bool counted = false;                  // since they were cleared
     PrefixPool own_pool = {};              // the own pool as the chunk kernels address it
     uint8_t* block_space = nullptr;        // lazyev_set_block_workspace()
     int indexed = 0;                       // blocks, from the first on, whose bounds are in it
@@ -981,8 +982,9 @@ int lazyev_reset(lazyev_t* h) {
     // Old rows stay in the pool: slots past n are masked, they only have to be finite.  The state arrays
     // are rewritten by the next prompt load and by every append; the device status word is cleared.
     cudaError_t e = cudaMemsetAsync(h->st.status, 0, 64, h->stream);
-    if (e == cudaSuccess) e = cudaMemsetAsync(h->counters, 0, 2 * kChunkCounters * sizeof(int32_t), h->stream);
+    if (e == cudaSuccess && h->counted) e = cudaMemsetAsync(h->counters, 0, 2 * kChunkCounters * sizeof(int32_t), h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "clearing the device status word");
+    h->counted = false;                     // (a launch that gave up may have left counts behind)
     h->indexed = 0;
     h->prefilled = false;
     h->t = h->n = h->prefill = h->pos_base = 0;
@@ -1509,6 +1511,7 @@ int lazyev_attend_chunk(lazyev_t* h, const lazyev_rows_t* q, int n_tokens, const
     a.status = h->st.status;
     a.wait_limit_ns = h->wait_limit_ns;
     a.stop_after_tiles = h->stop_after_pages;
+    h->counted = true;
     cudaError_t e = chunk_launch(plan, a, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "chunk kernel launch");
     h->launches += 1;

@@ -10,7 +10,6 @@ namespace lzk {
 
 namespace {
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kCachedKeys = 40 * 1024;     // keys of a unit kept in shared memory; longer caches read theirs from L2 in every pass
 
 // Orders like the weights; what is no number counts as heavier than any.
@@ -23,8 +22,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 // One block per unit.  Three passes over 4 bytes per candidate find the cut (fewer when keys are few), two more write the list; the
 // bytes are read from HBM once.
-template <bool kCached>
+template <int kThreads, bool kCached>
 __global__ void __launch_bounds__(kThreads) weigh_select_kernel(Geometry geo, StateView st, const float* weights, EvictArgs a) {
+    constexpr int kWarps = kThreads / 32;
     extern __shared__ uint32_t cached[];
     __shared__ TopShared<uint32_t> sh;
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kThreads) weigh_select_kernel(Geometry geo, St
     }
 }
 
-constexpr int kKeepThreads = 256, kRowsPerWarp = kPageTokens / (kKeepThreads / 32);
+constexpr int kKeepThreads = 512, kRowsPerWarp = kPageTokens / (kKeepThreads / 32);
 
 // One block per destination page: the rows of 64 tokens in flight at once, K in the lower half of each warp, V in the upper.
 // Bound by HBM: 528 bytes per kept token read and written, and its weight.
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(KeepArgs a) {
     int from[kRowsPerWarp];
 #pragma unroll
     for (int i = 0; i < kRowsPerWarp; ++i) {
-        const int d = d0 + warp + 8 * i;
+        const int d = d0 + warp + kKeepThreads / 32 * i;
         from[i] = d >= a.keep ? -1 : src ? src[d] : d;
         if (from[i] >= a.n) from[i] = -1;
     }
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(KeepArgs a) {
 #pragma unroll
     for (int i = 0; i < kRowsPerWarp; ++i) {
         if (from[i] < 0) continue;
-        const int dr = warp + 8 * i;
+        const int dr = warp + kKeepThreads / 32 * i;
         *reinterpret_cast<uint4*>(page + dr * kRowBytes + swz_chunk(cp ^ (from[i] & 7), dr) * 16) = val[i];
     }
     const int d = d0 + threadIdx.x;
@@ -133,12 +133,14 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(KeepArgs a) {
 }
 
 // One block per unit, destinations front to back: sources lie at or behind their destinations and ascend (as in compact_kernel).
-__global__ void __launch_bounds__(kThreads) compact_weights_kernel(Geometry geo, float* weights, EvictArgs a) {
+constexpr int kCompactThreads = 1024;
+
+__global__ void __launch_bounds__(kCompactThreads) compact_weights_kernel(Geometry geo, float* weights, EvictArgs a) {
     const int32_t* src = a.src + (size_t)blockIdx.x * a.budget;
     float* w = weights + (size_t)blockIdx.x * geo.capacity;
     const int first = a.first_moved[blockIdx.x];
     if (first < 0) return;
-    for (int d0 = first; d0 < a.budget; d0 += kThreads) {
+    for (int d0 = first; d0 < a.budget; d0 += kCompactThreads) {
         const int d = d0 + threadIdx.x, s = d < a.budget ? src[d] : -1;
         const float v = s >= 0 && s < a.n ? w[s] : 0.f;
         __syncthreads();
@@ -156,15 +158,20 @@ __global__ void weights_score_kernel(Geometry geo, const float* weights, int uni
 }  // namespace
 
 cudaError_t keep_prepare() {
-    return cudaFuncSetAttribute(weigh_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCachedKeys * (int)sizeof(uint32_t));
+    return cudaFuncSetAttribute(weigh_select_kernel<1024, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCachedKeys * (int)sizeof(uint32_t));
 }
 
 cudaError_t weigh_select_launch(const Geometry& geo, StateView st, const float* weights, const EvictArgs& a, cudaStream_t stream) {
     const int count = a.n - a.n_recent - a.n_initial;
-    if (count <= kCachedKeys)
-        weigh_select_kernel<true><<<geo.units, kThreads, (size_t)count * sizeof(uint32_t), stream>>>(geo, st, weights, a);
+    const size_t smem = (size_t)count * sizeof(uint32_t);
+    if (count <= 2048)
+        weigh_select_kernel<256, true><<<geo.units, 256, smem, stream>>>(geo, st, weights, a);
+    else if (count <= 8192)
+        weigh_select_kernel<512, true><<<geo.units, 512, smem, stream>>>(geo, st, weights, a);
+    else if (count <= kCachedKeys)
+        weigh_select_kernel<1024, true><<<geo.units, 1024, smem, stream>>>(geo, st, weights, a);
     else
-        weigh_select_kernel<false><<<geo.units, kThreads, 0, stream>>>(geo, st, weights, a);
+        weigh_select_kernel<1024, false><<<geo.units, 1024, 0, stream>>>(geo, st, weights, a);
     return cudaGetLastError();
 }
 
@@ -189,7 +196,7 @@ cudaError_t keep_launch(const KeepArgs& a, cudaStream_t stream) {
 }
 
 cudaError_t compact_weights_launch(const Geometry& geo, float* weights, const EvictArgs& a, cudaStream_t stream) {
-    compact_weights_kernel<<<geo.units, kThreads, 0, stream>>>(geo, weights, a);
+    compact_weights_kernel<<<geo.units, kCompactThreads, 0, stream>>>(geo, weights, a);
     return cudaGetLastError();
 }
 
