@@ -32,9 +32,9 @@
  *             memory free of ldmatrix bank conflicts.  Slot i of unit u lives
  *             in physical page page_table[u][i / 64], row i % 64.
  *   state   : page table, and per unit and slot: the pair (TS, MRI) as two int32 side by side,
- *             original position (int32), last probability (float32).
+ *             original position (int32), last probability (float32); with lazyev_set_weights() the weight (float32).
  *   scratch : eviction source lists, staging for the host-buffer entry point, score
- *             staging for lazyev_dump_state, the MRI histogram.
+ *             staging for lazyev_dump_state, the MRI histogram, counters of the chunk kernels.
  */
 #ifndef LAZYEV_H
 #define LAZYEV_H
@@ -600,7 +600,8 @@ int lazyev_mri_quantile(lazyev_t* h, int unit_begin, int unit_count, double frac
  *             one float probability written per token, queries read, outputs written
  *   select  : units * (8 * candidates + 4 * budget)       -- TS, MRI read; source list written
  *   compact : moved rows * (2 * (512 + 12) + 4)           -- rows and their state read and written
- * (Prefix and row launches are not among them.)
+ *   (LAZYEV_SCORE_WEIGHT: select reads 4 bytes per candidate)
+ * (Prefix, row, chunk and block launches, lazyev_evict_to() into another handle and the launches that keep weights are not among them.)
  * lazyev_get_profile() synchronises the stream; reset != 0 clears the sums.
  */
 typedef struct lazyev_profile {

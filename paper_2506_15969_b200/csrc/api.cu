@@ -55,7 +55,7 @@ struct lazyev {
     int weights_on = 0;
     float* weights = nullptr;              // [units][capacity], behind the status word in the state region
     int32_t* counters = nullptr;           // scratch of the chunk kernels, zero between launches: [2][kChunkCounters]
-    bool counted = false;                  // since they were cleared
+    bool counted = false;                  // such a kernel has been launched, or captured
     PrefixPool own_pool = {};              // the own pool as the chunk kernels address it
     uint8_t* block_space = nullptr;        // lazyev_set_block_workspace()
     int indexed = 0;                       // blocks, from the first on, whose bounds are in it
@@ -982,9 +982,9 @@ int lazyev_reset(lazyev_t* h) {
     // Old rows stay in the pool: slots past n are masked, they only have to be finite.  The state arrays
     // are rewritten by the next prompt load and by every append; the device status word is cleared.
     cudaError_t e = cudaMemsetAsync(h->st.status, 0, 64, h->stream);
+    // (a launch that gave up may have left counts behind, a replayed one too)
     if (e == cudaSuccess && h->counted) e = cudaMemsetAsync(h->counters, 0, 2 * kChunkCounters * sizeof(int32_t), h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "clearing the device status word");
-    h->counted = false;                     // (a launch that gave up may have left counts behind)
     h->indexed = 0;
     h->prefilled = false;
     h->t = h->n = h->prefill = h->pos_base = 0;
