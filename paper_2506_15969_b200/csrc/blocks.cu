@@ -81,9 +81,13 @@ __device__ __forceinline__ Sides sides_of(const BlocksArgs& a, int u) {
     const int lane = threadIdx.x & 31, c = lane & 15, G = a.geo.group;
     Sides s = {{0, 0, 0, 0, 0, 0, 0, 0}};
     const uint4* q = reinterpret_cast<const uint4*>(a.q) + (size_t)u * G * kChunksPerRow + c;
-    for (int g = 0; g < G; ++g) {
-        const uint4 x = q[g * kChunksPerRow];
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint4 x[kMaxGroup];                    // (all of them asked for at once)
+#pragma unroll
+    for (int g = 0; g < kMaxGroup; ++g) x[g] = g < G ? q[g * kChunksPerRow] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int g = 0; g < kMaxGroup; ++g) {
+        if (g >= G) break;
+        const uint32_t w[4] = {x[g].x, x[g].y, x[g].z, x[g].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float e0 = bf16_lo_as_float(w[i]), e1 = bf16_hi_as_float(w[i]);
@@ -222,8 +226,9 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(BlocksArgs a, int count,
     int32_t* list = a.selected ? a.selected + (size_t)u * asked : nullptr;
     uint32_t* keys = count <= kCachedKeys ? cached : stored;
     const bool chosen = picked > 0 && picked < count;
+    const int32_t own_page = tid <= count ? table[tid] : 0, last_page = table[count];      // (asked for before they are needed)
     auto put = [&](int j, int block) {
-        to[j] = table[block];
+        to[j] = block == tid ? own_page : block == count ? last_page : table[block];
         if (list) list[j] = block;
     };
     float size = 0.f;
