@@ -81,7 +81,7 @@ __host__ __device__ __forceinline__ int chunk_key_tiles(const ChunkPlan& p, int 
     return p.prefix_tiles + (p.context + (last < p.tokens ? last : p.tokens) + 127) / 128;
 }
 // Steps of an item in the walk: its key tiles, and what its beginning and end cost, in steps.
-constexpr int kChunkItemCost = 4;
+constexpr int kChunkItemCost = 3;
 __host__ __device__ __forceinline__ int chunk_item_steps(const ChunkPlan& p, int pair) { return chunk_key_tiles(p, pair) + kChunkItemCost; }
 
 struct RowView {           // head rows of 128 contiguous elements; strides in elements
