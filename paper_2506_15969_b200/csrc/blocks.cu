@@ -11,9 +11,11 @@
 // The newest block (the only one that may be partly filled) and the blocks - 1 best others, of equals the older, become a
 // page table of their own, in order, which the decode kernel reads like any other: K and V of blocks * 64 tokens instead of n.
 //
-//   bounds_kernel -- the bounds, once per block (keys behind the newest block do not change any more)
+//   bounds_kernel -- the bounds, once per block (keys behind the newest block do not change any more); HBM: 256 units of 16384 tokens,
+//                    1.07 GB, 166 us, 6.5 TB/s
 //   pick_kernel   -- one block of threads per unit: scores, radix select over them, page table, list.  512 bytes per block, a
-//                    warp per block, lanes 0-15 the high row, 16-31 the low one
+//                    warp per block, lanes 0-15 the high row, 16-31 the low one: 128 units of 2047 blocks 40 us, 3.4 TB/s, half of it
+//                    the select and the beginning
 //   score_kernel  -- the scores by many blocks of threads, for long caches of few units
 #include "internal.h"
 #include "select.cuh"

@@ -12,9 +12,20 @@
 // itself is written out directly; the sums of one that several blocks share go through memory, and the last of them
 // to arrive joins them, in the order of the keys (no second launch, and the same bits every time).
 //
-// P is one bf16 term (half a step is 2^-9 of a weight below a power of two's upper end, 2^-8 at worst; errors of different keys
-// do not add up in one direction) and l is summed in fp32 before that rounding: a second term, as the kernels for single tokens
-// have it, would be another P V product, a third of the tensor core's work where it is what bounds a long chunk.
+// P is one bf16 term (a weight is off by at most 2^-8 of itself, and errors of different keys do not add up in one direction:
+// outputs are 0.0023 off in the mean square where their own rounding to bf16 is 0.0017) and l is summed in fp32 before that rounding:
+// a second term, as the kernels for single tokens have it, would be another P V product, half as much again for the tensor core, whose
+// power is what limits a long chunk.
+//
+// What bounds it.  Long chunks: power, and behind it a stream's chain of logits, weights and products.  40 heads, 4096 tokens behind
+// 28671: 2070 us in short runs (1.24 PFLOP/s), 2450 over and over (1.05), the SM clock then at 1.47 GHz of 1.965; of the pair of
+// streams' turn of 3240 clocks the tensor core works 2050 (62 % under a profiler), 1830 are the softmax of one stream, the rest
+// its hand-overs; key tiles take 512 clocks of shared memory besides the products' own reads, which alone fill it.  Few tokens: HBM,
+// 4 tokens of 32 sequences, 8196 keys: 330 to 363 us for 2.16 GB.  Between them beginnings and ends of items: 4 sequences, 511
+// tokens behind 1000: 3 us besides 2 us a step for a whole item, 11 for the last one that is joined.
+// Tried and not kept: half key tiles with logits ahead (N = 64 takes 48 clocks of shared memory per product where N = 128 takes 64: long
+// document 2390 -> 2590); polynomials for a part of the exponentials (1 %); weights against the running reference with the maximum
+// beside them (8 % slower); polling instead of sleeping on barriers (none); two threads per row (2 to 8 % slower).
 //
 // Masks act on the logits by selection, so keys that a row does not see may hold anything.  Values enter a product, where a zero
 // weight times infinity is no zero: value rows that no row of the item sees are zeroed in shared memory before they are used, and a
@@ -731,7 +742,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         // ------------------------------------------------------------------ softmax and output
         // Accumulator row = TMEM lane = thread: a row's logits are all in one thread's registers, so nothing is exchanged between the
         // maximum and the weights (two threads per row halve the exponentials' chain, but not their time on the special function
-        // units, and wait for each other: the long document took 2180 us so).
+        // units, and wait for each other).
         const int s = warp / kStreamWarps, quarter = warp & 3, row = 32 * quarter + lane;
         const uint32_t s_cols = tmem_base + ((uint32_t)(32 * quarter) << 16) + kColS + s * 128;                // (O is kColO - kColS further)
         uint32_t s_uses = 0, o_uses = 0;

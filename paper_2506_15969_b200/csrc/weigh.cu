@@ -11,9 +11,10 @@
 // through memory and the last of them to arrive adds them up in order.  Three key tiles and the row tiles of three steps are in
 // shared memory, and two pairs of logit tiles in tensor memory, so that the tensor core runs ahead of the exponentials.
 //
-// Bound by the exponentials, one per row and key (the tensor core needs half their time): 16 units, 4096 rows of 4096 tokens each, 160 us,
-// special function units 72 % busy under a profiler (a quarter of them as polynomials of degree 5 on the fma pipe changed nothing); few
-// rows: HBM, the keys once.
+// Bound by the exponentials, one per row and key (the tensor core needs half their time): 16 units, 4096 rows of 4096 tokens each, 160 to
+// 187 us, special function units 70 % busy under a profiler (a quarter of them as polynomials of degree 5 on the fma pipe changed
+// nothing; the next columns fetched while these are summed, or a begin beside the end of the chunk launch, were slower); few rows: HBM,
+// the keys once.
 //
 // Warp roles: warps 0-15 exponentials, warp 16 TMA producer, warp 17 MMA issuer.  All mbarrier waits are bounded.
 #include <string.h>
