@@ -18,7 +18,7 @@
 // power is what limits a long chunk.
 //
 // What bounds it.  Long chunks: power, and behind it a stream's chain of logits, weights and products.  40 heads, 4096 tokens behind
-// 28671: 2070 us in short runs (1.24 PFLOP/s), 2450 over and over (1.05), the SM clock then at 1.47 GHz of 1.965; of the pair of
+// 28671: 1960 us in short runs (1.31 PFLOP/s), 2270 to 2290 over and over (1.13), the SM clock then near 1.5 GHz of 1.965; of the pair of
 // streams' turn of 3240 clocks the tensor core works 2050 (62 % under a profiler), 1830 are the softmax of one stream, the rest
 // its hand-overs; key tiles take 512 clocks of shared memory besides the products' own reads, which alone fill it.  Few tokens: HBM,
 // 4 tokens of 32 sequences, 8196 keys: 330 to 363 us for 2.16 GB.  Between them beginnings and ends of items: 4 sequences, 511
@@ -58,7 +58,8 @@ constexpr int kOffQ = 0;                           // two row tiles
 constexpr int kOffRing = kOffQ + 2 * kOperandBytes;
 constexpr int kOffMisc = kOffRing + kRing * kOperandBytes;
 constexpr int kOffExchange = kOffMisc + 1024;      // [2 streams][128 rows] (m, l): what the streams' threads of a row tell each other
-constexpr int kOffAside = kOffMisc + 576, kAsideInts = 12;      // per softmax warp
+constexpr int kOffAside = kOffMisc + 576, kAsideInts = 14;      // per softmax warp
+static_assert(kOffAside + 2 * kStreamWarps * kAsideInts * 4 <= kOffExchange, "");
 constexpr int kSmem = kOffExchange + 2048;
 
 constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;     // per stream: 128 columns of S / P, 128 of O
@@ -106,8 +107,12 @@ struct Piece {
     __device__ __forceinline__ int key_tile(int s, int t) const { return both ? k0 + t : k0 + 2 * t + s; }
 };
 
+// The pieces of a block's part.  An item that the block before has begun comes last: so all blocks begin at an item's first key tile,
+// and as whole items of a head are nearly of one length, the blocks of that head read the same key tiles at about the same time
+// (4096 tokens behind 28671, over and over: 2430 us in the items' order, 2290 like this).
 struct Walk {
     int x, end, unit, pair, start;
+    int last_unit, last_pair, last_start;          // the item that comes last; a unit below 0: none (any more)
     __device__ __forceinline__ void item_done(const ChunkPlan& pl) {
         start += chunk_item_steps(pl, pair);
         x = start;
@@ -124,6 +129,11 @@ struct Walk {
         pair = 0;
         for (int n = chunk_item_steps(pl, 0); x - start >= n; n = chunk_item_steps(pl, ++pair)) start += n;
         if (x - start >= chunk_key_tiles(pl, pair)) item_done(pl);     // (behind the item's key tiles)
+        last_unit = -1;
+        if (pl.pairs > 1 && x > start && start + chunk_item_steps(pl, pair) < end) {
+            last_unit = unit, last_pair = pair, last_start = start;
+            item_done(pl);
+        }
     }
     __device__ __forceinline__ bool more() const { return x < end; }
     __device__ __forceinline__ Piece next(const ChunkPlan& pl) {
@@ -137,6 +147,11 @@ struct Walk {
         pc.both = 2 * pair + 1 < pl.tiles;
         x += pc.tiles();
         if (pc.k1 == pc.kt) item_done(pl);
+        if (x >= end && last_unit >= 0) {
+            x = part_begin(pl, blockIdx.x), unit = last_unit, pair = last_pair, start = last_start;
+            end = start + chunk_key_tiles(pl, pair);
+            last_unit = -1;
+        }
         return pc;
     }
 };
@@ -758,6 +773,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         volatile int* aside = reinterpret_cast<volatile int*>(smem + kOffAside) + warp * kAsideInts;
         auto put_aside = [&](const Walk& w) {
             aside[0] = w.x, aside[1] = w.end, aside[2] = w.unit, aside[3] = w.pair, aside[4] = w.start;    // (all lanes the same)
+            aside[11] = w.last_unit, aside[12] = w.last_pair, aside[13] = w.last_start;
             __syncwarp();
         };
         put_aside(walk);
@@ -766,7 +782,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             bool warp_on;
             int nt;
             {
-                Walk here{aside[0], aside[1], aside[2], aside[3], aside[4]};
+                Walk here{aside[0], aside[1], aside[2], aside[3], aside[4], aside[11], aside[12], aside[13]};
                 const Piece pc = here.next(pl);
                 __syncwarp();
                 aside[5] = pc.unit, aside[6] = pc.pair, aside[7] = pc.start, aside[8] = pc.kt, aside[9] = pc.k0, aside[10] = pc.k1;

@@ -124,6 +124,24 @@ def test_chunk_against_64_bits(L, B, Hq, Hkv, context, T, dtype, weights):
     assert torch.equal(got, again)                             # the same bits every time
 
 
+@pytest.mark.parametrize("L,B,Hq,Hkv,context,T", [
+    (2, 4, 32, 8, 500, 300),                        # two to three items of 5 to 7 key tiles per block, begun and ended inside an item
+    (1, 9, 30, 6, 1100, 260),                       # 25 tokens of 5 heads, an odd number of tiles
+    (1, 2, 64, 32, 0, 1025),                        # a triangle: items of 1 to 9 key tiles
+])
+def test_chunk_of_many_items_in_any_order(L, B, Hq, Hkv, context, T):
+    """A block works on whole items first, then on the one that it shares with the next block, then on the one before's."""
+    g = gen(L + B + Hq + context)
+    n = context + T
+    e, k, v = loaded(g, L, B, Hq, Hkv, n, weights=True)
+    q = randn(g, L, B, T, Hq, D)
+    out = run_chunk(e, q, weights=binding.WEIGHTS_SET)
+    again = run_chunk(e, q, weights=binding.WEIGHTS_SET)
+    assert torch.equal(out, again)
+    ref, size, weights = chunk_ref(q, k, v, T)
+    assert_chunk(out, ref, size, e.state_views()["weights"][:, :n], weights)
+
+
 @pytest.mark.parametrize("L,B,P,Hq,Hkv,N,context,T", [
     (1, 2, 1, 8, 2, 1, 0, 1),
     (1, 4, 2, 28, 4, 127, 5, 30),
