@@ -1511,10 +1511,11 @@ int lazyev_attend_chunk(lazyev_t* h, const lazyev_rows_t* q, int n_tokens, const
     a.status = h->st.status;
     a.wait_limit_ns = h->wait_limit_ns;
     a.stop_after_tiles = h->stop_after_pages;
+    a.weighed = weights != LAZYEV_WEIGHTS_OFF;
     h->counted = true;
     cudaError_t e = chunk_launch(plan, a, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "chunk kernel launch");
-    h->launches += 1;
+    h->launches += plan.joins ? 2 : 1;
     if (weights == LAZYEV_WEIGHTS_OFF) return LAZYEV_OK;
     WeighArgs w = {};
     w.pool = &h->own_pool;

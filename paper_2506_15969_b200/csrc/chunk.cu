@@ -8,9 +8,9 @@
 // Structure: that of the kernel over a shared prefix (prefix.cu), with other rows.  A row tile is 128 accumulator rows =
 // floor(128 / G) tokens x G heads of one unit, an item is two neighbouring row tiles (or the odd last one), which share the key
 // tiles that they read; the walk over (item, key tile of 128 tokens) is cut into equal contiguous parts, one per persistent block,
-// so a causal chunk leaves no block idle and a few rows over a long cache are spread over all SMs.  An item that one block has for
-// itself is written out directly; the sums of one that several blocks share go through memory, and the last of them
-// to arrive joins them, in the order of the keys (no second launch, and the same bits every time).
+// so a causal chunk leaves no block idle and a few rows over a long cache are spread over all SMs; short items stay whole, one per block.
+// An item that one block has for itself is written out directly; the sums of one that several blocks share go through memory, and the
+// last of them to arrive joins them, or join_kernel where they are many: in the order of the blocks, the same bits every time.
 //
 // P is one bf16 term (a weight is off by at most 2^-8 of itself, and errors of different keys do not add up in one direction:
 // outputs are 0.0023 off in the mean square where their own rounding to bf16 is 0.0017) and l is summed in fp32 before that rounding:
@@ -50,8 +50,10 @@ constexpr int kOperandBytes = 2 * kBoxBytes;       // a 128 x 128 bf16 operand (
 constexpr int kRing = 5;                           // K and V tiles in flight, in the order they are used
 constexpr int kStreamWarps = 4;                    // a thread per accumulator row
 constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 3);      // an issuer per stream; a whole number of warpgroups
-constexpr int kLeastSteps = 6;                     // of a block's part
-constexpr int kWholeSteps = 14;                    // an item of fewer stays whole
+constexpr int kLeastSteps = 4;                     // of a block's part
+constexpr int kJoinSteps = 10;                      // that a join costs: items whose parts would not be shorter by more stay whole
+constexpr int kJoinFrom = 2, kJoinFromMany = 6;    // blocks that share an item: more are joined by a launch of their own (of many blocks itself)
+constexpr long long kInStepBytes = 64ll << 20;     // of keys and values: more do not stay in L2 by themselves (2000 tokens alone, 8 MB: 54.6 us, in step 58.5)
 constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the reference by
 
 constexpr int kOffQ = 0;                           // two row tiles
@@ -87,6 +89,8 @@ struct ChunkParams {
     float scale_log2;
     unsigned long long wait_limit_ns;
     int stop_after_tiles;
+    int beside;                                    // the next launch begins beside the end of this one
+    int weighed;                                   // ... and the weights' launch beside the end of join_kernel
 };
 
 __device__ __forceinline__ int part_begin(const ChunkPlan& p, int block) { return block * p.per + min(block, p.extra); }
@@ -122,6 +126,16 @@ struct Walk {
         }
     }
     __device__ __forceinline__ void begin(const ChunkPlan& pl, int block) {
+        last_unit = -1;
+        if (pl.whole) {                            // an item per block
+            unit = block / pl.pairs;
+            pair = block - unit * pl.pairs;
+            start = unit * pl.unit_steps;
+            for (int j = 0; j < pair; ++j) start += chunk_item_steps(pl, j);
+            x = start;
+            end = start + chunk_key_tiles(pl, pair);
+            return;
+        }
         x = part_begin(pl, block);
         end = part_begin(pl, block + 1);
         unit = x / pl.unit_steps;
@@ -129,8 +143,7 @@ struct Walk {
         pair = 0;
         for (int n = chunk_item_steps(pl, 0); x - start >= n; n = chunk_item_steps(pl, ++pair)) start += n;
         if (x - start >= chunk_key_tiles(pl, pair)) item_done(pl);     // (behind the item's key tiles)
-        last_unit = -1;
-        if (pl.pairs > 1 && x > start && start + chunk_item_steps(pl, pair) < end) {
+        if (pl.in_step && x > start && start + chunk_item_steps(pl, pair) < end) {
             last_unit = unit, last_pair = pair, last_start = start;
             item_done(pl);
         }
@@ -301,9 +314,9 @@ __device__ __noinline__ int last_bad_value(const ChunkParams& p, int unit, int f
 }
 
 // Rows (lanes of `again`) that a value reached which they do not see, or see: the first kind again, over their own keys.
-__device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair, int tile, unsigned again, float m, float l, int col0, int cols) {
+__device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair, int tile, int row, unsigned again, float m, float l, int col0, int cols) {
     const ChunkPlan& pl = p.plan;
-    const int lane = threadIdx.x & 31, row = 32 * ((threadIdx.x >> 5) & 3) + lane;
+    const int lane = threadIdx.x & 31;
     const int r_tok = row / pl.group, r_head = row - r_tok * pl.group, tok = tile * pl.tile_tokens + r_tok;
     const UnitAt at = unit_at(pl, unit);
     const int to = pl.context + min(pl.tokens, 2 * pl.tile_tokens * (pair + 1));       // (behind them there are zeros)
@@ -325,7 +338,7 @@ struct Finish {
     uint8_t* out;                                  // of this thread's row; null: no such row
     float4* o;                                     // shared sums, slot 0
     float2* ml;
-    int* counter;                                  // of this tile's quarter
+    int* counter;                                  // of this tile's quarter; null: join_kernel joins
     float* norm;                                   // of this thread's row, or null
     int dtype;
     int blocks, first_block, slot0;                // that share the item (1: whole), and the first one's slot
@@ -390,35 +403,37 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
 #pragma unroll
             for (int i = 0; i < 8; ++i) dst[(c / 4 + i) * kTile] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         }
-        // the last block of the item to come here joins the sums of all
-        volatile int* last_flag = reinterpret_cast<volatile int*>(smem + kOffMisc + 512 + 8) + half * 4 + quarter;
-        auto all_here = [&] {
-            if (f.both)
-                __syncwarp();
-            else
-                named_barrier_sync(both_bar, 64);
-        };
-        __threadfence();
-        all_here();
-        if (speaks && lane == 0) {
-            const bool last = atomicAdd(f.counter, 1) == f.blocks - 1;
-            if (last) *f.counter = 0;                      // (for the next launch)
-            *last_flag = last;
-        }
-        all_here();
-        emits = *last_flag != 0;
-        if (emits) {
+        if (f.counter) {
+            // the last block of the item to come here joins the sums of all
+            volatile int* last_flag = reinterpret_cast<volatile int*>(smem + kOffMisc + 512 + 8) + half * 4 + quarter;
+            auto all_here = [&] {
+                if (f.both)
+                    __syncwarp();
+                else
+                    named_barrier_sync(both_bar, 64);
+            };
             __threadfence();
-            m = -INFINITY;
-            l = 0.f;
-            if (f.out) {
-#pragma unroll 4
-                for (int b = 0; b < f.blocks; ++b) {
-                    const float2 ml = __ldcg(&f.ml[tile_of(slot_of(b)) + row]);
-                    const float top = fmaxf(m, ml.x);
-                    if (m > -INFINITY) l *= fast_exp2(m - top);
-                    m = top;
-                    l = fmaf(ml.y, ml.x > -INFINITY ? fast_exp2(ml.x - m) : 1.f, l);
+            all_here();
+            if (speaks && lane == 0) {
+                const bool last = atomicAdd(f.counter, 1) == f.blocks - 1;
+                if (last) *f.counter = 0;                      // (for the next launch)
+                *last_flag = last;
+            }
+            all_here();
+            emits = *last_flag != 0;
+            if (emits) {
+                __threadfence();
+                m = -INFINITY;
+                l = 0.f;
+                if (f.out) {
+    #pragma unroll 4
+                    for (int b = 0; b < f.blocks; ++b) {
+                        const float2 ml = __ldcg(&f.ml[tile_of(slot_of(b)) + row]);
+                        const float top = fmaxf(m, ml.x);
+                        if (m > -INFINITY) l *= fast_exp2(m - top);
+                        m = top;
+                        l = fmaf(ml.y, ml.x > -INFINITY ? fast_exp2(ml.x - m) : 1.f, l);
+                    }
                 }
             }
         }
@@ -500,12 +515,121 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
             f.norm[kTile] = inv;
         }
         const unsigned again = __ballot_sync(0xffffffffu, f.out && !sound && finite(l) && finite(m));
-        if (again) redo_rows(*p, f.unit, f.pair, 2 * f.pair + half, again, m, l, col0, cols);
+        if (again) redo_rows(*p, f.unit, f.pair, 2 * f.pair + half, row, again, m, l, col0, cols);
     }
     if (!f.both) {
         tmem_fence_before_sync();
         named_barrier_sync(both_bar, 64);                  // both are done with both accumulators and the exchange
     }
+}
+
+// The sums of items that several blocks share, where many share one.  A block of threads per 32 rows of a row tile and 32 columns: a
+// thread has a row, eight columns and every fourth of the item's blocks, kJoinBatch of them in flight, and the four parts are added up
+// in order.  Latency bounds it: in the chunk kernel the last block to come has all of an item's sums to fetch by itself (1 token behind
+// 30000, 2 KV heads: 67 us, like this 18.4; 4 tokens behind 131071, 8 KV heads: 108 and 89, of which 82 are the bytes).
+constexpr int kJoinColumns = 8, kJoinGroups = 4, kJoinParts = 4, kJoinBatch = 8;
+constexpr int kJoinThreads = 32 * kJoinGroups * kJoinParts;
+// (What it asks for keeps more than two blocks off an SM: with every SM at work in the chunk kernel, all would come to the first one free.
+// 4 tokens behind 30000, 14 / 2 heads: 52 us so, 29 where SMs were free.)
+constexpr int kJoinSmem = 100 * 1024, kJoinSpread = 148;
+
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ ChunkParams p) {
+    __shared__ float2 part_ml[kJoinParts][32];
+    __shared__ float part_o[kJoinParts][kJoinGroups * kJoinColumns][32];
+    const ChunkPlan& pl = p.plan;
+    if (p.weighed) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) % kJoinGroups, part = (threadIdx.x >> 5) / kJoinGroups;
+    constexpr int kAcross = kHeadDim / (kJoinGroups * kJoinColumns);
+    const int col0 = (blockIdx.z % kAcross * kJoinGroups + group) * kJoinColumns;
+    const int unit = blockIdx.x / pl.pairs, pair = blockIdx.x - unit * pl.pairs, half = blockIdx.y, tile = 2 * pair + half;
+    const int row = 32 * (blockIdx.z / kAcross) + lane, r_tok = row / pl.group, tok = tile * pl.tile_tokens + r_tok;
+    const bool valid = r_tok < pl.tile_tokens && tok < pl.tokens;
+    int start = unit * pl.unit_steps;
+    for (int j = 0; j < pair; ++j) start += chunk_item_steps(pl, j);
+    const int first_block = block_of(pl, start), blocks = block_of(pl, start + chunk_key_tiles(pl, pair) - 1) - first_block + 1;
+    const int slot0 = 2 * first_block + (start == part_begin(pl, first_block) ? 0 : 1);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blocks == 1 || tile >= pl.tiles) return;           // (whole: the output is there)
+    const int some = valid ? blocks : 0;
+    float m = -INFINITY, l = 0.f, o[kJoinColumns] = {};
+    for (int b0 = part; b0 < some; b0 += kJoinParts * kJoinBatch) {
+        float2 ml[kJoinBatch];
+        float4 v[kJoinBatch][kJoinColumns / 4];
+#pragma unroll
+        for (int i = 0; i < kJoinBatch; ++i) {
+            const int b = b0 + kJoinParts * i;
+            ml[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int c = 0; c < kJoinColumns / 4; ++c) v[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (b >= some) continue;
+            const int from = ((b == 0 ? slot0 : 2 * (first_block + b)) * 2 + half) * kTile;
+            ml[i] = __ldcg(&p.ml[from + row]);
+            const float4* src = reinterpret_cast<const float4*>(p.o) + (long long)from * (kHeadDim / 4) + row;
+#pragma unroll
+            for (int c = 0; c < kJoinColumns / 4; ++c) v[i][c] = __ldcg(&src[(col0 / 4 + c) * kTile]);
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < kJoinBatch; ++i) top = fmaxf(top, ml[i].x);
+        // (no logit above -inf: sums of zero, or not a number, that count as they are)
+        auto factor = [&](float x) { return x > -INFINITY ? fast_exp2(x - top) : 1.f; };
+        const float f = factor(m);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int k = 0; k < kJoinColumns; ++k) o[k] *= f;
+#pragma unroll
+        for (int i = 0; i < kJoinBatch; ++i) {
+            const float w = factor(ml[i].x);
+            l = fmaf(ml[i].y, w, l);
+#pragma unroll
+            for (int c = 0; c < kJoinColumns / 4; ++c) {
+                o[4 * c] = fmaf(v[i][c].x, w, o[4 * c]);
+                o[4 * c + 1] = fmaf(v[i][c].y, w, o[4 * c + 1]);
+                o[4 * c + 2] = fmaf(v[i][c].z, w, o[4 * c + 2]);
+                o[4 * c + 3] = fmaf(v[i][c].w, w, o[4 * c + 3]);
+            }
+        }
+    }
+    if (group == 0) part_ml[part][lane] = make_float2(m, l);
+#pragma unroll
+    for (int k = 0; k < kJoinColumns; ++k) part_o[part][group * kJoinColumns + k][lane] = o[k];
+    __syncthreads();
+    if (part > 0) return;
+    float2 ml[kJoinParts];
+    m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kJoinParts; ++i) {
+        ml[i] = part_ml[i][lane];
+        m = fmaxf(m, ml[i].x);
+    }
+    l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kJoinColumns; ++k) o[k] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinParts; ++i) {
+        const float w = ml[i].x > -INFINITY ? fast_exp2(ml[i].x - m) : 1.f;
+        l = fmaf(ml[i].y, w, l);
+#pragma unroll
+        for (int k = 0; k < kJoinColumns; ++k) o[k] = fmaf(part_o[i][group * kJoinColumns + k][lane], w, o[k]);
+    }
+    const float inv = 1.f / l;
+    const UnitAt at = unit_at(pl, unit);
+    const long long to = row_offset(p.out, at, tok, at.head * pl.group + row - r_tok * pl.group);
+    float odd = 0.f;                                       // (not a number as soon as an output is not finite)
+#pragma unroll
+    for (int i = 0; i < kJoinColumns; i += 4) {
+        const float4 v = make_float4(o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv);
+        odd = fmaf(v.x, 0.f, fmaf(v.y, 0.f, fmaf(v.z, 0.f, fmaf(v.w, 0.f, odd))));
+        if (valid) store4(p.out, to, col0 + i, v);
+    }
+    if (p.norms && col0 == 0 && valid) {
+        float* norm = p.norms + ((long long)unit * pl.tiles + tile) * 2 * kTile + row;
+        norm[0] = -m;
+        norm[kTile] = inv;
+    }
+    const unsigned again = __ballot_sync(0xffffffffu, valid && !(odd == 0.f) && finite(l) && finite(m));
+    if (again) redo_rows(p, unit, pair, tile, row, again, m, l, col0, kJoinColumns);
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -517,6 +641,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const ChunkPlan& pl = p.plan;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (p.beside) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Walk walk;
     walk.begin(pl, blockIdx.x);
 
@@ -898,7 +1023,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
                     f.blocks = block_of(pl, pc.start + pc.kt - 1) - f.first_block + 1;
                     f.slot0 = 2 * f.first_block + (pc.start == part_begin(pl, f.first_block) ? 0 : 1);
                     f.own_slot = 2 * (int)blockIdx.x + (pc.start + pc.k0 == part_begin(pl, blockIdx.x) ? 0 : 1);
-                    f.counter = p.counters + (f.first_block * 2 + half) * 4 + quarter;
+                    if (!pl.joins) f.counter = p.counters + (f.first_block * 2 + half) * 4 + quarter;
                 }
                 finish_piece(&p, smem, tmem_base, f, m, l);
             }
@@ -944,14 +1069,28 @@ ChunkPlan chunk_plan(int layers, int batch, int kv_heads, int group, int n, int 
     const long long work = (long long)layers * batch * kv_heads * steps;
     pl.unit_steps = steps > 0x40000000 ? 0 : (int)steps;
     if (num_sms > kChunkMaxBlocks) num_sms = kChunkMaxBlocks;
-    // Items that several blocks share cost a join (two units of 1000 tokens, 8 key tiles each: 15.0 us whole, 17.7 in three parts; of 1500: 18.5 either way).
     const long long items = (long long)layers * batch * kv_heads * pl.pairs;
-    const long long useful = work < kWholeSteps * items ? items : (work + kLeastSteps - 1) / kLeastSteps;
-    pl.blocks = work > 0x40000000 ? 0 : (int)(useful < num_sms ? useful : num_sms);
+    const long long parts = (work + kLeastSteps - 1) / kLeastSteps;
+    pl.blocks = work > 0x40000000 ? 0 : (int)(parts < num_sms ? parts : num_sms);
     pl.per = pl.extra = 0;
+    pl.whole = pl.joins = pl.in_step = false;
     if (pl.blocks == 0) return pl;
+    // Items that several blocks share cost a join, so items whose parts would not be much shorter stay whole, one per block, however
+    // unequal they are (8 KV heads, 32 heads: 200 tokens alone 12.7 us whole, 22.7 in equal parts; 500 behind 500 24.6 and 27.9; 500 behind
+    // 2500, 27 steps against 12: 50.8 whole, 40.4 in parts).
+    pl.whole = items <= num_sms && chunk_item_steps(pl, pl.pairs - 1) <= work / pl.blocks + kJoinSteps;
+    if (pl.whole) {
+        pl.blocks = (int)items;
+        return pl;
+    }
     pl.per = (int)(work / pl.blocks);
     pl.extra = (int)(work % pl.blocks);
+    pl.in_step = pl.pairs > 1 && (long long)layers * batch * kv_heads * chunk_key_tiles(pl, pl.pairs - 1) * 2 * kOperandBytes > kInStepBytes;
+    const long long join_blocks = items * (pl.tiles > 1 ? 2 : 1) * ((pl.tile_tokens * group + 31) / 32) * (kHeadDim / (kJoinGroups * kJoinColumns));
+    // The last block of an item to come joins it in the chunk kernel at the price of a launch for two or three; beyond that, or where the
+    // join's own blocks do not fit side by side beyond six, join_kernel does (64 tokens behind 3000: 31.9 and 22.6 us; 200 behind 4000,
+    // 1024 blocks for the join, 4 to an item: 35.8 and 41.1; 100 behind 12000, 9 to an item: 57.2 and 41.0).
+    if (chunk_key_tiles(pl, pl.pairs - 1) > (long long)(join_blocks <= 2 * num_sms ? kJoinFrom : kJoinFromMany) * pl.per) pl.joins = true;
     return pl;
 }
 
@@ -961,7 +1100,10 @@ size_t chunk_ml_offset(int num_sms) {
 }
 size_t chunk_sums_bytes(int num_sms) { return chunk_ml_offset(num_sms) / kHeadDim / sizeof(float) * (kHeadDim * sizeof(float) + sizeof(float2)); }
 
-cudaError_t chunk_prepare() { return cudaFuncSetAttribute(chunk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); }
+cudaError_t chunk_prepare() {
+    const cudaError_t e = cudaFuncSetAttribute(join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem);
+    return e == cudaSuccess ? cudaFuncSetAttribute(chunk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) : e;
+}
 
 bool chunk_query_map(const ChunkPlan& plan, const RowView& q, PrefixPool* out) {
     // q [layers][batch][tokens][heads][128]: box = 64 elements x G heads x a row tile's tokens, 128-byte swizzle; tokens behind the
@@ -1004,8 +1146,23 @@ cudaError_t chunk_launch(const ChunkPlan& plan, const ChunkArgs& a, cudaStream_t
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)kHeadDim);
     p.wait_limit_ns = a.wait_limit_ns;
     p.stop_after_tiles = a.stop_after_tiles;
+    p.beside = plan.joins || a.weighed;
+    p.weighed = a.weighed;
     chunk_kernel<<<plan.blocks, kThreads, kSmem, stream>>>(mq, mkv, mpre, p);
-    return cudaGetLastError();
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || !plan.joins) return e;
+    cudaLaunchAttribute beside = {};
+    beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    beside.val.programmaticStreamSerializationAllowed = 1;
+    const int rows = plan.tile_tokens * plan.group;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(plan.layers * plan.batch * plan.kv_heads * plan.pairs, plan.tiles > 1 ? 2 : 1, (rows + 31) / 32 * (kHeadDim / (kJoinGroups * kJoinColumns)));
+    c.blockDim = dim3(kJoinThreads);
+    c.dynamicSmemBytes = (long long)c.gridDim.x * c.gridDim.y * c.gridDim.z <= 2 * kJoinSpread ? kJoinSmem : 0;
+    c.stream = stream;
+    c.attrs = &beside;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, join_kernel, p);
 }
 
 }  // namespace lzk

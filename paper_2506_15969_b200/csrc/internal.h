@@ -72,6 +72,9 @@ struct ChunkPlan {
     int prefix_n, prefix_tiles, prefix_share;   // of an attached prefix: tokens, key tiles, sequences per prefix sequence
     int unit_steps;                     // steps of a unit's items together
     int blocks, per, extra;             // contiguous parts of the walk, as in PrefixPlan
+    bool whole;                         // an item per block instead
+    bool in_step;                       // whole items first
+    bool joins;                         // shared items are joined by a launch of their own
 };
 constexpr int kChunkMaxBlocks = 256;
 constexpr int kChunkCounters = kChunkMaxBlocks * 8;    // per block, stream and quarter of a row tile: who has written a shared item's sums
@@ -107,6 +110,7 @@ struct ChunkArgs {
     int32_t* status;
     unsigned long long wait_limit_ns;
     int stop_after_tiles;
+    bool weighed;                       // weigh_launch() comes next
 };
 // blocks = 0: more steps than an int counts.
 ChunkPlan chunk_plan(int layers, int batch, int kv_heads, int group, int n, int tokens, int prefix_n, int prefix_share, int num_sms);

@@ -13,7 +13,7 @@
 //
 // Bound by the exponentials, one per row and key (the tensor core needs half their time): 16 units, 4096 rows of 4096 tokens each, 160 to
 // 187 us, special function units 70 % busy under a profiler (a quarter of them as polynomials of degree 5 on the fma pipe changed
-// nothing; the next columns fetched while these are summed, or a begin beside the end of the chunk launch, were slower); few rows: HBM,
+// nothing; the next columns fetched while these are summed was slower); few rows: HBM,
 // the keys once.
 //
 // Warp roles: warps 0-15 exponentials, warp 16 TMA producer, warp 17 MMA issuer.  All mbarrier waits are bounded.
@@ -163,6 +163,7 @@ weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     __syncthreads();
     tmem_fence_after_sync();
     const uint32_t tmem_base = tmem_slot;
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // (the chunk launch's norms)
     const unsigned long long limit = p.wait_limit_ns;
 
     if (warp == kProducer) {
@@ -468,8 +469,17 @@ cudaError_t weigh_launch(const WeighPlan& plan, const ChunkPlan& chunk, const We
     p.inv_group = 1.f / (float)chunk.group;
     p.wait_limit_ns = a.wait_limit_ns;
     p.stop_after_tiles = a.stop_after_tiles;
-    weigh_kernel<<<plan.blocks, kThreads, kSmem, stream>>>(mq, mkv, p);
-    return cudaGetLastError();
+    cudaLaunchAttribute beside = {};
+    beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    beside.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(plan.blocks);
+    c.blockDim = dim3(kThreads);
+    c.dynamicSmemBytes = kSmem;
+    c.stream = stream;
+    c.attrs = &beside;
+    c.numAttrs = 1;                            // begins beside the end of the launch before (1 token: the call 20.5 -> 16.9 us)
+    return cudaLaunchKernelEx(&c, weigh_kernel, mq, mkv, p);
 }
 
 cudaError_t step_weights_launch(const Geometry& geo, float* weights, const float* pbar, int n, cudaStream_t stream) {

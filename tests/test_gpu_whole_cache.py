@@ -142,6 +142,43 @@ def test_chunk_of_many_items_in_any_order(L, B, Hq, Hkv, context, T):
     assert_chunk(out, ref, size, e.state_views()["weights"][:, :n], weights)
 
 
+@pytest.mark.parametrize("L,B,Hq,Hkv,context,T,dtype", [
+    (1, 1, 8, 2, 30001, 1, torch.bfloat16),         # about sixty blocks per item, joined by a launch of their own
+    (1, 1, 14, 2, 9000, 4, torch.float32),          # 28 rows
+    (1, 2, 12, 2, 5003, 9, torch.float16),          # 54 rows: two warps of them
+    (1, 1, 10, 2, 6000, 30, torch.float32),         # two row tiles, 25 tokens and 5
+    (1, 1, 16, 4, 9001, 100, torch.bfloat16),       # four row tiles
+])
+def test_chunk_of_few_rows_over_a_long_cache(L, B, Hq, Hkv, context, T, dtype):
+    g = gen(L + B + Hq + context)
+    n = context + T
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        v = randn(g, L, B, Hkv, n, D)
+        if T > 1:
+            v[..., n - 1, 3] = math.inf             # only the last token sees it
+        e, k, v = loaded(g, L, B, Hq, Hkv, n, v=v, weights=True, stream=stream)
+        q = randn(g, L, B, T, Hq, D)
+        out = run_chunk(e, q, dtype, weights=binding.WEIGHTS_SET)
+        assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(run_chunk(e, q, dtype, weights=binding.WEIGHTS_SET)))
+        if T > 1:
+            assert not bool(torch.isfinite(out[:, :, -1, :, 3]).any())
+        ref, size, weights = chunk_ref(q, k, v, T)
+        assert_chunk(out, ref, size, e.state_views()["weights"][:, :n], weights)
+        before, again, graph = e.state_views()["weights"][:, :n].clone(), torch.empty_like(out), torch.cuda.CUDAGraph()
+        stream.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            e.attend_chunk(q, again, weights=binding.WEIGHTS_ADD)
+        for _ in range(2):
+            graph.replay()
+        e.synchronize()
+        assert torch.equal(torch.nan_to_num(again), torch.nan_to_num(out))
+        # x = sum / G is rounded by the first call (1 step u = 2^-24 of x), and added unrounded by the others (rounded at 2 x and 3 x): 6 u x off
+        # 3 x; three times the first is 3 u x off, and 5 u x more by its own two additions: 14 u x between them, below 15 of `before`
+        three = before.double() * 3
+        assert bool(((e.state_views()["weights"][:, :n].double() - three).abs() <= 15 * 2.0 ** -24 * before.double()).all())
+
+
 @pytest.mark.parametrize("L,B,P,Hq,Hkv,N,context,T", [
     (1, 2, 1, 8, 2, 1, 0, 1),
     (1, 4, 2, 28, 4, 127, 5, 30),
