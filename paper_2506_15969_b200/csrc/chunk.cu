@@ -51,7 +51,7 @@ constexpr int kRing = 5;                           // K and V tiles in flight, i
 constexpr int kStreamWarps = 4;                    // a thread per accumulator row
 constexpr int kProducer = 2 * kStreamWarps, kIssuer = kProducer + 1, kThreads = 32 * (kIssuer + 3);      // an issuer per stream; a whole number of warpgroups
 constexpr int kLeastSteps = 4;                     // of a block's part
-constexpr int kJoinSteps = 10;                      // that a join costs: items whose parts would not be shorter by more stay whole
+constexpr int kJoinSteps = 10;                     // that a join costs: items whose parts would not be shorter by more stay whole
 constexpr int kJoinFrom = 2, kJoinFromMany = 6;    // blocks that share an item: more are joined by a launch of their own (of many blocks itself)
 constexpr long long kInStepBytes = 64ll << 20;     // of keys and values: more do not stay in L2 by themselves (2000 tokens alone, 8 MB: 54.6 us, in step 58.5)
 constexpr float kRaiseMargin = 8.f;                // log2 units a logit may exceed the reference by
@@ -426,7 +426,7 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
                 m = -INFINITY;
                 l = 0.f;
                 if (f.out) {
-    #pragma unroll 4
+#pragma unroll 4
                     for (int b = 0; b < f.blocks; ++b) {
                         const float2 ml = __ldcg(&f.ml[tile_of(slot_of(b)) + row]);
                         const float top = fmaxf(m, ml.x);
