@@ -86,7 +86,8 @@ constexpr int kKeepThreads = 512, kRowsPerWarp = kPageTokens / (kKeepThreads / 3
 
 // One block per destination page: the rows of 64 tokens in flight at once, K in the lower half of each warp, V in the upper.
 // Bound by HBM, rows of 256 bytes scattered over the pages: 528 bytes per kept token read and written, and its weight.  1024 units, 2048
-// of 8192 tokens: 385 us, 5.7 TB/s (four rows per warp; eight 420, two 550).
+// of 8192 tokens: 385 us, 5.7 TB/s (four rows per warp; eight 420, two 550).  A begin beside the end of the selection: nothing for few
+// units, 447 -> 462 us for the whole call of these.
 __global__ void __launch_bounds__(kKeepThreads) keep_kernel(KeepArgs a) {
     const int u = blockIdx.y, d0 = blockIdx.x * kPageTokens, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int half = lane < 16 ? 0 : kPageHalfBytes, cp = lane & 15;
