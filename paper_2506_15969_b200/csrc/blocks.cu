@@ -4,7 +4,8 @@
 //   high_b[d] = max_i k_i[d],   low_b[d] = min_i k_i[d]
 // and a unit's G query heads give it the score
 //   s_b = sum_g sum_d max(q_g[d] high_b[d], q_g[d] low_b[d]) = sum_d (P[d] high_b[d] + N[d] low_b[d]),
-//   P[d] = sum_g max(q_g[d], 0),  N[d] = sum_g min(q_g[d], 0):
+//   P[d] = sum_g max(q_g[d], 0),  N[d] = sum_g min(q_g[d], 0)
+// (a side that no head is on counts nothing, whatever its bound; a zero q times an infinite bound is no number):
 // no key between the bounds has larger logits summed over the heads.  Which blocks are read does not depend on fp32 rounding: blocks near
 // the cut are compared by scores in fp64, where the products are exact (all of them in fp64 is four times slower than their bytes:
 // 128 units of 2047 blocks, 77 us instead of 20, most of it conversions).
@@ -75,13 +76,14 @@ __device__ __forceinline__ uint32_t rough_key(float s) {
 }
 __device__ __forceinline__ float rough_score(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-// A lane's part of P (lanes 0-15) or N for its eight dimensions.
+// A lane's part of P (lanes 0-15) or N for its eight dimensions; which of these have a head on that side; which have one whose q is zero.
 struct Sides {
     double part[8];
+    unsigned on, zero;
 };
 __device__ __forceinline__ Sides sides_of(const BlocksArgs& a, int u) {
     const int lane = threadIdx.x & 31, c = lane & 15, G = a.geo.group;
-    Sides s = {{0, 0, 0, 0, 0, 0, 0, 0}};
+    Sides s = {{0, 0, 0, 0, 0, 0, 0, 0}, 0u, 0u};
     const uint4* q = reinterpret_cast<const uint4*>(a.q) + (size_t)u * G * kChunksPerRow + c;
     uint4 x[kMaxGroup];                    // (all of them asked for at once)
 #pragma unroll
@@ -94,8 +96,11 @@ __device__ __forceinline__ Sides sides_of(const BlocksArgs& a, int u) {
         for (int i = 0; i < 4; ++i) {
             const float e0 = bf16_lo_as_float(w[i]), e1 = bf16_hi_as_float(w[i]);
             // (what is no number goes into both sums)
-            s.part[2 * i] += e0 != e0 || (lane < 16 ? e0 > 0.f : e0 < 0.f) ? (double)e0 : 0.0;
-            s.part[2 * i + 1] += e1 != e1 || (lane < 16 ? e1 > 0.f : e1 < 0.f) ? (double)e1 : 0.0;
+            const bool on0 = e0 != e0 || (lane < 16 ? e0 > 0.f : e0 < 0.f), on1 = e1 != e1 || (lane < 16 ? e1 > 0.f : e1 < 0.f);
+            s.part[2 * i] += on0 ? (double)e0 : 0.0;
+            s.part[2 * i + 1] += on1 ? (double)e1 : 0.0;
+            s.on |= ((on0 ? 1u : 0u) | (on1 ? 2u : 0u)) << (2 * i);
+            s.zero |= ((e0 == 0.f ? 1u : 0u) | (e1 == 0.f ? 2u : 0u)) << (2 * i);
         }
     }
     return s;
@@ -105,15 +110,30 @@ __device__ __forceinline__ const uint4* bound_rows(const BlocksArgs& a, int u) {
     return reinterpret_cast<const uint4*>(a.bounds) + (size_t)u * a.geo.pages_per_unit * 2 * kChunksPerRow;
 }
 
+// Is either of two bf16 values infinite or no number?
+__device__ __forceinline__ bool pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// A side's factor with a bound of any value: nothing where no head is on that side, no number where a head's zero meets an infinity.
+__device__ __forceinline__ double side_term(const Sides& s, int i, float bound) {
+    if (fabsf(bound) < INFINITY) return s.part[i] * (double)bound;
+    if (s.zero >> i & 1u) return (double)NAN;
+    return s.on >> i & 1u ? s.part[i] * (double)bound : 0.0;
+}
+
 // The score of one block in fp64, in every lane.
 __device__ __forceinline__ double exact_score(const uint4* rows, const Sides& s, int b) {
     const uint4 x = __ldg(rows + (size_t)b * 2 * kChunksPerRow + (threadIdx.x & 31));
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     double v = 0.0;
+    if (pair_not_finite(w[0]) || pair_not_finite(w[1]) || pair_not_finite(w[2]) || pair_not_finite(w[3])) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        v = fma(s.part[2 * j], (double)bf16_lo_as_float(w[j]), v);
-        v = fma(s.part[2 * j + 1], (double)bf16_hi_as_float(w[j]), v);
+        for (int j = 0; j < 4; ++j) v += side_term(s, 2 * j, bf16_lo_as_float(w[j])) + side_term(s, 2 * j + 1, bf16_hi_as_float(w[j]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v = fma(s.part[2 * j], (double)bf16_lo_as_float(w[j]), v);
+            v = fma(s.part[2 * j + 1], (double)bf16_hi_as_float(w[j]), v);
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -1,0 +1,41 @@
+"""Calls on a whole cache at their edges: block scores of infinite and of tiny values, walks and branches that only long caches or
+many units reach, weights of every kind of decode step, caches behind a prefix, refusals that leave everything as it was.
+
+Tolerances are those of test_gpu_whole_cache.py where nothing else is said."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_operators import gen, randn
+from tests.test_gpu_whole_cache import loaded, sparse_ref
+
+pytestmark = pytest.mark.gpu
+
+D = 128
+
+
+# ---- selected blocks --------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n", [64 * 200 + 3, 64 * 700 + 3])       # scored by a unit's own block of threads, by many
+@pytest.mark.parametrize("Hq,Hkv", [(2, 2), (6, 2)])              # one head, a group of one sign
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("sign", [1, -1, 0, 2])
+def test_an_infinite_key_scores_by_its_sign(n, Hq, Hkv, value, sign):
+    """max(q high, q low) with high = inf is q low for a negative q, however many heads are negative; for q = 0 it is no number."""
+    g = gen(31)
+    L, B, blocks = 1, 2, 70
+    k, q = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hq, D)
+    for block, d in ((5, 7), (9, 100), (150, 7)):
+        k[:, :, :, 64 * block + 3, d] = value
+        q[..., d] = sign * (q[..., d].abs() + 0.125)
+        if sign == 2:                                                 # (one head of the first group is at zero)
+            q[:, :, 0, d] = 0
+    k[:, 0, :, 64 * 11:64 * 12, 30] = value                           # a block with no other key in that dimension
+    q[..., 30] = q[..., 30].abs() + 0.125
+    e, k, v = loaded(g, L, B, Hq, Hkv, n, k=k)
+    sel = torch.full((L * B * Hkv, blocks), 99, dtype=torch.int32, device="cuda")
+    e.attend_sparse(q, torch.empty_like(q), blocks, sel)
+    e.synchronize()
+    assert np.array_equal(sel.cpu().numpy(), sparse_ref(q, k, v, blocks)[2])
