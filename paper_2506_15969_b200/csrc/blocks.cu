@@ -142,8 +142,9 @@ __device__ __forceinline__ double exact_score(const uint4* rows, const Sides& s,
 
 constexpr int kBatch = 8;                  // blocks that a warp sums at once; as many are under way
 // An fp32 score is off by less than this of the sum of its terms' magnitudes: P rounded, eight products and five sums, 14 roundings
-// of 2^-24, with room.
-constexpr float kRoughError = 1.f / (1 << 19);
+// of 2^-24, with room; and, where products leave the range of normal numbers, by a step of 2^-150 each (256 of them, and as many that the
+// sum of magnitudes lacks), with room.
+constexpr float kRoughError = 1.f / (1 << 19), kRoughFloor = 0x1p-140f;
 
 // Rough scores of kBatch blocks, that of the i-th in the i-th kBatch-th of the lanes.  The sums over the lanes are folded into
 // each other: half of them go to the other half of the lanes at every step, nine exchanges instead of forty.  `size` grows to the
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(BlocksArgs a, int count,
                 kth = next;
             }
         }
-        const float t = rough_score(kth), reach = 2.f * kRoughError * size;
+        const float t = rough_score(kth), reach = 2.f * (kRoughError * size + kRoughFloor);
         // 1: above whatever the exact scores are, 0: below, 2: between (all of them where something is no number or infinite)
         const bool sane = fabsf(t) < INFINITY && reach < INFINITY;
         auto side_of = [&](uint32_t key) {

@@ -39,3 +39,17 @@ def test_an_infinite_key_scores_by_its_sign(n, Hq, Hkv, value, sign):
     e.attend_sparse(q, torch.empty_like(q), blocks, sel)
     e.synchronize()
     assert np.array_equal(sel.cpu().numpy(), sparse_ref(q, k, v, blocks)[2])
+
+
+@pytest.mark.parametrize("n", [64 * 200 + 3, 64 * 700 + 3])
+@pytest.mark.parametrize("k_size,q_size", [(2.0 ** -76, 2.0 ** -71), (2.0 ** -126, 2.0 ** -24), (2.0 ** -60, 2.0 ** -85)])
+def test_scores_of_tiny_values_are_those_of_64_bits(n, k_size, q_size):
+    """Products that 32 bits hold as a few steps, or not at all."""
+    g = gen(32)
+    L, B, Hq, Hkv, blocks = 1, 2, 8, 2, 70
+    k, q = (randn(g, L, B, Hkv, n, D).double() * k_size).to(torch.bfloat16), (randn(g, L, B, Hq, D).double() * q_size).to(torch.bfloat16)
+    e, k, v = loaded(g, L, B, Hq, Hkv, n, k=k)
+    sel = torch.full((L * B * Hkv, blocks), 99, dtype=torch.int32, device="cuda")
+    e.attend_sparse(q, torch.empty_like(q), blocks, sel)
+    e.synchronize()
+    assert np.array_equal(sel.cpu().numpy(), sparse_ref(q, k, v, blocks)[2])
