@@ -445,7 +445,8 @@ int lazyev_evict_to(lazyev_t* h, int keep, lazyev_t* dst, int* evicted);
  * The workspace, device memory of *bytes bytes, 256-byte aligned, is the caller's and must stay valid while it is set (NULL ends that);
  * the bounds lie in it from *bounds on: bf16 [units][pages_per_unit][2 (high, low)][128].
  * Capture and ordering as for lazyev_attend_chunk(); a graph makes the bounds that were missing at its capture at every replay.
- * Errors: EINVAL (null, misaligned, blocks <= 0), ESTATE (no workspace, no own token), ECUDA.
+ * Errors: EINVAL (null, misaligned, blocks <= 0; a selection so long that a decode step over as many tokens has no launch shape), ESTATE
+ * (no workspace, no own token), ECUDA.  They are found before anything is queued.
  */
 int lazyev_query_block_workspace(const lazyev_t* h, size_t* bytes, size_t* bounds);
 int lazyev_set_block_workspace(lazyev_t* h, void* workspace);

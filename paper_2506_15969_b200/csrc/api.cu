@@ -385,19 +385,22 @@ cudaError_t run_prefix(lazyev_t* h, const void* q) {
     return prefix_launch(h->prefix_plan, a, h->stream);
 }
 
-// The decode launches of one step: attention of q over the shared prefix, if there is one, and the first n cached tokens of
-// every unit with tracking (unless `track` is false) at time t.  `tok` (may be null) is the token to append at slot n - 1 first: as
-// a launch of its own, or -- when every block of the decode launch takes exactly one unit, the launch-latency-sized
-// problems -- inside the decode launch.
-// `view` (may be null) stands for the handle's own state: other pages, another place for the probabilities.
-int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPipe* pipe, const NewToken* tok = nullptr,
-               bool track = true, const StateView* view = nullptr) {
+// How a step's attention over n own tokens is launched.
+struct DecodeLaunch {
+    DecodeConfig config;
+    lazyev::Shape shape;
+    DecodePlan plan, tail_plan;
+    bool brief;                            // a warp per unit
+};
+
+// Chooses it, or refuses the call; queues nothing.
+int choose_decode(lazyev_t* h, const void* q, const void* out, int n, bool track, DecodeLaunch* launch) {
     // (the kernels load pairs of elements of q, or tiles of it over a prefix, and store single elements of out)
     if (h->shared && ((uintptr_t)q & 15)) return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned while a prefix is attached");
     if (((uintptr_t)q & 3) || ((uintptr_t)out & 1)) return fail(h, LAZYEV_EINVAL, "q must be 4-byte aligned, out 2-byte aligned");
     cudaError_t e = cudaSuccess;
-    DecodeConfig c{h->units, h->group, h->pages_per_unit, h->capacity, track ? h->alpha : INFINITY, h->force_splits, h->force_stages, h->force_groups,
-                   h->wait_limit_ns, h->stop_after_pages, h->shared != nullptr};
+    const DecodeConfig c{h->units, h->group, h->pages_per_unit, h->capacity, track ? h->alpha : INFINITY, h->force_splits, h->force_stages, h->force_groups,
+                         h->wait_limit_ns, h->stop_after_pages, h->shared != nullptr};
     // Launch shape, chosen per number of pages in use and cached.  For every cluster size whose logits
     // fit, a small time model gives the time of the rounds of the round-robin walk; the main launch is
     // the size with the least total.  A partly filled last round goes to a second launch with larger
@@ -471,17 +474,37 @@ int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPi
         if (best_time < 0) return fail(h, LAZYEV_EINVAL, "no decode launch shape fits %d tokens per unit in shared memory", n);
         cached = h->plan_cache.insert_or_assign(np, best).first;
     }
-    lazyev::Shape shape;                    // (brief: one walk over all units)
-    shape.clusters = h->units;
-    if (!brief) shape = cached->second;
-    DecodePlan plan = {};
+    launch->config = c;
+    launch->brief = brief;
+    launch->shape = lazyev::Shape();
+    launch->shape.clusters = h->units;      // (brief: one walk over all units)
+    if (!brief) launch->shape = cached->second;
+    launch->plan = {};
     if (brief)
-        plan = decode_short_plan();
-    else if (decode_plan(c, n, h->max_smem, shape.splits, &plan) != 0)
+        launch->plan = decode_short_plan();
+    else if (decode_plan(c, n, h->max_smem, launch->shape.splits, &launch->plan) != 0)
         return fail(h, LAZYEV_EINVAL, "no decode launch shape fits %d tokens per unit in shared memory", n);
-    DecodePlan tail_plan = {};
-    if (shape.tail_units > 0 && decode_plan(c, n, h->max_smem, shape.tail_splits, &tail_plan) != 0)
+    launch->tail_plan = {};
+    if (launch->shape.tail_units > 0 && decode_plan(c, n, h->max_smem, launch->shape.tail_splits, &launch->tail_plan) != 0)
         return fail(h, LAZYEV_EINVAL, "no decode launch shape fits %d tokens per unit in shared memory", n);
+    return LAZYEV_OK;
+}
+
+// The decode launches of one step: attention of q over the shared prefix, if there is one, and the first n cached tokens of
+// every unit with tracking (unless `track` is false) at time t.  `tok` (may be null) is the token to append at slot n - 1 first: as
+// a launch of its own, or -- when every block of the decode launch takes exactly one unit, the launch-latency-sized
+// problems -- inside the decode launch.
+// `view` (may be null) stands for the handle's own state: other pages, another place for the probabilities.
+int run_decode(lazyev_t* h, const void* q, void* out, int n, int t, const HostPipe* pipe, const NewToken* tok = nullptr,
+               bool track = true, const StateView* view = nullptr) {
+    DecodeLaunch launch;
+    const int rc = choose_decode(h, q, out, n, track, &launch);
+    if (rc != LAZYEV_OK) return rc;
+    const DecodeConfig& c = launch.config;
+    const lazyev::Shape& shape = launch.shape;
+    const DecodePlan &plan = launch.plan, &tail_plan = launch.tail_plan;
+    const bool brief = launch.brief;
+    cudaError_t e = cudaSuccess;
     const int main_units = h->units - shape.tail_units;
     const int clusters = shape.clusters < main_units ? shape.clusters : main_units;
     const bool fuse_append = tok && h->fuse_append && !brief && shape.tail_units == 0 && main_units <= clusters;
@@ -1620,8 +1643,11 @@ int lazyev_attend_sparse(lazyev_t* h, const void* q, int blocks, void* out, int3
         return fail(h, LAZYEV_EINVAL, "q must be 16-byte aligned, out 2-byte and selected 4-byte aligned");
     if (!h->block_space) return fail(h, LAZYEV_ESTATE, "no block workspace (lazyev_set_block_workspace)");
     if (!h->prefilled || h->n == 0) return fail(h, LAZYEV_ESTATE, "attend_sparse with no own token cached");
-    if ((rc = run_index(h, h->indexed)) != LAZYEV_OK) return rc;
     const int last = (h->n - 1) / kPageTokens, picked = blocks - 1 < last ? blocks - 1 : last;
+    const int tokens = picked * kPageTokens + h->n - last * kPageTokens;       // that are read
+    DecodeLaunch launch;                     // (refuses before anything is queued)
+    if ((rc = choose_decode(h, q, out, tokens, false, &launch)) != LAZYEV_OK) return rc;
+    if ((rc = run_index(h, h->indexed)) != LAZYEV_OK) return rc;
     BlocksArgs a = blocks_args(h);
     a.q = q;
     a.selected = selected;
@@ -1632,7 +1658,7 @@ int lazyev_attend_sparse(lazyev_t* h, const void* q, int blocks, void* out, int3
     StateView view = h->st;
     view.page_table = a.table;
     view.pbar = (float*)(h->block_space + block_space(h).pbar);
-    return run_decode(h, q, out, picked * kPageTokens + h->n - last * kPageTokens, h->t, nullptr, nullptr, false, &view);
+    return run_decode(h, q, out, tokens, h->t, nullptr, nullptr, false, &view);
 }
 
 int lazyev_evict_to(lazyev_t* h, int keep, lazyev_t* dst, int* evicted) {

@@ -8,8 +8,9 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2506_15969_b200 import binding
 from tests.test_gpu_operators import gen, randn
-from tests.test_gpu_whole_cache import loaded, sparse_ref
+from tests.test_gpu_whole_cache import check_sparse, loaded, sparse_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +54,21 @@ def test_scores_of_tiny_values_are_those_of_64_bits(n, k_size, q_size):
     e.attend_sparse(q, torch.empty_like(q), blocks, sel)
     e.synchronize()
     assert np.array_equal(sel.cpu().numpy(), sparse_ref(q, k, v, blocks)[2])
+
+
+def test_blocks_that_no_decode_launch_holds_are_refused_before_anything_is_queued():
+    g = gen(35)
+    L, B, Hq, Hkv, n = 1, 1, 8, 2, 140001
+    e, k, v = loaded(g, L, B, Hq, Hkv, n)
+    q, out = randn(g, L, B, Hq, D), torch.full((L, B, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(binding.LazyEvError) as err:                   # (nor does a dense step have a launch shape)
+        e.attend(q, out)
+    assert err.value.code == binding.EINVAL
+    sel = torch.full((L * B * Hkv, 2200), 99, dtype=torch.int32, device="cuda")
+    launches = e.info().launches
+    with pytest.raises(binding.LazyEvError) as err:
+        e.attend_sparse(q, out, 2200, sel)
+    assert err.value.code == binding.EINVAL
+    e.synchronize()
+    assert e.info().launches == launches and bool((sel == 99).all()) and bool((out == 7).all())
+    check_sparse(e, q, k, v, 40)
