@@ -321,6 +321,7 @@ __device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair,
     const UnitAt at = unit_at(pl, unit);
     const int to = pl.context + min(pl.tokens, 2 * pl.tile_tokens * (pair + 1));       // (behind them there are zeros)
     const int bad = last_bad_value(p, unit, pl.context + tile * pl.tile_tokens + 1, to);
+    __syncwarp();                                          // other lanes have stored parts of the rows that are stored again here
     again &= __ballot_sync(0xffffffffu, bad > pl.context + tok);
     while (again) {
         const int i = __ffs(again) - 1;

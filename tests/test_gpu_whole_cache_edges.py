@@ -10,7 +10,7 @@ import torch
 
 from paper_2506_15969_b200 import binding
 from tests.test_gpu_operators import gen, randn
-from tests.test_gpu_whole_cache import check_sparse, loaded, sparse_ref
+from tests.test_gpu_whole_cache import assert_chunk, check_sparse, chunk_ref, loaded, run_chunk, sparse_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +72,26 @@ def test_blocks_that_no_decode_launch_holds_are_refused_before_anything_is_queue
     e.synchronize()
     assert e.info().launches == launches and bool((sel == 99).all()) and bool((out == 7).all())
     check_sparse(e, q, k, v, 40)
+
+
+# ---- a chunk ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("L,B,Hq,Hkv,context,T", [
+    (1, 2, 8, 2, 100, 60),                          # whole items, one row tile or two
+    (1, 4, 8, 2, 1000, 200),                        # joined by the last block to come
+    (1, 1, 8, 2, 9000, 20),                         # by a launch of its own
+])
+def test_rows_beside_a_later_value_that_is_not_finite(L, B, Hq, Hkv, context, T, dtype):
+    """They are computed again and stored over what was there first, by other threads: every time the same."""
+    g = gen(context + T)
+    n = context + T
+    k, v, q = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D), randn(g, L, B, T, Hq, D)
+    v[..., n - 1, 1::8], v[..., n - T // 3, 64::16] = math.inf, math.nan
+    e, k, v = loaded(g, L, B, Hq, Hkv, n, k=k, v=v)
+    ref, size, _ = chunk_ref(q, k, v, T)
+    out = run_chunk(e, q, dtype)
+    assert_chunk(out, ref, size)
+    bits = out.view(torch.int32 if dtype == torch.float32 else torch.int16)
+    for _ in range(20):
+        assert torch.equal(run_chunk(e, q, dtype).view(bits.dtype)[torch.isfinite(out)], bits[torch.isfinite(out)])
