@@ -216,57 +216,6 @@ struct KeyPages {
     }
 };
 
-// A row over its own keys alone, from global memory, for a known reference and sum: a whole warp, lane -> columns 4 lane .. + 3.
-__device__ __noinline__ float4 redo_row(const ChunkParams& p, int unit, int tok, int g, float m, float l) {
-    const ChunkPlan& pl = p.plan;
-    const UnitAt at = unit_at(pl, unit);
-    const int lane = threadIdx.x & 31;
-    const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q.data) +
-                                                    row_offset(p.q, at, tok, at.head * pl.group + g));
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int own = 0; own < 2; ++own) {
-        const int keys = own ? pl.context + tok + 1 : pl.prefix_n, total = own ? p.total_pages : p.prefix_total_pages;
-        const int32_t* table = own ? p.page_table + (long long)unit * p.pages_per_unit
-                                   : p.prefix_table + (long long)at.prefix_unit * p.prefix_pages_per_unit;
-        const uint8_t* pool = own ? p.pages : p.prefix_pages;
-        auto page_of = [&](int j) {
-            const int32_t pp = table[j / kPageTokens];
-            return pp >= 0 && pp < total ? pp : 0;
-        };
-        for (int base = 0; base < keys; base += 32) {
-            float w = 0.f;
-            if (base + lane < keys) {
-                const int j = base + lane, r = j % kPageTokens;
-                const uint8_t* row = pool + (size_t)page_of(j) * kPageBytes + r * kRowBytes;
-                float x = 0.f;
-                for (int c = 0; c < kChunksPerRow; ++c) {
-                    const uint4 a = q[c], b = *reinterpret_cast<const uint4*>(row + swz_chunk(c, r) * 16);
-                    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x = fmaf(bf16_lo_as_float(aw[i]), bf16_lo_as_float(bw[i]), x);
-                        x = fmaf(bf16_hi_as_float(aw[i]), bf16_hi_as_float(bw[i]), x);
-                    }
-                }
-                w = fast_exp2(fmaf(x, p.scale_log2, -m));
-            }
-            const int some = min(32, keys - base);
-            for (int i = 0; i < some; ++i) {
-                const float wi = __shfl_sync(0xffffffffu, w, i);
-                const int j = base + i, r = j % kPageTokens;
-                const uint8_t* row = pool + (size_t)page_of(j) * kPageBytes + kPageHalfBytes + r * kRowBytes;
-                const uint2 v = *reinterpret_cast<const uint2*>(row + swz_chunk(lane >> 1, r) * 16 + (lane & 1) * 8);
-                acc[0] = fmaf(wi, bf16_lo_as_float(v.x), acc[0]);
-                acc[1] = fmaf(wi, bf16_hi_as_float(v.x), acc[1]);
-                acc[2] = fmaf(wi, bf16_lo_as_float(v.y), acc[2]);
-                acc[3] = fmaf(wi, bf16_hi_as_float(v.y), acc[3]);
-            }
-        }
-    }
-    const float inv = 1.f / l;
-    return make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-}
-
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -313,7 +262,15 @@ __device__ __noinline__ int last_bad_value(const ChunkParams& p, int unit, int f
     return -1;
 }
 
-// Rows (lanes of `again`) that a value reached which they do not see, or see: the first kind again, over their own keys.
+// Rows that are computed again side by side: a key or value that is fetched serves all of them.  65536 keys, 32 rows in each of eight warps:
+// 690 ms one at a time, 216 two, 166 three, 135 four -- which takes registers from the loop over the keys, as does eight
+// (long document 1960 -> 2045 us).
+constexpr int kRedoRows = 3;
+constexpr unsigned long long kRedoNs = 10000;      // that a warp's rows take per key, at most: 2.5 us as above, with room
+
+// Rows (lanes of `again`) that a value reached which they do not see, or see: the first kind again, over their own keys alone, for the
+// references and sums that are known, from global memory.  A whole warp: a key per lane, then columns 4 lane .. + 3 of the outputs.
+// The block's other warps wait meanwhile: chunk_launch() adds to their limit what it may take.
 __device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair, int tile, int row, unsigned again, float m, float l, int col0, int cols) {
     const ChunkPlan& pl = p.plan;
     const int lane = threadIdx.x & 31;
@@ -323,14 +280,85 @@ __device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair,
     const int bad = last_bad_value(p, unit, pl.context + tile * pl.tile_tokens + 1, to);
     __syncwarp();                                          // other lanes have stored parts of the rows that are stored again here
     again &= __ballot_sync(0xffffffffu, bad > pl.context + tok);
+    const float inv = 1.f / l;
     while (again) {
-        const int i = __ffs(again) - 1;
-        again &= again - 1;
-        const int tok_i = __shfl_sync(0xffffffffu, tok, i), head_i = __shfl_sync(0xffffffffu, r_head, i);
-        const float m_i = __shfl_sync(0xffffffffu, m, i), l_i = __shfl_sync(0xffffffffu, l, i);
-        const float4 o = redo_row(p, unit, tok_i, head_i, m_i, l_i);
-        if (4 * lane >= col0 && 4 * lane < col0 + cols)
-            store4(p.out, row_offset(p.out, at, tok_i, at.head * pl.group + head_i), 4 * lane, o);
+        int who[kRedoRows], sees[kRedoRows];               // (where fewer are left, the last one several times)
+        const uint4* q[kRedoRows];
+        float ref[kRedoRows], acc[kRedoRows][4];
+        int most = 0;
+#pragma unroll
+        for (int r = 0; r < kRedoRows; ++r) {
+            who[r] = again ? __ffs(again) - 1 : who[r > 0 ? r - 1 : 0];
+            again &= again - 1;                            // (0 stays 0)
+            const int tok_r = __shfl_sync(0xffffffffu, tok, who[r]), head_r = __shfl_sync(0xffffffffu, r_head, who[r]);
+            q[r] = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q.data) + row_offset(p.q, at, tok_r, at.head * pl.group + head_r));
+            ref[r] = __shfl_sync(0xffffffffu, m, who[r]);
+            sees[r] = pl.context + tok_r + 1;
+            most = max(most, sees[r]);
+            acc[r][0] = acc[r][1] = acc[r][2] = acc[r][3] = 0.f;
+        }
+#pragma unroll 1
+        for (int own = 0; own < 2; ++own) {
+            const int keys = own ? most : pl.prefix_n, total = own ? p.total_pages : p.prefix_total_pages;
+            const int32_t* table = own ? p.page_table + (long long)unit * p.pages_per_unit
+                                       : p.prefix_table + (long long)at.prefix_unit * p.prefix_pages_per_unit;
+            const uint8_t* pool = own ? p.pages : p.prefix_pages;
+#pragma unroll 1
+            for (int base = 0; base < keys; base += 32) {  // (half a page: rows behind the last key are there, whatever they hold)
+                const int32_t pp = table[base / kPageTokens];
+                const uint8_t* page = pool + (size_t)(pp >= 0 && pp < total ? pp : 0) * kPageBytes;
+                const int first = base % kPageTokens, kr = first + lane;
+                float w[kRedoRows];
+#pragma unroll
+                for (int r = 0; r < kRedoRows; ++r) w[r] = 0.f;
+#pragma unroll 2
+                for (int c = 0; c < kChunksPerRow; ++c) {
+                    const uint4 b = *reinterpret_cast<const uint4*>(page + kr * kRowBytes + swz_chunk(c, kr) * 16);
+                    const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int r = 0; r < kRedoRows; ++r) {
+                        const uint4 a = q[r][c];
+                        const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            w[r] = fmaf(bf16_lo_as_float(aw[i]), bf16_lo_as_float(bw[i]), w[r]);
+                            w[r] = fmaf(bf16_hi_as_float(aw[i]), bf16_hi_as_float(bw[i]), w[r]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < kRedoRows; ++r)        // (below zero: not seen)
+                    w[r] = base + lane < (own ? sees[r] : keys) ? fast_exp2(fmaf(w[r], p.scale_log2, -ref[r])) : -1.f;
+#pragma unroll 1
+                for (int i0 = 0; i0 < 32; i0 += 8) {
+                    uint2 v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int vr = first + i0 + i;
+                        v[i] = *reinterpret_cast<const uint2*>(page + kPageHalfBytes + vr * kRowBytes + swz_chunk(lane >> 1, vr) * 16 + (lane & 1) * 8);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int r = 0; r < kRedoRows; ++r) {
+                            const float wi = __shfl_sync(0xffffffffu, w[r], i0 + i);
+                            if (wi < 0.f) continue;
+                            acc[r][0] = fmaf(wi, bf16_lo_as_float(v[i].x), acc[r][0]);
+                            acc[r][1] = fmaf(wi, bf16_hi_as_float(v[i].x), acc[r][1]);
+                            acc[r][2] = fmaf(wi, bf16_lo_as_float(v[i].y), acc[r][2]);
+                            acc[r][3] = fmaf(wi, bf16_hi_as_float(v[i].y), acc[r][3]);
+                        }
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRedoRows; ++r) {
+            const float inv_r = __shfl_sync(0xffffffffu, inv, who[r]);
+            const int tok_r = __shfl_sync(0xffffffffu, tok, who[r]), head_r = __shfl_sync(0xffffffffu, r_head, who[r]);
+            if (4 * lane >= col0 && 4 * lane < col0 + cols)
+                store4(p.out, row_offset(p.out, at, tok_r, at.head * pl.group + head_r), 4 * lane,
+                       make_float4(acc[r][0] * inv_r, acc[r][1] * inv_r, acc[r][2] * inv_r, acc[r][3] * inv_r));
+        }
     }
 }
 
@@ -1145,7 +1173,7 @@ cudaError_t chunk_launch(const ChunkPlan& plan, const ChunkArgs& a, cudaStream_t
     p.norms = a.norms;
     p.status = a.status;
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)kHeadDim);
-    p.wait_limit_ns = a.wait_limit_ns;
+    p.wait_limit_ns = a.wait_limit_ns + kRedoNs * (unsigned long long)(plan.prefix_n + plan.context + plan.tokens);
     p.stop_after_tiles = a.stop_after_tiles;
     p.beside = plan.joins || a.weighed;
     p.weighed = a.weighed;

@@ -95,3 +95,20 @@ def test_rows_beside_a_later_value_that_is_not_finite(L, B, Hq, Hkv, context, T,
     bits = out.view(torch.int32 if dtype == torch.float32 else torch.int16)
     for _ in range(20):
         assert torch.equal(run_chunk(e, q, dtype).view(bits.dtype)[torch.isfinite(out)], bits[torch.isfinite(out)])
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_rows_computed_again_over_a_long_cache_keep_nobody_waiting(value):
+    """The last token's value reaches no other row, and the rows that it had got into are done again without a wait that gives up."""
+    g = gen(42)
+    L, B, Hq, Hkv, n, T = 1, 20, 32, 8, 65536, 64                     # more items than blocks: behind most pieces of work there is another
+    k, v, q = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D), randn(g, L, B, T, Hq, D)
+    v[..., n - 1, :] = value
+    e, k, v = loaded(g, L, B, Hq, Hkv, n, k=k, v=v)
+    e.set_wait_limit(0.01)
+    out = run_chunk(e, q)
+    assert not bool(torch.isfinite(out[:, :, -1]).any()) and bool(torch.isfinite(out[:, :, :-1]).all())
+    for b, h in ((0, 0), (7, 3), (19, 7)):
+        at = (slice(None), slice(b, b + 1), slice(None), slice(4 * h, 4 * h + 4))
+        ref, size, _ = chunk_ref(q[at], k[:, b:b + 1, h:h + 1], v[:, b:b + 1, h:h + 1], T)
+        assert_chunk(out[at], ref, size)
