@@ -193,7 +193,7 @@ int lazyev_set_prompt_dump(lazyev_t* h, float* device_rows, int unit_begin, int 
 /*
  * How long a kernel waits on one of its internal barriers (a page that never arrives, a peer
  * block that never answers) before it gives up, sets the device status word and ends: default
- * 2 s, settable between 0.1 ms and 60 s (in lazyev_attend_chunk() 10 us more for every token that the newest one sees, because
+ * 2 s, settable between 0.1 ms and 60 s (in lazyev_attend_chunk() 20 us more for every token that the newest one sees, because
  * rows that a later token's infinity or NaN got into are computed again while others wait).  A kernel that gave up leaves the context usable;
  * lazyev_synchronize() then returns EDEVICE and lazyev_reset() clears the word.
  */

@@ -263,10 +263,10 @@ __device__ __noinline__ int last_bad_value(const ChunkParams& p, int unit, int f
 }
 
 // Rows that are computed again side by side: a key or value that is fetched serves all of them.  65536 keys, 32 rows in each of eight warps:
-// 690 ms one at a time, 216 two, 166 three, 135 four -- which takes registers from the loop over the keys, as does eight
-// (long document 1960 -> 2045 us).
-constexpr int kRedoRows = 3;
-constexpr unsigned long long kRedoNs = 10000;      // that a warp's rows take per key, at most: 2.5 us as above, with room
+// 690 ms one at a time, 283 two.  Few instructions count as well, also where none is ever run: three rows and longer unrolled loops, 166 ms,
+// made calls without any such row slower by what no longer fits beside the rest of the kernels (64 tokens behind 30000: 44 -> 50 us).
+constexpr int kRedoRows = 2;
+constexpr unsigned long long kRedoNs = 20000;      // that a warp's rows take per key, at most: 4.3 us as above, with room
 
 // Rows (lanes of `again`) that a value reached which they do not see, or see: the first kind again, over their own keys alone, for the
 // references and sums that are known, from global memory.  A whole warp: a key per lane, then columns 4 lane .. + 3 of the outputs.
@@ -311,7 +311,7 @@ __device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair,
                 float w[kRedoRows];
 #pragma unroll
                 for (int r = 0; r < kRedoRows; ++r) w[r] = 0.f;
-#pragma unroll 2
+#pragma unroll 1
                 for (int c = 0; c < kChunksPerRow; ++c) {
                     const uint4 b = *reinterpret_cast<const uint4*>(page + kr * kRowBytes + swz_chunk(c, kr) * 16);
                     const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
@@ -330,15 +330,15 @@ __device__ __noinline__ void redo_rows(const ChunkParams& p, int unit, int pair,
                 for (int r = 0; r < kRedoRows; ++r)        // (below zero: not seen)
                     w[r] = base + lane < (own ? sees[r] : keys) ? fast_exp2(fmaf(w[r], p.scale_log2, -ref[r])) : -1.f;
 #pragma unroll 1
-                for (int i0 = 0; i0 < 32; i0 += 8) {
-                    uint2 v[8];
+                for (int i0 = 0; i0 < 32; i0 += 4) {
+                    uint2 v[4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < 4; ++i) {
                         const int vr = first + i0 + i;
                         v[i] = *reinterpret_cast<const uint2*>(page + kPageHalfBytes + vr * kRowBytes + swz_chunk(lane >> 1, vr) * 16 + (lane & 1) * 8);
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int r = 0; r < kRedoRows; ++r) {
                             const float wi = __shfl_sync(0xffffffffu, w[r], i0 + i);
