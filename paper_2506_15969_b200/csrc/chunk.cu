@@ -557,10 +557,10 @@ __device__ __noinline__ void finish_piece(const ChunkParams* p, uint8_t* smem, u
 // in order.  Latency bounds it: in the chunk kernel the last block to come has all of an item's sums to fetch by itself (1 token behind
 // 30000, 2 KV heads: 67 us, like this 18.4; 4 tokens behind 131071, 8 KV heads: 108 and 89, of which 82 are the bytes).
 constexpr int kJoinColumns = 8, kJoinGroups = 4, kJoinParts = 4, kJoinBatch = 8;
-constexpr int kJoinThreads = 32 * kJoinGroups * kJoinParts;
-// (What it asks for keeps more than two blocks off an SM: with every SM at work in the chunk kernel, all would come to the first one free.
-// 4 tokens behind 30000, 14 / 2 heads: 52 us so, 29 where SMs were free.)
-constexpr int kJoinSmem = 100 * 1024, kJoinSpread = 148;
+constexpr int kJoinThreads = 32 * kJoinGroups * kJoinParts;       // (and registers that an SM holds one block of)
+// Shared memory that it asks for and does not use: without it 32 tokens behind 16000 take 25.7 us
+// instead of 24.8, 16 behind 65535 54.3 instead of 53.5, others the same.
+constexpr int kJoinSmem = 100 * 1024;
 
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ ChunkParams p) {
     __shared__ float2 part_ml[kJoinParts][32];
@@ -1117,8 +1117,8 @@ ChunkPlan chunk_plan(int layers, int batch, int kv_heads, int group, int n, int 
     pl.in_step = pl.pairs > 1 && (long long)layers * batch * kv_heads * chunk_key_tiles(pl, pl.pairs - 1) * 2 * kOperandBytes > kInStepBytes;
     const long long join_blocks = items * (pl.tiles > 1 ? 2 : 1) * ((pl.tile_tokens * group + 31) / 32) * (kHeadDim / (kJoinGroups * kJoinColumns));
     // The last block of an item to come joins it in the chunk kernel at the price of a launch for two or three; beyond that, or where the
-    // join's own blocks do not fit side by side beyond six, join_kernel does (64 tokens behind 3000: 31.9 and 22.6 us; 200 behind 4000,
-    // 1024 blocks for the join, 4 to an item: 35.8 and 41.1; 100 behind 12000, 9 to an item: 57.2 and 41.0).
+    // join's own blocks, of which an SM holds one at a time, take more than two turns, beyond six, join_kernel does (64 tokens behind
+    // 3000: 31.9 and 22.6 us; 200 behind 4000, 1024 blocks for the join, 4 to an item: 35.8 and 41.1; 100 behind 12000, 9 to an item: 57.2 and 41.0).
     if (chunk_key_tiles(pl, pl.pairs - 1) > (long long)(join_blocks <= 2 * num_sms ? kJoinFrom : kJoinFromMany) * pl.per) pl.joins = true;
     return pl;
 }
@@ -1187,7 +1187,7 @@ cudaError_t chunk_launch(const ChunkPlan& plan, const ChunkArgs& a, cudaStream_t
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(plan.layers * plan.batch * plan.kv_heads * plan.pairs, plan.tiles > 1 ? 2 : 1, (rows + 31) / 32 * (kHeadDim / (kJoinGroups * kJoinColumns)));
     c.blockDim = dim3(kJoinThreads);
-    c.dynamicSmemBytes = (long long)c.gridDim.x * c.gridDim.y * c.gridDim.z <= 2 * kJoinSpread ? kJoinSmem : 0;
+    c.dynamicSmemBytes = kJoinSmem;
     c.stream = stream;
     c.attrs = &beside;
     c.numAttrs = 1;
