@@ -218,7 +218,7 @@ struct SpanGuard {
     lazyev_t* h;
     lazyev::Span span;
     bool on;
-    SpanGuard(lazyev_t* h_, int kind, double bytes) : h(h_), on(h_->profiling) {
+    SpanGuard(lazyev_t* h_, int kind, double bytes, bool counted = true) : h(h_), on(h_->profiling && counted) {
         if (!on) return;
         span.start = take_event(h);
         span.stop = take_event(h);
@@ -263,8 +263,8 @@ int candidates_of(const lazyev_t* h, int n) {
 bool evict_due_at(const lazyev_t* h, int t, int n) { return t != 0 && t % h->window == 0 && n > h->budget_now; }
 
 // Which tokens stay when every unit is cut to `keep` of its h->n tokens: the select launches, into the work lists `src` and
-// `first_moved`, the bound scratch region's or the library's own.
-int run_select(lazyev_t* h, int keep, int32_t* src, int32_t* first_moved, int32_t* radix_list, EvictArgs* args) {
+// `first_moved`, the bound scratch region's or the library's own.  `counted`: the profile's sums take them in.
+int run_select(lazyev_t* h, int keep, int32_t* src, int32_t* first_moved, int32_t* radix_list, bool counted, EvictArgs* args) {
     const int ncand = candidates_of(h, h->n);
     if (ncand < 0)
         return fail(h, LAZYEV_EINVAL, "eviction over %d candidates is not supported", h->n - h->n_recent - h->n_initial);
@@ -292,7 +292,7 @@ int run_select(lazyev_t* h, int keep, int32_t* src, int32_t* first_moved, int32_
     const Geometry geo = geometry(h);
     {
         // algorithmic bytes: TS and MRI (the weight) of every candidate read, the source list written
-        SpanGuard g(h, kSpanSelect, (double)h->units * ((by_weight ? 4.0 : 8.0) * ncand + 4.0 * a.budget));
+        SpanGuard g(h, kSpanSelect, (double)h->units * ((by_weight ? 4.0 : 8.0) * ncand + 4.0 * a.budget), counted);
         e = by_weight ? weigh_select_launch(geo, h->st, h->weights, a, h->stream) : select_launch(geo, h->st, a, h->num_sms, h->stream);
     }
     if (e != cudaSuccess) return cuda_fail(h, e, "select kernel launch");
@@ -303,7 +303,7 @@ int run_select(lazyev_t* h, int keep, int32_t* src, int32_t* first_moved, int32_
 // Cuts every unit to its `keep` < h->n best tokens, in place.
 int run_cut(lazyev_t* h, int keep, int* evicted, int32_t* src, int32_t* first_moved, int32_t* radix_list) {
     EvictArgs a;
-    const int rc = run_select(h, keep, src, first_moved, radix_list, &a);
+    const int rc = run_select(h, keep, src, first_moved, radix_list, true, &a);
     if (rc != LAZYEV_OK) return rc;
     const Geometry geo = geometry(h);
     cudaError_t e;
@@ -1684,7 +1684,7 @@ int lazyev_evict_to(lazyev_t* h, int keep, lazyev_t* dst, int* evicted) {
     if (dst->shared != h->shared) return fail(h, LAZYEV_ESTATE, "evict_to needs the same prefix attached to both handles, or to neither");
     if (kept > dst->capacity) return fail(h, LAZYEV_ECAPACITY, "%d tokens exceed the capacity of %d slots per unit", kept, dst->capacity);
     EvictArgs sel = {};
-    if (!all && (rc = run_select(h, keep, h->src, h->first_moved, h->radix_list, &sel)) != LAZYEV_OK) return rc;
+    if (!all && (rc = run_select(h, keep, h->src, h->first_moved, h->radix_list, false, &sel)) != LAZYEV_OK) return rc;
     KeepArgs a = {};
     a.from_geo = geometry(h);
     a.to_geo = geometry(dst);

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2506_15969_b200 import binding
-from tests.test_gpu_operators import gen, randn
+from tests.test_gpu_operators import engine, gen, randn
 from tests.test_gpu_whole_cache import assert_chunk, check_sparse, chunk_ref, loaded, run_chunk, sparse_ref
 
 pytestmark = pytest.mark.gpu
@@ -112,3 +112,18 @@ def test_rows_computed_again_over_a_long_cache_keep_nobody_waiting(value):
         at = (slice(None), slice(b, b + 1), slice(None), slice(4 * h, 4 * h + 4))
         ref, size, _ = chunk_ref(q[at], k[:, b:b + 1, h:h + 1], v[:, b:b + 1, h:h + 1], T)
         assert_chunk(out[at], ref, size)
+
+
+# ---- into another cache ------------------------------------------------------------------------------------------------------
+
+def test_a_cut_into_another_handle_is_not_among_the_profiles_evictions():
+    g = gen(39)
+    e, k, v = loaded(g, 1, 2, 8, 2, 200, weights=True)
+    e.set_score_mode(binding.SCORE_WEIGHT)
+    e.set_profiling(True)
+    assert e.evict_to(100, engine(1, 8, 2, 2, 100)) == 100
+    p = e.get_profile()
+    assert p.select_launches == 0 and p.select_bytes == 0 and p.compact_launches == 0
+    assert e.evict_to(100) == 100
+    p = e.get_profile()
+    assert p.select_launches == 1 and p.compact_launches == 1
