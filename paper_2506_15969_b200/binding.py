@@ -376,13 +376,15 @@ class Engine:
 
     def reserve_chunk(self, tokens: int, weights: int = WEIGHTS_OFF) -> None:
         """The workspace of attend_chunk for up to `tokens` tokens.  attend_chunk makes room by itself; a caller that captures it into a
-        graph without having called it at this size before reserves it beforehand.  Earlier ones stay (graphs may use them)."""
+        graph without having called it at this size before reserves it beforehand.  Earlier ones stay (graphs may use them); each is
+        at least twice as large as the one before, so that all of them together are less than twice the last."""
         n = C.c_size_t()
         self._check(lib().lazyev_query_chunk_workspace(self._h, tokens, weights, C.byref(n)))
         self._chunk_room[tokens, weights] = n.value
-        if not self._chunk_space or self._chunk_space[-1].numel() < n.value:
+        last = self._chunk_space[-1].numel() if self._chunk_space else 0
+        if last < n.value:
             with self._torch.cuda.stream(self.stream):
-                self._chunk_space.append(self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device))
+                self._chunk_space.append(self._torch.empty(max(n.value, 2 * last), dtype=self._torch.uint8, device=self.device))
 
     def attend_chunk(self, q, out, weights: int = WEIGHTS_OFF) -> None:
         """lazyev_attend_chunk of the last q.shape[2] cached tokens: q, out [layers, batch, tokens, q_heads, 128], strided as they are."""

@@ -127,3 +127,15 @@ def test_a_cut_into_another_handle_is_not_among_the_profiles_evictions():
     assert e.evict_to(100) == 100
     p = e.get_profile()
     assert p.select_launches == 1 and p.compact_launches == 1
+
+
+# ---- the binding -----------------------------------------------------------------------------------------------------------------
+
+def test_workspaces_of_growing_chunks_do_not_pile_up():
+    e, _, _ = loaded(gen(40), 2, 4, 16, 2, 2000, weights=True)
+    largest = 0
+    for tokens in range(1, 2001, 13):
+        e.reserve_chunk(tokens, binding.WEIGHTS_SET)
+        largest = max(largest, e._chunk_room[tokens, binding.WEIGHTS_SET])
+        assert e._chunk_space[-1].numel() >= largest
+    assert sum(x.numel() for x in e._chunk_space) <= 4 * largest
