@@ -475,8 +475,10 @@ class Engine:
         keep = {}
         for name, dt in (("pos", np.int32), ("ts", np.int32), ("mri", np.int32), ("pbar", np.float32), ("score", np.float64),
                          ("k", np.uint16), ("v", np.uint16)):
-            if name in snap:
+            if snap.get(name) is not None:
                 keep[name] = np.ascontiguousarray(snap[name], dtype=dt)
+                if name == "score" and keep[name].shape != (cnt, n):
+                    raise ValueError(f"score must be [{cnt}, {n}], not {list(keep[name].shape)}")
                 setattr(d, name, keep[name].ctypes.data)
         self._check(lib().lazyev_load_state(self._h, C.byref(d), prefill))
 

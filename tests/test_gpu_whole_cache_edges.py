@@ -139,3 +139,22 @@ def test_workspaces_of_growing_chunks_do_not_pile_up():
         largest = max(largest, e._chunk_room[tokens, binding.WEIGHTS_SET])
         assert e._chunk_space[-1].numel() >= largest
     assert sum(x.numel() for x in e._chunk_space) <= 4 * largest
+
+
+def test_a_snapshot_whose_weights_do_not_fit_is_refused():
+    g = gen(41)
+    make = lambda: engine(1, 8, 2, 1, 64, weights=True)
+    a, b = make(), make()
+    for e in (a, b):
+        e.set_score_mode(binding.SCORE_WEIGHT)
+    a.prefill(randn(g, 1, 1, 2, 50, D), randn(g, 1, 1, 2, 50, D))
+    a.state_views()["weights"][:, :50] = torch.rand(2, 50, generator=g, device="cuda")
+    snap = a.dump_state(kv=True, score=True)
+    for bad in (snap["score"][:, :49], snap["score"][:1], snap["score"][0, 0]):
+        with pytest.raises(ValueError):
+            b.load_state(dict(snap, score=bad), 50)
+    b.load_state(dict(snap, score=None), 50)                          # (none: zeros)
+    assert not bool(b.state_views()["weights"][:, :50].any())
+    b.reset()
+    b.load_state(snap, 50)
+    assert torch.equal(b.state_views()["weights"][:, :50], a.state_views()["weights"][:, :50])
