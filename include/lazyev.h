@@ -410,13 +410,19 @@ enum { LAZYEV_WEIGHTS_OFF = 0, LAZYEV_WEIGHTS_SET = 1, LAZYEV_WEIGHTS_ADD = 2 };
  *             used during the call's kernels only
  * Nothing else changes: probabilities, TS, MRI, t and n stay.  The logits, the softmax and its sums are float32; the weights of the
  * value product are bfloat16 (single tokens: lazyev_attend() keeps 16 bits of them).  A key or value that a row does not see does
- * not touch it, whatever it holds.  Any number of tokens, also where a decode step has no launch shape for so long a cache.
+ * not touch it, whatever it holds.  Any number of tokens, also where a decode step has no launch shape for so long a cache, up to about
+ * 2^45 pairs of a query row and a token that it may see (layers x batch x q_heads x n_tokens x n, half of it for a whole prompt).
  * It may be captured into a CUDA graph and replayed for other queries in the same buffers while the cache and its
  * prefix stay as they were at capture.  Calls on one handle share its scratch: order them, replays too.
- * Errors: EINVAL (views, types, n_tokens, misaligned workspace), ESTATE (weights asked of a handle that keeps none), ECUDA.
+ * Errors: EINVAL (views, types, n_tokens, more pairs than that, misaligned workspace), ESTATE (weights asked of a handle that keeps none),
+ * ECUDA.  They are found before anything is queued.
  */
 int lazyev_query_chunk_workspace(const lazyev_t* h, int n_tokens, int weights, size_t* bytes);
 int lazyev_attend_chunk(lazyev_t* h, const lazyev_rows_t* q, int n_tokens, const lazyev_rows_t* out, int weights, void* workspace);
+/* Diagnostics: how a chunk of the last n_tokens of n own tokens would be launched behind the prefix that is attached.  plan receives the blocks
+ * of the attention's launch (0: too many pairs), those of the weights' launch, and whether every piece of work stays whole, whole pieces
+ * come first, pieces that blocks share are joined by a launch of their own.  Errors: EINVAL, ESTATE (not bound). */
+int lazyev_debug_chunk_plan(const lazyev_t* h, int n, int n_tokens, int plan[5]);
 
 /*
  * Evicts now, whatever the step: every unit is cut to `keep` tokens (n_recent + n_initial < keep <= the create-time budget) by the

@@ -95,6 +95,7 @@ _PROTOS = {
     "lazyev_query_weights_layout": [C.c_void_p, C.POINTER(C.c_size_t)],
     "lazyev_query_chunk_workspace": [C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_size_t)],
     "lazyev_attend_chunk": [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p],
+    "lazyev_debug_chunk_plan": [C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_int)],
     "lazyev_evict_to": [C.c_void_p, C.c_int, C.c_void_p, C.POINTER(C.c_int)],
     "lazyev_query_block_workspace": [C.c_void_p, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
     "lazyev_set_block_workspace": [C.c_void_p, C.c_void_p],
@@ -399,6 +400,12 @@ class Engine:
                 self.reserve_chunk(tokens, weights)
             space = self._chunk_space[-1].data_ptr()
         self._check(lib().lazyev_attend_chunk(self._h, qi, tokens, oi, weights, space))
+
+    def debug_chunk_plan(self, n: int, tokens: int) -> dict:
+        """lazyev_debug_chunk_plan"""
+        plan = (C.c_int * 5)()
+        self._check(lib().lazyev_debug_chunk_plan(self._h, n, tokens, plan))
+        return dict(blocks=plan[0], weight_blocks=plan[1], whole=bool(plan[2]), whole_first=bool(plan[3]), joined_apart=bool(plan[4]))
 
     def evict_to(self, keep: int, dst: Optional["Engine"] = None) -> int:
         """lazyev_evict_to: cut this cache to `keep` tokens per unit now, in place or into another engine; tokens removed."""

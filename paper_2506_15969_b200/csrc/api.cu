@@ -1480,7 +1480,26 @@ ChunkSpace chunk_space(const lazyev_t* h, int n_tokens, int weights) {
     return s;
 }
 
+ChunkPlan plan_of(const lazyev_t* h, int n, int n_tokens) {
+    const lazyev_t* pre = h->shared;
+    return chunk_plan(h->layers, h->batch, h->kv_heads, h->group, n, n_tokens, pre ? pre->n : 0, pre ? h->batch / pre->batch : 1, h->num_sms);
+}
+
 }  // namespace
+
+int lazyev_debug_chunk_plan(const lazyev_t* h, int n, int n_tokens, int plan[5]) {
+    if (!h || !plan) return LAZYEV_EINVAL;
+    lazyev_t* w = const_cast<lazyev_t*>(h);
+    if (!h->bound) return fail(w, LAZYEV_ESTATE, "debug_chunk_plan before bind");
+    if (n_tokens <= 0 || n_tokens > n) return fail(w, LAZYEV_EINVAL, "a chunk is the last 1 to %d cached tokens, not %d", n, n_tokens);
+    const ChunkPlan p = plan_of(h, n, n_tokens);
+    plan[0] = p.blocks;
+    plan[1] = p.blocks > 0 ? weigh_plan(p, h->num_sms).blocks : 0;
+    plan[2] = p.whole;
+    plan[3] = p.in_step;
+    plan[4] = p.joins;
+    return LAZYEV_OK;
+}
 
 int lazyev_query_chunk_workspace(const lazyev_t* h, int n_tokens, int weights, size_t* bytes) {
     if (!h || !bytes) return LAZYEV_EINVAL;
@@ -1509,7 +1528,7 @@ int lazyev_attend_chunk(lazyev_t* h, const lazyev_rows_t* q, int n_tokens, const
         if (extent[i] > 1 && (strides[i] <= 0 || strides[i] >= (1ll << 38))) return fail(h, LAZYEV_EINVAL, "q: strides must be positive and below 2^38");
     if (!workspace || ((uintptr_t)workspace & 255)) return fail(h, LAZYEV_EINVAL, "the workspace must be 256-byte aligned");
     const lazyev_t* pre = h->shared;
-    const ChunkPlan plan = chunk_plan(h->layers, h->batch, h->kv_heads, h->group, h->n, n_tokens, pre ? pre->n : 0, pre ? h->batch / pre->batch : 1, h->num_sms);
+    const ChunkPlan plan = plan_of(h, h->n, n_tokens);
     const WeighPlan wplan = weigh_plan(plan, h->num_sms);
     if (plan.blocks == 0 || wplan.blocks == 0) return fail(h, LAZYEV_EINVAL, "a chunk of %d tokens over %d is not supported", n_tokens, h->n);
     PrefixPool q_map;

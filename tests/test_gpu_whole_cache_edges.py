@@ -114,6 +114,30 @@ def test_rows_computed_again_over_a_long_cache_keep_nobody_waiting(value):
         assert_chunk(out[at], ref, size)
 
 
+def test_a_chunk_of_more_work_than_a_launch_counts_is_refused():
+    g = gen(43)
+    L, B, Hq, Hkv, n = 1, 1, 4, 1, 4400000
+    e = engine(L, Hq, Hkv, B, n)
+    one = randn(g, L, B, 1, Hkv, D)
+    e.append(one.expand(L, B, n, Hkv, D), one.expand(L, B, n, Hkv, D))
+    assert e.debug_chunk_plan(n, n)["blocks"] == 0 and e.debug_chunk_plan(n, n // 2)["blocks"] > 0
+    q, out = (torch.empty(L, B, n, Hq, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    e.reserve_chunk(n)
+    launches = e.info().launches
+    with pytest.raises(binding.LazyEvError) as err:
+        e.attend_chunk(q, out)
+    assert err.value.code == binding.EINVAL and "not supported" in str(err.value) and e.info().launches == launches
+    q, out = randn(g, L, B, 100, Hq, D), out[:, :, :100]
+    e.attend_chunk(q, out)
+    e.synchronize()
+    want = one.double().expand(L, B, 100, Hkv, D).repeat_interleave(Hq, 3)
+    assert bool(((out.double() - want).abs() <= (2.0 ** -7 + 2.0 ** -13 + 2.0 ** -16) * want.abs()).all())
+    for n, tokens in ((0, 0), (5, 0), (5, 6), (5, -1)):
+        with pytest.raises(binding.LazyEvError) as err:
+            e.debug_chunk_plan(n, tokens)
+        assert err.value.code == binding.EINVAL
+
+
 # ---- into another cache ------------------------------------------------------------------------------------------------------
 
 def test_a_cut_into_another_handle_is_not_among_the_profiles_evictions():

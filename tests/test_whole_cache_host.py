@@ -57,3 +57,10 @@ def test_block_workspace_holds_bounds_keys_and_pages(handle):
     assert lib.lazyev_query_block_workspace(handle, C.byref(n), C.byref(at)) == binding.OK
     pages = info.units * info.pages_per_unit
     assert at.value == 0 and n.value >= pages * (512 + 8 + 4) + 4 * info.units * info.capacity
+
+
+def test_a_chunks_plan_needs_a_bound_handle(handle):
+    lib, plan = binding.lib(), (C.c_int * 5)()
+    assert lib.lazyev_debug_chunk_plan(handle, 100, 4, plan) == binding.ESTATE and b"bind" in lib.lazyev_last_error(handle)
+    assert lib.lazyev_debug_chunk_plan(None, 100, 4, plan) == binding.EINVAL
+    assert lib.lazyev_debug_chunk_plan(handle, 100, 4, None) == binding.EINVAL
