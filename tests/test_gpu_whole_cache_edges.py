@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2506_15969_b200 import binding
-from tests.test_gpu_operators import engine, gen, randn
+from tests.test_gpu_operators import TYPES, engine, gen, randn
 from tests.test_gpu_whole_cache import assert_chunk, check_sparse, chunk_ref, loaded, run_chunk, sparse_ref
 
 pytestmark = pytest.mark.gpu
@@ -75,6 +75,94 @@ def test_blocks_that_no_decode_launch_holds_are_refused_before_anything_is_queue
 
 
 # ---- a chunk ------------------------------------------------------------------------------------------------------------
+
+def chunk_squares(q, k, v, T, kp=None, vp=None):
+    """sum p^2 v^2 of every output."""
+    L, B, _, Hq, _ = q.shape
+    Hkv, n = k.shape[2:4]
+    G, N = Hq // Hkv, 0 if kp is None else kp.shape[3]
+    out = torch.empty(q.shape, dtype=torch.float64, device="cuda")
+    for l in range(L):
+        for b in range(B):
+            for h in range(Hkv):
+                kk, vv = k[l, b, h].double(), v[l, b, h].double()
+                if N:
+                    p = b // (B // kp.shape[1])
+                    kk, vv = torch.cat((kp[l, p, h].double(), kk)), torch.cat((vp[l, p, h].double(), vv))
+                x = torch.einsum("tgd,jd->tgj", q[l, b, :, h * G:(h + 1) * G].double(), kk) / math.sqrt(D)
+                sees = torch.ones(T, N + n, dtype=torch.bool, device="cuda").tril(N + n - T)
+                p = torch.softmax(x.masked_fill(~sees[:, None], -math.inf), -1)
+                out[l, b, :, h * G:(h + 1) * G] = p.square() @ vv.square()
+    return out
+
+
+def rms_of_tolerance(got, ref, squares, dtype):
+    """Weights of the value product are off by at most 2^-8 of themselves, each on its own: the mean square of an output's error is at most
+    2^-16 sum p^2 v^2 from them (a third of it for roundings that lie anywhere).  An output's own rounding and the row's sum (2^-13 bounds it) go
+    with the output."""
+    err = (got.double() - ref).square().mean()
+    tol = (2.0 ** -16 * squares + ((TYPES[dtype] + 2.0 ** -13) * ref).square()).mean()
+    return float((err / tol).sqrt())
+
+
+@pytest.mark.parametrize("Hq,Hkv,B,context,T,N", [
+    (16, 8, 8, 2100, 300, 0),                       # 64 units, 3 items each, the last of one row tile
+    (28, 4, 20, 1500, 80, 0),                       # 18 tokens of 7 heads, an odd number of tiles
+    (8, 8, 12, 300, 700, 1300),                     # behind a prefix
+    (32, 8, 2, 9000, 200, 0),                       # an item longer than a block's part
+])
+def test_chunk_with_whole_items_first(Hq, Hkv, B, context, T, N):
+    """Caches that do not stay in L2: a block begins with its whole items and ends with the one that the block before began."""
+    g = gen(B + context + T)
+    L, n = 1, context + T
+    e = engine(L, Hq, Hkv, B, n, weights=True)
+    e.set_page_table(np.random.RandomState(n).permutation(e.info().units * e.info().pages_per_unit))
+    kp = vp = None
+    if N:
+        pre, kp, vp = loaded(g, L, 1, Hq, Hkv, N)
+        e.attach_prefix(pre)
+    k, v, q = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D), randn(g, L, B, T, Hq, D)
+    e.append(k.transpose(2, 3), v.transpose(2, 3))
+    plan = e.debug_chunk_plan(n, T)
+    assert plan["whole_first"] and not plan["whole"] and not plan["joined_apart"]
+    for dtype in (torch.float32, torch.bfloat16):
+        out = run_chunk(e, q, dtype, weights=binding.WEIGHTS_SET)
+        assert torch.equal(out, run_chunk(e, q, dtype, weights=binding.WEIGHTS_SET))
+        ref, size, weights = chunk_ref(q, k, v, T, kp, vp)
+        assert_chunk(out, ref, size, e.state_views()["weights"][:, :n], weights)
+        assert rms_of_tolerance(out, ref, chunk_squares(q, k, v, T, kp, vp), dtype) <= 1
+    # a value that only the last token sees, and one in the middle of the chunk
+    v[..., n - 1, 5] = math.inf
+    v[:, 1::2, :, n - T // 2, 77] = math.nan
+    e.reset()
+    if N:
+        e.attach_prefix(pre)                                          # (a reset detaches it)
+    e.append(k.transpose(2, 3), v.transpose(2, 3))
+    out = run_chunk(e, q, weights=binding.WEIGHTS_SET)
+    ref, size, weights = chunk_ref(q, k, v, T, kp, vp)
+    assert_chunk(out, ref, size, e.state_views()["weights"][:, :n], weights)
+
+
+@pytest.mark.parametrize("tiles", [0, 5])
+def test_a_chunk_with_whole_items_first_that_starves_reports_and_recovers(tiles):
+    g = gen(36)
+    L, B, Hq, Hkv, context, T = 1, 8, 16, 8, 2100, 300
+    e, k, v = loaded(g, L, B, Hq, Hkv, context + T, weights=True)
+    q = randn(g, L, B, T, Hq, D)
+    assert e.debug_chunk_plan(context + T, T)["whole_first"]
+    e.set_wait_limit(0.002)
+    e.debug_starve_page_ring(tiles)
+    e.attend_chunk(q, torch.empty_like(q), weights=binding.WEIGHTS_SET)
+    with pytest.raises(binding.LazyEvError) as err:
+        e.synchronize()
+    assert err.value.code == binding.EDEVICE
+    e.debug_starve_page_ring(-1)
+    e.set_wait_limit(2.0)
+    e.reset()
+    e.append(k.transpose(2, 3), v.transpose(2, 3))
+    ref, size, w = chunk_ref(q, k, v, T)
+    assert_chunk(run_chunk(e, q, weights=binding.WEIGHTS_SET), ref, size, e.state_views()["weights"][:, :context + T], w)
+
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 @pytest.mark.parametrize("L,B,Hq,Hkv,context,T", [
