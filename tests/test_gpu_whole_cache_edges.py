@@ -105,6 +105,30 @@ def rms_of_tolerance(got, ref, squares, dtype):
     return float((err / tol).sqrt())
 
 
+@pytest.mark.parametrize("L,B,Hq,Hkv,context,T", [
+    (1, 1, 5, 1, 20000, 1),
+    (1, 1, 8, 2, 30001, 4),                         # joined by a launch of its own
+    (1, 1, 4, 1, 300000, 1),
+    (1, 2, 8, 2, 4000, 200),
+    (1, 8, 16, 8, 2100, 300),                       # whole items first
+])
+def test_chunk_takes_every_key_tile_into_the_value_product(L, B, Hq, Hkv, context, T):
+    """Held to the mean square, where no tile of 128 keys can go missing: over long caches one is less than the sum of all roundings'
+    largest sizes."""
+    g = gen(context + T)
+    e, k, v = loaded(g, L, B, Hq, Hkv, context + T)
+    q = randn(g, L, B, T, Hq, D)
+    got = run_chunk(e, q, torch.float32)
+    ref, _, _ = chunk_ref(q, k, v, T)
+    squares = chunk_squares(q, k, v, T)
+    assert rms_of_tolerance(got, ref, squares, torch.float32) <= 1
+    # (the bound sees one tile, wherever it is: an output of all keys but those)
+    for at in (0, context // 256 * 128):
+        some = v.clone()
+        some[..., at:at + 128, :] = 0
+        assert rms_of_tolerance(chunk_ref(q, k, some, T)[0], ref, squares, torch.float32) > 1
+
+
 @pytest.mark.parametrize("Hq,Hkv,B,context,T,N", [
     (16, 8, 8, 2100, 300, 0),                       # 64 units, 3 items each, the last of one row tile
     (28, 4, 20, 1500, 80, 0),                       # 18 tokens of 7 heads, an odd number of tiles
