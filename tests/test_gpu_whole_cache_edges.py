@@ -10,7 +10,7 @@ import torch
 
 from paper_2506_15969_b200 import binding
 from tests.test_gpu_operators import TYPES, engine, gen, randn
-from tests.test_gpu_whole_cache import assert_chunk, check_sparse, chunk_ref, loaded, run_chunk, sparse_ref
+from tests.test_gpu_whole_cache import assert_chunk, check_kept, check_sparse, chunk_ref, loaded, run_chunk, sparse_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -54,6 +54,45 @@ def test_scores_of_tiny_values_are_those_of_64_bits(n, k_size, q_size):
     e.attend_sparse(q, torch.empty_like(q), blocks, sel)
     e.synchronize()
     assert np.array_equal(sel.cpu().numpy(), sparse_ref(q, k, v, blocks)[2])
+
+
+@pytest.mark.parametrize("kind", ["normal", "alike", "two values"])
+def test_more_blocks_than_shared_memory_holds_scores_of(kind):
+    """Over a million tokens: the scores of a unit stay in device memory, and every way to the cut rewrites them there."""
+    g = gen(33)
+    L, B, Hq, Hkv, n = 1, 1, 4, 1, 64 * 16390 + 5
+    k = randn(g, L, B, Hkv, n, D)
+    if kind != "normal":
+        k = k[:, :, :, :64].repeat(1, 1, 1, n // 64 + 1, 1)[:, :, :, :n].contiguous()
+    if kind == "two values":
+        k[:, :, :, 64 * 9000:64 * 9100] *= 2
+    e, k, v = loaded(g, L, B, Hq, Hkv, n, k=k)
+    for blocks in (3, 77, 300):
+        check_sparse(e, randn(g, L, B, Hq, D), k, v, blocks)
+
+
+def test_many_units_with_more_blocks_than_shared_memory_holds_scores_of():
+    """The same with enough units for a block of threads each: bounds laid down by the caller, every key and value of a unit alike."""
+    g = gen(34)
+    L, B, Hq, Hkv, n, blocks = 1, 80, 1, 1, 64 * 16386 + 1, 40
+    last = n // 64
+    e = engine(L, Hq, Hkv, B, n)
+    one = randn(g, L, B, 1, Hkv, D)
+    e.append(one.expand(L, B, n, Hkv, D), one.expand(L, B, n, Hkv, D))
+    e.index_blocks()
+    assert torch.equal(e.block_bounds()[:, :last, 0], one.view(B, 1, D).expand(B, last, D))
+    low = randn(g, B, last, D)
+    high = torch.maximum(low, randn(g, B, last, D))
+    e.block_bounds()[:, :last, 0], e.block_bounds()[:, :last, 1] = high, low
+    q, out = randn(g, L, B, Hq, D), torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    sel = torch.full((B, blocks), 99, dtype=torch.int32, device="cuda")
+    e.attend_sparse(q, out, blocks, sel)
+    e.synchronize()
+    for u in range(B):
+        s = torch.maximum(high[u].double() * q[0, u].double(), low[u].double() * q[0, u].double()).sum(-1).cpu().numpy()
+        best = np.lexsort((np.arange(last), -s))[:blocks - 1]
+        assert sel[u].tolist() == sorted(best.tolist()) + [last]
+    assert bool(((out[:, :, 0].double() - one[:, :, 0, 0].double()).abs() <= (2.0 ** -8 + 2.0 ** -13) * one[:, :, 0, 0].double().abs()).all())
 
 
 def test_blocks_that_no_decode_launch_holds_are_refused_before_anything_is_queued():
@@ -250,7 +289,113 @@ def test_a_chunk_of_more_work_than_a_launch_counts_is_refused():
         assert err.value.code == binding.EINVAL
 
 
+# ---- weights of decode steps ----------------------------------------------------------------------------------------------
+
+def joint_probabilities(q, kp, k):
+    """Of the own tokens, averaged over a group's heads: q [L, B, Hq, D]; kp [L, P, Hkv, N, D]; k [L, B, Hkv, n, D]."""
+    L, B, Hkv, n = k.shape[:4]
+    G, N = q.shape[2] // Hkv, kp.shape[3]
+    kk = torch.cat((kp.double().repeat_interleave(B // kp.shape[1], 1), k.double()), 3)
+    x = torch.einsum("lbhgd,lbhjd->lbhgj", q.double().unflatten(2, (Hkv, G)), kk) / math.sqrt(D)
+    return torch.softmax(x, -1)[..., N:].mean(3).flatten(0, 2)
+
+
+@pytest.mark.parametrize("L,B,Hq,Hkv,n", [
+    (2, 6, 28, 4, 333),                             # a block per unit
+    (4, 40, 16, 4, 70),                             # a warp per unit
+    (4, 40, 16, 4, 0),                              # no own token before the first step
+])
+@pytest.mark.parametrize("how", ["device", "rows", "host", "async"])
+def test_decode_steps_behind_a_prefix_add_their_weights(L, B, Hq, Hkv, n, how):
+    g = gen(n + L)
+    N = 200
+    pre, kp, vp = loaded(g, L, 2, Hq, Hkv, N)
+    e = engine(L, Hq, Hkv, B, n + 4, weights=True)
+    e.attach_prefix(pre)
+    k, v = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    if n:
+        e.prefill(k, v)
+    total = torch.zeros(L * B * Hkv, n, device="cuda")
+    exact = total.double()
+    for _ in range(3):
+        q, kn, vn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+        k = torch.cat((k, kn.unsqueeze(3)), 3)
+        if how in ("device", "rows"):
+            out = torch.empty_like(q)
+            (e.decode_step if how == "device" else e.decode_step_rows)(q, kn, vn, out)
+        else:
+            host = [x.cpu().pin_memory() for x in (q, kn, vn)]
+            out = torch.empty(q.shape, dtype=torch.bfloat16).pin_memory()
+            if how == "host":
+                e.decode_step_host(*host, out)
+            else:
+                e.decode_step_host_async(*host, out)
+                e.host_wait(0)
+        e.synchronize()
+        n += 1
+        views = e.state_views()
+        total = torch.cat((total, torch.zeros(total.shape[0], 1, device="cuda")), 1) + views["pbar"][:, :n]
+        assert torch.equal(views["weights"][:, :n], total)            # the same float32 sums
+        exact = torch.cat((exact, torch.zeros(exact.shape[0], 1, dtype=torch.float64, device="cuda")), 1) + joint_probabilities(q, kp, k)
+        assert bool(((views["weights"][:, :n].double() - exact).abs() <= (2.0 ** -13 + 2.0 ** -14) * exact + 1e-30).all())
+
+
+@pytest.mark.parametrize("how", ["host", "async"])
+def test_wide_steps_from_host_buffers_add_their_weights(how):
+    """More units than blocks: the step runs in ranges of units."""
+    g = gen(37)
+    L, B, Hq, Hkv, n = 14, 32, 28, 4, 400
+    k, v = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    engines = [engine(L, Hq, Hkv, B, n + 4, weights=True) for _ in range(2)]
+    for e in engines:
+        e.prefill(k, v)
+    out, ho = torch.empty(L, B, Hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(L, B, Hq, D, dtype=torch.bfloat16).pin_memory()
+    for step in range(3):
+        q, kn, vn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+        engines[0].decode_step(q, kn, vn, out)
+        host = [x.cpu().pin_memory() for x in (q, kn, vn)]
+        if how == "host":
+            engines[1].decode_step_host(*host, ho)
+        else:
+            engines[1].decode_step_host_async(*host, ho)
+            engines[1].host_wait(0)
+        for e in engines:
+            e.synchronize()
+        a, b = (e.state_views()["weights"][:, :n + step + 1] for e in engines)
+        assert torch.equal(a, b) and torch.equal(out.cpu(), ho) and bool((a.sum(1) - step - 1 <= 1e-4).all())
+    assert how == "async" or engines[1].info().host_ranges >= 3       # (of the last host step)
+
+
 # ---- into another cache ------------------------------------------------------------------------------------------------------
+
+def test_evict_to_between_two_handles_behind_the_same_prefix():
+    g = gen(38)
+    L, B, P, Hq, Hkv, N, n, keep = 2, 4, 2, 8, 2, 150, 300, 100
+    pre, kp, vp = loaded(g, L, P, Hq, Hkv, N)
+    big, small = engine(L, Hq, Hkv, B, n, weights=True, n_recent=16, window=16), engine(L, Hq, Hkv, B, keep, weights=True)
+    for e in (big, small):
+        e.attach_prefix(pre)
+        e.set_score_mode(binding.SCORE_WEIGHT)
+    k, v, q = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D), randn(g, L, B, 40, Hq, D)
+    big.append(k.transpose(2, 3), v.transpose(2, 3))
+    run_chunk(big, q, weights=binding.WEIGHTS_SET)
+    before, w = big.dump_state(), big.state_views()["weights"][:, :n].cpu().numpy()
+    assert big.evict_to(keep, small) == n - keep
+    check_kept(before, None, small, k, v, w, keep, 16, 0)
+    assert big.evict_to(keep) == n - keep
+    check_kept(before, None, big, k, v, w, keep, 16, 0)
+    assert small.info().next_position == big.info().next_position == N + n
+    for _ in range(3):                                                # both go on alike, over the prefix and what was kept
+        q, kn, vn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        big.decode_step(q, kn, vn, a)
+        small.decode_step(q, kn, vn, b)
+        x, y = big.dump_state(kv=True, score=True), small.dump_state(kv=True, score=True)
+        assert torch.equal(a, b) and all(np.array_equal(x[i], y[i]) for i in ("pos", "ts", "mri", "k", "v", "score"))
+    kk, vv = (torch.from_numpy(x[i].view(np.int16).copy()).view(torch.bfloat16).view(L, B, Hkv, -1, D).cuda() for i in ("k", "v"))
+    ref, size, _ = chunk_ref(q[:, :, None], kk, vv, 1, kp, vp)
+    assert bool(((a.double() - ref[:, :, 0]).abs() <= 2.0 ** -8 * ref[:, :, 0].abs() + 2.0 ** -13 * size[:, :, 0]).all())
+
 
 def test_a_cut_into_another_handle_is_not_among_the_profiles_evictions():
     g = gen(39)
