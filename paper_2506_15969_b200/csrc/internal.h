@@ -103,7 +103,7 @@ struct ChunkArgs {
     int pages_per_unit, total_pages, prefix_pages_per_unit, prefix_total_pages;
     RowView q, out;                     // q bf16
     const PrefixPool* q_map;            // of chunk_query_map()
-    float* o;                           // sums of items that several blocks share (chunk_workspace_bytes)
+    float* o;                           // sums of items that several blocks share (chunk_sums_bytes)
     float2* ml;
     int32_t* counters;                  // [kChunkCounters], zero
     float* norms;                       // [units][tiles][2][128]: minus a row's reference, and 1 / its sum of exp2(x - reference); or null
