@@ -113,6 +113,31 @@ def test_blocks_that_no_decode_launch_holds_are_refused_before_anything_is_queue
     check_sparse(e, q, k, v, 40)
 
 
+def test_steps_that_append_a_token_and_read_selected_blocks():
+    """The step that saves something: no dense pass before it.  t, what is tracked and the weights stay as they are, a new token's weight is 0,
+    and no eviction comes due by itself."""
+    g = gen(44)
+    L, B, Hq, Hkv, n = 1, 2, 8, 2, 190
+    e = binding.Engine(L, Hq, Hkv, D, 250, 16, 1e-3, batch=B, n_recent=8, max_prefill=300, weights=True)
+    e.set_score_mode(binding.SCORE_WEIGHT)
+    k, v = randn(g, L, B, Hkv, n, D), randn(g, L, B, Hkv, n, D)
+    e.append(k.transpose(2, 3), v.transpose(2, 3))
+    run_chunk(e, randn(g, L, B, 50, Hq, D), weights=binding.WEIGHTS_SET)
+    before, weights = e.dump_state(), e.state_views()["weights"][:, :n].clone()
+    for _ in range(75):                                               # (past the ends of two blocks)
+        q, kn, vn = randn(g, L, B, Hq, D), randn(g, L, B, Hkv, D), randn(g, L, B, Hkv, D)
+        e.append(kn.unsqueeze(2), vn.unsqueeze(2))
+        k, v = torch.cat((k, kn.unsqueeze(3)), 3), torch.cat((v, vn.unsqueeze(3)), 3)
+        check_sparse(e, q, k, v, 3)
+    after, now = e.dump_state(), e.state_views()["weights"][:, :n + 75]
+    assert after["n"] == n + 75 and after["t"] == before["t"] and e.info().evictions == 0
+    assert all(np.array_equal(after[x][:, :n], before[x]) for x in ("pos", "ts", "mri"))
+    assert np.array_equal(after["pos"][:, n:], np.tile(np.arange(n, n + 75), (L * B * Hkv, 1)))
+    assert torch.equal(now[:, :n], weights) and not bool(now[:, n:].any())
+    assert e.evict_to(200) == 65                                      # when the caller says so
+    assert e.dump_state()["pos"][:, -8:].tolist() == [list(range(n + 67, n + 75))] * (L * B * Hkv)
+
+
 # ---- a chunk ------------------------------------------------------------------------------------------------------------
 
 def chunk_squares(q, k, v, T, kp=None, vp=None):
