@@ -1491,7 +1491,8 @@ int lazyev_debug_chunk_plan(const lazyev_t* h, int n, int n_tokens, int plan[5])
     if (!h || !plan) return LAZYEV_EINVAL;
     lazyev_t* w = const_cast<lazyev_t*>(h);
     if (!h->bound) return fail(w, LAZYEV_ESTATE, "debug_chunk_plan before bind");
-    if (n_tokens <= 0 || n_tokens > n) return fail(w, LAZYEV_EINVAL, "a chunk is the last 1 to %d cached tokens, not %d", n, n_tokens);
+    if (n_tokens <= 0 || n_tokens > n || n > h->capacity)
+        return fail(w, LAZYEV_EINVAL, "a chunk is the last 1 to %d of up to %d cached tokens, not %d", n, h->capacity, n_tokens);
     const ChunkPlan p = plan_of(h, n, n_tokens);
     plan[0] = p.blocks;
     plan[1] = p.blocks > 0 ? weigh_plan(p, h->num_sms).blocks : 0;

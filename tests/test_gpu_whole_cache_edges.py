@@ -308,7 +308,7 @@ def test_a_chunk_of_more_work_than_a_launch_counts_is_refused():
     e.synchronize()
     want = one.double().expand(L, B, 100, Hkv, D).repeat_interleave(Hq, 3)
     assert bool(((out.double() - want).abs() <= (2.0 ** -7 + 2.0 ** -13 + 2.0 ** -16) * want.abs()).all())
-    for n, tokens in ((0, 0), (5, 0), (5, 6), (5, -1)):
+    for n, tokens in ((0, 0), (5, 0), (5, 6), (5, -1), (e.info().capacity + 1, 4)):
         with pytest.raises(binding.LazyEvError) as err:
             e.debug_chunk_plan(n, tokens)
         assert err.value.code == binding.EINVAL
