@@ -446,7 +446,8 @@ int lazyev_evict_to(lazyev_t* h, int keep, lazyev_t* dst, int* evicted);
  *   out = softmax(q [K_prefix, K_selected]^T / sqrt(128)) [V_prefix; V_selected]
  *   q, out   : as for lazyev_decode_step(), q 16-byte aligned
  *   selected : device int32 [units][blocks], or NULL: the selected blocks in ascending order, -1 behind the last
- * Nothing in the cache changes (the stored probabilities neither).  Bounds that are missing are made first: those of blocks that have filled since
+ * Nothing in the cache changes (the stored probabilities neither); a step over selected blocks is lazyev_append() of its token and then this call, in
+ * the place of lazyev_decode_step(), and moves no t, TS, MRI or weight.  Bounds that are missing are made first: those of blocks that have filled since
  * the last call, all of them after a prompt load or an eviction.  lazyev_index_blocks() makes them beforehand, and again from
  * first_block on for a caller that has written to the pages itself.
  * The workspace, device memory of *bytes bytes, 256-byte aligned, is the caller's and must stay valid while it is set (NULL ends that);
